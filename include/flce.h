@@ -250,6 +250,111 @@ FLCE_API int flce_cross_entropy_inplace_noalloc(void* Z, const int64_t* targets,
                                        int64_t ldz, int64_t ignore_index, int dtype, float* loss,
                                        void* stream);
 
+/*
+ * Norms before and after a block, fused with the block's gate, the residual scale and the
+ * residual sum (paper section 3.2, RMSNorm paragraph, Eq. RMSNorm-forward / RMSNorm-backward):
+ * what stands between two blocks of a model, and between the last one and the head.  Row by row
+ * of [rows x H] matrices, with x the residual stream and y the block's output:
+ *
+ *     z = y                                   or, with gamma_post,   z = y / rms(y) * gamma_post
+ *     h = x + scale * a(gate) * z             (without gate: x + scale * z; without x: the rest alone)
+ *     n = h / rms(h) * gamma_pre              (with gamma_pre)           rms(v) = sqrt(mean_j v_j^2 + eps)
+ *
+ * h is the new residual stream (what flce_rmsnorm_fwd_bwd takes behind the last block), n the next
+ * block's input.  n comes from h before it is rounded to dtype.  Without y (in front of the first
+ * block) h = x is not written again and n is all there is.
+ *
+ * The backward takes the forward's h and y and the gradients dn of n and dh of h (what flows back
+ * along the residual stream, e.g. the dh of flce_rmsnorm_fwd_bwd), and returns
+ *
+ *     dx = dh + rms-norm backward of dn       (the gradient of x, and of all of h)
+ *     dy, dgate, dgamma_post, dgamma_pre
+ *
+ * Gradients of what several rows share (gammas, gates) are summed in fp32 without atomics, in an
+ * order that depends on the shape and the room for partial sums alone; every output is rounded
+ * once.
+ *
+ *   size            must be sizeof(flce_block_norm) (FLCE_ERR_ARG otherwise)
+ *   rows, H         1 .. 2^30 and 1 .. 2^24
+ *   dtype           of every matrix and vector
+ *   gate_act        a: FLCE_GATE_*
+ *   rows_per_gate   0: gate is one row of H elements (a gain per channel) for all rows;
+ *                   r >= 1: row i takes row i / r of gate[ceil(rows / r) x H] (r = 1: a gate per
+ *                   token, r = sequence length: per sequence)
+ *   scale, eps      finite, eps >= 0
+ *   ldx .. lddgate  row strides in elements of the matrices of these names, 0 = H, else >= H.
+ *                   Any stride and any pointer that fits its elements is taken; the gammas and
+ *                   a single row have none.
+ *   workspace       device buffer (256-byte aligned) for the backward's partial sums, or NULL for
+ *                   the device's shared workspace; workspace_bytes: flce_block_norm_workspace_bytes
+ *                   of the same arguments, or less at the price of fewer workgroups
+ *                   (12 H bytes always do; FLCE_ERR_WORKSPACE if not even one serves).  The
+ *                   forward uses none.
+ *
+ * Forward: x or y may be NULL (not both; without y there is no gate, gamma_post or h); gate,
+ * gamma_post and gamma_pre may be NULL (without gamma_pre there is no n).  Backward: dh may be
+ * NULL (zero) where there is a gamma_pre, y where neither dy nor anything of the block is there;
+ * h and dn go with gamma_pre.  Outputs may be NULL where they are not wanted, but not all of them.
+ * h may lie exactly on x and dx exactly on dh; no output may share other memory with an input
+ * or another output (FLCE_ERR_ARG).
+ */
+enum { FLCE_GATE_LINEAR = 0, FLCE_GATE_SIGMOID = 1, FLCE_GATE_SILU = 2, FLCE_GATE_TANH = 3 };
+typedef struct {
+    size_t size;
+    int64_t rows, H;
+    int dtype;
+    int gate_act;
+    int64_t rows_per_gate;
+    float scale, eps;
+    int64_t ldx, ldy, ldh, ldn, ldgate;
+    int64_t lddx, lddy, lddh, lddn, lddgate;
+    void* workspace;
+    size_t workspace_bytes;
+} flce_block_norm;
+FLCE_API int flce_block_norm_fwd(const void* x, const void* y, const void* gate, const void* gamma_post,
+                        const void* gamma_pre, const flce_block_norm* args, void* h, void* n, void* stream);
+FLCE_API int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const void* y, const void* gate,
+                        const void* gamma_post, const void* gamma_pre, const flce_block_norm* args, void* dx,
+                        void* dy, void* dgate, void* dgamma_post, void* dgamma_pre, void* stream);
+FLCE_API size_t flce_block_norm_workspace_bytes(const flce_block_norm* args);
+
+/*
+ * Global norm of gradients, and clipping by it: the step between the backward calls above (dW of
+ * every head, dgammas, ...) and the optimizer's.  Over all elements of n_tensors dense tensors,
+ * fp32 and bf16 mixed as they come:
+ *
+ *     norm = sqrt(sum g^2)  (FLCE_NORM_2, summed in fp64)   or   max |g|  (FLCE_NORM_INF)
+ *     out  = g * min(1, max_norm / (norm + 1e-6))
+ *
+ * A norm that is infinite or NaN is returned as it is and nothing is scaled.  flce_grad_norm is
+ * the norm alone, flce_grad_clip the scaling by a norm that the caller has (of a sharded model:
+ * the root of the sum of the ranks' squares), flce_clip_grad_norm both, without a launch between
+ * them.  All of them leave the norm on the device; nothing waits for it.
+ *
+ *   grads, outs   HOST arrays of n_tensors DEVICE pointers, aligned to their elements; read before
+ *                 the call returns.  outs == NULL, or outs[i] == grads[i]: in place (where nothing
+ *                 is to be scaled the tensor is not written).  No two outs may share memory, nor an
+ *                 out and a grad other than its own (FLCE_ERR_ARG): a gradient that is listed twice
+ *                 would be scaled twice.
+ *   counts        HOST array, elements of each tensor, 0 .. 2^40 (0: its pointers may be NULL)
+ *   dtypes        HOST array, flce_dtype of each tensor and its out
+ *   n_tensors     >= 0 (0: norm = 0)
+ *   norm          device, 1 float        out (flce_grad_clip: in)
+ *   max_norm      finite, >= 0
+ *   workspace     device buffer (256-byte aligned, at least flce_grad_norm_workspace_bytes(n_tensors))
+ *                 for the partial results, or NULL for the device's shared workspace
+ * Every 120 tensors take a launch for the norm and one for the scaling.
+ */
+enum { FLCE_NORM_2 = 0, FLCE_NORM_INF = 1 };
+FLCE_API int flce_grad_norm(const void* const* grads, const int64_t* counts, const int* dtypes, int n_tensors,
+                   int norm_type, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+FLCE_API int flce_grad_clip(const void* const* grads, void* const* outs, const int64_t* counts, const int* dtypes,
+                   int n_tensors, const float* norm, float max_norm, void* stream);
+FLCE_API int flce_clip_grad_norm(const void* const* grads, void* const* outs, const int64_t* counts,
+                        const int* dtypes, int n_tensors, int norm_type, float max_norm, float* norm,
+                        void* workspace, size_t workspace_bytes, void* stream);
+FLCE_API size_t flce_grad_norm_workspace_bytes(int n_tensors);
+
 /* Bytes of device scratch flce_fwd_bwd uses for this problem.  For fixed H, V
  * and dtype it does not grow with BT once BT exceeds one chunk:
  * flce_workspace_bytes(BT, ...) <= flce_workspace_bytes_max(...). */

@@ -47,6 +47,13 @@ def lib() -> ctypes.CDLL:
             "flce_rmsnorm_workspace_bytes": ([i64, i64, i64, ci], sz),
             "flce_cross_entropy_inplace": ([p, p, i64, i64, i64, i64, ci, p, p], ci),
             "flce_cross_entropy_inplace_noalloc": ([p, p, i64, i64, i64, i64, ci, p, p], ci),
+            "flce_block_norm_fwd": ([p] * 9, ci),
+            "flce_block_norm_bwd": ([p] * 14, ci),
+            "flce_block_norm_workspace_bytes": ([p], sz),
+            "flce_grad_norm": ([p, p, p, ci, ci, p, p, sz, p], ci),
+            "flce_grad_clip": ([p, p, p, p, ci, p, ctypes.c_float, p], ci),
+            "flce_clip_grad_norm": ([p, p, p, p, ci, ci, ctypes.c_float, p, p, sz, p], ci),
+            "flce_grad_norm_workspace_bytes": ([ci], sz),
             "flce_workspace_bytes": ([i64, i64, i64, ci], sz),
             "flce_workspace_bytes_max": ([i64, i64, ci], sz),
             "flce_set_workspace": ([p, sz], ci),
@@ -307,6 +314,236 @@ def flce_rmsnorm_fwd_bwd(h, gamma, eps, W, targets, ignore_index=-100, loss=None
 
 def flce_rmsnorm_workspace_bytes(BT, H, V, dtype) -> int:
     return int(lib().flce_rmsnorm_workspace_bytes(BT, H, V, _DTYPES.get(dtype, dtype)))
+
+
+class FlceBlockNorm(ctypes.Structure):
+    """flce_block_norm of include/flce.h."""
+    _fields_ = [("size", ctypes.c_size_t), ("rows", ctypes.c_int64), ("H", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("gate_act", ctypes.c_int), ("rows_per_gate", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float)] + \
+               [(ld, ctypes.c_int64) for ld in ("ldx", "ldy", "ldh", "ldn", "ldgate",
+                                                "lddx", "lddy", "lddh", "lddn", "lddgate")] + \
+               [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+GATE_ACTS = ("linear", "sigmoid", "silu", "tanh")
+
+
+def _block_norm_args(like, gate, gate_act, rows_per_gate, scale, eps, workspace=None) -> FlceBlockNorm:
+    if like.dim() != 2:
+        raise ValueError("expected [rows, H]")
+    if gate_act not in GATE_ACTS:
+        raise ValueError(f"gate_act must be one of {GATE_ACTS}")
+    rows, H = like.shape
+    rows_per_gate = int(rows_per_gate)
+    if rows_per_gate < 0:
+        raise ValueError("rows_per_gate must be 0 (one gate row for all) or positive")
+    if gate is not None:
+        want = ((rows + rows_per_gate - 1) // rows_per_gate, H) if rows_per_gate else (H,)
+        if gate.shape != want:
+            raise ValueError(f"expected gate {want}")
+    b = FlceBlockNorm()
+    b.size, b.rows, b.H, b.dtype = ctypes.sizeof(FlceBlockNorm), rows, H, _dtype_code(like)
+    b.gate_act, b.rows_per_gate, b.scale, b.eps = GATE_ACTS.index(gate_act), rows_per_gate, float(scale), float(eps)
+    if workspace is not None:
+        b.workspace = _dev_ptr(workspace, "workspace")
+        b.workspace_bytes = workspace.numel() * workspace.element_size()
+    return b
+
+
+def _rows_ptr(t, name, like, shape, args=None, ld=None) -> int | None:
+    """The pointer of a matrix whose rows may be apart (its stride goes to args.ld) or, without ld, a vector."""
+    if t is None:
+        return None
+    if t.device != like.device:
+        raise ValueError(f"{name} must live on {like.device}")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must have dtype {like.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    if ld is not None and t.dim() == 2 and t.shape[0] > 1:
+        if t.stride(0) < t.shape[1]:
+            raise ValueError(f"the rows of {name} must not overlap")
+        setattr(args, ld, t.stride(0))
+    return t.data_ptr()
+
+
+def flce_block_norm_fwd(x, y=None, gamma_pre=None, gamma_post=None, gate=None, gate_act="linear", rows_per_gate=0,
+                        scale=1.0, eps=1e-6, h=None, n=None, stream=None):
+    """h = x + scale * a(gate) * z and n = rmsnorm(h; gamma_pre), z = y or rmsnorm(y; gamma_post).
+
+    x, y [rows, H] (float32 or bfloat16; rows may be apart), gammas [H], gate [H] (rows_per_gate = 0) or
+    [ceil(rows / rows_per_gate), H].  x may be None (no residual), y too (n alone).  Returns (h, n), None for
+    what there is not; outputs are allocated when not passed, h may be x itself.
+    """
+    like = x if x is not None else y
+    if like is None:
+        raise ValueError("x or y is needed")
+    if not like.is_cuda:
+        raise ValueError("x and y must live on the GPU")
+    b = _block_norm_args(like, gate, gate_act, rows_per_gate, scale, eps)
+    shape, vec = like.shape, like.shape[1:]
+    if y is not None and h is None:
+        h = torch.empty(shape, dtype=like.dtype, device=like.device)
+    if gamma_pre is not None and n is None:
+        n = torch.empty(shape, dtype=like.dtype, device=like.device)
+    with _OnDevice(like.device):
+        st = lib().flce_block_norm_fwd(
+            _rows_ptr(x, "x", like, shape, b, "ldx"), _rows_ptr(y, "y", like, shape, b, "ldy"),
+            _rows_ptr(gate, "gate", like, gate.shape if gate is not None else vec, b, "ldgate"),
+            _rows_ptr(gamma_post, "gamma_post", like, vec), _rows_ptr(gamma_pre, "gamma_pre", like, vec),
+            ctypes.byref(b), _rows_ptr(h, "h", like, shape, b, "ldh"), _rows_ptr(n, "n", like, shape, b, "ldn"),
+            _stream_handle(stream, like.device))
+    _check(st, "flce_block_norm_fwd")
+    return h, n
+
+
+def flce_block_norm_bwd(h=None, dn=None, dh=None, y=None, gamma_pre=None, gamma_post=None, gate=None,
+                        gate_act="linear", rows_per_gate=0, scale=1.0, eps=1e-6, dx=None, dy=None, dgate=None,
+                        dgamma_post=None, dgamma_pre=None, flags=0, workspace=None, stream=None):
+    """Gradients of flce_block_norm_fwd from its h and y and the gradients dn of n, dh of h (None = zero).
+
+    Returns (dx, dy, dgate, dgamma_post, dgamma_pre), None for what there is not.  Outputs are allocated when
+    not passed; dx may be dh itself, and without gamma_pre it is dh (nothing is computed for it).
+    flags: SKIP_DX leaves dx out, SKIP_DW the gradients of the gammas and the gate.
+    """
+    like = dn if dn is not None else dh
+    if like is None:
+        raise ValueError("dn or dh is needed")
+    if not like.is_cuda:
+        raise ValueError("dn and dh must live on the GPU")
+    if flags & ~(SKIP_DX | SKIP_DW):
+        raise ValueError("unknown flags")
+    b = _block_norm_args(like, gate, gate_act, rows_per_gate, scale, eps, workspace)
+    shape, vec = like.shape, like.shape[1:]
+    want_dx, want_dw = not flags & SKIP_DX, not flags & SKIP_DW
+
+    def output(given, wanted, size):
+        if not wanted:
+            return None
+        return given if given is not None else torch.empty(size, dtype=like.dtype, device=like.device)
+
+    passed_on = want_dx and gamma_pre is None and dx is None
+    dx = output(dx, want_dx and not passed_on, shape)
+    dy = output(dy, y is not None, shape)
+    dgate = output(dgate, want_dw and gate is not None, gate.shape if gate is not None else None)
+    dgamma_post = output(dgamma_post, want_dw and gamma_post is not None, vec)
+    dgamma_pre = output(dgamma_pre, want_dw and gamma_pre is not None, vec)
+    gshape = gate.shape if gate is not None else vec
+    if passed_on and y is None:
+        raise ValueError("without y and gamma_pre there is nothing to compute")
+    with _OnDevice(like.device):
+        st = lib().flce_block_norm_bwd(
+            _rows_ptr(h, "h", like, shape, b, "ldh"), _rows_ptr(dn, "dn", like, shape, b, "lddn"),
+            _rows_ptr(dh, "dh", like, shape, b, "lddh"), _rows_ptr(y, "y", like, shape, b, "ldy"),
+            _rows_ptr(gate, "gate", like, gshape, b, "ldgate"),
+            _rows_ptr(gamma_post, "gamma_post", like, vec), _rows_ptr(gamma_pre, "gamma_pre", like, vec),
+            ctypes.byref(b), _rows_ptr(dx, "dx", like, shape, b, "lddx"), _rows_ptr(dy, "dy", like, shape, b, "lddy"),
+            _rows_ptr(dgate, "dgate", like, gshape, b, "lddgate"), _rows_ptr(dgamma_post, "dgamma_post", like, vec),
+            _rows_ptr(dgamma_pre, "dgamma_pre", like, vec), _stream_handle(stream, like.device))
+    _check(st, "flce_block_norm_bwd")
+    return dh if passed_on else dx, dy, dgate, dgamma_post, dgamma_pre
+
+
+def flce_block_norm_workspace_bytes(rows, H, dtype, rows_per_gate=0) -> int:
+    """Bytes flce_block_norm_bwd uses at most for this shape (with both gammas and a gate)."""
+    b = FlceBlockNorm()
+    b.size, b.rows, b.H, b.dtype = ctypes.sizeof(FlceBlockNorm), rows, H, _DTYPES.get(dtype, dtype)
+    b.rows_per_gate = rows_per_gate
+    return int(lib().flce_block_norm_workspace_bytes(ctypes.byref(b)))
+
+
+NORM_TYPES = {2.0: 0, float("inf"): 1}
+
+
+def _tensor_list(grads, device=None):
+    """(device, host arrays of pointers, element counts and dtypes) of a list of dense tensors on one GPU."""
+    n = len(grads)
+    ptrs, counts, dtypes = [], [], []
+    for t in grads:
+        if device is None:
+            device = t.device
+        if t.device != device or device.type != "cuda":
+            raise ValueError("every tensor must live on the same GPU")
+        if not t.is_contiguous():
+            raise ValueError("every tensor must be contiguous")
+        ptrs.append(t.data_ptr())
+        counts.append(t.numel())
+        dtypes.append(_dtype_code(t))
+    return device, (ctypes.c_void_p * n)(*ptrs), (ctypes.c_int64 * n)(*counts), (ctypes.c_int * n)(*dtypes)
+
+
+def _norm_out(norm, device):
+    if norm is None:
+        if device is None:
+            raise ValueError("an empty list needs `norm`")
+        return torch.empty((), dtype=torch.float32, device=device)
+    if norm.dtype != torch.float32 or norm.numel() != 1 or not norm.is_cuda or device not in (None, norm.device):
+        raise ValueError("norm must be one float32 value on the tensors' GPU")
+    return norm
+
+
+def _norm_type(norm_type) -> int:
+    try:
+        return NORM_TYPES[float(norm_type)]
+    except KeyError:
+        raise ValueError("norm_type must be 2 or inf") from None
+
+
+def _out_list(outs, grads, device):
+    if outs is None:
+        return None
+    if len(outs) != len(grads):
+        raise ValueError("outs must hold one tensor per gradient")
+    for o, g in zip(outs, grads):
+        if o.shape != g.shape or o.dtype != g.dtype:
+            raise ValueError("every out must match its gradient in shape and dtype")
+    return _tensor_list(outs, device)[1]
+
+
+def _workspace_args(workspace):
+    if workspace is None:
+        return None, 0
+    return _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def flce_grad_norm(grads, norm_type=2.0, norm=None, workspace=None, stream=None):
+    """Norm (2 or inf) over all elements of a list of tensors (float32 and bfloat16 mixed): one float32 on the GPU."""
+    grads = list(grads)
+    device, ptrs, counts, dtypes = _tensor_list(grads)
+    norm = _norm_out(norm, device)
+    with _OnDevice(norm.device):
+        st = lib().flce_grad_norm(ptrs, counts, dtypes, len(grads), _norm_type(norm_type), norm.data_ptr(),
+                                  *_workspace_args(workspace), _stream_handle(stream, norm.device))
+    _check(st, "flce_grad_norm")
+    return norm
+
+
+def flce_grad_clip(grads, norm, max_norm, outs=None, stream=None):
+    """Scales a list of tensors by min(1, max_norm / (norm + 1e-6)), in place or into `outs`; norm: one float32 on
+    the GPU, e.g. over all shards of a model."""
+    grads = list(grads)
+    device, ptrs, counts, dtypes = _tensor_list(grads)
+    norm = _norm_out(norm, device)
+    with _OnDevice(norm.device):
+        st = lib().flce_grad_clip(ptrs, _out_list(outs, grads, device), counts, dtypes, len(grads), norm.data_ptr(),
+                                  float(max_norm), _stream_handle(stream, norm.device))
+    _check(st, "flce_grad_clip")
+
+
+def flce_clip_grad_norm(grads, max_norm, norm_type=2.0, outs=None, norm=None, workspace=None, stream=None):
+    """flce_grad_norm, then flce_grad_clip by it; returns the norm before clipping (one float32 on the GPU)."""
+    grads = list(grads)
+    device, ptrs, counts, dtypes = _tensor_list(grads)
+    norm = _norm_out(norm, device)
+    with _OnDevice(norm.device):
+        st = lib().flce_clip_grad_norm(ptrs, _out_list(outs, grads, device), counts, dtypes, len(grads),
+                                       _norm_type(norm_type), float(max_norm), norm.data_ptr(),
+                                       *_workspace_args(workspace), _stream_handle(stream, norm.device))
+    _check(st, "flce_clip_grad_norm")
+    return norm
 
 
 CE_NOALLOC_MAX_ROWS = 65536

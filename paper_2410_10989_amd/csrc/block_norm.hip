@@ -1,0 +1,367 @@
+// C ABI of the norms before and after a block (see block_norm.h): argument checks, shapes of the kernels,
+// plan of the backward's sums over rows, launches.
+#include "block_norm.h"
+
+#include <algorithm>
+
+#include "flce_host.h"
+
+using namespace flce;
+
+namespace {
+
+constexpr int64_t BN_MAX_H = (int64_t)1 << 24;      // keeps launches and column numbers within 32 bits
+constexpr int64_t BN_GRID_X = (int64_t)1 << 20;     // workgroups along x, the rest along y
+constexpr int BN_CU_THREADS = 1024;                 // threads per CU that the backward is launched for
+constexpr int BN_CUS = 256;
+
+size_t bn_elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
+
+// A strided matrix in memory.
+struct Span {
+    const char* p;
+    size_t pitch, width;   // bytes from row to row, bytes of a row
+    int64_t rows;
+};
+Span span(const void* p, int64_t ld, int64_t rows, int64_t H, size_t es) {
+    return {static_cast<const char*>(p), (size_t)ld * es, (size_t)H * es, rows};
+}
+// Whether two of them share a byte.  Column windows of one wider buffer (equal pitch) may interleave; with
+// different pitches any common stretch of addresses counts.
+bool overlap(const Span& a, const Span& b) {
+    if (!a.p || !b.p) return false;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+    const uintptr_t a1 = a0 + (a.rows - 1) * a.pitch + a.width, b1 = b0 + (b.rows - 1) * b.pitch + b.width;
+    if (a1 <= b0 || b1 <= a0) return false;
+    if (a.pitch != b.pitch || a.rows == 1 || b.rows == 1) return true;
+    const size_t off = b0 >= a0 ? (b0 - a0) % a.pitch : (a.pitch - (a0 - b0) % a.pitch) % a.pitch;
+    return off < a.width || a.pitch - off < b.width;
+}
+bool same(const Span& a, const Span& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1); }
+
+struct Strides {
+    int64_t x, y, h, n, gate, dx, dy, dh, dn, dgate;
+};
+
+int check_common(const flce_block_norm* b, Strides* st, int64_t* gate_rows) {
+    if (!b) return FLCE_ERR_NULL;
+    if (b->size != sizeof(flce_block_norm)) return FLCE_ERR_ARG;
+    if (b->dtype != FLCE_F32 && b->dtype != FLCE_BF16) return FLCE_ERR_DTYPE;
+    if (b->rows < 1 || b->rows > MAX_DIM || b->H < 1 || b->H > BN_MAX_H) return FLCE_ERR_SHAPE;
+    if (b->gate_act < FLCE_GATE_LINEAR || b->gate_act > FLCE_GATE_TANH) return FLCE_ERR_ARG;
+    if (b->rows_per_gate < 0 || b->rows_per_gate > MAX_DIM) return FLCE_ERR_ARG;
+    if (!(b->eps >= 0.0f) || b->eps - b->eps != 0.0f || b->scale - b->scale != 0.0f) return FLCE_ERR_ARG;
+    *gate_rows = b->rows_per_gate ? (b->rows + b->rows_per_gate - 1) / b->rows_per_gate : 1;
+    const int64_t given[] = {b->ldx, b->ldy, b->ldh, b->ldn, b->ldgate, b->lddx, b->lddy, b->lddh, b->lddn, b->lddgate};
+    int64_t* to[] = {&st->x, &st->y, &st->h, &st->n, &st->gate, &st->dx, &st->dy, &st->dh, &st->dn, &st->dgate};
+    for (int i = 0; i < 10; ++i) {
+        const bool one = (i == 4 || i == 9) ? *gate_rows == 1 : b->rows == 1;   // (a single row has no stride)
+        if (given[i] && !one && (given[i] < b->H || given[i] > MAX_DIM * 4)) return FLCE_ERR_SHAPE;
+        *to[i] = given[i] && !one ? given[i] : b->H;
+    }
+    return FLCE_OK;
+}
+
+// The register forms: TPR threads per row with E elements each (dividing a row by 8 elements per thread keeps
+// the backward's three sets of sums and four streams within the registers of two workgroups per CU).
+struct BnShape {
+    int tpr, e;   // tpr = 0: the long form
+};
+BnShape bn_shape(int64_t H, bool backward) {
+    for (const int tpr : {16, 64, 128, 256, 512})
+        if (H <= tpr * 8) return {tpr, 8};
+    if (H <= 512 * 16) return {512, 16};
+    if (H <= 1024 * 16 && !backward) return {1024, 16};
+    return {0, 0};
+}
+int bn_groups(const BnShape& s) { return s.tpr && s.tpr < 256 ? 256 / s.tpr : 1; }
+int bn_threads(const BnShape& s) { return s.tpr ? std::max(256, s.tpr) : BN_LONG_THREADS; }
+
+// How the backward deals rows to workgroups, and where its partial sums lie (floats from the workspace's start).
+struct BnPlan {
+    int64_t blocks, segments, parts, per;
+    bool direct;   // a segment holds all rows of its gate row
+    size_t off_post, off_gate, total_bytes;
+};
+
+// per: rows per gate row where rows share one, else all rows; gate_sum: its gradient is wanted.
+BnPlan bn_plan_for(int64_t rows, int64_t H, int64_t per, bool pre, bool post, bool gate_sum, int64_t target) {
+    const BnShape s = bn_shape(H, true);
+    const int64_t groups = bn_groups(s);
+    BnPlan p{};
+    p.per = std::min(per, rows);
+    const int64_t G = (rows + p.per - 1) / p.per;
+    p.parts = 1;
+    if (G == 1) {
+        p.parts = std::max<int64_t>(1, std::min(target, (rows + groups - 1) / groups));
+    } else if (G < target) {
+        // rounds of segments over the workgroups times the steps of one (a step is `groups` rows; writing a
+        // segment's sums counts as one)
+        int64_t best = INT64_MAX;
+        for (int64_t c = 1; c <= std::min<int64_t>(p.per, 4 * ((target + G - 1) / G)); ++c) {
+            const int64_t cost = ((G * c + target - 1) / target) * (((p.per + c - 1) / c + groups - 1) / groups + 1);
+            if (cost < best) {
+                best = cost;
+                p.parts = c;
+            }
+        }
+    }
+    p.segments = G * p.parts;
+    p.blocks = std::min(p.segments, target);
+    p.direct = gate_sum && p.parts == 1;
+    const int64_t gate_rows = !gate_sum ? 0 : p.direct ? (s.tpr ? 0 : p.blocks) : p.segments;
+    size_t at = 0;
+    auto take = [&](int64_t n) {
+        const size_t here = at;
+        at += (size_t)n * (size_t)H;
+        return here;
+    };
+    take(pre ? p.blocks : 0);
+    p.off_post = take(post ? p.blocks : 0);
+    p.off_gate = take(gate_rows);
+    p.total_bytes = at * sizeof(float);
+    return p;
+}
+// The plan of the whole chip, or the largest power-of-two fraction of it whose sums fit `cap` bytes.
+BnPlan bn_plan(int64_t rows, int64_t H, int64_t per, bool pre, bool post, bool gate_sum, size_t cap) {
+    int64_t target = (int64_t)BN_CUS * BN_CU_THREADS / bn_threads(bn_shape(H, true));
+    for (;; target /= 2) {
+        const BnPlan p = bn_plan_for(rows, H, per, pre, post, gate_sum, target);
+        if (p.total_bytes <= cap || target == 1) return p;
+    }
+}
+
+template <typename T, int TPR, int E>
+void launch_fwd(const BnArgs& a, hipStream_t s) {
+    constexpr int NV = E / RowVec<T>::N, GROUPS = TPR < 256 ? 256 / TPR : 1;
+    const int64_t blocks = (a.rows + GROUPS - 1) / GROUPS;
+    const dim3 grid((unsigned)std::min(blocks, BN_GRID_X), (unsigned)((blocks + BN_GRID_X - 1) / BN_GRID_X));
+    const dim3 block(TPR < 256 ? 256 : TPR);
+#define BN_FWD(POST, GATE) hipLaunchKernelGGL((block_norm_fwd_kernel<T, TPR, NV, POST, GATE>), grid, block, 0, s, a)
+    if (a.gpost) {
+        if (a.gate) BN_FWD(true, true); else BN_FWD(true, false);
+    } else {
+        if (a.gate) BN_FWD(false, true); else BN_FWD(false, false);
+    }
+#undef BN_FWD
+}
+template <typename T, int TPR, int E>
+void launch_bwd(const BnArgs& a, const dim3& grid, hipStream_t s) {
+    constexpr int NV = E / RowVec<T>::N;
+    const dim3 block(TPR < 256 ? 256 : TPR);
+#define BN_BWD(POST, GATE) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TPR, NV, POST, GATE>), grid, block, 0, s, a)
+#define BN_BWD_GATE(POST)                             \
+    do {                                              \
+        if (!a.gate) BN_BWD(POST, BN_GATE_NONE);      \
+        else if (a.by_row) BN_BWD(POST, BN_GATE_ROW); \
+        else BN_BWD(POST, BN_GATE_SUM);               \
+    } while (0)
+    if (a.gpost) BN_BWD_GATE(true); else BN_BWD_GATE(false);
+#undef BN_BWD_GATE
+#undef BN_BWD
+}
+template <typename T>
+int run_fwd(const BnArgs& a, hipStream_t s) {
+    const BnShape sh = bn_shape(a.H, false);
+    if (sh.e == 8) {
+        switch (sh.tpr) {
+            case 16: launch_fwd<T, 16, 8>(a, s); break;
+            case 64: launch_fwd<T, 64, 8>(a, s); break;
+            case 128: launch_fwd<T, 128, 8>(a, s); break;
+            case 256: launch_fwd<T, 256, 8>(a, s); break;
+            default: launch_fwd<T, 512, 8>(a, s); break;
+        }
+    } else if (sh.tpr == 512) {
+        launch_fwd<T, 512, 16>(a, s);
+    } else if (sh.tpr == 1024) {
+        launch_fwd<T, 1024, 16>(a, s);
+    } else {
+        const int64_t rows = a.rows;
+        hipLaunchKernelGGL((block_norm_fwd_long<T>), dim3((unsigned)std::min(rows, BN_GRID_X), (unsigned)((rows + BN_GRID_X - 1) / BN_GRID_X)),
+                           dim3(BN_LONG_THREADS), 0, s, a);
+    }
+    HIP_TRY(hipGetLastError());
+    return FLCE_OK;
+}
+template <typename T>
+int run_bwd(const BnArgs& a, const BnPlan& p, void* dgamma_pre, void* dgamma_post, hipStream_t s) {
+    const BnShape sh = bn_shape(a.H, true);
+    const dim3 grid((unsigned)p.blocks);
+    if (sh.e == 8) {
+        switch (sh.tpr) {
+            case 16: launch_bwd<T, 16, 8>(a, grid, s); break;
+            case 64: launch_bwd<T, 64, 8>(a, grid, s); break;
+            case 128: launch_bwd<T, 128, 8>(a, grid, s); break;
+            case 256: launch_bwd<T, 256, 8>(a, grid, s); break;
+            default: launch_bwd<T, 512, 8>(a, grid, s); break;
+        }
+    } else if (sh.tpr) {
+        launch_bwd<T, 512, 16>(a, grid, s);
+    } else {
+        hipLaunchKernelGGL((block_norm_bwd_long<T>), grid, dim3(BN_LONG_THREADS), 0, s, a);
+    }
+    HIP_TRY(hipGetLastError());
+    BnSums b{};
+    int set = 0, rows = 0;
+    auto add = [&](const float* part, void* out, int64_t ld, int64_t parts, int64_t out_rows) {
+        b.part[set] = part;
+        b.out[set] = out;
+        b.ld[set] = ld;
+        b.parts[set] = (int)parts;
+        b.first[set] = rows;
+        rows += (int)out_rows;
+        ++set;
+    };
+    if (a.part_pre) add(a.part_pre, dgamma_pre, a.H, p.blocks, 1);
+    if (a.part_post) add(a.part_post, dgamma_post, a.H, p.blocks, 1);
+    if (a.part_gate && !p.direct) add(a.part_gate, a.dgate, a.lddgate, p.parts, p.segments / p.parts);
+    if (!rows) return FLCE_OK;
+    for (int i = set; i < 4; ++i) b.first[i] = rows;
+    const int col_blocks = (a.H + BN_SUM_COLS - 1) / BN_SUM_COLS;
+    hipLaunchKernelGGL((bn_sum_partials_kernel<T>), dim3((unsigned)col_blocks, (unsigned)rows), dim3(BN_SUM_COLS * BN_SUM_PARTS),
+                       0, s, b, a.H);
+    HIP_TRY(hipGetLastError());
+    return FLCE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int flce_block_norm_fwd(const void* x, const void* y, const void* gate, const void* gamma_post, const void* gamma_pre,
+                        const flce_block_norm* args, void* h, void* n, void* stream) {
+    Strides ld;
+    int64_t gate_rows;
+    FLCE_TRY(check_common(args, &ld, &gate_rows));
+    const flce_block_norm& b = *args;
+    if ((!x && !y) || (y && !h) || (gamma_pre && !n)) return FLCE_ERR_NULL;
+    if ((!y && (gate || gamma_post || h)) || (!gamma_pre && n) || (!y && !gamma_pre)) return FLCE_ERR_ARG;
+    const size_t es = bn_elem(b.dtype);
+    for (const void* p : {x, y, gate, gamma_post, gamma_pre, static_cast<const void*>(h), static_cast<const void*>(n)})
+        if (p && !aligned(p, es)) return FLCE_ERR_ALIGN;
+    const Span in[] = {span(x, ld.x, b.rows, b.H, es), span(y, ld.y, b.rows, b.H, es), span(gate, ld.gate, gate_rows, b.H, es),
+                       span(gamma_post, b.H, 1, b.H, es), span(gamma_pre, b.H, 1, b.H, es)};
+    const Span oh = span(h, ld.h, b.rows, b.H, es), on = span(n, ld.n, b.rows, b.H, es);
+    if (overlap(oh, on)) return FLCE_ERR_ARG;
+    for (const Span& i : in) {
+        if (overlap(oh, i) && !(i.p == in[0].p && same(oh, in[0]))) return FLCE_ERR_ARG;
+        if (overlap(on, i)) return FLCE_ERR_ARG;
+    }
+    BnArgs a{};
+    a.x = x;
+    a.y = y;
+    a.gate = gate;
+    a.gpost = gamma_post;
+    a.gpre = gamma_pre;
+    a.out_h = h;
+    a.out_n = n;
+    a.ldx = ld.x;
+    a.ldy = ld.y;
+    a.ldgate = ld.gate;
+    a.ldh = ld.h;
+    a.ldn = ld.n;
+    a.rows = (int)b.rows;
+    a.H = (int)b.H;
+    a.per = (int)(b.rows_per_gate ? b.rows_per_gate : MAX_DIM);
+    a.act = b.gate_act;
+    a.scale = b.scale;
+    a.eps = b.eps;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return b.dtype == FLCE_F32 ? run_fwd<float>(a, s) : run_fwd<bf16_t>(a, s);
+}
+
+int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const void* y, const void* gate,
+                        const void* gamma_post, const void* gamma_pre, const flce_block_norm* args, void* dx, void* dy,
+                        void* dgate, void* dgamma_post, void* dgamma_pre, void* stream) {
+    Strides ld;
+    int64_t gate_rows;
+    FLCE_TRY(check_common(args, &ld, &gate_rows));
+    const flce_block_norm& b = *args;
+    if ((gamma_pre && (!h || !dn)) || (!gamma_pre && !dh) || ((gate || gamma_post || dy) && !y)) return FLCE_ERR_NULL;
+    if ((!gamma_pre && (h || dn || dgamma_pre)) || (!gate && dgate) || (!gamma_post && dgamma_post) ||
+        (!dx && !dy && !dgate && !dgamma_post && !dgamma_pre))
+        return FLCE_ERR_ARG;
+    const size_t es = bn_elem(b.dtype);
+    const Span in[] = {span(dh, ld.dh, b.rows, b.H, es),        span(h, ld.h, b.rows, b.H, es),
+                       span(dn, ld.dn, b.rows, b.H, es),        span(y, ld.y, b.rows, b.H, es),
+                       span(gate, ld.gate, gate_rows, b.H, es), span(gamma_post, b.H, 1, b.H, es),
+                       span(gamma_pre, b.H, 1, b.H, es)};
+    const Span out[] = {span(dx, ld.dx, b.rows, b.H, es), span(dy, ld.dy, b.rows, b.H, es),
+                        span(dgate, ld.dgate, gate_rows, b.H, es), span(dgamma_post, b.H, 1, b.H, es),
+                        span(dgamma_pre, b.H, 1, b.H, es)};
+    for (const Span& i : in)
+        if (i.p && !aligned(i.p, es)) return FLCE_ERR_ALIGN;
+    for (const Span& o : out)
+        if (o.p && !aligned(o.p, es)) return FLCE_ERR_ALIGN;
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return FLCE_ERR_ARG;
+        for (int j = 0; j < 7; ++j)
+            if (overlap(out[i], in[j]) && !(i == 0 && j == 0 && same(out[0], in[0]))) return FLCE_ERR_ARG;
+    }
+    if (b.workspace && !aligned(b.workspace, 256)) return FLCE_ERR_ALIGN;
+
+    const bool by_row = gate && b.rows_per_gate == 1 && b.rows > 1;
+    const bool sums = dgate && !by_row;
+    const int64_t per = b.rows_per_gate ? b.rows_per_gate : b.rows;
+    size_t cap = SIZE_MAX;
+    if (b.workspace) cap = b.workspace_bytes;
+    else {
+        size_t lent = 0;
+        FLCE_TRY(shared_workspace_lent(&lent));
+        if (lent) cap = lent;
+    }
+    const BnPlan p = bn_plan(b.rows, b.H, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
+    if (p.total_bytes > cap) return FLCE_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(b.workspace);
+    if (!ws && p.total_bytes) FLCE_TRY(shared_workspace(p.total_bytes, &ws));
+    float* f = reinterpret_cast<float*>(ws);
+    BnArgs a{};
+    a.h = h;
+    a.dn = dn;
+    a.dh = dh;
+    a.y = y;
+    a.gate = gate;
+    a.gpost = gamma_post;
+    a.gpre = gamma_pre;
+    a.dx = dx;
+    a.dy = dy;
+    a.dgate = dgate;
+    a.ldh = ld.h;
+    a.lddn = ld.dn;
+    a.lddh = ld.dh;
+    a.ldy = ld.y;
+    a.ldgate = ld.gate;
+    a.lddx = ld.dx;
+    a.lddy = ld.dy;
+    a.lddgate = ld.dgate;
+    a.part_pre = dgamma_pre ? f : nullptr;
+    a.part_post = dgamma_post ? f + p.off_post : nullptr;
+    a.part_gate = sums && (!p.direct || !bn_shape(b.H, true).tpr) ? f + p.off_gate : nullptr;
+    a.rows = (int)b.rows;
+    a.H = (int)b.H;
+    a.per = (int)p.per;
+    a.act = b.gate_act;
+    a.scale = b.scale;
+    a.eps = b.eps;
+    a.segments = (int)p.segments;
+    a.parts = (int)p.parts;
+    a.by_row = by_row;
+    a.gate_direct = p.direct;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return b.dtype == FLCE_F32 ? run_bwd<float>(a, p, dgamma_pre, dgamma_post, s)
+                               : run_bwd<bf16_t>(a, p, dgamma_pre, dgamma_post, s);
+}
+
+size_t flce_block_norm_workspace_bytes(const flce_block_norm* args) {
+    Strides ld;
+    int64_t gate_rows;
+    if (check_common(args, &ld, &gate_rows) != FLCE_OK) return 0;
+    const int64_t per = args->rows_per_gate ? args->rows_per_gate : args->rows;
+    const size_t with_gate = bn_plan(args->rows, args->H, per, true, true, true, SIZE_MAX).total_bytes;
+    // (a gate row per row, or no gate: the gammas' sums alone, in a plan of their own)
+    const size_t without = bn_plan(args->rows, args->H, args->rows, true, true, false, SIZE_MAX).total_bytes;
+    return std::max(with_gate, without);
+}
+
+}  // extern "C"

@@ -9,6 +9,7 @@
 #include "../../include/flce.h"
 #include "compact.h"
 #include "flce_device.h"
+#include "flce_host.h"
 #include "gemm_bf16_nt.h"
 #include "gemm_generic.h"
 #include "mfma_ceiling.h"
@@ -32,7 +33,6 @@ static __device__ done_t ce_done[2 * DONE_WORDS];
 namespace {
 
 constexpr int MAX_DEVICES = 64;
-constexpr int64_t MAX_DIM = (int64_t)1 << 30;      // per-dimension limit, keeps int tile math safe
 constexpr int64_t CE_ROWS_PER_LAUNCH = 65536;
 constexpr int64_t SEL_IN_LOGITS_ROWS = TileRows<4>::MAX_ROWS, SEL_ROWS_IN_LOGITS = 8;   // 2048
 constexpr int RIDE_BLOCKS = 1024;   // finish_dx as workgroups of the dW launch: at most this many
@@ -134,16 +134,6 @@ struct ScopedKernelTimer {
         g_records.push_back(rec);
     }
 };
-
-#define HIP_TRY(expr)                          \
-    do {                                       \
-        if ((expr) != hipSuccess) {            \
-            (void)hipGetLastError();           \
-            return FLCE_ERR_HIP;               \
-        }                                      \
-    } while (0)
-
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // The device's shared workspace: the lent buffer, or memory of the library's own that grows as needed.
 // last = false: the caller has a plan that needs less, so an allocation that found too little memory is
@@ -375,12 +365,6 @@ int launch_loss(const float* row_loss, int64_t rows, DeviceHeader* hdr, const Lo
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
 }
-
-#define FLCE_TRY(expr)                 \
-    do {                               \
-        const int rc_ = (expr);        \
-        if (rc_ != FLCE_OK) return rc_; \
-    } while (0)
 
 static_assert(MAX_HEADS * sizeof(DeviceHeader) <= 256, "header slot too small");
 
@@ -989,6 +973,9 @@ int multihead_fwd_bwd(const Settings& st, const void* X, const void* const* W, c
 }
 
 }  // namespace
+
+int flce::shared_workspace(size_t need, char** out) { return acquire_workspace(need, out); }
+int flce::shared_workspace_lent(size_t* bytes) { return lent_workspace(bytes); }
 
 extern "C" {
 
