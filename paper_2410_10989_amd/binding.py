@@ -6,6 +6,7 @@ There is no fallback: if the library is missing or a call fails, this raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -329,45 +330,47 @@ class FlceBlockNorm(ctypes.Structure):
 GATE_ACTS = ("linear", "sigmoid", "silu", "tanh")
 
 
-def _block_norm_args(like, gate, gate_act, rows_per_gate, scale, eps, workspace=None) -> FlceBlockNorm:
-    if like.dim() != 2:
-        raise ValueError("expected [rows, H]")
-    if gate_act not in GATE_ACTS:
-        raise ValueError(f"gate_act must be one of {GATE_ACTS}")
-    rows, H = like.shape
-    rows_per_gate = int(rows_per_gate)
-    if rows_per_gate < 0:
-        raise ValueError("rows_per_gate must be 0 (one gate row for all) or positive")
-    if gate is not None:
-        want = ((rows + rows_per_gate - 1) // rows_per_gate, H) if rows_per_gate else (H,)
-        if gate.shape != want:
-            raise ValueError(f"expected gate {want}")
-    b = FlceBlockNorm()
-    b.size, b.rows, b.H, b.dtype = ctypes.sizeof(FlceBlockNorm), rows, H, _dtype_code(like)
-    b.gate_act, b.rows_per_gate, b.scale, b.eps = GATE_ACTS.index(gate_act), rows_per_gate, float(scale), float(eps)
-    if workspace is not None:
-        b.workspace = _dev_ptr(workspace, "workspace")
-        b.workspace_bytes = workspace.numel() * workspace.element_size()
-    return b
-
-
-def _rows_ptr(t, name, like, shape, args=None, ld=None) -> int | None:
-    """The pointer of a matrix whose rows may be apart (its stride goes to args.ld) or, without ld, a vector."""
-    if t is None:
-        return None
+def _refuse(t, name, like, shape):
     if t.device != like.device:
         raise ValueError(f"{name} must live on {like.device}")
     if t.dtype != like.dtype:
         raise TypeError(f"{name} must have dtype {like.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}")
+    raise ValueError(f"{name} must be {tuple(shape)}")
+
+
+def _rows_ptr(t, name, like, shape):
+    """Pointer and row stride (0: dense) of a matrix whose rows may be apart, or of a vector."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype is not like.dtype or t.get_device() != like.get_device():
+        _refuse(t, name, like, shape)
+    if t.is_contiguous():
+        return t.data_ptr(), 0
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} must have unit column stride")
-    if ld is not None and t.dim() == 2 and t.shape[0] > 1:
-        if t.stride(0) < t.shape[1]:
-            raise ValueError(f"the rows of {name} must not overlap")
-        setattr(args, ld, t.stride(0))
-    return t.data_ptr()
+    if t.dim() == 1 or t.shape[0] == 1:
+        return t.data_ptr(), 0
+    if t.stride(0) < t.shape[1]:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return t.data_ptr(), t.stride(0)
+
+
+def _gate_shape(gate, shape, rows_per_gate):
+    if rows_per_gate < 0:
+        raise ValueError("rows_per_gate must be 0 (one gate row for all) or positive")
+    if gate is None:
+        return shape
+    return ((shape[0] + rows_per_gate - 1) // rows_per_gate, shape[1]) if rows_per_gate else shape[1:]
+
+
+def _gate_act(kind) -> int:
+    try:
+        return GATE_ACTS.index(kind)
+    except ValueError:
+        raise ValueError(f"gate_act must be one of {GATE_ACTS}") from None
+
+
+_BLOCK_NORM_BYTES = ctypes.sizeof(FlceBlockNorm)
 
 
 def flce_block_norm_fwd(x, y=None, gamma_pre=None, gamma_post=None, gate=None, gate_act="linear", rows_per_gate=0,
@@ -383,19 +386,25 @@ def flce_block_norm_fwd(x, y=None, gamma_pre=None, gamma_post=None, gate=None, g
         raise ValueError("x or y is needed")
     if not like.is_cuda:
         raise ValueError("x and y must live on the GPU")
-    b = _block_norm_args(like, gate, gate_act, rows_per_gate, scale, eps)
-    shape, vec = like.shape, like.shape[1:]
+    shape = like.shape
+    if len(shape) != 2:
+        raise ValueError("expected [rows, H]")
+    code, vec, device = _dtype_code(like), shape[1:], like.device
     if y is not None and h is None:
-        h = torch.empty(shape, dtype=like.dtype, device=like.device)
+        h = torch.empty_like(like)   # (dense, also where `like` is not; a third of the time of torch.empty)
     if gamma_pre is not None and n is None:
-        n = torch.empty(shape, dtype=like.dtype, device=like.device)
-    with _OnDevice(like.device):
-        st = lib().flce_block_norm_fwd(
-            _rows_ptr(x, "x", like, shape, b, "ldx"), _rows_ptr(y, "y", like, shape, b, "ldy"),
-            _rows_ptr(gate, "gate", like, gate.shape if gate is not None else vec, b, "ldgate"),
-            _rows_ptr(gamma_post, "gamma_post", like, vec), _rows_ptr(gamma_pre, "gamma_pre", like, vec),
-            ctypes.byref(b), _rows_ptr(h, "h", like, shape, b, "ldh"), _rows_ptr(n, "n", like, shape, b, "ldn"),
-            _stream_handle(stream, like.device))
+        n = torch.empty_like(like)
+    px, ldx = _rows_ptr(x, "x", like, shape)
+    py, ldy = _rows_ptr(y, "y", like, shape)
+    pg, ldg = _rows_ptr(gate, "gate", like, _gate_shape(gate, shape, rows_per_gate))
+    ph, ldh = _rows_ptr(h, "h", like, shape)
+    pn, ldn = _rows_ptr(n, "n", like, shape)
+    args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), rows_per_gate, scale, eps,
+                         ldx, ldy, ldh, ldn, ldg)
+    with _OnDevice(device):
+        st = lib().flce_block_norm_fwd(px, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec)[0],
+                                       _rows_ptr(gamma_pre, "gamma_pre", like, vec)[0], ctypes.byref(args), ph, pn,
+                                       _stream_handle(stream, device))
     _check(st, "flce_block_norm_fwd")
     return h, n
 
@@ -416,33 +425,40 @@ def flce_block_norm_bwd(h=None, dn=None, dh=None, y=None, gamma_pre=None, gamma_
         raise ValueError("dn and dh must live on the GPU")
     if flags & ~(SKIP_DX | SKIP_DW):
         raise ValueError("unknown flags")
-    b = _block_norm_args(like, gate, gate_act, rows_per_gate, scale, eps, workspace)
-    shape, vec = like.shape, like.shape[1:]
+    shape = like.shape
+    if len(shape) != 2:
+        raise ValueError("expected [rows, H]")
+    code, vec, device = _dtype_code(like), shape[1:], like.device
+    gshape = _gate_shape(gate, shape, rows_per_gate)
     want_dx, want_dw = not flags & SKIP_DX, not flags & SKIP_DW
-
-    def output(given, wanted, size):
-        if not wanted:
-            return None
-        return given if given is not None else torch.empty(size, dtype=like.dtype, device=like.device)
-
     passed_on = want_dx and gamma_pre is None and dx is None
-    dx = output(dx, want_dx and not passed_on, shape)
-    dy = output(dy, y is not None, shape)
-    dgate = output(dgate, want_dw and gate is not None, gate.shape if gate is not None else None)
-    dgamma_post = output(dgamma_post, want_dw and gamma_post is not None, vec)
-    dgamma_pre = output(dgamma_pre, want_dw and gamma_pre is not None, vec)
-    gshape = gate.shape if gate is not None else vec
     if passed_on and y is None:
         raise ValueError("without y and gamma_pre there is nothing to compute")
-    with _OnDevice(like.device):
-        st = lib().flce_block_norm_bwd(
-            _rows_ptr(h, "h", like, shape, b, "ldh"), _rows_ptr(dn, "dn", like, shape, b, "lddn"),
-            _rows_ptr(dh, "dh", like, shape, b, "lddh"), _rows_ptr(y, "y", like, shape, b, "ldy"),
-            _rows_ptr(gate, "gate", like, gshape, b, "ldgate"),
-            _rows_ptr(gamma_post, "gamma_post", like, vec), _rows_ptr(gamma_pre, "gamma_pre", like, vec),
-            ctypes.byref(b), _rows_ptr(dx, "dx", like, shape, b, "lddx"), _rows_ptr(dy, "dy", like, shape, b, "lddy"),
-            _rows_ptr(dgate, "dgate", like, gshape, b, "lddgate"), _rows_ptr(dgamma_post, "dgamma_post", like, vec),
-            _rows_ptr(dgamma_pre, "dgamma_pre", like, vec), _stream_handle(stream, like.device))
+
+    def output(given, of, wanted, name, size):   # of: the input it is the gradient of
+        if of is None or not wanted:
+            return None, None, 0
+        if given is None:
+            given = torch.empty_like(of)
+            return given, given.data_ptr(), 0
+        return given, *_rows_ptr(given, name, like, size)
+
+    dx, pdx, lddx = output(dx, like, want_dx and not passed_on, "dx", shape)
+    dy, pdy, lddy = output(dy, y, True, "dy", shape)
+    dgate, pdg, lddg = output(dgate, gate, want_dw, "dgate", gshape)
+    dgamma_post, pdpost, _ = output(dgamma_post, gamma_post, want_dw, "dgamma_post", vec)
+    dgamma_pre, pdpre, _ = output(dgamma_pre, gamma_pre, want_dw, "dgamma_pre", vec)
+    ph, ldh = _rows_ptr(h, "h", like, shape)
+    pdn, lddn = _rows_ptr(dn, "dn", like, shape)
+    pdh, lddh = _rows_ptr(dh, "dh", like, shape)
+    py, ldy = _rows_ptr(y, "y", like, shape)
+    pg, ldg = _rows_ptr(gate, "gate", like, gshape)
+    args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), rows_per_gate, scale, eps,
+                         0, ldy, ldh, 0, ldg, lddx, lddy, lddh, lddn, lddg, *_workspace_args(workspace))
+    with _OnDevice(device):
+        st = lib().flce_block_norm_bwd(ph, pdn, pdh, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec)[0],
+                                       _rows_ptr(gamma_pre, "gamma_pre", like, vec)[0], ctypes.byref(args), pdx, pdy, pdg,
+                                       pdpost, pdpre, _stream_handle(stream, device))
     _check(st, "flce_block_norm_bwd")
     return dh if passed_on else dx, dy, dgate, dgamma_post, dgamma_pre
 
@@ -458,21 +474,28 @@ def flce_block_norm_workspace_bytes(rows, H, dtype, rows_per_gate=0) -> int:
 NORM_TYPES = {2.0: 0, float("inf"): 1}
 
 
-def _tensor_list(grads, device=None):
-    """(device, host arrays of pointers, element counts and dtypes) of a list of dense tensors on one GPU."""
-    n = len(grads)
-    ptrs, counts, dtypes = [], [], []
-    for t in grads:
-        if device is None:
-            device = t.device
-        if t.device != device or device.type != "cuda":
-            raise ValueError("every tensor must live on the same GPU")
-        if not t.is_contiguous():
-            raise ValueError("every tensor must be contiguous")
-        ptrs.append(t.data_ptr())
-        counts.append(t.numel())
-        dtypes.append(_dtype_code(t))
-    return device, (ctypes.c_void_p * n)(*ptrs), (ctypes.c_int64 * n)(*counts), (ctypes.c_int * n)(*dtypes)
+def _tensor_list(grads):
+    """(device, host arrays of pointers, element counts and dtypes) of a list of dense tensors on one GPU.
+    (Attribute by attribute over the whole list: a call over 300 tensors spends most of its time here.)"""
+    T = torch.Tensor
+    if not grads:
+        return None, None, None, None
+    device = grads[0].device
+    index = device.index if device.type == "cuda" else -1
+    if index < 0 or any(map(index.__ne__, map(T.get_device, grads))):
+        raise ValueError("every tensor must live on the same GPU")
+    if not all(map(T.is_contiguous, grads)):
+        raise ValueError("every tensor must be contiguous")
+    try:
+        dtypes = array.array("i", map(_DTYPES.__getitem__, map(T.dtype.__get__, grads)))
+    except KeyError as e:
+        raise TypeError(f"unsupported dtype {e.args[0]}; use float32 or bfloat16") from None
+    return device, array.array("Q", map(T.data_ptr, grads)), array.array("q", map(T.numel, grads)), dtypes
+
+
+def _at(a):
+    """The address of an array's elements."""
+    return a.buffer_info()[0] if a is not None else None
 
 
 def _norm_out(norm, device):
@@ -492,15 +515,14 @@ def _norm_type(norm_type) -> int:
         raise ValueError("norm_type must be 2 or inf") from None
 
 
-def _out_list(outs, grads, device):
+def _out_list(outs, device, counts, dtypes):
     if outs is None:
         return None
-    if len(outs) != len(grads):
-        raise ValueError("outs must hold one tensor per gradient")
-    for o, g in zip(outs, grads):
-        if o.shape != g.shape or o.dtype != g.dtype:
-            raise ValueError("every out must match its gradient in shape and dtype")
-    return _tensor_list(outs, device)[1]
+    outs = list(outs)
+    out_device, ptrs, out_counts, out_dtypes = _tensor_list(outs)
+    if (out_device, out_counts, out_dtypes) != (device, counts, dtypes):
+        raise ValueError("outs must hold one tensor per gradient, of its size and dtype and on its GPU")
+    return ptrs
 
 
 def _workspace_args(workspace):
@@ -515,7 +537,7 @@ def flce_grad_norm(grads, norm_type=2.0, norm=None, workspace=None, stream=None)
     device, ptrs, counts, dtypes = _tensor_list(grads)
     norm = _norm_out(norm, device)
     with _OnDevice(norm.device):
-        st = lib().flce_grad_norm(ptrs, counts, dtypes, len(grads), _norm_type(norm_type), norm.data_ptr(),
+        st = lib().flce_grad_norm(_at(ptrs), _at(counts), _at(dtypes), len(grads), _norm_type(norm_type), norm.data_ptr(),
                                   *_workspace_args(workspace), _stream_handle(stream, norm.device))
     _check(st, "flce_grad_norm")
     return norm
@@ -527,8 +549,9 @@ def flce_grad_clip(grads, norm, max_norm, outs=None, stream=None):
     grads = list(grads)
     device, ptrs, counts, dtypes = _tensor_list(grads)
     norm = _norm_out(norm, device)
+    to = _out_list(outs, device, counts, dtypes)
     with _OnDevice(norm.device):
-        st = lib().flce_grad_clip(ptrs, _out_list(outs, grads, device), counts, dtypes, len(grads), norm.data_ptr(),
+        st = lib().flce_grad_clip(_at(ptrs), _at(to), _at(counts), _at(dtypes), len(grads), norm.data_ptr(),
                                   float(max_norm), _stream_handle(stream, norm.device))
     _check(st, "flce_grad_clip")
 
@@ -538,8 +561,9 @@ def flce_clip_grad_norm(grads, max_norm, norm_type=2.0, outs=None, norm=None, wo
     grads = list(grads)
     device, ptrs, counts, dtypes = _tensor_list(grads)
     norm = _norm_out(norm, device)
+    to = _out_list(outs, device, counts, dtypes)
     with _OnDevice(norm.device):
-        st = lib().flce_clip_grad_norm(ptrs, _out_list(outs, grads, device), counts, dtypes, len(grads),
+        st = lib().flce_clip_grad_norm(_at(ptrs), _at(to), _at(counts), _at(dtypes), len(grads),
                                        _norm_type(norm_type), float(max_norm), norm.data_ptr(),
                                        *_workspace_args(workspace), _stream_handle(stream, norm.device))
     _check(st, "flce_clip_grad_norm")

@@ -45,12 +45,15 @@ struct BnArgs {
     int gate_direct;   // a segment is all rows of its gate row: dgate is written at once
 };
 
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // at any element
+
+// Vector v of a row: whole for v < nfull; vector nfull has rem elements.
 template <typename T>
 __device__ __forceinline__ u32x4 bn_load(const T* row, int v, int nfull, int rem) {
     constexpr int N = RowVec<T>::N;
     u32x4 r = {0u, 0u, 0u, 0u};
     if (v < nfull) {
-        __builtin_memcpy(&r, row + (int64_t)v * N, 16);
+        r = *reinterpret_cast<const u32x4_any*>(row + (int64_t)v * N);
     } else if (v == nfull && rem) {
         const T* p = row + (int64_t)v * N;
         float f[N];
@@ -60,12 +63,13 @@ __device__ __forceinline__ u32x4 bn_load(const T* row, int v, int nfull, int rem
     }
     return r;
 }
-template <typename T>
+template <typename T, bool NT>
 __device__ __forceinline__ void bn_store(T* row, int v, int nfull, int rem, const float (&f)[RowVec<T>::N]) {
     constexpr int N = RowVec<T>::N;
     if (v < nfull) {
-        const u32x4 r = RowVec<T>::pack(f);
-        __builtin_memcpy(row + (int64_t)v * N, &r, 16);
+        u32x4_any* p = reinterpret_cast<u32x4_any*>(row + (int64_t)v * N);
+        if constexpr (NT) __builtin_nontemporal_store(RowVec<T>::pack(f), p);
+        else *p = RowVec<T>::pack(f);
     } else if (v == nfull && rem) {
         T* p = row + (int64_t)v * N;
 #pragma unroll
@@ -73,10 +77,27 @@ __device__ __forceinline__ void bn_store(T* row, int v, int nfull, int rem, cons
             if (e < rem) p[e] = from_f32<T>(f[e]);
     }
 }
-__device__ __forceinline__ void bn_store_f32(float* row, int64_t j, int n, const float* f, int count) {
+
+// The same for loads that are issued a row ahead (H of at least one vector): putting a partial vector together
+// waits for every load before it, so its place is taken by the 16 bytes that end with the row, and bn_shift_tail
+// moves its elements to the front when the row's turn comes (rows of 4095 bf16: 158 -> 109 us, 8192 of them).
+template <typename T>
+__device__ __forceinline__ u32x4 bn_load_ahead(const T* row, int v, int nvec, int H) {
+    constexpr int N = RowVec<T>::N;
+    u32x4 r = {0u, 0u, 0u, 0u};
+    if (v < nvec) r = *reinterpret_cast<const u32x4_any*>(row + min(v * N, H - N));
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void bn_shift_tail(u32x4& r, int rem) {
+    const int drop = (RowVec<T>::N - rem) * (int)sizeof(T), words = drop / 4, bits = drop % 4 * 8;
+    const u32x4 from = r;
 #pragma unroll
-    for (int e = 0; e < count; ++e)
-        if (j + e < n) row[j + e] = f[e];
+    for (int w = 0; w < 4; ++w) {
+        auto word = [&](int i) { return i == 0 ? from[0] : i == 1 ? from[1] : i == 2 ? from[2] : i == 3 ? from[3] : 0u; };
+        const uint32_t lo = word(w + words), hi = word(w + words + 1);
+        r[w] = bits ? lo >> bits | hi << (32 - bits) : lo;
+    }
 }
 
 // a(g) and a'(g).  exp is taken of -|g| only, and 1 - sigmoid and the derivatives come as products of what
@@ -88,67 +109,104 @@ __device__ __forceinline__ float bn_act(int act, float g) {
     const float sig = g >= 0.f ? d : e * d;
     return act == BN_ACT_SIGMOID ? sig : g * sig;
 }
-__device__ __forceinline__ float bn_act_grad(int act, float g) {
-    if (act == BN_ACT_LINEAR) return 1.0f;
-    if (act == BN_ACT_TANH) {
+__device__ __forceinline__ void bn_act_both(int act, float g, float& a, float& da) {
+    if (act == BN_ACT_LINEAR) {
+        a = g;
+        da = 1.0f;
+    } else if (act == BN_ACT_TANH) {
         const float e = expf(-2.0f * fabsf(g)), d = 1.0f / (1.0f + e);
-        return 4.0f * e * d * d;
+        a = tanhf(g);
+        da = 4.0f * e * d * d;
+    } else {
+        const float e = expf(-fabsf(g)), d = 1.0f / (1.0f + e);
+        const float sig = g >= 0.f ? d : e * d, rest = g >= 0.f ? e * d : d;
+        a = act == BN_ACT_SIGMOID ? sig : g * sig;
+        da = act == BN_ACT_SIGMOID ? sig * rest : sig * (1.0f + g * rest);
     }
-    const float e = expf(-fabsf(g)), d = 1.0f / (1.0f + e);
-    const float sig = g >= 0.f ? d : e * d, rest = g >= 0.f ? e * d : d;
-    return act == BN_ACT_SIGMOID ? sig * rest : sig * (1.0f + g * rest);
 }
 
-// Sum over the TPR threads of a row's group, the same value in every one of them.  slot: LDS of this sum
-// alone (a group of several wavefronts is a whole workgroup), read until the workgroup's next barrier.
-template <int TPR>
-__device__ __forceinline__ float bn_sum(float v, float* slot) {
-#pragma unroll
-    for (int o = (TPR < WAVE ? TPR : WAVE) / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
-    if constexpr (TPR > WAVE) {
-        if ((threadIdx.x & (WAVE - 1)) == 0) slot[threadIdx.x % TPR / WAVE] = v;
-        __syncthreads();
-        v = slot[0];
-#pragma unroll
-        for (int w = 1; w < TPR / WAVE; ++w) v += slot[w];
+template <int CTRL>
+__device__ __forceinline__ float bn_dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// Sum over the aligned group of 16 or 64 lanes, the same bits in every lane: neighbours within a quad, quads and
+// halves of a row of 16 by mirroring, then rows and halves of the wavefront exchanged.
+template <int LANES>
+__device__ __forceinline__ float bn_lane_sum(float v) {
+    static_assert(LANES == 16 || LANES == 64, "");
+    v = bn_dpp_add<0xB1>(v);    // quad_perm 1 0 3 2
+    v = bn_dpp_add<0x4E>(v);    // quad_perm 2 3 0 1
+    v = bn_dpp_add<0x141>(v);   // row_half_mirror
+    v = bn_dpp_add<0x140>(v);   // row_mirror
+    if constexpr (LANES == 64) {
+        const uint32_t a = __float_as_uint(v);
+        const auto p = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        const uint32_t b = __float_as_uint(v);
+        const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+        v = __uint_as_float(q[0]) + __uint_as_float(q[1]);
     }
     return v;
 }
 
-// Forward: a workgroup holds BLOCK / TPR rows.
-template <typename T, int TPR, int NV, bool POST, bool GATE>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_fwd_kernel(BnArgs a) {
-    constexpr int N = RowVec<T>::N, GROUPS = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float red[2][GROUPS][TPR > WAVE ? TPR / WAVE : 1];
-    const int grp = threadIdx.x / TPR, t = threadIdx.x % TPR;
+// K sums over the TPR threads of a row's group, the same values in every one of them.  slot: LDS of these sums
+// alone ([K][TPR / 64]; a group of several wavefronts is a whole workgroup), read until the next barrier.
+template <int TPR, int K>
+__device__ __forceinline__ void bn_sums(float (&v)[K], float* slot) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] = bn_lane_sum<(TPR < WAVE ? TPR : WAVE)>(v[i]);
+    if constexpr (TPR > WAVE) {
+        constexpr int NW = TPR / WAVE;
+        if ((threadIdx.x & (WAVE - 1)) == 0)
+#pragma unroll
+            for (int i = 0; i < K; ++i) slot[i * NW + threadIdx.x / WAVE] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            v[i] = slot[i * NW];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) v[i] += slot[i * NW + w];
+        }
+    }
+}
+template <int TPR>
+__device__ __forceinline__ float bn_sum(float v, float* slot) {
+    float k[1] = {v};
+    bn_sums<TPR, 1>(k, slot);
+    return k[0];
+}
+// Threads of a workgroup, rows of it, and a thread's row in it (the same in a whole wavefront, if it is).
+template <int TPR> constexpr int bn_block = TPR > WAVE ? TPR : 256;
+template <int TPR> constexpr int bn_group_count = bn_block<TPR> / TPR;
+template <int TPR>
+__device__ __forceinline__ int bn_group() {
+    if constexpr (TPR > WAVE) return 0;
+    if constexpr (TPR == WAVE) return __builtin_amdgcn_readfirstlane((int)threadIdx.x / WAVE);
+    return (int)threadIdx.x / TPR;
+}
+
+// Forward: a workgroup holds bn_group_count rows.
+template <typename T, int TPR, int NV, bool POST, bool GATE, bool NT>
+__global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a) {
+    constexpr int N = RowVec<T>::N, GROUPS = bn_group_count<TPR>;
+    __shared__ float red[2][TPR > WAVE ? TPR / WAVE : 1];
+    const int grp = bn_group<TPR>(), t = threadIdx.x % TPR;
+    const float inv_H = 1.0f / (float)a.H;
     const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * GROUPS + grp;
     const bool live = row < a.rows;   // (a group past the last row takes part in the barriers)
     const int nfull = live ? a.H / N : 0, rem = live ? a.H % N : 0;
     const int64_t at = live ? row : 0;
     u32x4 xv[NV], yv[NV], gv[NV], pv[NV], nv[NV];
-    if (a.x) {
-        const T* p = static_cast<const T*>(a.x) + at * a.ldx;
+    auto load = [&](u32x4 (&to)[NV], const void* m, int64_t offset) {
+        const T* p = static_cast<const T*>(m) + offset;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) xv[k] = bn_load(p, t + k * TPR, nfull, rem);
-    }
-    if (a.y) {
-        const T* p = static_cast<const T*>(a.y) + at * a.ldy;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) yv[k] = bn_load(p, t + k * TPR, nfull, rem);
-    }
-    if constexpr (GATE) {
-        const T* p = static_cast<const T*>(a.gate) + (int64_t)((uint32_t)at / (uint32_t)a.per) * a.ldgate;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) gv[k] = bn_load(p, t + k * TPR, nfull, rem);
-    }
-    if constexpr (POST) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) pv[k] = bn_load(static_cast<const T*>(a.gpost), t + k * TPR, nfull, rem);
-    }
-    if (a.gpre) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) nv[k] = bn_load(static_cast<const T*>(a.gpre), t + k * TPR, nfull, rem);
-    }
+        for (int k = 0; k < NV; ++k) to[k] = bn_load(p, t + k * TPR, nfull, rem);
+    };
+    if (a.x) load(xv, a.x, at * a.ldx);
+    if (a.y) load(yv, a.y, at * a.ldy);
+    if constexpr (GATE) load(gv, a.gate, (int64_t)((uint32_t)at / (uint32_t)a.per) * a.ldgate);
+    if constexpr (POST) load(pv, a.gpost, 0);
+    if (a.gpre) load(nv, a.gpre, 0);
     float f[NV][N];
     if (a.y) {
         float q = 1.0f;
@@ -160,8 +218,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_fwd_kernel(B
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < N; ++e) ss += f[k][e] * f[k][e];
-            ss = bn_sum<TPR>(ss, red[0][grp]);
-            q = 1.0f / sqrtf(ss / (float)a.H + a.eps);
+            q = rsqrtf(bn_sum<TPR>(ss, red[0]) * inv_H + a.eps);
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -183,7 +240,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_fwd_kernel(B
         if (a.out_h) {
             T* p = static_cast<T*>(a.out_h) + at * a.ldh;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) bn_store<T>(p, t + k * TPR, nfull, rem, f[k]);
+            for (int k = 0; k < NV; ++k) bn_store<T, NT>(p, t + k * TPR, nfull, rem, f[k]);
         }
     } else {
 #pragma unroll
@@ -195,8 +252,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_fwd_kernel(B
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < N; ++e) ss += f[k][e] * f[k][e];
-        ss = bn_sum<TPR>(ss, red[1][grp]);
-        const float r = 1.0f / sqrtf(ss / (float)a.H + a.eps);
+        const float r = rsqrtf(bn_sum<TPR>(ss, red[1]) * inv_H + a.eps);
         T* p = static_cast<T*>(a.out_n) + at * a.ldn;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -204,7 +260,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_fwd_kernel(B
             RowVec<T>::unpack(nv[k], w);
 #pragma unroll
             for (int e = 0; e < N; ++e) w[e] *= f[k][e] * r;
-            bn_store<T>(p, t + k * TPR, nfull, rem, w);
+            bn_store<T, NT>(p, t + k * TPR, nfull, rem, w);
         }
     }
 }
@@ -247,7 +303,7 @@ __device__ __forceinline__ float bn_long_rstd(const T* row, int nvec, int nfull,
 
 // Rows beyond the register forms: one workgroup per row, swept up to three times; the last sweep alone writes,
 // and a thread writes only where it has read, so that h may lie on x.
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_fwd_long(BnArgs a) {
     constexpr int N = RowVec<T>::N;
     __shared__ float red[BN_LONG_THREADS / WAVE];
@@ -281,51 +337,61 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_fwd_long(BnArgs a)
     for (int v = threadIdx.x; v < nvec; v += BN_LONG_THREADS) {
         float f[N];
         sum_at(v, f);
-        if (a.out_h) bn_store<T>(static_cast<T*>(a.out_h) + row * a.ldh, v, nfull, rem, f);
+        if (a.out_h) bn_store<T, NT>(static_cast<T*>(a.out_h) + row * a.ldh, v, nfull, rem, f);
         if (a.gpre) {
             float w[N];
             RowVec<T>::unpack(bn_load(static_cast<const T*>(a.gpre), v, nfull, rem), w);
 #pragma unroll
             for (int e = 0; e < N; ++e) w[e] *= f[e] * r;
-            bn_store<T>(static_cast<T*>(a.out_n) + row * a.ldn, v, nfull, rem, w);
+            bn_store<T, NT>(static_cast<T*>(a.out_n) + row * a.ldn, v, nfull, rem, w);
         }
     }
 }
 
-// First and last row of a segment.
+// Segment s: the rows row, row + step, ... below end of gate row g, `groups` rows side by side each time.
 struct BnSegment {
-    int g, row, end;
+    int g, row, end, step;
 };
-__device__ __forceinline__ BnSegment bn_segment(const BnArgs& a, int s) {
-    const int g = s / a.parts, p = s - g * a.parts;
-    const int64_t first = (int64_t)g * a.per;
-    const int64_t len = min((int64_t)a.per, (int64_t)a.rows - first);
-    return {g, (int)(first + len * p / a.parts), (int)(first + len * (p + 1) / a.parts)};
+__device__ __forceinline__ BnSegment bn_segment(const BnArgs& a, int s, int groups) {
+    const int g = s / a.parts;
+    const int first = g * a.per;
+    return {g, first + (s - g * a.parts) * groups, first + min(a.per, a.rows - first), a.parts * groups};
 }
+
+// A thread's part of a row of every stream the backward reads.
+template <int NV>
+struct BnRow {
+    u32x4 h[NV], dn[NV], y[NV], dh[NV], gate[NV];
+};
 
 // Backward: workgroup b takes segments b, b + gridDim.x, ...; its GROUPS rows at a time.  The sums over rows
 // stay in registers: the gammas' until the workgroup's last row, a shared gate's until its segment's; then the
 // groups of a workgroup add theirs up in a fixed order.  Sums of several workgroups are left as rows of fp32
 // partial sums for bn_sum_partials_kernel: no atomics, the order of additions depends on the shape alone.
-template <typename T, int TPR, int NV, bool POST, int GATE>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_bwd_kernel(BnArgs a) {
-    constexpr int N = RowVec<T>::N, GROUPS = TPR < 256 ? 256 / TPR : 1, BLOCK = TPR * GROUPS;
-    __shared__ float red[4][GROUPS][TPR > WAVE ? TPR / WAVE : 1];
+template <typename T, int TPR, int NV, bool POST, int GATE, bool AHEAD, bool NT>
+__global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a) {
+    constexpr int N = RowVec<T>::N, BLOCK = bn_block<TPR>, GROUPS = bn_group_count<TPR>, NW = TPR > WAVE ? TPR / WAVE : 1;
+    __shared__ float red[3][3 * NW];
     __shared__ float cols[GROUPS > 1 ? BLOCK * NV * N : 1];
-    const int grp = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int grp = bn_group<TPR>(), t = threadIdx.x % TPR;
     const int nfull_all = a.H / N, rem_all = a.H % N;
-    u32x4 prev[NV], postv[NV], gv[NV];
+    const float inv_H = 1.0f / (float)a.H;
+    u32x4 prev[NV], postv[NV];
     float acc_pre[NV][N], acc_post[NV][N], acc_gate[NV][N];
+    float ga[NV][N], gd[NV][N];   // scale a(g), scale a'(g)
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < N; ++e) acc_pre[k][e] = acc_post[k][e] = acc_gate[k][e] = 0.f;
+    auto load_shared = [&](const void* m, int64_t offset, int v) {   // of what many rows share
+        return bn_load(static_cast<const T*>(m) + offset, v, nfull_all, rem_all);
+    };
     if (a.gpre)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) prev[k] = bn_load(static_cast<const T*>(a.gpre), t + k * TPR, nfull_all, rem_all);
+        for (int k = 0; k < NV; ++k) prev[k] = load_shared(a.gpre, 0, t + k * TPR);
     if constexpr (POST)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) postv[k] = bn_load(static_cast<const T*>(a.gpost), t + k * TPR, nfull_all, rem_all);
+        for (int k = 0; k < NV; ++k) postv[k] = load_shared(a.gpost, 0, t + k * TPR);
 
     // The sum over the workgroup's groups of a row of sums, handed column by column to put(column, value).
     auto over_groups = [&](float (&acc)[NV][N], auto put) {
@@ -350,149 +416,185 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_bwd_kernel(B
         }
     };
 
-    for (int s = blockIdx.x; s < a.segments; s += gridDim.x) {
-        const BnSegment seg = bn_segment(a, s);
-        if constexpr (GATE == BN_GATE_SUM) {
-            const T* p = static_cast<const T*>(a.gate) + (int64_t)seg.g * a.ldgate;
+    auto load_row = [&](BnRow<NV>& r, int base, int end) {
+        const bool live = GROUPS == 1 || base + grp < end;   // (a group past the last row loads nothing)
+        const int64_t row = live ? base + grp : base;
+        const int nvec = live ? nfull_all + (rem_all ? 1 : 0) : 0;
+        auto load = [&](u32x4 (&to)[NV], const void* m, int64_t ld) {
+            const T* p = static_cast<const T*>(m) + row * ld;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) gv[k] = bn_load(p, t + k * TPR, nfull_all, rem_all);
+            for (int k = 0; k < NV; ++k) to[k] = bn_load_ahead(p, t + k * TPR, nvec, a.H);
+        };
+        if (a.gpre) {
+            load(r.h, a.h, a.ldh);
+            load(r.dn, a.dn, a.lddn);
         }
-        for (int base = seg.row; base < seg.end; base += GROUPS) {
-            const bool live = base + grp < seg.end;   // (a group past the last row takes part in the barriers)
-            const int64_t row = live ? base + grp : base;
-            const int nfull = live ? nfull_all : 0, rem = live ? rem_all : 0;
-            u32x4 hv[NV], nv[NV], dv[NV], yv[NV];
-            if (a.gpre) {
-                const T *p = static_cast<const T*>(a.h) + row * a.ldh, *p2 = static_cast<const T*>(a.dn) + row * a.lddn;
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    hv[k] = bn_load(p, t + k * TPR, nfull, rem);
-                    nv[k] = bn_load(p2, t + k * TPR, nfull, rem);
-                }
-            }
-            if (a.dh) {
-                const T* p = static_cast<const T*>(a.dh) + row * a.lddh;
-#pragma unroll
-                for (int k = 0; k < NV; ++k) dv[k] = bn_load(p, t + k * TPR, nfull, rem);
-            }
-            if (a.y) {
-                const T* p = static_cast<const T*>(a.y) + row * a.ldy;
-#pragma unroll
-                for (int k = 0; k < NV; ++k) yv[k] = bn_load(p, t + k * TPR, nfull, rem);
-            }
-            if constexpr (GATE == BN_GATE_ROW) {
-                const T* p = static_cast<const T*>(a.gate) + row * a.ldgate;
-#pragma unroll
-                for (int k = 0; k < NV; ++k) gv[k] = bn_load(p, t + k * TPR, nfull, rem);
-            }
-            // D, the gradient of h
-            float D[NV][N];
+        if (a.y) load(r.y, a.y, a.ldy);
+        if (a.dh) load(r.dh, a.dh, a.lddh);
+        if constexpr (GATE == BN_GATE_ROW) load(r.gate, a.gate, a.ldgate);
+    };
+
+    int turn = 0;
+    for (int s = blockIdx.x; s < a.segments; s += gridDim.x) {
+        const BnSegment seg = bn_segment(a, s, GROUPS);
+        if constexpr (GATE == BN_GATE_SUM) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (a.dh) RowVec<T>::unpack(dv[k], D[k]);
+                float g[N];
+                RowVec<T>::unpack(load_shared(a.gate, (int64_t)seg.g * a.ldgate, t + k * TPR), g);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    bn_act_both(a.act, g[e], ga[k][e], gd[k][e]);
+                    ga[k][e] *= a.scale;
+                    gd[k][e] *= a.scale;
+                }
+            }
+        }
+        BnRow<NV> next;
+        if (AHEAD && seg.row < seg.end) load_row(next, seg.row, seg.end);
+        for (int base = seg.row; base < seg.end; base += seg.step, turn ^= 1) {
+            const bool live = GROUPS == 1 || base + grp < seg.end;
+            const int64_t row = live ? base + grp : base;
+            const int nfull = live ? nfull_all : 0, rem = live ? rem_all : 0;
+            BnRow<NV> in;
+            if constexpr (AHEAD) {
+                in = next;
+                if (base + seg.step < seg.end) load_row(next, base + seg.step, seg.end);
+            } else {
+                load_row(in, base, seg.end);
+            }
+            if (rem) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (t + k * TPR == nfull) {
+                        if (a.gpre) {
+                            bn_shift_tail<T>(in.h[k], rem);
+                            bn_shift_tail<T>(in.dn[k], rem);
+                        }
+                        if (a.y) bn_shift_tail<T>(in.y[k], rem);
+                        if (a.dh) bn_shift_tail<T>(in.dh[k], rem);
+                        if constexpr (GATE == BN_GATE_ROW) bn_shift_tail<T>(in.gate[k], rem);
+                    }
+            }
+            // sum h^2, sum u h and sum y^2 in one exchange
+            float sums[3] = {0.f, 0.f, 0.f};
+            if (a.gpre) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    float h[N], d[N], w[N];
+                    RowVec<T>::unpack(in.h[k], h);
+                    RowVec<T>::unpack(in.dn[k], d);
+                    RowVec<T>::unpack(prev[k], w);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        sums[0] = fmaf(h[e], h[e], sums[0]);
+                        sums[1] = fmaf(d[e] * w[e], h[e], sums[1]);
+                    }
+                }
+            }
+            if constexpr (POST) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    float y[N];
+                    RowVec<T>::unpack(in.y[k], y);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) sums[2] = fmaf(y[e], y[e], sums[2]);
+                }
+            }
+            if constexpr (POST) {
+                bn_sums<TPR, 3>(sums, red[0]);   // (the barrier of the second exchange stands between two of these)
+            } else if (a.gpre) {
+                float two[2] = {sums[0], sums[1]};
+                bn_sums<TPR, 2>(two, red[turn]);
+                sums[0] = two[0];
+                sums[1] = two[1];
+            }
+            // D = dh + r u - r^2 mean(u h r) h, the gradient of h
+            float D[NV][N];
+            auto unpack_dh = [&](float (&to)[N], int k) {
+                if (a.dh) RowVec<T>::unpack(in.dh[k], to);
                 else
 #pragma unroll
-                    for (int e = 0; e < N; ++e) D[k][e] = 0.f;
-            }
+                    for (int e = 0; e < N; ++e) to[e] = 0.f;
+            };
             if (a.gpre) {
-                float hh = 0.f, uh = 0.f;
+                const float r = rsqrtf(sums[0] * inv_H + a.eps), hk = -(r * (r * (sums[1] * r * inv_H)));
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    float h[N], u[N], w[N];
-                    RowVec<T>::unpack(hv[k], h);
-                    RowVec<T>::unpack(nv[k], u);
+                    float h[N], d[N], w[N];
+                    RowVec<T>::unpack(in.h[k], h);
+                    RowVec<T>::unpack(in.dn[k], d);
                     RowVec<T>::unpack(prev[k], w);
+                    unpack_dh(D[k], k);
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        hh += h[e] * h[e];
-                        uh += u[e] * w[e] * h[e];
+                        const float dr = d[e] * r;
+                        D[k][e] = fmaf(dr, w[e], fmaf(hk, h[e], D[k][e]));
+                        acc_pre[k][e] = fmaf(dr, h[e], acc_pre[k][e]);
                     }
                 }
-                hh = bn_sum<TPR>(hh, red[0][grp]);
-                uh = bn_sum<TPR>(uh, red[1][grp]);
-                const float r = 1.0f / sqrtf(hh / (float)a.H + a.eps), c = uh * r / (float)a.H;
+            } else {
 #pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    float h[N], u[N], w[N];
-                    RowVec<T>::unpack(hv[k], h);
-                    RowVec<T>::unpack(nv[k], u);
-                    RowVec<T>::unpack(prev[k], w);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const float xh = h[e] * r;
-                        D[k][e] += r * (u[e] * w[e] - xh * c);
-                        acc_pre[k][e] += u[e] * xh;
-                    }
-                }
+                for (int k = 0; k < NV; ++k) unpack_dh(D[k], k);
             }
             if (a.dx) {
                 T* p = static_cast<T*>(a.dx) + row * a.lddx;
 #pragma unroll
-                for (int k = 0; k < NV; ++k) bn_store<T>(p, t + k * TPR, nfull, rem, D[k]);
+                for (int k = 0; k < NV; ++k) bn_store<T, NT>(p, t + k * TPR, nfull, rem, D[k]);
             }
-            if (a.y) {
-                float q = 1.0f;
-                if constexpr (POST) {
-                    float yy = 0.f;
+            if (!a.y) continue;
+            const float q = POST ? rsqrtf(sums[2] * inv_H + a.eps) : 1.0f;
+            // D becomes dz, then (with a norm after the block) v = dz gamma_post
+            float vy[1] = {0.f};
 #pragma unroll
-                    for (int k = 0; k < NV; ++k) {
-                        float y[N];
-                        RowVec<T>::unpack(yv[k], y);
+            for (int k = 0; k < NV; ++k) {
+                float y[N], w[N], g[N];
+                RowVec<T>::unpack(in.y[k], y);
+                if constexpr (POST) RowVec<T>::unpack(postv[k], w);
+                if constexpr (GATE == BN_GATE_ROW) RowVec<T>::unpack(in.gate[k], g);
 #pragma unroll
-                        for (int e = 0; e < N; ++e) yy += y[e] * y[e];
-                    }
-                    yy = bn_sum<TPR>(yy, red[2][grp]);
-                    q = 1.0f / sqrtf(yy / (float)a.H + a.eps);
-                }
-                // D becomes dz, then (with a norm after the block) v = dz gamma_post
-                float vy = 0.f, dg[NV][N];
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    float y[N], w[N], g[N];
-                    RowVec<T>::unpack(yv[k], y);
-                    if constexpr (POST) RowVec<T>::unpack(postv[k], w);
-                    if constexpr (GATE != BN_GATE_NONE) RowVec<T>::unpack(gv[k], g);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
+                for (int e = 0; e < N; ++e) {
+                    if constexpr (POST) y[e] *= q;
+                    if constexpr (GATE == BN_GATE_NONE) {
                         D[k][e] *= a.scale;
-                        const float yh = POST ? y[e] * q : y[e];
-                        if constexpr (GATE != BN_GATE_NONE) {
-                            const float z = POST ? yh * w[e] : yh;
-                            dg[k][e] = D[k][e] * z * bn_act_grad(a.act, g[e]);
-                            if constexpr (GATE == BN_GATE_SUM) acc_gate[k][e] += dg[k][e];
-                            D[k][e] *= bn_act(a.act, g[e]);
-                        }
-                        if constexpr (POST) {
-                            acc_post[k][e] += D[k][e] * yh;
-                            D[k][e] *= w[e];
-                            vy += D[k][e] * yh;
-                        }
+                    } else if constexpr (GATE == BN_GATE_SUM) {
+                        const float z = POST ? y[e] * w[e] : y[e];
+                        acc_gate[k][e] = fmaf(D[k][e] * gd[k][e], z, acc_gate[k][e]);
+                        D[k][e] *= ga[k][e];
+                    } else {
+                        const float z = POST ? y[e] * w[e] : y[e];
+                        float act, slope;
+                        bn_act_both(a.act, g[e], act, slope);
+                        D[k][e] *= a.scale;
+                        g[e] = D[k][e] * z * slope;
+                        D[k][e] *= act;
+                    }
+                    if constexpr (POST) {
+                        acc_post[k][e] = fmaf(D[k][e], y[e], acc_post[k][e]);
+                        D[k][e] *= w[e];
+                        vy[0] = fmaf(D[k][e], y[e], vy[0]);
                     }
                 }
                 if constexpr (GATE == BN_GATE_ROW) {
-                    if (a.dgate) {
-                        T* p = static_cast<T*>(a.dgate) + row * a.lddgate;
-#pragma unroll
-                        for (int k = 0; k < NV; ++k) bn_store<T>(p, t + k * TPR, nfull, rem, dg[k]);
-                    }
-                }
-                if constexpr (POST) {
-                    const float c = bn_sum<TPR>(vy, red[3][grp]) / (float)a.H;
-#pragma unroll
-                    for (int k = 0; k < NV; ++k) {
-                        float y[N];
-                        RowVec<T>::unpack(yv[k], y);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) D[k][e] = q * (D[k][e] - y[e] * q * c);
-                    }
-                }
-                if (a.dy) {
-                    T* p = static_cast<T*>(a.dy) + row * a.lddy;
-#pragma unroll
-                    for (int k = 0; k < NV; ++k) bn_store<T>(p, t + k * TPR, nfull, rem, D[k]);
+                    if (a.dgate) bn_store<T, NT>(static_cast<T*>(a.dgate) + row * a.lddgate, t + k * TPR, nfull, rem, g);
                 }
             }
-            if constexpr (TPR > WAVE) __syncthreads();   // the next row's sums reuse the LDS
+            if constexpr (POST) {
+                bn_sums<TPR, 1>(vy, red[2]);
+                const float yk = -(q * (q * (vy[0] * inv_H)));
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    float y[N];
+                    RowVec<T>::unpack(in.y[k], y);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) D[k][e] = fmaf(yk, y[e], q * D[k][e]);
+                }
+            }
+            if (a.dy) {
+                T* p = static_cast<T*>(a.dy) + row * a.lddy;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) bn_store<T, NT>(p, t + k * TPR, nfull, rem, D[k]);
+            }
         }
         if constexpr (GATE == BN_GATE_SUM) {
             if (a.gate_direct) {
@@ -523,7 +625,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_bwd_kernel(B
 // Rows beyond the register forms (see block_norm_fwd_long).  The sums over rows live in the partial sums'
 // memory (a gate's: a row per workgroup, or per segment where several share a gate row); a column always
 // belongs to the same thread.
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a) {
     constexpr int N = RowVec<T>::N;
     __shared__ float red[BN_LONG_THREADS / WAVE];
@@ -541,10 +643,10 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
     if (pre) each(pre, [](float* p, int j) { p[j] = 0.f; });
     if (post) each(post, [](float* p, int j) { p[j] = 0.f; });
     for (int s = blockIdx.x; s < a.segments; s += gridDim.x) {
-        const BnSegment seg = bn_segment(a, s);
+        const BnSegment seg = bn_segment(a, s, 1);
         float* gsum = a.part_gate ? a.part_gate + (int64_t)(a.gate_direct ? blockIdx.x : s) * a.H : nullptr;
         if (gsum) each(gsum, [](float* p, int j) { p[j] = 0.f; });
-        for (int64_t row = seg.row; row < seg.end; ++row) {
+        for (int64_t row = seg.row; row < seg.end; row += seg.step) {
             const T* h = gpre ? static_cast<const T*>(a.h) + row * a.ldh : nullptr;
             const T* dn = gpre ? static_cast<const T*>(a.dn) + row * a.lddn : nullptr;
             const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.lddh : nullptr;
@@ -623,11 +725,13 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
 #pragma unroll
                         for (int e = 0; e < N; ++e) {
                             const float z = gpost ? yf[e] * q * w[e] : yf[e];
-                            dg[e] = a.scale * D[e] * z * bn_act_grad(a.act, g[e]);
+                            float act, slope;
+                            bn_act_both(a.act, g[e], act, slope);
+                            dg[e] = a.scale * D[e] * z * slope;
                             if (gsum && v * N + e < a.H) gsum[v * N + e] += dg[e];
                         }
                         if (a.by_row && a.dgate)
-                            bn_store<T>(static_cast<T*>(a.dgate) + row * a.lddgate, v, nfull, rem, dg);
+                            bn_store<T, NT>(static_cast<T*>(a.dgate) + row * a.lddgate, v, nfull, rem, dg);
                     }
                     if (gpost) {
 #pragma unroll
@@ -637,9 +741,9 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
                             dz[e] = q * (dz[e] * w[e] - yh * cy);
                         }
                     }
-                    if (a.dy) bn_store<T>(static_cast<T*>(a.dy) + row * a.lddy, v, nfull, rem, dz);
+                    if (a.dy) bn_store<T, NT>(static_cast<T*>(a.dy) + row * a.lddy, v, nfull, rem, dz);
                 }
-                if (a.dx) bn_store<T>(static_cast<T*>(a.dx) + row * a.lddx, v, nfull, rem, D);
+                if (a.dx) bn_store<T, NT>(static_cast<T*>(a.dx) + row * a.lddx, v, nfull, rem, D);
             }
         }
         if (gsum && a.gate_direct) {

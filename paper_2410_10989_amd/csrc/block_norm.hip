@@ -3,6 +3,7 @@
 #include "block_norm.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "flce_host.h"
 
@@ -12,8 +13,10 @@ namespace {
 
 constexpr int64_t BN_MAX_H = (int64_t)1 << 24;      // keeps launches and column numbers within 32 bits
 constexpr int64_t BN_GRID_X = (int64_t)1 << 20;     // workgroups along x, the rest along y
-constexpr int BN_CU_THREADS = 1024;                 // threads per CU that the backward is launched for
+constexpr int BN_CU_THREADS = 512;                 // threads per CU that the backward is launched for
 constexpr int BN_CUS = 256;
+constexpr int64_t BN_FEW_BLOCKS = 128;
+constexpr int64_t BN_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
 size_t bn_elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
 
@@ -62,20 +65,34 @@ int check_common(const flce_block_norm* b, Strides* st, int64_t* gate_rows) {
     return FLCE_OK;
 }
 
-// The register forms: TPR threads per row with E elements each (dividing a row by 8 elements per thread keeps
-// the backward's three sets of sums and four streams within the registers of two workgroups per CU).
+// The register forms: TPR threads per row with E elements each (a table by width, not by size: each row of it was the
+// fastest of its neighbours over its range).  Twice the elements per thread halve what a row costs besides them (sums
+// over lanes, addresses), half of them leaves registers for more wavefronts: backward, us, 8 / 16 elements: 8192 x 2048
+// 46 / 50, 8192 x 2304 45 / 38, 8192 x 1000 29 / 24, 16384 x 512 20 / 22.  fp32 rows have half the elements per load
+// in flight: 4096 x 4096 67 / 72.
 struct BnShape {
     int tpr, e;   // tpr = 0: the long form
 };
-BnShape bn_shape(int64_t H, bool backward) {
-    for (const int tpr : {16, 64, 128, 256, 512})
-        if (H <= tpr * 8) return {tpr, 8};
-    if (H <= 512 * 16) return {512, 16};
-    if (H <= 1024 * 16 && !backward) return {1024, 16};
+BnShape bn_shape(int64_t H, int dtype, bool backward) {
+    if (backward && H < 8) return {0, 0};   // (its loads are whole vectors)
+    if (H <= 128) return {16, 8};
+    if (H <= 512) return {64, 8};
+    if (H <= 1024) return {64, 16};
+    if (H <= 2048) return {256, 8};
+    if (H <= 4096) return dtype == FLCE_F32 ? BnShape{512, 8} : BnShape{256, 16};
+    if (H <= 8192) return {512, 16};
+    if (H <= 16384 && !backward) return {1024, 16};
     return {0, 0};
 }
-int bn_groups(const BnShape& s) { return s.tpr && s.tpr < 256 ? 256 / s.tpr : 1; }
-int bn_threads(const BnShape& s) { return s.tpr ? std::max(256, s.tpr) : BN_LONG_THREADS; }
+int bn_threads(const BnShape& s) { return s.tpr > WAVE ? s.tpr : s.tpr ? 256 : BN_LONG_THREADS; }
+int bn_groups(const BnShape& s) { return s.tpr && s.tpr <= WAVE ? 256 / s.tpr : 1; }
+
+// Nontemporal stores where a call's rows do not fit the memory-side cache anyway: what the call reads then stays in
+// it.  us, ordinary / nontemporal: 402 MB of rows 76 / 60 (backward), 470 MB 89 / 68 (forward); between a kernel that
+// writes y and one that reads n: 470 MB 161 / 149, 403 MB 139 / 128, but 268 MB 85 / 87.
+bool bn_nontemporal(const flce_block_norm& b, int streams) {
+    return (int64_t)streams * b.rows * b.H * (int64_t)bn_elem(b.dtype) > BN_CACHE_BYTES;
+}
 
 // How the backward deals rows to workgroups, and where its partial sums lie (floats from the workspace's start).
 struct BnPlan {
@@ -85,8 +102,8 @@ struct BnPlan {
 };
 
 // per: rows per gate row where rows share one, else all rows; gate_sum: its gradient is wanted.
-BnPlan bn_plan_for(int64_t rows, int64_t H, int64_t per, bool pre, bool post, bool gate_sum, int64_t target) {
-    const BnShape s = bn_shape(H, true);
+BnPlan bn_plan_for(int64_t rows, int64_t H, int dtype, int64_t per, bool pre, bool post, bool gate_sum, int64_t target) {
+    const BnShape s = bn_shape(H, dtype, true);
     const int64_t groups = bn_groups(s);
     BnPlan p{};
     p.per = std::min(per, rows);
@@ -122,22 +139,33 @@ BnPlan bn_plan_for(int64_t rows, int64_t H, int64_t per, bool pre, bool post, bo
     p.total_bytes = at * sizeof(float);
     return p;
 }
-// The plan of the whole chip, or the largest power-of-two fraction of it whose sums fit `cap` bytes.
-BnPlan bn_plan(int64_t rows, int64_t H, int64_t per, bool pre, bool post, bool gate_sum, size_t cap) {
-    int64_t target = (int64_t)BN_CUS * BN_CU_THREADS / bn_threads(bn_shape(H, true));
-    for (;; target /= 2) {
-        const BnPlan p = bn_plan_for(rows, H, per, pre, post, gate_sum, target);
+// Workgroups of the backward.  Up to two of 256 threads per CU (or one of 512), but one where a row fills nearly all
+// of the (256, 16) form's vectors: their loads a row ahead fill the memory pipes, and every workgroup more costs its
+// partial sums (us, 256 / 512 workgroups: 16384 x 3584 with three sums 136 / 149, 8192 x 4096 72 / 75; but 8192 x
+// 2304 48 / 38, and rows that do not start on 16 bytes 8192 x 3583 96 / 78).  Small batches: few rows per workgroup,
+// because sums of few rows cost as much as the rows (512 / 256 / 128 workgroups, H = 4096 with a norm after the block:
+// 256 rows 16.7 / 16.8 / 14.6, 1024 rows 26.7 / 22.1 / 25.0, 4096 x 2048 26.2 / 27.8 / 44.0; below 128 rows one each).
+int64_t bn_target(int64_t rows, int64_t H, int dtype) {
+    const BnShape s = bn_shape(H, dtype, true);
+    int64_t most = BN_CUS * std::max(1, BN_CU_THREADS / bn_threads(s));
+    if (s.tpr == 256 && s.e == 16 && 4 * H > 3 * 256 * 16 && H % 8 == 0) most = BN_CUS;
+    return std::min(most, std::max({BN_FEW_BLOCKS, std::min<int64_t>(BN_CUS, rows / 4), rows / 8}));
+}
+// That plan, or the largest power-of-two fraction of it whose sums fit `cap` bytes.
+BnPlan bn_plan(int64_t rows, int64_t H, int dtype, int64_t per, bool pre, bool post, bool gate_sum, size_t cap) {
+    for (int64_t target = bn_target(rows, H, dtype);; target /= 2) {
+        const BnPlan p = bn_plan_for(rows, H, dtype, per, pre, post, gate_sum, target);
         if (p.total_bytes <= cap || target == 1) return p;
     }
 }
 
-template <typename T, int TPR, int E>
+template <typename T, bool NT, int TPR, int E>
 void launch_fwd(const BnArgs& a, hipStream_t s) {
-    constexpr int NV = E / RowVec<T>::N, GROUPS = TPR < 256 ? 256 / TPR : 1;
+    constexpr int NV = E / RowVec<T>::N, GROUPS = bn_group_count<TPR>;
     const int64_t blocks = (a.rows + GROUPS - 1) / GROUPS;
     const dim3 grid((unsigned)std::min(blocks, BN_GRID_X), (unsigned)((blocks + BN_GRID_X - 1) / BN_GRID_X));
-    const dim3 block(TPR < 256 ? 256 : TPR);
-#define BN_FWD(POST, GATE) hipLaunchKernelGGL((block_norm_fwd_kernel<T, TPR, NV, POST, GATE>), grid, block, 0, s, a)
+    const dim3 block(bn_block<TPR>);
+#define BN_FWD(POST, GATE) hipLaunchKernelGGL((block_norm_fwd_kernel<T, TPR, NV, POST, GATE, NT>), grid, block, 0, s, a)
     if (a.gpost) {
         if (a.gate) BN_FWD(true, true); else BN_FWD(true, false);
     } else {
@@ -145,11 +173,12 @@ void launch_fwd(const BnArgs& a, hipStream_t s) {
     }
 #undef BN_FWD
 }
-template <typename T, int TPR, int E>
+template <typename T, bool NT, int TPR, int E>
 void launch_bwd(const BnArgs& a, const dim3& grid, hipStream_t s) {
     constexpr int NV = E / RowVec<T>::N;
-    const dim3 block(TPR < 256 ? 256 : TPR);
-#define BN_BWD(POST, GATE) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TPR, NV, POST, GATE>), grid, block, 0, s, a)
+    const dim3 block(bn_block<TPR>);
+#define BN_BWD(POST, GATE) \
+    hipLaunchKernelGGL((block_norm_bwd_kernel<T, TPR, NV, POST, GATE, (NV <= 2), NT>), grid, block, 0, s, a)
 #define BN_BWD_GATE(POST)                             \
     do {                                              \
         if (!a.gate) BN_BWD(POST, BN_GATE_NONE);      \
@@ -160,45 +189,51 @@ void launch_bwd(const BnArgs& a, const dim3& grid, hipStream_t s) {
 #undef BN_BWD_GATE
 #undef BN_BWD
 }
-template <typename T>
+template <typename T, bool NT>
 int run_fwd(const BnArgs& a, hipStream_t s) {
-    const BnShape sh = bn_shape(a.H, false);
-    if (sh.e == 8) {
-        switch (sh.tpr) {
-            case 16: launch_fwd<T, 16, 8>(a, s); break;
-            case 64: launch_fwd<T, 64, 8>(a, s); break;
-            case 128: launch_fwd<T, 128, 8>(a, s); break;
-            case 256: launch_fwd<T, 256, 8>(a, s); break;
-            default: launch_fwd<T, 512, 8>(a, s); break;
-        }
+    constexpr bool F32 = std::is_same<T, float>::value;
+    const BnShape sh = bn_shape(a.H, F32 ? FLCE_F32 : FLCE_BF16, false);
+    if (sh.tpr == 16 && sh.e == 8) {
+        launch_fwd<T, NT, 16, 8>(a, s);
+    } else if (sh.tpr == 64 && sh.e == 8) {
+        launch_fwd<T, NT, 64, 8>(a, s);
+    } else if (sh.tpr == 64 && sh.e == 16) {
+        launch_fwd<T, NT, 64, 16>(a, s);
+    } else if (sh.tpr == 256 && sh.e == 8) {
+        launch_fwd<T, NT, 256, 8>(a, s);
+    } else if (sh.tpr == (F32 ? 512 : 256) && sh.e == (F32 ? 8 : 16)) {
+        launch_fwd<T, NT, F32 ? 512 : 256, F32 ? 8 : 16>(a, s);
     } else if (sh.tpr == 512) {
-        launch_fwd<T, 512, 16>(a, s);
+        launch_fwd<T, NT, 512, 16>(a, s);
     } else if (sh.tpr == 1024) {
-        launch_fwd<T, 1024, 16>(a, s);
+        launch_fwd<T, NT, 1024, 16>(a, s);
     } else {
         const int64_t rows = a.rows;
-        hipLaunchKernelGGL((block_norm_fwd_long<T>), dim3((unsigned)std::min(rows, BN_GRID_X), (unsigned)((rows + BN_GRID_X - 1) / BN_GRID_X)),
+        hipLaunchKernelGGL((block_norm_fwd_long<T, NT>), dim3((unsigned)std::min(rows, BN_GRID_X), (unsigned)((rows + BN_GRID_X - 1) / BN_GRID_X)),
                            dim3(BN_LONG_THREADS), 0, s, a);
     }
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
 }
-template <typename T>
+template <typename T, bool NT>
 int run_bwd(const BnArgs& a, const BnPlan& p, void* dgamma_pre, void* dgamma_post, hipStream_t s) {
-    const BnShape sh = bn_shape(a.H, true);
+    constexpr bool F32 = std::is_same<T, float>::value;
+    const BnShape sh = bn_shape(a.H, F32 ? FLCE_F32 : FLCE_BF16, true);
     const dim3 grid((unsigned)p.blocks);
-    if (sh.e == 8) {
-        switch (sh.tpr) {
-            case 16: launch_bwd<T, 16, 8>(a, grid, s); break;
-            case 64: launch_bwd<T, 64, 8>(a, grid, s); break;
-            case 128: launch_bwd<T, 128, 8>(a, grid, s); break;
-            case 256: launch_bwd<T, 256, 8>(a, grid, s); break;
-            default: launch_bwd<T, 512, 8>(a, grid, s); break;
-        }
-    } else if (sh.tpr) {
-        launch_bwd<T, 512, 16>(a, grid, s);
+    if (sh.tpr == 16 && sh.e == 8) {
+        launch_bwd<T, NT, 16, 8>(a, grid, s);
+    } else if (sh.tpr == 64 && sh.e == 8) {
+        launch_bwd<T, NT, 64, 8>(a, grid, s);
+    } else if (sh.tpr == 64 && sh.e == 16) {
+        launch_bwd<T, NT, 64, 16>(a, grid, s);
+    } else if (sh.tpr == 256 && sh.e == 8) {
+        launch_bwd<T, NT, 256, 8>(a, grid, s);
+    } else if (sh.tpr == (F32 ? 512 : 256) && sh.e == (F32 ? 8 : 16)) {
+        launch_bwd<T, NT, F32 ? 512 : 256, F32 ? 8 : 16>(a, grid, s);
+    } else if (sh.tpr == 512) {
+        launch_bwd<T, NT, 512, 16>(a, grid, s);
     } else {
-        hipLaunchKernelGGL((block_norm_bwd_long<T>), grid, dim3(BN_LONG_THREADS), 0, s, a);
+        hipLaunchKernelGGL((block_norm_bwd_long<T, NT>), grid, dim3(BN_LONG_THREADS), 0, s, a);
     }
     HIP_TRY(hipGetLastError());
     BnSums b{};
@@ -266,8 +301,10 @@ int flce_block_norm_fwd(const void* x, const void* y, const void* gate, const vo
     a.act = b.gate_act;
     a.scale = b.scale;
     a.eps = b.eps;
+    const bool nt = bn_nontemporal(b, (x != nullptr) + 2 * (y != nullptr) + (gamma_pre != nullptr) + (gate && b.rows_per_gate == 1));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return b.dtype == FLCE_F32 ? run_fwd<float>(a, s) : run_fwd<bf16_t>(a, s);
+    if (nt) return b.dtype == FLCE_F32 ? run_fwd<float, true>(a, s) : run_fwd<bf16_t, true>(a, s);
+    return b.dtype == FLCE_F32 ? run_fwd<float, false>(a, s) : run_fwd<bf16_t, false>(a, s);
 }
 
 int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const void* y, const void* gate,
@@ -311,7 +348,7 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
         FLCE_TRY(shared_workspace_lent(&lent));
         if (lent) cap = lent;
     }
-    const BnPlan p = bn_plan(b.rows, b.H, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
+    const BnPlan p = bn_plan(b.rows, b.H, b.dtype, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
     if (p.total_bytes > cap) return FLCE_ERR_WORKSPACE;
     char* ws = static_cast<char*>(b.workspace);
     if (!ws && p.total_bytes) FLCE_TRY(shared_workspace(p.total_bytes, &ws));
@@ -337,7 +374,7 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     a.lddgate = ld.dgate;
     a.part_pre = dgamma_pre ? f : nullptr;
     a.part_post = dgamma_post ? f + p.off_post : nullptr;
-    a.part_gate = sums && (!p.direct || !bn_shape(b.H, true).tpr) ? f + p.off_gate : nullptr;
+    a.part_gate = sums && (!p.direct || !bn_shape(b.H, b.dtype, true).tpr) ? f + p.off_gate : nullptr;
     a.rows = (int)b.rows;
     a.H = (int)b.H;
     a.per = (int)p.per;
@@ -348,9 +385,13 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     a.parts = (int)p.parts;
     a.by_row = by_row;
     a.gate_direct = p.direct;
+    const bool nt = bn_nontemporal(b, 2 * (h != nullptr) + (dh != nullptr) + (y != nullptr) + (dx != nullptr) + (dy != nullptr) + by_row + (by_row && dgate));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return b.dtype == FLCE_F32 ? run_bwd<float>(a, p, dgamma_pre, dgamma_post, s)
-                               : run_bwd<bf16_t>(a, p, dgamma_pre, dgamma_post, s);
+    if (nt)
+        return b.dtype == FLCE_F32 ? run_bwd<float, true>(a, p, dgamma_pre, dgamma_post, s)
+                                   : run_bwd<bf16_t, true>(a, p, dgamma_pre, dgamma_post, s);
+    return b.dtype == FLCE_F32 ? run_bwd<float, false>(a, p, dgamma_pre, dgamma_post, s)
+                               : run_bwd<bf16_t, false>(a, p, dgamma_pre, dgamma_post, s);
 }
 
 size_t flce_block_norm_workspace_bytes(const flce_block_norm* args) {
@@ -358,9 +399,9 @@ size_t flce_block_norm_workspace_bytes(const flce_block_norm* args) {
     int64_t gate_rows;
     if (check_common(args, &ld, &gate_rows) != FLCE_OK) return 0;
     const int64_t per = args->rows_per_gate ? args->rows_per_gate : args->rows;
-    const size_t with_gate = bn_plan(args->rows, args->H, per, true, true, true, SIZE_MAX).total_bytes;
+    const size_t with_gate = bn_plan(args->rows, args->H, args->dtype, per, true, true, true, SIZE_MAX).total_bytes;
     // (a gate row per row, or no gate: the gammas' sums alone, in a plan of their own)
-    const size_t without = bn_plan(args->rows, args->H, args->rows, true, true, false, SIZE_MAX).total_bytes;
+    const size_t without = bn_plan(args->rows, args->H, args->dtype, args->rows, true, true, false, SIZE_MAX).total_bytes;
     return std::max(with_gate, without);
 }
 
