@@ -11,9 +11,12 @@ using namespace flce;
 namespace {
 
 constexpr int64_t GN_MAX_COUNT = (int64_t)1 << 40;   // elements of one tensor
-constexpr int64_t GN_CHUNK = 64 << 10, GN_CHUNK_MIN = 4 << 10;   // bytes: 16 and 1 accesses per thread
-constexpr int GN_BLOCKS = 2048;        // workgroups of all launches of a sweep together: 8 per CU
-constexpr int GN_BLOCKS_MIN = 64;      // of one launch
+constexpr int64_t GN_CHUNK = 32 << 10, GN_CHUNK_MIN = 4 << 10;   // bytes: 8 and 1 accesses per thread
+constexpr int GN_BLOCKS = 1024;        // workgroups of a launch: 4 per CU
+constexpr int64_t GN_PARTIALS = 8192;  // partial results of all launches, while each has GN_BLOCKS_MIN workgroups
+constexpr size_t GN_SMALL_BYTES = 64 << 10;
+constexpr size_t GN_CACHE_BYTES = (size_t)256 << 20, GN_KEEP_BYTES = (size_t)192 << 20;   // memory-side cache
+constexpr int64_t GN_BLOCKS_MIN = 64;
 
 struct Tensors {
     const void* const* in;
@@ -24,7 +27,9 @@ struct Tensors {
 };
 
 int64_t launches_of(int64_t n) { return std::max<int64_t>(1, (n + GN_TENSORS - 1) / GN_TENSORS); }
-int blocks_per_launch(int64_t n) { return (int)std::max<int64_t>(GN_BLOCKS_MIN, GN_BLOCKS / launches_of(n)); }
+int blocks_per_launch(int64_t n) {
+    return (int)std::min<int64_t>(GN_BLOCKS, std::max(GN_BLOCKS_MIN, GN_PARTIALS / launches_of(n)));
+}
 size_t partial_bytes(int64_t n) { return (size_t)launches_of(n) * blocks_per_launch(n) * sizeof(double); }
 size_t bytes_of(const Tensors& t, int i) { return (size_t)t.count[i] * (t.dtype[i] == FLCE_F32 ? 4 : 2); }
 
@@ -71,33 +76,43 @@ int check_outputs(const Tensors& t) {
     return rc;
 }
 
-// The launch of tensors first .. (at most GN_TENSORS of them); blocks: its workgroups, 0 if there is nothing in them.
-GnArgs launch_args(const Tensors& t, int first, int64_t chunk_bytes, int max_blocks, int* blocks) {
+// How the tensors are cut for both sweeps.
+struct Cut {
+    size_t total;          // bytes of all tensors
+    int64_t chunk_bytes;   // as long as they may be while there are enough of them for every workgroup
+    int blocks;            // most workgroups of a launch
+};
+Cut cut_of(const Tensors& t) {
+    Cut c{0, GN_CHUNK, blocks_per_launch(t.n)};
+    for (int i = 0; i < t.n; ++i) c.total += bytes_of(t, i);
+    while (c.chunk_bytes > GN_CHUNK_MIN && c.total / (size_t)c.chunk_bytes < (size_t)GN_BLOCKS) c.chunk_bytes /= 2;
+    while (c.total / (size_t)c.chunk_bytes > ((size_t)1 << 30)) c.chunk_bytes *= 2;   // (counted in 32 bits)
+    return c;
+}
+// The launch of tensors first .. (at most GN_TENSORS of them), whose bytes begin at `at` of all; those below `until`
+// are streamed past the cache.  bytes: its bytes; blocks: its workgroups, 0 if there is nothing in them.
+GnArgs launch_args(const Tensors& t, int first, const Cut& cut, size_t at, size_t until, size_t* bytes, int* blocks) {
     GnArgs a{};
     int64_t chunks = 0;
+    const size_t begin = at;
+    a.in_place = 1;
     for (int i = first; i < t.n && i < first + GN_TENSORS; ++i) {
         if (!t.count[i]) continue;
         const int k = a.tensors++;
         a.in[k] = t.in[i];
         a.out[k] = t.out ? t.out[i] : const_cast<void*>(t.in[i]);
+        if (a.out[k] != a.in[k]) a.in_place = 0;
         a.count[k] = t.dtype[i] == FLCE_BF16 ? ~t.count[i] : t.count[i];
-        chunks += ((int64_t)bytes_of(t, i) + chunk_bytes - 1) / chunk_bytes;
+        const size_t b = bytes_of(t, i), size = (size_t)cut.chunk_bytes;
+        if (at < until) a.streamed = (int)(chunks + (std::min(b, until - at) + size - 1) / size);
+        chunks += (int64_t)((b + size - 1) / size);
         a.first_chunk[k + 1] = (int)chunks;
+        at += b;
     }
-    a.chunk_bytes = (int)chunk_bytes;
-    *blocks = (int)std::min<int64_t>(chunks, max_blocks);
+    a.chunk_bytes = (int)cut.chunk_bytes;
+    *bytes = at - begin;
+    *blocks = (int)std::min<int64_t>(chunks, cut.blocks);
     return a;
-}
-
-// Chunks as long as they may be while there are enough of them for every workgroup.
-int64_t chunk_bytes_of(const Tensors& t) {
-    size_t total = 0;
-    for (int i = 0; i < t.n; ++i) total += bytes_of(t, i);
-    int64_t c = GN_CHUNK;
-    while (c > GN_CHUNK_MIN && total / (size_t)c < (size_t)GN_BLOCKS) c /= 2;
-    // (a launch counts its chunks in 32 bits)
-    while (total / (size_t)c > ((size_t)1 << 30)) c *= 2;
-    return c;
 }
 
 int partial_memory(const Tensors& t, void* workspace, size_t workspace_bytes, double** out) {
@@ -114,14 +129,18 @@ int partial_memory(const Tensors& t, void* workspace, size_t workspace_bytes, do
     return FLCE_OK;
 }
 
-// Sweep 1; *partials: the results it leaves.
+// Sweep 1; *partials: the results it leaves.  Tensors that do not fit the memory-side cache together are read past
+// it, but for the end of them where a second sweep follows, which begins there.
 template <typename Op>
-int sweep_norm(const Tensors& t, int64_t chunk_bytes, double* partial, int* partials, hipStream_t s) {
-    const int max_blocks = blocks_per_launch(t.n);
+int sweep_norm(const Tensors& t, const Cut& cut, bool second_sweep, double* partial, int* partials, hipStream_t s) {
+    const size_t until = cut.total <= GN_CACHE_BYTES ? 0 : second_sweep ? cut.total - GN_KEEP_BYTES : cut.total;
+    size_t at = 0;
     *partials = 0;
     for (int first = 0; first < t.n; first += GN_TENSORS) {
         int blocks;
-        GnArgs a = launch_args(t, first, chunk_bytes, max_blocks, &blocks);
+        size_t bytes;
+        GnArgs a = launch_args(t, first, cut, at, until, &bytes, &blocks);
+        at += bytes;
         if (!blocks) continue;
         a.partial = partial + *partials;
         hipLaunchKernelGGL((grad_norm_kernel<Op>), dim3((unsigned)blocks), dim3(GN_THREADS), 0, s, a);
@@ -133,12 +152,13 @@ int sweep_norm(const Tensors& t, int64_t chunk_bytes, double* partial, int* part
 
 // Sweep 2, the last tensors first.  The norm is given, or added up from the partial results and stored.
 template <typename Op>
-int sweep_scale(const Tensors& t, int64_t chunk_bytes, const double* partial, int partials, const float* norm_in,
+int sweep_scale(const Tensors& t, const Cut& cut, const double* partial, int partials, const float* norm_in,
                 float* norm_out, float max_norm, hipStream_t s) {
-    const int max_blocks = blocks_per_launch(t.n);
+    const size_t until = (t.out ? 2 : 1) * cut.total <= GN_CACHE_BYTES ? 0 : cut.total;
     for (int64_t l = launches_of(t.n) - 1; l >= 0; --l) {
         int blocks;
-        GnArgs a = launch_args(t, (int)(l * GN_TENSORS), chunk_bytes, max_blocks, &blocks);
+        size_t bytes;
+        GnArgs a = launch_args(t, (int)(l * GN_TENSORS), cut, 0, until, &bytes, &blocks);
         if (!blocks && !norm_out) continue;
         a.partial = const_cast<double*>(partial);
         a.partials = partials;
@@ -152,20 +172,27 @@ int sweep_scale(const Tensors& t, int64_t chunk_bytes, const double* partial, in
     return FLCE_OK;
 }
 
+// clip: scale too.
 template <typename Op>
-int run_norm(const Tensors& t, double* partial, float* norm, hipStream_t s) {
+int run(const Tensors& t, bool clip, double* partial, float max_norm, float* norm, hipStream_t s) {
+    const Cut cut = cut_of(t);
     int partials;
-    FLCE_TRY(sweep_norm<Op>(t, chunk_bytes_of(t), partial, &partials, s));
+    if (cut.total <= GN_SMALL_BYTES && t.n <= GN_TENSORS) {
+        size_t bytes;
+        GnArgs a = launch_args(t, 0, cut, 0, 0, &bytes, &partials);
+        a.norm_out = norm;
+        a.max_norm = max_norm;
+        hipLaunchKernelGGL((grad_small_kernel<Op>), dim3(1), dim3(GN_THREADS), 0, s, a, clip ? 1 : 0);
+        HIP_TRY(hipGetLastError());
+        return FLCE_OK;
+    }
+    FLCE_TRY(sweep_norm<Op>(t, cut, clip, partial, &partials, s));
+    // One scaling launch adds the partial results up in each of its workgroups (1 us); several of them, of more
+    // partial results, share a launch that does it once (4 us).
+    if (clip && launches_of(t.n) == 1) return sweep_scale<Op>(t, cut, partial, partials, nullptr, norm, max_norm, s);
     hipLaunchKernelGGL((grad_norm_final_kernel<Op>), dim3(1), dim3(GN_THREADS), 0, s, partial, partials, norm);
     HIP_TRY(hipGetLastError());
-    return FLCE_OK;
-}
-template <typename Op>
-int run_clip(const Tensors& t, double* partial, float max_norm, float* norm, hipStream_t s) {
-    int partials;
-    const int64_t chunk_bytes = chunk_bytes_of(t);
-    FLCE_TRY(sweep_norm<Op>(t, chunk_bytes, partial, &partials, s));
-    return sweep_scale<Op>(t, chunk_bytes, partial, partials, nullptr, norm, max_norm, s);
+    return clip ? sweep_scale<Op>(t, cut, nullptr, 0, norm, nullptr, max_norm, s) : FLCE_OK;
 }
 
 bool finite_not_negative(float v) { return v >= 0.0f && v - v == 0.0f; }
@@ -186,7 +213,8 @@ int flce_grad_norm(const void* const* grads, const int64_t* counts, const int* d
     double* partial;
     FLCE_TRY(partial_memory(t, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return norm_type == FLCE_NORM_2 ? run_norm<GnSumSq>(t, partial, norm, s) : run_norm<GnMax>(t, partial, norm, s);
+    return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, false, partial, 0.0f, norm, s)
+                                    : run<GnMax>(t, false, partial, 0.0f, norm, s);
 }
 
 int flce_grad_clip(const void* const* grads, void* const* outs, const int64_t* counts, const int* dtypes, int n_tensors,
@@ -197,7 +225,7 @@ int flce_grad_clip(const void* const* grads, void* const* outs, const int64_t* c
     if (!aligned(norm, 4)) return FLCE_ERR_ALIGN;
     if (!finite_not_negative(max_norm)) return FLCE_ERR_ARG;
     FLCE_TRY(check_outputs(t));
-    return sweep_scale<GnSumSq>(t, chunk_bytes_of(t), nullptr, 0, norm, nullptr, max_norm, static_cast<hipStream_t>(stream));
+    return sweep_scale<GnSumSq>(t, cut_of(t), nullptr, 0, norm, nullptr, max_norm, static_cast<hipStream_t>(stream));
 }
 
 int flce_clip_grad_norm(const void* const* grads, void* const* outs, const int64_t* counts, const int* dtypes,
@@ -212,8 +240,8 @@ int flce_clip_grad_norm(const void* const* grads, void* const* outs, const int64
     double* partial;
     FLCE_TRY(partial_memory(t, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return norm_type == FLCE_NORM_2 ? run_clip<GnSumSq>(t, partial, max_norm, norm, s)
-                                    : run_clip<GnMax>(t, partial, max_norm, norm, s);
+    return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, true, partial, max_norm, norm, s)
+                                    : run<GnMax>(t, true, partial, max_norm, norm, s);
 }
 
 }  // extern "C"
