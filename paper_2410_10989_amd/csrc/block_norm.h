@@ -368,34 +368,74 @@ struct BnRow {
 // stay in registers: the gammas' until the workgroup's last row, a shared gate's until its segment's; then the
 // groups of a workgroup add theirs up in a fixed order.  Sums of several workgroups are left as rows of fp32
 // partial sums for bn_sum_partials_kernel: no atomics, the order of additions depends on the shape alone.
-template <typename T, int TPR, int NV, bool POST, int GATE, bool AHEAD, bool NT>
+// AHEAD: the next row's loads are issued before a row is worked on.  WIDE: the sums over rows are kept in LDS, where
+// registers do not hold them beside the rows of 1024 threads; each column belongs to one thread.
+constexpr int BN_WIDE_COLS = 16384, BN_WIDE_COLS_3 = 13312;   // of up to two and of three sets of sums: 160 KB
+template <typename T, int TPR, int NV, bool POST, int GATE, bool AHEAD, bool WIDE, bool NT>
 __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a) {
     constexpr int N = RowVec<T>::N, BLOCK = bn_block<TPR>, GROUPS = bn_group_count<TPR>, NW = TPR > WAVE ? TPR / WAVE : 1;
     __shared__ float red[3][3 * NW];
     __shared__ float cols[GROUPS > 1 ? BLOCK * NV * N : 1];
+    constexpr int SETS = 1 + POST + (GATE == BN_GATE_SUM), COLS = SETS == 3 ? BN_WIDE_COLS_3 : BN_WIDE_COLS;
+    constexpr int AT_PRE = 0, AT_POST = COLS, AT_GATE = (1 + POST) * COLS;
+    __shared__ __align__(16) float wide[WIDE ? SETS * COLS : 4];
     const int grp = bn_group<TPR>(), t = threadIdx.x % TPR;
     const int nfull_all = a.H / N, rem_all = a.H % N;
     const float inv_H = 1.0f / (float)a.H;
     u32x4 prev[NV], postv[NV];
-    float acc_pre[NV][N], acc_post[NV][N], acc_gate[NV][N];
-    float ga[NV][N], gd[NV][N];   // scale a(g), scale a'(g)
+    constexpr int NA = WIDE ? 1 : NV;
+    float acc_pre[NA][N], acc_post[NA][N], acc_gate[NA][N];
+    float ga[NA][N], gd[NA][N];   // scale a(g), scale a'(g); WIDE: of the vector at hand
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NA; ++k)
 #pragma unroll
         for (int e = 0; e < N; ++e) acc_pre[k][e] = acc_post[k][e] = acc_gate[k][e] = 0.f;
+    // the sums of a thread's vector k in LDS, and what is added to them
+    auto wide_at = [&](int set, int k) { return wide + set + (t + k * TPR) * N; };
+    auto wide_clear = [&](int set) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if ((t + k * TPR) * N < a.H)
+#pragma unroll
+                for (int e = 0; e < N; ++e) wide_at(set, k)[e] = 0.f;
+    };
+    auto wide_add = [&](int set, int k, const float (&v)[N]) {
+        if ((t + k * TPR) * N < a.H) {
+            f32x4* p = reinterpret_cast<f32x4*>(wide_at(set, k));
+#pragma unroll
+            for (int q = 0; q < N / 4; ++q) {
+                f32x4 s = p[q];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] += v[q * 4 + e];
+                p[q] = s;
+            }
+        }
+    };
+    if constexpr (WIDE)
+        for (int i = 0; i < SETS; ++i) wide_clear(i * COLS);
     auto load_shared = [&](const void* m, int64_t offset, int v) {   // of what many rows share
+        // (WIDE reads it again for every row: kept over the rows it would take the registers of the rows)
+        if constexpr (WIDE) asm volatile("" : "+s"(m));
         return bn_load(static_cast<const T*>(m) + offset, v, nfull_all, rem_all);
     };
-    if (a.gpre)
+    if (a.gpre && !WIDE)
 #pragma unroll
         for (int k = 0; k < NV; ++k) prev[k] = load_shared(a.gpre, 0, t + k * TPR);
-    if constexpr (POST)
+    if constexpr (POST && !WIDE)
 #pragma unroll
         for (int k = 0; k < NV; ++k) postv[k] = load_shared(a.gpost, 0, t + k * TPR);
+    auto pre_vector = [&](int k) { return WIDE ? load_shared(a.gpre, 0, t + k * TPR) : prev[k]; };
+    [[maybe_unused]] auto post_vector = [&](int k) { return WIDE ? load_shared(a.gpost, 0, t + k * TPR) : postv[k]; };
 
     // The sum over the workgroup's groups of a row of sums, handed column by column to put(column, value).
-    auto over_groups = [&](float (&acc)[NV][N], auto put) {
-        if constexpr (GROUPS > 1) {
+    auto over_groups = [&](float (&acc)[NA][N], [[maybe_unused]] int set, auto put) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if ((t + k * TPR) * N + e < a.H) put((t + k * TPR) * N + e, wide_at(set, k)[e]);
+        } else if constexpr (GROUPS > 1) {
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < NV; ++k)
@@ -437,18 +477,19 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
     int turn = 0;
     for (int s = blockIdx.x; s < a.segments; s += gridDim.x) {
         const BnSegment seg = bn_segment(a, s, GROUPS);
-        if constexpr (GATE == BN_GATE_SUM) {
+        auto gate_vector = [&](int k, float (&act)[N], float (&slope)[N]) {
+            float g[N];
+            RowVec<T>::unpack(load_shared(a.gate, (int64_t)seg.g * a.ldgate, t + k * TPR), g);
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                float g[N];
-                RowVec<T>::unpack(load_shared(a.gate, (int64_t)seg.g * a.ldgate, t + k * TPR), g);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    bn_act_both(a.act, g[e], ga[k][e], gd[k][e]);
-                    ga[k][e] *= a.scale;
-                    gd[k][e] *= a.scale;
-                }
+            for (int e = 0; e < N; ++e) {
+                bn_act_both(a.act, g[e], act[e], slope[e]);
+                act[e] *= a.scale;
+                slope[e] *= a.scale;
             }
+        };
+        if constexpr (GATE == BN_GATE_SUM && !WIDE) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) gate_vector(k, ga[k], gd[k]);
         }
         BnRow<NV> next;
         if (AHEAD && seg.row < seg.end) load_row(next, seg.row, seg.end);
@@ -484,7 +525,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                     float h[N], d[N], w[N];
                     RowVec<T>::unpack(in.h[k], h);
                     RowVec<T>::unpack(in.dn[k], d);
-                    RowVec<T>::unpack(prev[k], w);
+                    RowVec<T>::unpack(pre_vector(k), w);
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
                         sums[0] = fmaf(h[e], h[e], sums[0]);
@@ -524,14 +565,16 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                     float h[N], d[N], w[N];
                     RowVec<T>::unpack(in.h[k], h);
                     RowVec<T>::unpack(in.dn[k], d);
-                    RowVec<T>::unpack(prev[k], w);
+                    RowVec<T>::unpack(pre_vector(k), w);
                     unpack_dh(D[k], k);
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
                         const float dr = d[e] * r;
                         D[k][e] = fmaf(dr, w[e], fmaf(hk, h[e], D[k][e]));
-                        acc_pre[k][e] = fmaf(dr, h[e], acc_pre[k][e]);
+                        if constexpr (WIDE) d[e] = dr * h[e];
+                        else acc_pre[k][e] = fmaf(dr, h[e], acc_pre[k][e]);
                     }
+                    if constexpr (WIDE) wide_add(AT_PRE, k, d);
                 }
             } else {
 #pragma unroll
@@ -550,8 +593,10 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
             for (int k = 0; k < NV; ++k) {
                 float y[N], w[N], g[N];
                 RowVec<T>::unpack(in.y[k], y);
-                if constexpr (POST) RowVec<T>::unpack(postv[k], w);
+                if constexpr (POST) RowVec<T>::unpack(post_vector(k), w);
                 if constexpr (GATE == BN_GATE_ROW) RowVec<T>::unpack(in.gate[k], g);
+                if constexpr (GATE == BN_GATE_SUM && WIDE) gate_vector(k, ga[0], gd[0]);
+                [[maybe_unused]] float to_post[N], to_gate[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     if constexpr (POST) y[e] *= q;
@@ -559,8 +604,9 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                         D[k][e] *= a.scale;
                     } else if constexpr (GATE == BN_GATE_SUM) {
                         const float z = POST ? y[e] * w[e] : y[e];
-                        acc_gate[k][e] = fmaf(D[k][e] * gd[k][e], z, acc_gate[k][e]);
-                        D[k][e] *= ga[k][e];
+                        if constexpr (WIDE) to_gate[e] = D[k][e] * gd[0][e] * z;
+                        else acc_gate[k][e] = fmaf(D[k][e] * gd[k][e], z, acc_gate[k][e]);
+                        D[k][e] *= ga[WIDE ? 0 : k][e];
                     } else {
                         const float z = POST ? y[e] * w[e] : y[e];
                         float act, slope;
@@ -570,11 +616,14 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                         D[k][e] *= act;
                     }
                     if constexpr (POST) {
-                        acc_post[k][e] = fmaf(D[k][e], y[e], acc_post[k][e]);
+                        if constexpr (WIDE) to_post[e] = D[k][e] * y[e];
+                        else acc_post[k][e] = fmaf(D[k][e], y[e], acc_post[k][e]);
                         D[k][e] *= w[e];
                         vy[0] = fmaf(D[k][e], y[e], vy[0]);
                     }
                 }
+                if constexpr (WIDE && GATE == BN_GATE_SUM) wide_add(AT_GATE, k, to_gate);
+                if constexpr (WIDE && POST) wide_add(AT_POST, k, to_post);
                 if constexpr (GATE == BN_GATE_ROW) {
                     if (a.dgate) bn_store<T, NT>(static_cast<T*>(a.dgate) + row * a.lddgate, t + k * TPR, nfull, rem, g);
                 }
@@ -599,25 +648,26 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
         if constexpr (GATE == BN_GATE_SUM) {
             if (a.gate_direct) {
                 T* p = static_cast<T*>(a.dgate) + (int64_t)seg.g * a.lddgate;
-                if (a.dgate) over_groups(acc_gate, [&](int j, float v) { p[j] = from_f32<T>(v); });
+                if (a.dgate) over_groups(acc_gate, AT_GATE, [&](int j, float v) { p[j] = from_f32<T>(v); });
             } else if (a.part_gate) {
                 float* p = a.part_gate + (int64_t)s * a.H;
-                over_groups(acc_gate, [&](int j, float v) { p[j] = v; });
+                over_groups(acc_gate, AT_GATE, [&](int j, float v) { p[j] = v; });
             }
+            if constexpr (WIDE) wide_clear(AT_GATE);
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NA; ++k)
 #pragma unroll
                 for (int e = 0; e < N; ++e) acc_gate[k][e] = 0.f;
         }
     }
     if (a.part_pre) {
         float* p = a.part_pre + (int64_t)blockIdx.x * a.H;
-        over_groups(acc_pre, [&](int j, float v) { p[j] = v; });
+        over_groups(acc_pre, AT_PRE, [&](int j, float v) { p[j] = v; });
     }
     if constexpr (POST) {
         if (a.part_post) {
             float* p = a.part_post + (int64_t)blockIdx.x * a.H;
-            over_groups(acc_post, [&](int j, float v) { p[j] = v; });
+            over_groups(acc_post, AT_POST, [&](int j, float v) { p[j] = v; });
         }
     }
 }
@@ -755,7 +805,8 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
 
 // out[g][j] = sum over p of rows [g * parts + p][j] of fp32 partial sums, for up to three sets of them: the two
 // gammas (one output row each) and the gate.  As in rmsnorm_dgamma_kernel a workgroup owns 64 columns of an
-// output row, thread (c, q) adds rows q, q + 16, ... of column c, then the 16 sums are added in order.
+// output row, thread (c, q) adds rows q, q + 16, ... of column c, then the 16 sums are added in order; in fp64, which
+// costs nothing here and leaves the fp32 sums of a workgroup's own rows as the only ones.
 struct BnSums {
     const float* part[3];
     void* out[3];
@@ -766,21 +817,21 @@ struct BnSums {
 constexpr int BN_SUM_COLS = 64, BN_SUM_PARTS = 16;
 template <typename T>
 __global__ __launch_bounds__(BN_SUM_COLS * BN_SUM_PARTS) void bn_sum_partials_kernel(BnSums b, int n) {
-    __shared__ float sums[BN_SUM_PARTS][BN_SUM_COLS];
+    __shared__ double sums[BN_SUM_PARTS][BN_SUM_COLS];
     const int c = threadIdx.x % BN_SUM_COLS, q = threadIdx.x / BN_SUM_COLS;
     const int r = blockIdx.y, j = blockIdx.x * BN_SUM_COLS + c;
     const int set = r >= b.first[2] ? 2 : r >= b.first[1] ? 1 : 0;
     const int g = r - b.first[set], parts = b.parts[set];
     const float* from = b.part[set] + (int64_t)g * parts * n + j;
-    float s = 0.f;
+    double s = 0.0;
     if (j < n)
 #pragma unroll 8
-        for (int p = q; p < parts; p += BN_SUM_PARTS) s += from[(int64_t)p * n];
+        for (int p = q; p < parts; p += BN_SUM_PARTS) s += (double)from[(int64_t)p * n];
     sums[q][c] = s;
     __syncthreads();
     if (q == 0 && j < n) {
         for (int k = 1; k < BN_SUM_PARTS; ++k) s += sums[k][c];
-        (static_cast<T*>(b.out[set]) + (int64_t)g * b.ld[set])[j] = from_f32<T>(s);
+        (static_cast<T*>(b.out[set]) + (int64_t)g * b.ld[set])[j] = from_f32<T>((float)s);
     }
 }
 

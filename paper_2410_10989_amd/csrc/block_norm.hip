@@ -73,7 +73,7 @@ int check_common(const flce_block_norm* b, Strides* st, int64_t* gate_rows) {
 struct BnShape {
     int tpr, e;   // tpr = 0: the long form
 };
-BnShape bn_shape(int64_t H, int dtype, bool backward) {
+BnShape bn_shape(int64_t H, int dtype, bool backward, bool three_sums = false) {
     if (backward && H < 8) return {0, 0};   // (its loads are whole vectors)
     if (H <= 128) return {16, 8};
     if (H <= 512) return {64, 8};
@@ -81,7 +81,8 @@ BnShape bn_shape(int64_t H, int dtype, bool backward) {
     if (H <= 2048) return {256, 8};
     if (H <= 4096) return dtype == FLCE_F32 ? BnShape{512, 8} : BnShape{256, 16};
     if (H <= 8192) return {512, 16};
-    if (H <= 16384 && !backward) return {1024, 16};
+    if (H <= BN_WIDE_COLS && !backward) return {1024, 16};
+    if (H <= (three_sums ? BN_WIDE_COLS_3 : BN_WIDE_COLS) && backward) return {512, 32};
     return {0, 0};
 }
 int bn_threads(const BnShape& s) { return s.tpr > WAVE ? s.tpr : s.tpr ? 256 : BN_LONG_THREADS; }
@@ -102,8 +103,8 @@ struct BnPlan {
 };
 
 // per: rows per gate row where rows share one, else all rows; gate_sum: its gradient is wanted.
-BnPlan bn_plan_for(int64_t rows, int64_t H, int dtype, int64_t per, bool pre, bool post, bool gate_sum, int64_t target) {
-    const BnShape s = bn_shape(H, dtype, true);
+BnPlan bn_plan_for(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool pre, bool post, bool gate_sum,
+                   int64_t target) {
     const int64_t groups = bn_groups(s);
     BnPlan p{};
     p.per = std::min(per, rows);
@@ -145,16 +146,15 @@ BnPlan bn_plan_for(int64_t rows, int64_t H, int dtype, int64_t per, bool pre, bo
 // 2304 48 / 38, and rows that do not start on 16 bytes 8192 x 3583 96 / 78).  Small batches: few rows per workgroup,
 // because sums of few rows cost as much as the rows (512 / 256 / 128 workgroups, H = 4096 with a norm after the block:
 // 256 rows 16.7 / 16.8 / 14.6, 1024 rows 26.7 / 22.1 / 25.0, 4096 x 2048 26.2 / 27.8 / 44.0; below 128 rows one each).
-int64_t bn_target(int64_t rows, int64_t H, int dtype) {
-    const BnShape s = bn_shape(H, dtype, true);
+int64_t bn_target(const BnShape& s, int64_t rows, int64_t H) {
     int64_t most = BN_CUS * std::max(1, BN_CU_THREADS / bn_threads(s));
     if (s.tpr == 256 && s.e == 16 && 4 * H > 3 * 256 * 16 && H % 8 == 0) most = BN_CUS;
     return std::min(most, std::max({BN_FEW_BLOCKS, std::min<int64_t>(BN_CUS, rows / 4), rows / 8}));
 }
 // That plan, or the largest power-of-two fraction of it whose sums fit `cap` bytes.
-BnPlan bn_plan(int64_t rows, int64_t H, int dtype, int64_t per, bool pre, bool post, bool gate_sum, size_t cap) {
-    for (int64_t target = bn_target(rows, H, dtype);; target /= 2) {
-        const BnPlan p = bn_plan_for(rows, H, dtype, per, pre, post, gate_sum, target);
+BnPlan bn_plan(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool pre, bool post, bool gate_sum, size_t cap) {
+    for (int64_t target = bn_target(s, rows, H);; target /= 2) {
+        const BnPlan p = bn_plan_for(s, rows, H, per, pre, post, gate_sum, target);
         if (p.total_bytes <= cap || target == 1) return p;
     }
 }
@@ -178,7 +178,7 @@ void launch_bwd(const BnArgs& a, const dim3& grid, hipStream_t s) {
     constexpr int NV = E / RowVec<T>::N;
     const dim3 block(bn_block<TPR>);
 #define BN_BWD(POST, GATE) \
-    hipLaunchKernelGGL((block_norm_bwd_kernel<T, TPR, NV, POST, GATE, (NV <= 2), NT>), grid, block, 0, s, a)
+    hipLaunchKernelGGL((block_norm_bwd_kernel<T, TPR, NV, POST, GATE, (NV <= 2), (E == 32), NT>), grid, block, 0, s, a)
 #define BN_BWD_GATE(POST)                             \
     do {                                              \
         if (!a.gate) BN_BWD(POST, BN_GATE_NONE);      \
@@ -216,9 +216,8 @@ int run_fwd(const BnArgs& a, hipStream_t s) {
     return FLCE_OK;
 }
 template <typename T, bool NT>
-int run_bwd(const BnArgs& a, const BnPlan& p, void* dgamma_pre, void* dgamma_post, hipStream_t s) {
+int run_bwd(const BnArgs& a, const BnShape& sh, const BnPlan& p, void* dgamma_pre, void* dgamma_post, hipStream_t s) {
     constexpr bool F32 = std::is_same<T, float>::value;
-    const BnShape sh = bn_shape(a.H, F32 ? FLCE_F32 : FLCE_BF16, true);
     const dim3 grid((unsigned)p.blocks);
     if (sh.tpr == 16 && sh.e == 8) {
         launch_bwd<T, NT, 16, 8>(a, grid, s);
@@ -230,8 +229,10 @@ int run_bwd(const BnArgs& a, const BnPlan& p, void* dgamma_pre, void* dgamma_pos
         launch_bwd<T, NT, 256, 8>(a, grid, s);
     } else if (sh.tpr == (F32 ? 512 : 256) && sh.e == (F32 ? 8 : 16)) {
         launch_bwd<T, NT, F32 ? 512 : 256, F32 ? 8 : 16>(a, grid, s);
-    } else if (sh.tpr == 512) {
+    } else if (sh.tpr == 512 && sh.e == 16) {
         launch_bwd<T, NT, 512, 16>(a, grid, s);
+    } else if (sh.tpr == 512) {
+        launch_bwd<T, NT, 512, 32>(a, grid, s);
     } else {
         hipLaunchKernelGGL((block_norm_bwd_long<T, NT>), grid, dim3(BN_LONG_THREADS), 0, s, a);
     }
@@ -348,7 +349,8 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
         FLCE_TRY(shared_workspace_lent(&lent));
         if (lent) cap = lent;
     }
-    const BnPlan p = bn_plan(b.rows, b.H, b.dtype, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
+    const BnShape shape = bn_shape(b.H, b.dtype, true, gamma_post && gate && !by_row);
+    const BnPlan p = bn_plan(shape, b.rows, b.H, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
     if (p.total_bytes > cap) return FLCE_ERR_WORKSPACE;
     char* ws = static_cast<char*>(b.workspace);
     if (!ws && p.total_bytes) FLCE_TRY(shared_workspace(p.total_bytes, &ws));
@@ -374,7 +376,7 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     a.lddgate = ld.dgate;
     a.part_pre = dgamma_pre ? f : nullptr;
     a.part_post = dgamma_post ? f + p.off_post : nullptr;
-    a.part_gate = sums && (!p.direct || !bn_shape(b.H, b.dtype, true).tpr) ? f + p.off_gate : nullptr;
+    a.part_gate = sums && (!p.direct || !shape.tpr) ? f + p.off_gate : nullptr;
     a.rows = (int)b.rows;
     a.H = (int)b.H;
     a.per = (int)p.per;
@@ -388,10 +390,10 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     const bool nt = bn_nontemporal(b, 2 * (h != nullptr) + (dh != nullptr) + (y != nullptr) + (dx != nullptr) + (dy != nullptr) + by_row + (by_row && dgate));
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (nt)
-        return b.dtype == FLCE_F32 ? run_bwd<float, true>(a, p, dgamma_pre, dgamma_post, s)
-                                   : run_bwd<bf16_t, true>(a, p, dgamma_pre, dgamma_post, s);
-    return b.dtype == FLCE_F32 ? run_bwd<float, false>(a, p, dgamma_pre, dgamma_post, s)
-                               : run_bwd<bf16_t, false>(a, p, dgamma_pre, dgamma_post, s);
+        return b.dtype == FLCE_F32 ? run_bwd<float, true>(a, shape, p, dgamma_pre, dgamma_post, s)
+                                   : run_bwd<bf16_t, true>(a, shape, p, dgamma_pre, dgamma_post, s);
+    return b.dtype == FLCE_F32 ? run_bwd<float, false>(a, shape, p, dgamma_pre, dgamma_post, s)
+                               : run_bwd<bf16_t, false>(a, shape, p, dgamma_pre, dgamma_post, s);
 }
 
 size_t flce_block_norm_workspace_bytes(const flce_block_norm* args) {
@@ -399,10 +401,12 @@ size_t flce_block_norm_workspace_bytes(const flce_block_norm* args) {
     int64_t gate_rows;
     if (check_common(args, &ld, &gate_rows) != FLCE_OK) return 0;
     const int64_t per = args->rows_per_gate ? args->rows_per_gate : args->rows;
-    const size_t with_gate = bn_plan(args->rows, args->H, args->dtype, per, true, true, true, SIZE_MAX).total_bytes;
-    // (a gate row per row, or no gate: the gammas' sums alone, in a plan of their own)
-    const size_t without = bn_plan(args->rows, args->H, args->dtype, args->rows, true, true, false, SIZE_MAX).total_bytes;
-    return std::max(with_gate, without);
+    const int64_t rows = args->rows, H = args->H;
+    // three sets of sums, or (a gate row per row, or none) the gammas' alone, each in a plan of its own
+    const size_t with_gate = bn_plan(bn_shape(H, args->dtype, true, true), rows, H, per, true, true, true, SIZE_MAX).total_bytes;
+    const size_t two_sums = bn_plan(bn_shape(H, args->dtype, true), rows, H, per, true, false, true, SIZE_MAX).total_bytes;
+    const size_t without = bn_plan(bn_shape(H, args->dtype, true), rows, H, rows, true, true, false, SIZE_MAX).total_bytes;
+    return std::max({with_gate, two_sums, without});
 }
 
 }  // extern "C"

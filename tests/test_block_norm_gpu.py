@@ -128,7 +128,7 @@ def check_backward(c, **kw):
 
 
 # the edges of the kernels' shapes: 16 .. 1024 threads per row, vectors that end inside a row, the long form
-WIDTHS = [1, 3, 8, 9, 100, 127, 128, 129, 500, 512, 520, 1000, 1025, 2048, 2051, 2304, 4095, 4096, 4100, 8192, 8195, 16384, 16392, 20001]
+WIDTHS = [1, 3, 8, 9, 100, 127, 128, 129, 500, 512, 520, 1000, 1025, 2048, 2051, 2304, 4095, 4096, 4100, 8192, 8195, 13312, 13320, 16384, 16392, 20001]
 VARIANTS = [dict(), dict(post=True), dict(gate="channel", kind="sigmoid"), dict(post=True, gate="channel", kind="linear"),
             dict(post=True, gate="sequence", per=5, kind="silu"), dict(gate="sequence", per=2, kind="tanh"),
             dict(post=True, gate="token", kind="tanh"), dict(gate="token", kind="silu"), dict(y=False),
@@ -176,8 +176,10 @@ def test_every_variant(variant, dtype):
     (1500, 520, "bf16", dict(post=True, gate="sequence", per=400, kind="tanh")),   # gate rows cut into parts
     (1301, 2048, "bf16", dict(post=True)), (2600, 1024, "f32", dict(gate="token", kind="linear")),
     (1111, 4096, "bf16", dict(gate="sequence", per=1200, kind="silu")),      # one gate row, not quite used up
-    (700, 8200, "bf16", dict(post=True, gate="sequence", per=100)),          # long form, several rows per workgroup
+    (700, 8200, "bf16", dict(post=True, gate="sequence", per=100)),          # sums in LDS, several rows per workgroup
     (600, 8200, "f32", dict(gate="sequence", per=2, kind="tanh")),           # ... and more gate rows than workgroups
+    (500, 13400, "bf16", dict(post=True, gate="sequence", per=100)),         # long form: three sets beyond the LDS
+    (300, 16500, "f32", dict(gate="sequence", per=1, kind="tanh")), (520, 16500, "bf16", dict(gate="sequence", per=2)),
 ], ids=_name)
 def test_many_rows(rows, H, dtype, variant):
     print(f"case many rows={rows} H={H} {dtype} {variant}", flush=True)
