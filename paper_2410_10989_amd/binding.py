@@ -399,7 +399,7 @@ def flce_block_norm_fwd(x, y=None, gamma_pre=None, gamma_post=None, gate=None, g
     pg, ldg = _rows_ptr(gate, "gate", like, _gate_shape(gate, shape, rows_per_gate))
     ph, ldh = _rows_ptr(h, "h", like, shape)
     pn, ldn = _rows_ptr(n, "n", like, shape)
-    args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), rows_per_gate, scale, eps,
+    args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), int(rows_per_gate), scale, eps,
                          ldx, ldy, ldh, ldn, ldg)
     with _OnDevice(device):
         st = lib().flce_block_norm_fwd(px, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec)[0],
@@ -453,7 +453,7 @@ def flce_block_norm_bwd(h=None, dn=None, dh=None, y=None, gamma_pre=None, gamma_
     pdh, lddh = _rows_ptr(dh, "dh", like, shape)
     py, ldy = _rows_ptr(y, "y", like, shape)
     pg, ldg = _rows_ptr(gate, "gate", like, gshape)
-    args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), rows_per_gate, scale, eps,
+    args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), int(rows_per_gate), scale, eps,
                          0, ldy, ldh, 0, ldg, lddx, lddy, lddh, lddn, lddg, *_workspace_args(workspace))
     with _OnDevice(device):
         st = lib().flce_block_norm_bwd(ph, pdn, pdh, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec)[0],

@@ -100,12 +100,17 @@ __device__ __forceinline__ void bn_shift_tail(u32x4& r, int rem) {
     }
 }
 
+// 1 / (1 + e), e in [0, 1]: the hardware's reciprocal (1 ulp) and one Newton step.
+__device__ __forceinline__ float bn_one_over_1p(float e) {
+    const float x = 1.0f + e, d = __builtin_amdgcn_rcpf(x);
+    return fmaf(fmaf(-x, d, 1.0f), d, d);
+}
 // a(g) and a'(g).  exp is taken of -|g| only, and 1 - sigmoid and the derivatives come as products of what
 // does not cancel, so that they keep their relative accuracy where a gate saturates.
 __device__ __forceinline__ float bn_act(int act, float g) {
     if (act == BN_ACT_LINEAR) return g;
     if (act == BN_ACT_TANH) return tanhf(g);
-    const float e = expf(-fabsf(g)), d = 1.0f / (1.0f + e);
+    const float e = expf(-fabsf(g)), d = bn_one_over_1p(e);
     const float sig = g >= 0.f ? d : e * d;
     return act == BN_ACT_SIGMOID ? sig : g * sig;
 }
@@ -114,11 +119,11 @@ __device__ __forceinline__ void bn_act_both(int act, float g, float& a, float& d
         a = g;
         da = 1.0f;
     } else if (act == BN_ACT_TANH) {
-        const float e = expf(-2.0f * fabsf(g)), d = 1.0f / (1.0f + e);
+        const float e = expf(-2.0f * fabsf(g)), d = bn_one_over_1p(e);
         a = tanhf(g);
         da = 4.0f * e * d * d;
     } else {
-        const float e = expf(-fabsf(g)), d = 1.0f / (1.0f + e);
+        const float e = expf(-fabsf(g)), d = bn_one_over_1p(e);
         const float sig = g >= 0.f ? d : e * d, rest = g >= 0.f ? e * d : d;
         a = act == BN_ACT_SIGMOID ? sig : g * sig;
         da = act == BN_ACT_SIGMOID ? sig * rest : sig * (1.0f + g * rest);
@@ -804,8 +809,9 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
 }
 
 // out[g][j] = sum over p of rows [g * parts + p][j] of fp32 partial sums, for up to three sets of them: the two
-// gammas (one output row each) and the gate.  As in rmsnorm_dgamma_kernel a workgroup owns 64 columns of an
-// output row, thread (c, q) adds rows q, q + 16, ... of column c, then the 16 sums are added in order; in fp64, which
+// gammas (one output row each) and the gate.  As in rmsnorm_dgamma_kernel a workgroup owns some columns of an
+// output row (32: lines of 128 bytes), thread (c, q) adds rows q, q + 32, ... of column c, then the 32 sums are added in
+// order; in fp64, which
 // costs nothing here and leaves the fp32 sums of a workgroup's own rows as the only ones.
 struct BnSums {
     const float* part[3];
@@ -814,7 +820,7 @@ struct BnSums {
     int parts[3];
     int first[4];   // the sets' output rows are rows first[i] .. first[i + 1] of the grid
 };
-constexpr int BN_SUM_COLS = 64, BN_SUM_PARTS = 16;
+constexpr int BN_SUM_COLS = 32, BN_SUM_PARTS = 32;
 template <typename T>
 __global__ __launch_bounds__(BN_SUM_COLS * BN_SUM_PARTS) void bn_sum_partials_kernel(BnSums b, int n) {
     __shared__ double sums[BN_SUM_PARTS][BN_SUM_COLS];
@@ -825,8 +831,13 @@ __global__ __launch_bounds__(BN_SUM_COLS * BN_SUM_PARTS) void bn_sum_partials_ke
     const float* from = b.part[set] + (int64_t)g * parts * n + j;
     double s = 0.0;
     if (j < n)
-#pragma unroll 8
-        for (int p = q; p < parts; p += BN_SUM_PARTS) s += (double)from[(int64_t)p * n];
+        for (int p0 = q; p0 < parts; p0 += 8 * BN_SUM_PARTS) {   // (eight loads under way, also where there are fewer)
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = from[(int64_t)min(p0 + k * BN_SUM_PARTS, parts - 1) * n];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += p0 + k * BN_SUM_PARTS < parts ? (double)v[k] : 0.0;
+        }
     sums[q][c] = s;
     __syncthreads();
     if (q == 0 && j < n) {
