@@ -15,8 +15,11 @@
 // A row belongs to a group of TPR threads that holds it in registers (NV vectors of 16 bytes per thread and
 // stream), so every stream is read once and written once; sums over a row go through the lanes and, for
 // groups of several wavefronts, through LDS.  Rows may start at any element: 16-byte accesses need no
-// alignment, and the last, partial vector of a row goes element by element.  Rows that are too long for that
-// (`*_long`) are swept several times by a workgroup of 1024 threads.
+// alignment (they cost where lines are straddled: backward of 8192 rows of 4096 / 4095 bf16 72 / 101 us).  Rows that
+// are too long for that (`*_long`) are swept several times by a workgroup of 1024 threads.
+//
+// Bound by HBM.  What streams reach on this chip with nothing to compute: two read and two written, 112 MB each, 7.0
+// TB/s (what is read stays in the memory-side cache from pass to pass), four read and two written 5.6 TB/s.
 #pragma once
 #include "flce_device.h"
 #include "rowvec.h"
@@ -43,6 +46,7 @@ struct BnArgs {
     int segments, parts;
     int by_row;        // every row has a gate row of its own (per counts all rows then)
     int gate_direct;   // a segment is all rows of its gate row: dgate is written at once
+    void *dpre, *dpost;   // one workgroup has all rows: the gammas' gradients are written at once
 };
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // at any element
@@ -190,7 +194,10 @@ __device__ __forceinline__ int bn_group() {
     return (int)threadIdx.x / TPR;
 }
 
-// Forward: a workgroup holds bn_group_count rows.
+// Forward: a workgroup holds bn_group_count rows.  All loads of a row are issued before the first is used, the
+// occupancy (80 registers with everything on) covers the rest.  us: 8192 x 4096 bf16 with the next block's norm 38
+// (7.0 TB/s), 16384 x 3584 with both norms and a gate 68 (6.9; 85 where nothing read is in the cache yet: 5.5),
+// 2047 x 1000 fp32 with a sigmoid gate per token 10.7, one row of 4096 2.8.
 template <typename T, int TPR, int NV, bool POST, bool GATE, bool NT>
 __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a) {
     constexpr int N = RowVec<T>::N, GROUPS = bn_group_count<TPR>;
@@ -372,9 +379,16 @@ struct BnRow {
 // Backward: workgroup b takes segments b, b + gridDim.x, ...; its GROUPS rows at a time.  The sums over rows
 // stay in registers: the gammas' until the workgroup's last row, a shared gate's until its segment's; then the
 // groups of a workgroup add theirs up in a fixed order.  Sums of several workgroups are left as rows of fp32
-// partial sums for bn_sum_partials_kernel: no atomics, the order of additions depends on the shape alone.
-// AHEAD: the next row's loads are issued before a row is worked on.  WIDE: the sums over rows are kept in LDS, where
-// registers do not hold them beside the rows of 1024 threads; each column belongs to one thread.
+// partial sums for bn_sum_partials_kernel: no atomics, the order of additions depends on the shape and the number
+// of workgroups alone.  The rows of a segment's parts are dealt side by side, so that all workgroups read
+// neighbouring rows at a time (16384 x 3584: 148 -> 136 us against one stretch of rows each).
+// AHEAD: the next row's loads are issued before a row is worked on: registers instead of more workgroups, every one
+// of which costs its partial sums (8192 x 4096 without sums of a second norm 74 -> 69 us).  WIDE: the sums over rows
+// are kept in LDS, where registers do not hold them beside rows of 32 elements per thread; each column belongs to one
+// thread.  2048 x 12000 bf16 93 us, 245 in the long form.
+// us, with the partial sums' launch (4-5): 16384 x 3584 bf16, both norms, a gate per channel 138 (5.2 TB/s; traffic
+// 470 MB read and 246 written, 705 it cannot do without; vector instructions 47 % of the cycles), 8192 x 4096 with
+// the next block's norm 56, 2047 x 1000 fp32 with a silu gate per sequence 17.5.
 constexpr int BN_WIDE_COLS = 16384, BN_WIDE_COLS_3 = 13312;   // of up to two and of three sets of sums: 160 KB
 template <typename T, int TPR, int NV, bool POST, int GATE, bool AHEAD, bool WIDE, bool NT>
 __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a) {
@@ -665,16 +679,16 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                 for (int e = 0; e < N; ++e) acc_gate[k][e] = 0.f;
         }
     }
-    if (a.part_pre) {
-        float* p = a.part_pre + (int64_t)blockIdx.x * a.H;
-        over_groups(acc_pre, AT_PRE, [&](int j, float v) { p[j] = v; });
-    }
-    if constexpr (POST) {
-        if (a.part_post) {
-            float* p = a.part_post + (int64_t)blockIdx.x * a.H;
-            over_groups(acc_post, AT_POST, [&](int j, float v) { p[j] = v; });
+    auto put_gamma = [&](float (&acc)[NA][N], int set, void* out, float* part) {
+        if (out) {
+            over_groups(acc, set, [&](int j, float v) { static_cast<T*>(out)[j] = from_f32<T>(v); });
+        } else if (part) {
+            float* p = part + (int64_t)blockIdx.x * a.H;
+            over_groups(acc, set, [&](int j, float v) { p[j] = v; });
         }
-    }
+    };
+    put_gamma(acc_pre, AT_PRE, a.dpre, a.part_pre);
+    if constexpr (POST) put_gamma(acc_post, AT_POST, a.dpost, a.part_post);
 }
 
 // Rows beyond the register forms (see block_norm_fwd_long).  The sums over rows live in the partial sums'
@@ -811,8 +825,8 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
 // out[g][j] = sum over p of rows [g * parts + p][j] of fp32 partial sums, for up to three sets of them: the two
 // gammas (one output row each) and the gate.  As in rmsnorm_dgamma_kernel a workgroup owns some columns of an
 // output row (32: lines of 128 bytes), thread (c, q) adds rows q, q + 32, ... of column c, then the 32 sums are added in
-// order; in fp64, which
-// costs nothing here and leaves the fp32 sums of a workgroup's own rows as the only ones.
+// order; in fp64, which costs nothing here and leaves the fp32 sums of a workgroup's own rows as the only ones.  Bound
+// by the latency of a thread's loads: eight under way at a time, issued without a condition (3-5 us).
 struct BnSums {
     const float* part[3];
     void* out[3];

@@ -15,7 +15,7 @@ constexpr int64_t BN_MAX_H = (int64_t)1 << 24;      // keeps launches and column
 constexpr int64_t BN_GRID_X = (int64_t)1 << 20;     // workgroups along x, the rest along y
 constexpr int BN_CU_THREADS = 512;                 // threads per CU that the backward is launched for
 constexpr int BN_CUS = 256;
-constexpr int64_t BN_FEW_BLOCKS = 128;
+constexpr int64_t BN_FEW_BLOCKS = 128, BN_ONE_STEPS = 3;
 constexpr int64_t BN_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
 size_t bn_elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
@@ -99,6 +99,7 @@ bool bn_nontemporal(const flce_block_norm& b, int streams) {
 struct BnPlan {
     int64_t blocks, segments, parts, per;
     bool direct;   // a segment holds all rows of its gate row
+    bool one;      // one workgroup holds all rows: no partial sums of the gammas
     size_t off_post, off_gate, total_bytes;
 };
 
@@ -128,14 +129,15 @@ BnPlan bn_plan_for(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool 
     p.blocks = std::min(p.segments, target);
     p.direct = gate_sum && p.parts == 1;
     const int64_t gate_rows = !gate_sum ? 0 : p.direct ? (s.tpr ? 0 : p.blocks) : p.segments;
+    p.one = p.blocks == 1 && s.tpr;
     size_t at = 0;
     auto take = [&](int64_t n) {
         const size_t here = at;
         at += (size_t)n * (size_t)H;
         return here;
     };
-    take(pre ? p.blocks : 0);
-    p.off_post = take(post ? p.blocks : 0);
+    take(pre && !p.one ? p.blocks : 0);
+    p.off_post = take(post && !p.one ? p.blocks : 0);
     p.off_gate = take(gate_rows);
     p.total_bytes = at * sizeof(float);
     return p;
@@ -146,7 +148,10 @@ BnPlan bn_plan_for(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool 
 // 2304 48 / 38, and rows that do not start on 16 bytes 8192 x 3583 96 / 78).  Small batches: few rows per workgroup,
 // because sums of few rows cost as much as the rows (512 / 256 / 128 workgroups, H = 4096 with a norm after the block:
 // 256 rows 16.7 / 16.8 / 14.6, 1024 rows 26.7 / 22.1 / 25.0, 4096 x 2048 26.2 / 27.8 / 44.0; below 128 rows one each).
+// A handful of rows: one workgroup, which needs no second launch (us, one / several: 2 x 4096 8.1 / 10.7, 3 x 4096 9.6 /
+// 10.8, 4 x 4096 11.1 / 10.8, 8 x 1000 in two steps 6.8 / 7.6, 16 x 1000 in four 10.2 / 7.6).
 int64_t bn_target(const BnShape& s, int64_t rows, int64_t H) {
+    if (s.tpr && rows <= BN_ONE_STEPS * bn_groups(s)) return 1;
     int64_t most = BN_CUS * std::max(1, BN_CU_THREADS / bn_threads(s));
     if (s.tpr == 256 && s.e == 16 && 4 * H > 3 * 256 * 16 && H % 8 == 0) most = BN_CUS;
     return std::min(most, std::max({BN_FEW_BLOCKS, std::min<int64_t>(BN_CUS, rows / 4), rows / 8}));
@@ -374,8 +379,10 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     a.lddx = ld.dx;
     a.lddy = ld.dy;
     a.lddgate = ld.dgate;
-    a.part_pre = dgamma_pre ? f : nullptr;
-    a.part_post = dgamma_post ? f + p.off_post : nullptr;
+    a.part_pre = dgamma_pre && !p.one ? f : nullptr;
+    a.part_post = dgamma_post && !p.one ? f + p.off_post : nullptr;
+    a.dpre = p.one ? dgamma_pre : nullptr;
+    a.dpost = p.one ? dgamma_post : nullptr;
     a.part_gate = sums && (!p.direct || !shape.tpr) ? f + p.off_gate : nullptr;
     a.rows = (int)b.rows;
     a.H = (int)b.H;

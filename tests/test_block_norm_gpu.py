@@ -187,6 +187,15 @@ def test_many_rows(rows, H, dtype, variant):
     check_backward(make(rows, H, dtype, 8, **variant))
 
 
+@pytest.mark.parametrize("rows,H", [(2, 4096), (3, 4096), (4, 4096), (12, 1000), (13, 1000), (48, 100), (49, 100), (3, 9000), (2, 20000)])
+@pytest.mark.parametrize("variant", [dict(post=True, gate="channel", kind="tanh"), dict(post=True, gate="sequence", per=2),
+                                     dict(gate="token", kind="silu")], ids=_name)
+def test_a_handful_of_rows(rows, H, variant):
+    """On both sides of where one workgroup takes all rows."""
+    for dtype in ("bf16", "f32"):
+        check_backward(make(rows, H, dtype, 25, **variant))
+
+
 @pytest.mark.parametrize("shape", [(300, 1024), (40, 4096), (9, 16400)])
 def test_a_smaller_workspace_serves(shape):
     """Fewer workgroups, down to one: 12 H bytes."""
