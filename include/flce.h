@@ -270,9 +270,10 @@ FLCE_API int flce_cross_entropy_inplace_noalloc(void* Z, const int64_t* targets,
  *     dx = dh + rms-norm backward of dn       (the gradient of x, and of all of h)
  *     dy, dgate, dgamma_post, dgamma_pre
  *
- * Gradients of what several rows share (gammas, gates) are summed in fp32 without atomics, in an
- * order that depends on the shape and the room for partial sums alone; every output is rounded
- * once.
+ * Gradients of what several rows share (gammas, gates) are summed in fp32 (the workgroups' sums
+ * in fp64) without atomics, in an order that depends on the shape and the room for partial sums
+ * alone; every output is rounded to dtype once.  A row's sums are fp32: rows whose mean square
+ * leaves that type's range give what fp32 arithmetic gives.
  *
  *   size            must be sizeof(flce_block_norm) (FLCE_ERR_ARG otherwise)
  *   rows, H         1 .. 2^30 and 1 .. 2^24
@@ -288,8 +289,8 @@ FLCE_API int flce_cross_entropy_inplace_noalloc(void* Z, const int64_t* targets,
  *   workspace       device buffer (256-byte aligned) for the backward's partial sums, or NULL for
  *                   the device's shared workspace; workspace_bytes: flce_block_norm_workspace_bytes
  *                   of the same arguments, or less at the price of fewer workgroups
- *                   (12 H bytes always do; FLCE_ERR_WORKSPACE if not even one serves).  The
- *                   forward uses none.
+ *                   (12 H bytes always do; FLCE_ERR_WORKSPACE if not even one serves).  A few
+ *                   rows need none (0 bytes), nor does the forward.
  *
  * Forward: x or y may be NULL (not both; without y there is no gate, gamma_post or h); gate,
  * gamma_post and gamma_pre may be NULL (without gamma_pre there is no n).  Backward: dh may be

@@ -16,7 +16,7 @@ from .binding import (  # noqa: F401
     flce_workspace_bytes_max, lib, status_string, flce_timing_enable, flce_timing_collect,
     flce_mfma_ceiling_launch,
     flce_block_norm_fwd, flce_block_norm_bwd, flce_block_norm_workspace_bytes, FlceBlockNorm, GATE_ACTS,
-    flce_grad_norm, flce_grad_clip, flce_clip_grad_norm,
+    flce_grad_norm, flce_grad_clip, flce_clip_grad_norm, flce_grad_norm_workspace_bytes,
     KERNEL_KINDS,
 )
 

@@ -454,7 +454,7 @@ def flce_block_norm_bwd(h=None, dn=None, dh=None, y=None, gamma_pre=None, gamma_
     py, ldy = _rows_ptr(y, "y", like, shape)
     pg, ldg = _rows_ptr(gate, "gate", like, gshape)
     args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), int(rows_per_gate), scale, eps,
-                         0, ldy, ldh, 0, ldg, lddx, lddy, lddh, lddn, lddg, *_workspace_args(workspace))
+                         0, ldy, ldh, 0, ldg, lddx, lddy, lddh, lddn, lddg, *_workspace_args(workspace, device))
     with _OnDevice(device):
         st = lib().flce_block_norm_bwd(ph, pdn, pdh, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec)[0],
                                        _rows_ptr(gamma_pre, "gamma_pre", like, vec)[0], ctypes.byref(args), pdx, pdy, pdg,
@@ -469,6 +469,11 @@ def flce_block_norm_workspace_bytes(rows, H, dtype, rows_per_gate=0) -> int:
     b.size, b.rows, b.H, b.dtype = ctypes.sizeof(FlceBlockNorm), rows, H, _DTYPES.get(dtype, dtype)
     b.rows_per_gate = rows_per_gate
     return int(lib().flce_block_norm_workspace_bytes(ctypes.byref(b)))
+
+
+def flce_grad_norm_workspace_bytes(n_tensors) -> int:
+    """Bytes flce_grad_norm and flce_clip_grad_norm use for a list of that many tensors."""
+    return int(lib().flce_grad_norm_workspace_bytes(int(n_tensors)))
 
 
 NORM_TYPES = {2.0: 0, float("inf"): 1}
@@ -525,9 +530,11 @@ def _out_list(outs, device, counts, dtypes):
     return ptrs
 
 
-def _workspace_args(workspace):
+def _workspace_args(workspace, device):
     if workspace is None:
         return None, 0
+    if workspace.device != device:
+        raise ValueError(f"workspace must live on {device}")
     return _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
 
 
@@ -538,7 +545,7 @@ def flce_grad_norm(grads, norm_type=2.0, norm=None, workspace=None, stream=None)
     norm = _norm_out(norm, device)
     with _OnDevice(norm.device):
         st = lib().flce_grad_norm(_at(ptrs), _at(counts), _at(dtypes), len(grads), _norm_type(norm_type), norm.data_ptr(),
-                                  *_workspace_args(workspace), _stream_handle(stream, norm.device))
+                                  *_workspace_args(workspace, norm.device), _stream_handle(stream, norm.device))
     _check(st, "flce_grad_norm")
     return norm
 
@@ -565,7 +572,7 @@ def flce_clip_grad_norm(grads, max_norm, norm_type=2.0, outs=None, norm=None, wo
     with _OnDevice(norm.device):
         st = lib().flce_clip_grad_norm(_at(ptrs), _at(to), _at(counts), _at(dtypes), len(grads),
                                        _norm_type(norm_type), float(max_norm), norm.data_ptr(),
-                                       *_workspace_args(workspace), _stream_handle(stream, norm.device))
+                                       *_workspace_args(workspace, norm.device), _stream_handle(stream, norm.device))
     _check(st, "flce_clip_grad_norm")
     return norm
 

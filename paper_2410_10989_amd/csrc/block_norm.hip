@@ -68,7 +68,8 @@ int check_common(const flce_block_norm* b, Strides* st, int64_t* gate_rows) {
 // The register forms: TPR threads per row with E elements each (a table by width, not by size: each row of it was the
 // fastest of its neighbours over its range).  Twice the elements per thread halve what a row costs besides them (sums
 // over lanes, addresses), half of them leaves registers for more wavefronts: backward, us, 8 / 16 elements: 8192 x 2048
-// 46 / 50, 8192 x 2304 45 / 38, 8192 x 1000 29 / 24, 16384 x 512 20 / 22.  fp32 rows have half the elements per load
+// 46 / 50, 8192 x 2304 45 / 38, 16384 x 512 20 / 22; rows of 513 .. 1024 in one wavefront of 16 elements per lane, or two
+// of 8: 16384 x 768 26 / 40 (forward 16.4 / 16.9), 2048 x 1000 9.6 / 13.1.  fp32 rows have half the elements per load
 // in flight: 4096 x 4096 67 / 72.
 struct BnShape {
     int tpr, e;   // tpr = 0: the long form

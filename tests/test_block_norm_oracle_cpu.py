@@ -161,14 +161,25 @@ def test_block_norm_refuses_missing_misaligned_and_overlapping_memory():
     assert bwd(dy=a + 1537) == 4 and bwd(dh=a + 513) == 4
     assert bwd(dx=a) == 7 and bwd(dx=a + 514) == 7 and bwd(dy=a + 512) == 7 and bwd(dy=a + 1280) == 7 and bwd(dpre=a + 1024) == 7
     assert bwd(workspace=a + 2050, workspace_bytes=1 << 20) == 4
-    assert bwd(workspace=a + 2048, workspace_bytes=31) == 5      # 4 H bytes for each set of sums
-    assert bwd(workspace=a + 2048, workspace_bytes=63, gate=a + 4096, post=a + 4352, dgate=a + 4608, dpost=a + 4864) == 5
+    # rows that do not fit registers: 4 H bytes for each of the shared gradients at the least
+    long = (ctypes.c_char * (4 << 20))()
+    w = ctypes.addressof(long)
+    w += (-w) % 256
+    at = lambda k: w + (1 << 18) * k
+
+    def rows_of_17000(nbytes, gate=None, post=None):
+        b = _args(H=17000, workspace=at(13), workspace_bytes=nbytes)
+        return L.flce_block_norm_bwd(at(0), at(1), at(2), at(3), gate, post, at(4), ctypes.byref(b), at(5), at(6),
+                                     at(7) if gate else None, at(8) if post else None, at(9), None)
+
+    for sets, gate, post in ((1, None, None), (2, at(10), None), (3, at(10), at(11))):
+        assert rows_of_17000(4 * 17000 * sets - 1, gate, post) == 5
 
 
 def test_block_norm_workspace_is_bounded():
     need = [flce.flce_block_norm_workspace_bytes(rows, 4096, torch.bfloat16, per)
             for rows in (1, 1000, 10 ** 6, 2 ** 30) for per in (0, 1, 5, 2048)]
-    assert all(8 * 4096 <= n <= 128 << 20 for n in need)
+    assert all(n <= 128 << 20 for n in need) and all(n >= 8 * 4096 for n in need[4:])
     assert flce.flce_block_norm_workspace_bytes(2 ** 30, 2 ** 24, torch.float32) <= 3 * 256 * 2 ** 24 * 4
     assert flce.flce_block_norm_workspace_bytes(0, 8, torch.float32) == 0
 

@@ -132,12 +132,11 @@ def test_a_norm_of_several_shards():
 def test_same_bits_on_another_stream_and_with_a_workspace_of_its_own():
     import paper_2410_10989_amd as flce
     _, grads = make([100_003, 70_000, 5] * 60, [B, F], 7)
-    L = flce.lib()
     outs = [torch.empty_like(g) for g in grads]
     want = flce.flce_clip_grad_norm(grads, 1.0, outs=outs)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
-    need = L.flce_grad_norm_workspace_bytes(len(grads))
+    need = flce.flce_grad_norm_workspace_bytes(len(grads))
     ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")
     for _ in range(3):
         outs2 = [torch.empty_like(g) for g in grads]
@@ -151,7 +150,7 @@ def test_same_bits_on_another_stream_and_with_a_workspace_of_its_own():
 def test_captured_and_replayed():
     import paper_2410_10989_amd as flce
     _, grads = make([50_001, 333, 8] * 50, [F, B], 8)
-    ws = torch.empty(flce.lib().flce_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(flce.flce_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device="cuda")
     norm = torch.empty((), device="cuda")
     outs = [torch.empty_like(g) for g in grads]
     flce.flce_clip_grad_norm(grads, 1.0, outs=outs, norm=norm, workspace=ws)
@@ -196,6 +195,8 @@ def test_binding_refusals():
                dict(norm=torch.zeros((), dtype=torch.float64, device="cuda"))):
         with pytest.raises((ValueError, KeyError)):
             flce.flce_clip_grad_norm([g], 1.0, **kw)
+    with pytest.raises(ValueError):
+        flce.flce_grad_norm([g], workspace=torch.empty(1 << 20, dtype=torch.uint8))
     for grads in ([g, g], [g, g[1:3]]):
         with pytest.raises(flce.FlceError) as e:
             flce.flce_clip_grad_norm(grads, 1.0)
