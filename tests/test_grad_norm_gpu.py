@@ -105,6 +105,18 @@ def test_values_whose_squares_leave_the_range_of_fp32():
         clip(grads, 2.0, 0.5, outs=[torch.empty_like(g) for g in grads])
 
 
+def test_the_smallest_numbers_are_kept():
+    """Numbers below the normal range of fp32 and bf16, scaled by 1 and by 1/2."""
+    import paper_2410_10989_amd as flce
+    t = [torch.full((300,), 2.0 ** -140, device="cuda"), torch.full((70,), 2.0 ** -130, dtype=torch.bfloat16, device="cuda")]
+    norm = torch.ones((), device="cuda")
+    outs = [torch.zeros_like(v) for v in t]
+    flce.flce_grad_clip(t, norm, 2.0, outs=outs)
+    assert all(torch.equal(a, b) for a, b in zip(outs, t))
+    flce.flce_grad_clip(t, norm * (2.0 - 1e-6), 1.0, outs=outs)
+    assert (outs[0] == 2.0 ** -141).all() and (outs[1] == 2.0 ** -131).all()
+
+
 def test_zero_gradients_and_a_threshold_of_zero():
     import paper_2410_10989_amd as flce
     z = [torch.zeros(1000, device="cuda"), torch.zeros(3, dtype=B, device="cuda")]
