@@ -50,6 +50,7 @@ struct BnArgs {
 };
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // at any element
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 
 // Vector v of a row: whole for v < nfull; vector nfull has rem elements.
 template <typename T>
@@ -446,15 +447,9 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
     auto pre_vector = [&](int k) { return WIDE ? load_shared(a.gpre, 0, t + k * TPR) : prev[k]; };
     [[maybe_unused]] auto post_vector = [&](int k) { return WIDE ? load_shared(a.gpost, 0, t + k * TPR) : postv[k]; };
 
-    // The sum over the workgroup's groups of a row of sums, handed column by column to put(column, value).
-    auto over_groups = [&](float (&acc)[NA][N], [[maybe_unused]] int set, auto put) {
-        if constexpr (WIDE) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if ((t + k * TPR) * N + e < a.H) put((t + k * TPR) * N + e, wide_at(set, k)[e]);
-        } else if constexpr (GROUPS > 1) {
+    // The workgroup's row of sums (over its groups, in order), rounded to `out` or as it is to `part`.
+    auto put_sums = [&](float (&acc)[NA][N], [[maybe_unused]] int set, T* out, float* part) {
+        if constexpr (GROUPS > 1) {
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < NV; ++k)
@@ -464,14 +459,26 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
             for (int j = threadIdx.x; j < TPR * NV * N && j < a.H; j += BLOCK) {
                 float s = cols[j];
                 for (int q = 1; q < GROUPS; ++q) s += cols[q * (TPR * NV * N) + j];
-                put(j, s);
+                if (out) out[j] = from_f32<T>(s); else part[j] = s;
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NV; ++k) {
+                float v[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if ((t + k * TPR) * N + e < a.H) put((t + k * TPR) * N + e, acc[k][e]);
+                for (int e = 0; e < N; ++e) v[e] = WIDE ? wide_at(set, k)[e] : acc[WIDE ? 0 : k][e];
+                const int at = t + k * TPR;
+                if (out) {
+                    bn_store<T, false>(out, at, nfull_all, rem_all, v);
+                } else if (at < nfull_all) {
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) *reinterpret_cast<f32x4_any*>(part + at * N + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+                } else if (at == nfull_all) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (e < rem_all) part[at * N + e] = v[e];
+                }
+            }
         }
     };
 
@@ -665,13 +672,8 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
             }
         }
         if constexpr (GATE == BN_GATE_SUM) {
-            if (a.gate_direct) {
-                T* p = static_cast<T*>(a.dgate) + (int64_t)seg.g * a.lddgate;
-                if (a.dgate) over_groups(acc_gate, AT_GATE, [&](int j, float v) { p[j] = from_f32<T>(v); });
-            } else if (a.part_gate) {
-                float* p = a.part_gate + (int64_t)s * a.H;
-                over_groups(acc_gate, AT_GATE, [&](int j, float v) { p[j] = v; });
-            }
+            if (a.gate_direct) put_sums(acc_gate, AT_GATE, static_cast<T*>(a.dgate) + (int64_t)seg.g * a.lddgate, nullptr);
+            else if (a.part_gate) put_sums(acc_gate, AT_GATE, nullptr, a.part_gate + (int64_t)s * a.H);
             if constexpr (WIDE) wide_clear(AT_GATE);
 #pragma unroll
             for (int k = 0; k < NA; ++k)
@@ -679,16 +681,12 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                 for (int e = 0; e < N; ++e) acc_gate[k][e] = 0.f;
         }
     }
-    auto put_gamma = [&](float (&acc)[NA][N], int set, void* out, float* part) {
-        if (out) {
-            over_groups(acc, set, [&](int j, float v) { static_cast<T*>(out)[j] = from_f32<T>(v); });
-        } else if (part) {
-            float* p = part + (int64_t)blockIdx.x * a.H;
-            over_groups(acc, set, [&](int j, float v) { p[j] = v; });
-        }
-    };
-    put_gamma(acc_pre, AT_PRE, a.dpre, a.part_pre);
-    if constexpr (POST) put_gamma(acc_post, AT_POST, a.dpost, a.part_post);
+    if (a.dpre) put_sums(acc_pre, AT_PRE, static_cast<T*>(a.dpre), nullptr);
+    else if (a.part_pre) put_sums(acc_pre, AT_PRE, nullptr, a.part_pre + (int64_t)blockIdx.x * a.H);
+    if constexpr (POST) {
+        if (a.dpost) put_sums(acc_post, AT_POST, static_cast<T*>(a.dpost), nullptr);
+        else if (a.part_post) put_sums(acc_post, AT_POST, nullptr, a.part_post + (int64_t)blockIdx.x * a.H);
+    }
 }
 
 // Rows beyond the register forms (see block_norm_fwd_long).  The sums over rows live in the partial sums'
