@@ -15,7 +15,7 @@
 // A row belongs to a group of TPR threads that holds it in registers (NV vectors of 16 bytes per thread and
 // stream), so every stream is read once and written once; sums over a row go through the lanes and, for
 // groups of several wavefronts, through LDS.  Rows may start at any element: 16-byte accesses need no
-// alignment (they cost where lines are straddled: backward of 8192 rows of 4096 / 4095 bf16 72 / 101 us).  Rows that
+// alignment (they cost where lines are straddled: backward of 8192 rows of 4096 / 4095 bf16 71 / 98 us).  Rows that
 // are too long for that (`*_long`) are swept several times by a workgroup of 1024 threads.
 //
 // Bound by HBM.  What streams reach on this chip with nothing to compute: two read and two written, 112 MB each, 7.0
@@ -382,20 +382,21 @@ struct BnRow {
 // groups of a workgroup add theirs up in a fixed order.  Sums of several workgroups are left as rows of fp32
 // partial sums for bn_sum_partials_kernel: no atomics, the order of additions depends on the shape and the number
 // of workgroups alone.  The rows of a segment's parts are dealt side by side, so that all workgroups read
-// neighbouring rows at a time (16384 x 3584: 148 -> 136 us against one stretch of rows each).
+// neighbouring rows at a time (16384 x 3584: 149 -> 136 us against one stretch of rows each), and the sums are stored
+// in 16-byte pieces (element by element, 32 x 4096 11.3 instead of 8.3 us).
 // AHEAD: the next row's loads are issued before a row is worked on: registers instead of more workgroups, every one
 // of which costs its partial sums (8192 x 4096 without sums of a second norm 74 -> 69 us).  WIDE: the sums over rows
 // are kept in LDS, where registers do not hold them beside rows of 32 elements per thread; each column belongs to one
-// thread.  2048 x 12000 bf16 93 us, 245 in the long form.
-// us, with the partial sums' launch (4-5): 16384 x 3584 bf16, both norms, a gate per channel 138 (5.2 TB/s; traffic
+// thread.  2048 x 12000 bf16 83 us, 245 in the long form.
+// us, with the partial sums' launch (4-5): 16384 x 3584 bf16, both norms, a gate per channel 135 (5.2 TB/s; traffic
 // 470 MB read and 246 written, 705 it cannot do without; vector instructions 47 % of the cycles), 8192 x 4096 with
-// the next block's norm 56, 2047 x 1000 fp32 with a silu gate per sequence 17.5.
+// the next block's norm 54, 2047 x 1000 fp32 with a silu gate per sequence 17.5.
 constexpr int BN_WIDE_COLS = 16384, BN_WIDE_COLS_3 = 13312;   // of up to two and of three sets of sums: 160 KB
 template <typename T, int TPR, int NV, bool POST, int GATE, bool AHEAD, bool WIDE, bool NT>
 __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a) {
     constexpr int N = RowVec<T>::N, BLOCK = bn_block<TPR>, GROUPS = bn_group_count<TPR>, NW = TPR > WAVE ? TPR / WAVE : 1;
     __shared__ float red[3][3 * NW];
-    __shared__ float cols[GROUPS > 1 ? BLOCK * NV * N : 1];
+    __shared__ __align__(16) float cols[GROUPS > 1 ? BLOCK * NV * N : 4];
     constexpr int SETS = 1 + POST + (GATE == BN_GATE_SUM), COLS = SETS == 3 ? BN_WIDE_COLS_3 : BN_WIDE_COLS;
     constexpr int AT_PRE = 0, AT_POST = COLS, AT_GATE = (1 + POST) * COLS;
     __shared__ __align__(16) float wide[WIDE ? SETS * COLS : 4];
@@ -454,7 +455,9 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int e = 0; e < N; ++e) cols[grp * (TPR * NV * N) + (t + k * TPR) * N + e] = acc[k][e];
+                for (int e = 0; e < N; e += 4)
+                    *reinterpret_cast<f32x4*>(&cols[grp * (TPR * NV * N) + (t + k * TPR) * N + e]) =
+                        f32x4{acc[k][e], acc[k][e + 1], acc[k][e + 2], acc[k][e + 3]};
             __syncthreads();
             for (int j = threadIdx.x; j < TPR * NV * N && j < a.H; j += BLOCK) {
                 float s = cols[j];

@@ -68,9 +68,9 @@ int check_common(const flce_block_norm* b, Strides* st, int64_t* gate_rows) {
 // The register forms: TPR threads per row with E elements each (a table by width, not by size: each row of it was the
 // fastest of its neighbours over its range).  Twice the elements per thread halve what a row costs besides them (sums
 // over lanes, addresses), half of them leaves registers for more wavefronts: backward, us, 8 / 16 elements: 8192 x 2048
-// 46 / 50, 8192 x 2304 45 / 38, 16384 x 512 20 / 22; rows of 513 .. 1024 in one wavefront of 16 elements per lane, or two
-// of 8: 16384 x 768 26 / 40 (forward 16.4 / 16.9), 2048 x 1000 9.6 / 13.1.  fp32 rows have half the elements per load
-// in flight: 4096 x 4096 67 / 72.
+// 41 / 44, 8192 x 2560 55 / 47, 16384 x 512 20 / 22; rows of 513 .. 1024 in one wavefront of 16 elements per lane, or two
+// of 8: 16384 x 768 26 / 38 (forward 16.8 / 16.9), 2048 x 1000 9.8 / 12.7.  fp32 rows have half the elements per load
+// in flight: 4096 x 4096 66 / 79.
 struct BnShape {
     int tpr, e;   // tpr = 0: the long form
 };
@@ -145,16 +145,17 @@ BnPlan bn_plan_for(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool 
 }
 // Workgroups of the backward.  Up to two of 256 threads per CU (or one of 512), but one where a row fills nearly all
 // of the (256, 16) form's vectors: their loads a row ahead fill the memory pipes, and every workgroup more costs its
-// partial sums (us, 256 / 512 workgroups: 16384 x 3584 with three sums 136 / 149, 8192 x 4096 72 / 75; but 8192 x
-// 2304 48 / 38, and rows that do not start on 16 bytes 8192 x 3583 96 / 78).  Small batches: few rows per workgroup,
-// because sums of few rows cost as much as the rows (512 / 256 / 128 workgroups, H = 4096 with a norm after the block:
-// 256 rows 16.7 / 16.8 / 14.6, 1024 rows 26.7 / 22.1 / 25.0, 4096 x 2048 26.2 / 27.8 / 44.0; below 128 rows one each).
-// A handful of rows: one workgroup, which needs no second launch (us, one / several: 2 x 4096 8.1 / 10.7, 3 x 4096 9.6 /
-// 10.8, 4 x 4096 11.1 / 10.8, 8 x 1000 in two steps 6.8 / 7.6, 16 x 1000 in four 10.2 / 7.6).
+// partial sums (us, 256 / 512 workgroups: 16384 x 3584 with three sums 135 / 146, 8192 x 4096 70 / 72; but 8192 x 3328
+// 62 / 57, 8192 x 2304 45 / 36, and rows that do not start on 16 bytes 8192 x 3583 93 / 72).  Small batches: few rows
+// per workgroup, because sums of few rows cost as much as the rows (512 / 256 / 128 workgroups, H = 4096 with a norm
+// after the block: 256 rows 12.9 / 13.0 / 11.9, 1024 rows 19.8 / 19.2 / 22.8, 4096 x 2048 24.1 / 29.0 / 48.0; below 128
+// rows one each).
+// A handful of rows: one workgroup, which needs no second launch (us on the GPU, one / several: 2 x 4096 6.4 / 7.6, 8 x
+// 1000 in two steps 6.6 / 7.4, 3 x 4096 8.0 / 7.6, 4 x 4096 9.6 / 7.6; a call that is not captured 15.5 / 18.3).
 int64_t bn_target(const BnShape& s, int64_t rows, int64_t H) {
     if (s.tpr && rows <= BN_ONE_STEPS * bn_groups(s)) return 1;
     int64_t most = BN_CUS * std::max(1, BN_CU_THREADS / bn_threads(s));
-    if (s.tpr == 256 && s.e == 16 && 4 * H > 3 * 256 * 16 && H % 8 == 0) most = BN_CUS;
+    if (s.tpr == 256 && s.e == 16 && 8 * H >= 7 * 256 * 16 && H % 8 == 0) most = BN_CUS;
     return std::min(most, std::max({BN_FEW_BLOCKS, std::min<int64_t>(BN_CUS, rows / 4), rows / 8}));
 }
 // That plan, or the largest power-of-two fraction of it whose sums fit `cap` bytes.
