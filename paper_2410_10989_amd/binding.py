@@ -338,11 +338,12 @@ def _refuse(t, name, like, shape):
     raise ValueError(f"{name} must be {tuple(shape)}")
 
 
-def _rows_ptr(t, name, like, shape):
-    """Pointer and row stride (0: dense) of a matrix whose rows may be apart, or of a vector."""
+def _rows_ptr(t, name, like, shape, dtype, index):
+    """Pointer and row stride (0: dense) of a matrix whose rows may be apart, or of a vector; dtype, index: those of
+    `like` and its device, asked for once."""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype is not like.dtype or t.get_device() != like.get_device():
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
         _refuse(t, name, like, shape)
     if t.is_contiguous():
         return t.data_ptr(), 0
@@ -390,20 +391,21 @@ def flce_block_norm_fwd(x, y=None, gamma_pre=None, gamma_post=None, gate=None, g
     if len(shape) != 2:
         raise ValueError("expected [rows, H]")
     code, vec, device = _dtype_code(like), shape[1:], like.device
+    dtype, index = like.dtype, device.index
     if y is not None and h is None:
         h = torch.empty_like(like)   # (dense, also where `like` is not; a third of the time of torch.empty)
     if gamma_pre is not None and n is None:
         n = torch.empty_like(like)
-    px, ldx = _rows_ptr(x, "x", like, shape)
-    py, ldy = _rows_ptr(y, "y", like, shape)
-    pg, ldg = _rows_ptr(gate, "gate", like, _gate_shape(gate, shape, rows_per_gate))
-    ph, ldh = _rows_ptr(h, "h", like, shape)
-    pn, ldn = _rows_ptr(n, "n", like, shape)
+    px, ldx = _rows_ptr(x, "x", like, shape, dtype, index)
+    py, ldy = _rows_ptr(y, "y", like, shape, dtype, index)
+    pg, ldg = _rows_ptr(gate, "gate", like, _gate_shape(gate, shape, rows_per_gate), dtype, index)
+    ph, ldh = _rows_ptr(h, "h", like, shape, dtype, index)
+    pn, ldn = _rows_ptr(n, "n", like, shape, dtype, index)
     args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), int(rows_per_gate), scale, eps,
                          ldx, ldy, ldh, ldn, ldg)
     with _OnDevice(device):
-        st = lib().flce_block_norm_fwd(px, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec)[0],
-                                       _rows_ptr(gamma_pre, "gamma_pre", like, vec)[0], ctypes.byref(args), ph, pn,
+        st = lib().flce_block_norm_fwd(px, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec, dtype, index)[0],
+                                       _rows_ptr(gamma_pre, "gamma_pre", like, vec, dtype, index)[0], ctypes.byref(args), ph, pn,
                                        _stream_handle(stream, device))
     _check(st, "flce_block_norm_fwd")
     return h, n
@@ -429,6 +431,7 @@ def flce_block_norm_bwd(h=None, dn=None, dh=None, y=None, gamma_pre=None, gamma_
     if len(shape) != 2:
         raise ValueError("expected [rows, H]")
     code, vec, device = _dtype_code(like), shape[1:], like.device
+    dtype, index = like.dtype, device.index
     gshape = _gate_shape(gate, shape, rows_per_gate)
     want_dx, want_dw = not flags & SKIP_DX, not flags & SKIP_DW
     passed_on = want_dx and gamma_pre is None and dx is None
@@ -441,23 +444,23 @@ def flce_block_norm_bwd(h=None, dn=None, dh=None, y=None, gamma_pre=None, gamma_
         if given is None:
             given = torch.empty_like(of)
             return given, given.data_ptr(), 0
-        return given, *_rows_ptr(given, name, like, size)
+        return given, *_rows_ptr(given, name, like, size, dtype, index)
 
     dx, pdx, lddx = output(dx, like, want_dx and not passed_on, "dx", shape)
     dy, pdy, lddy = output(dy, y, True, "dy", shape)
     dgate, pdg, lddg = output(dgate, gate, want_dw, "dgate", gshape)
     dgamma_post, pdpost, _ = output(dgamma_post, gamma_post, want_dw, "dgamma_post", vec)
     dgamma_pre, pdpre, _ = output(dgamma_pre, gamma_pre, want_dw, "dgamma_pre", vec)
-    ph, ldh = _rows_ptr(h, "h", like, shape)
-    pdn, lddn = _rows_ptr(dn, "dn", like, shape)
-    pdh, lddh = _rows_ptr(dh, "dh", like, shape)
-    py, ldy = _rows_ptr(y, "y", like, shape)
-    pg, ldg = _rows_ptr(gate, "gate", like, gshape)
+    ph, ldh = _rows_ptr(h, "h", like, shape, dtype, index)
+    pdn, lddn = _rows_ptr(dn, "dn", like, shape, dtype, index)
+    pdh, lddh = _rows_ptr(dh, "dh", like, shape, dtype, index)
+    py, ldy = _rows_ptr(y, "y", like, shape, dtype, index)
+    pg, ldg = _rows_ptr(gate, "gate", like, gshape, dtype, index)
     args = FlceBlockNorm(_BLOCK_NORM_BYTES, shape[0], shape[1], code, _gate_act(gate_act), int(rows_per_gate), scale, eps,
                          0, ldy, ldh, 0, ldg, lddx, lddy, lddh, lddn, lddg, *_workspace_args(workspace, device))
     with _OnDevice(device):
-        st = lib().flce_block_norm_bwd(ph, pdn, pdh, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec)[0],
-                                       _rows_ptr(gamma_pre, "gamma_pre", like, vec)[0], ctypes.byref(args), pdx, pdy, pdg,
+        st = lib().flce_block_norm_bwd(ph, pdn, pdh, py, pg, _rows_ptr(gamma_post, "gamma_post", like, vec, dtype, index)[0],
+                                       _rows_ptr(gamma_pre, "gamma_pre", like, vec, dtype, index)[0], ctypes.byref(args), pdx, pdy, pdg,
                                        pdpost, pdpre, _stream_handle(stream, device))
     _check(st, "flce_block_norm_bwd")
     return dh if passed_on else dx, dy, dgate, dgamma_post, dgamma_pre
