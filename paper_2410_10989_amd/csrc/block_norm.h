@@ -468,14 +468,16 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 float v[N];
+                const int at = t + k * TPR;
+                if (at * N >= a.H) continue;   // (the sets in LDS end there)
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[e] = WIDE ? wide_at(set, k)[e] : acc[WIDE ? 0 : k][e];
-                const int at = t + k * TPR;
                 if (out) {
                     bn_store<T, false>(out, at, nfull_all, rem_all, v);
                 } else if (at < nfull_all) {
 #pragma unroll
-                    for (int e = 0; e < N; e += 4) *reinterpret_cast<f32x4_any*>(part + at * N + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+                    for (int e = 0; e < N; e += 4)
+                        *reinterpret_cast<f32x4_any*>(part + at * N + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
                 } else if (at == nfull_all) {
 #pragma unroll
                     for (int e = 0; e < N; ++e)

@@ -216,8 +216,8 @@ int run_fwd(const BnArgs& a, hipStream_t s) {
         launch_fwd<T, NT, 1024, 16>(a, s);
     } else {
         const int64_t rows = a.rows;
-        hipLaunchKernelGGL((block_norm_fwd_long<T, NT>), dim3((unsigned)std::min(rows, BN_GRID_X), (unsigned)((rows + BN_GRID_X - 1) / BN_GRID_X)),
-                           dim3(BN_LONG_THREADS), 0, s, a);
+        const dim3 grid((unsigned)std::min(rows, BN_GRID_X), (unsigned)((rows + BN_GRID_X - 1) / BN_GRID_X));
+        hipLaunchKernelGGL((block_norm_fwd_long<T, NT>), grid, dim3(BN_LONG_THREADS), 0, s, a);
     }
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
@@ -282,8 +282,8 @@ int flce_block_norm_fwd(const void* x, const void* y, const void* gate, const vo
     const size_t es = bn_elem(b.dtype);
     for (const void* p : {x, y, gate, gamma_post, gamma_pre, static_cast<const void*>(h), static_cast<const void*>(n)})
         if (p && !aligned(p, es)) return FLCE_ERR_ALIGN;
-    const Span in[] = {span(x, ld.x, b.rows, b.H, es), span(y, ld.y, b.rows, b.H, es), span(gate, ld.gate, gate_rows, b.H, es),
-                       span(gamma_post, b.H, 1, b.H, es), span(gamma_pre, b.H, 1, b.H, es)};
+    const Span in[] = {span(x, ld.x, b.rows, b.H, es), span(y, ld.y, b.rows, b.H, es),
+                       span(gate, ld.gate, gate_rows, b.H, es), span(gamma_post, b.H, 1, b.H, es), span(gamma_pre, b.H, 1, b.H, es)};
     const Span oh = span(h, ld.h, b.rows, b.H, es), on = span(n, ld.n, b.rows, b.H, es);
     if (overlap(oh, on)) return FLCE_ERR_ARG;
     for (const Span& i : in) {
@@ -309,7 +309,8 @@ int flce_block_norm_fwd(const void* x, const void* y, const void* gate, const vo
     a.act = b.gate_act;
     a.scale = b.scale;
     a.eps = b.eps;
-    const bool nt = bn_nontemporal(b, (x != nullptr) + 2 * (y != nullptr) + (gamma_pre != nullptr) + (gate && b.rows_per_gate == 1));
+    const bool by_row = gate && b.rows_per_gate == 1;
+    const bool nt = bn_nontemporal(b, (x != nullptr) + 2 * (y != nullptr) + (gamma_pre != nullptr) + by_row);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (nt) return b.dtype == FLCE_F32 ? run_fwd<float, true>(a, s) : run_fwd<bf16_t, true>(a, s);
     return b.dtype == FLCE_F32 ? run_fwd<float, false>(a, s) : run_fwd<bf16_t, false>(a, s);
@@ -396,7 +397,8 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     a.parts = (int)p.parts;
     a.by_row = by_row;
     a.gate_direct = p.direct;
-    const bool nt = bn_nontemporal(b, 2 * (h != nullptr) + (dh != nullptr) + (y != nullptr) + (dx != nullptr) + (dy != nullptr) + by_row + (by_row && dgate));
+    const bool nt = bn_nontemporal(b, 2 * (h != nullptr) + (dh != nullptr) + (y != nullptr) + (dx != nullptr) +
+                                          (dy != nullptr) + by_row + (by_row && dgate));
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (nt)
         return b.dtype == FLCE_F32 ? run_bwd<float, true>(a, shape, p, dgamma_pre, dgamma_post, s)
@@ -412,10 +414,11 @@ size_t flce_block_norm_workspace_bytes(const flce_block_norm* args) {
     const int64_t per = args->rows_per_gate ? args->rows_per_gate : args->rows;
     const int64_t rows = args->rows, H = args->H;
     // three sets of sums, or (a gate row per row, or none) the gammas' alone, each in a plan of its own
-    const size_t with_gate = bn_plan(bn_shape(H, args->dtype, true, true), rows, H, per, true, true, true, SIZE_MAX).total_bytes;
-    const size_t two_sums = bn_plan(bn_shape(H, args->dtype, true), rows, H, per, true, false, true, SIZE_MAX).total_bytes;
-    const size_t without = bn_plan(bn_shape(H, args->dtype, true), rows, H, rows, true, true, false, SIZE_MAX).total_bytes;
-    return std::max({with_gate, two_sums, without});
+    auto bytes = [&](bool post, bool gate) {
+        return bn_plan(bn_shape(H, args->dtype, true, post && gate), rows, H, gate ? per : rows, true, post, gate, SIZE_MAX)
+            .total_bytes;
+    };
+    return std::max({bytes(true, true), bytes(false, true), bytes(true, false)});
 }
 
 }  // extern "C"
