@@ -525,9 +525,12 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
         BnRow<NV> next;
         if (AHEAD && seg.row < seg.end) load_row(next, seg.row, seg.end);
         for (int base = seg.row; base < seg.end; base += seg.step, turn ^= 1) {
-            const bool live = GROUPS == 1 || base + grp < seg.end;
-            const int64_t row = live ? base + grp : base;
-            const int nfull = live ? nfull_all : 0, rem = live ? rem_all : 0;
+            // A group past the segment's last row (at most a wavefront: no barrier in here is meant for it) has none in
+            // any later step either.  It must not go on with zeros: with eps = 0 their 1 / rms is infinite, and 0 times
+            // that would be NaN in the sums over rows.
+            if (GROUPS > 1 && base + grp >= seg.end) break;
+            const int64_t row = base + grp;
+            const int nfull = nfull_all, rem = rem_all;
             BnRow<NV> in;
             if constexpr (AHEAD) {
                 in = next;

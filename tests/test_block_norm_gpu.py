@@ -280,6 +280,21 @@ def test_rows_do_not_see_each_other():
             assert torch.equal(a[keep], b[keep])
 
 
+@pytest.mark.parametrize("variant", [dict(), dict(post=True), dict(post=True, gate="channel", kind="silu"),
+                                     dict(post=True, gate="sequence", per=5, kind="tanh"), dict(gate="sequence", per=7),
+                                     dict(post=True, gate="token", kind="sigmoid"), dict(pre=False, post=True, gate="channel")],
+                         ids=_name)
+def test_eps_of_zero_where_rows_do_not_fill_a_workgroup(variant):
+    """1 / rms of the rows that are not there is infinite; the sums over rows must not see it.  Row counts on both
+    sides of where one workgroup takes all rows (48 of up to 128 elements, 12 of up to 1024)."""
+    for i, (rows, H) in enumerate([(5, 9), (17, 64), (50, 100), (131, 128), (5, 300), (13, 512), (70, 520), (11, 1000), (3, 2000)]):
+        for dtype in ("bf16", "f32"):
+            print(f"case eps=0 rows={rows} H={H} {dtype} {variant}", flush=True)
+            c = make(rows, H, dtype, 300 + i, eps=0.0, **variant)
+            check_forward(c)
+            check_backward(c)
+
+
 def test_rows_of_zeros_and_large_eps():
     c = make(6, 130, "f32", 16, post=True, eps=0.5)
     for k in ("x", "y", "h"):
