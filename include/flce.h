@@ -296,8 +296,8 @@ FLCE_API int flce_cross_entropy_inplace_noalloc(void* Z, const int64_t* targets,
  * gamma_post and gamma_pre may be NULL (without gamma_pre there is no n).  Backward: dh may be
  * NULL (zero) where there is a gamma_pre, y where neither dy nor anything of the block is there;
  * h and dn go with gamma_pre.  Outputs may be NULL where they are not wanted, but not all of them.
- * h may lie exactly on x and dx exactly on dh; no output may share other memory with an input
- * or another output (FLCE_ERR_ARG).
+ * h may lie exactly on x (also where y, or a gate with a row per row, is that very matrix) and dx
+ * exactly on dh; no output may share other memory with an input or another output (FLCE_ERR_ARG).
  */
 enum { FLCE_GATE_LINEAR = 0, FLCE_GATE_SIGMOID = 1, FLCE_GATE_SILU = 2, FLCE_GATE_TANH = 3 };
 typedef struct {

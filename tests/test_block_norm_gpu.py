@@ -220,6 +220,17 @@ def test_h_may_lie_on_x_and_dx_on_dh():
         assert b[0] is dh and all(torch.equal(u, v) for u, v in zip(a, b) if u is not None)
 
 
+def test_h_on_x_that_is_y_and_the_gate_too():
+    import paper_2410_10989_amd as flce
+    for H in (96, 2304, 20000):
+        c = make(21, H, "bf16", 27, post=True)
+        x = _dev(c, "x")
+        kw = dict(_kw(c), gate=x, gate_act="sigmoid", rows_per_gate=1)
+        h, n = flce.flce_block_norm_fwd(x, x, **kw)
+        h2, n2 = flce.flce_block_norm_fwd(x, x, **kw, h=x)
+        assert h2 is x and torch.equal(h, h2) and torch.equal(n, n2)
+
+
 def test_outputs_as_columns_of_one_wider_buffer():
     import paper_2410_10989_amd as flce
     c = make(31, 200, "f32", 11, post=True)

@@ -176,6 +176,21 @@ def test_block_norm_refuses_missing_misaligned_and_overlapping_memory():
         assert rows_of_17000(4 * 17000 * sets - 1, gate, post) == 5
 
 
+def test_h_on_x_excuses_no_other_input():
+    """h may lie on x; a vector that is one of x's rows, or y with rows of another length from the same address, would
+    be overwritten by h while other rows still need it."""
+    buf, a = _memory()
+    L = flce.lib()
+
+    def fwd(x=a, y=a + 256, gate=None, post=None, pre=a + 512, h=a, n=a + 1024, **kw):
+        return L.flce_block_norm_fwd(x, y, gate, post, pre, ctypes.byref(_args(**kw)), h, n, None)
+
+    assert fwd(pre=a) == 7 and fwd(post=a) == 7
+    assert fwd(gate=a) == 7 and fwd(gate=a, rows_per_gate=2) == 7 and fwd(gate=a, rows_per_gate=1, ldgate=16) == 7
+    assert fwd(y=a, ldy=16) == 7 and fwd(y=a, ldx=16, ldh=16) == 7
+    assert fwd(rows=1, pre=a) == 7 and fwd(rows=1, post=a) == 7
+
+
 def test_block_norm_workspace_is_bounded():
     need = [flce.flce_block_norm_workspace_bytes(rows, 4096, torch.bfloat16, per)
             for rows in (1, 1000, 10 ** 6, 2 ** 30) for per in (0, 1, 5, 2048)]
