@@ -556,6 +556,8 @@ def flce_grad_norm(grads, norm_type=2.0, norm=None, workspace=None, stream=None)
 def flce_grad_clip(grads, norm, max_norm, outs=None, stream=None):
     """Scales a list of tensors by min(1, max_norm / (norm + 1e-6)), in place or into `outs`; norm: one float32 on
     the GPU, e.g. over all shards of a model."""
+    if norm is None:   # (_norm_out makes one for the calls that write it)
+        raise ValueError("norm must be one float32 value on the tensors' GPU")
     grads = list(grads)
     device, ptrs, counts, dtypes = _tensor_list(grads)
     norm = _norm_out(norm, device)

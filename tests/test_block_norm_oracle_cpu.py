@@ -244,6 +244,13 @@ def test_binding_refuses_what_the_library_cannot_see():
         flce.flce_clip_grad_norm([], 1.0)
 
 
+def test_clipping_by_a_norm_needs_one():
+    """None would be memory that nobody has written."""
+    for grads in ([torch.zeros(3)], []):
+        with pytest.raises(ValueError, match="norm must be one float32 value"):
+            flce.flce_grad_clip(grads, None, 1.0)
+
+
 def test_clip_definition():
     t = [np.array([3.0, -4.0]), np.array([[12.0]])]
     assert oracle.grad_norm(t) == 13.0 and oracle.grad_norm(t, "inf") == 12.0
