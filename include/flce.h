@@ -340,10 +340,12 @@ FLCE_API size_t flce_block_norm_workspace_bytes(const flce_block_norm* args);
  *   counts        HOST array, elements of each tensor, 0 .. 2^40 (0: its pointers may be NULL)
  *   dtypes        HOST array, flce_dtype of each tensor and its out
  *   n_tensors     >= 0 (0: norm = 0)
- *   norm          device, 1 float        out (flce_grad_clip: in)
+ *   norm          device, 1 float        out (flce_grad_clip: in); in no tensor (flce_grad_clip: in no
+ *                 out) and not in the workspace (FLCE_ERR_ARG)
  *   max_norm      finite, >= 0
  *   workspace     device buffer (256-byte aligned, at least flce_grad_norm_workspace_bytes(n_tensors))
- *                 for the partial results, or NULL for the device's shared workspace
+ *                 for the partial results, or NULL for the device's shared workspace; shares no
+ *                 memory with the tensors (FLCE_ERR_ARG)
  * Every 120 tensors take a launch for the norm and one for the scaling.
  */
 enum { FLCE_NORM_2 = 0, FLCE_NORM_INF = 1 };

@@ -76,6 +76,18 @@ int check_outputs(const Tensors& t) {
     return rc;
 }
 
+// Whether `bytes` bytes at p lie in an output, or (ins) in an input.
+bool touches(const Tensors& t, bool ins, const void* p, size_t bytes) {
+    const uintptr_t p0 = reinterpret_cast<uintptr_t>(p), p1 = p0 + bytes;
+    auto in = [&](const void* q, int i) {
+        const uintptr_t q0 = reinterpret_cast<uintptr_t>(q);
+        return q0 < p1 && p0 < q0 + bytes_of(t, i);
+    };
+    for (int i = 0; i < t.n; ++i)
+        if (t.count[i] && (in(t.out ? t.out[i] : t.in[i], i) || (ins && in(t.in[i], i)))) return true;
+    return false;
+}
+
 // How the tensors are cut for both sweeps.
 struct Cut {
     size_t total;          // bytes of all tensors
@@ -115,16 +127,18 @@ GnArgs launch_args(const Tensors& t, int first, const Cut& cut, size_t at, size_
     return a;
 }
 
-int partial_memory(const Tensors& t, void* workspace, size_t workspace_bytes, double** out) {
+// Memory for the partial results; it may not lie where they or the norm would overwrite what is still read.
+int partial_memory(const Tensors& t, const float* norm, void* workspace, size_t workspace_bytes, double** out) {
     const size_t need = partial_bytes(t.n);
+    char* ws = static_cast<char*>(workspace);
     if (workspace) {
         if (!aligned(workspace, 256)) return FLCE_ERR_ALIGN;
         if (workspace_bytes < need) return FLCE_ERR_WORKSPACE;
-        *out = static_cast<double*>(workspace);
-        return FLCE_OK;
+    } else {
+        FLCE_TRY(shared_workspace(need, &ws));
     }
-    char* ws = nullptr;
-    FLCE_TRY(shared_workspace(need, &ws));
+    const char* n = reinterpret_cast<const char*>(norm);
+    if (touches(t, true, ws, need) || (n < ws + need && ws < n + sizeof(float))) return FLCE_ERR_ARG;
     *out = reinterpret_cast<double*>(ws);
     return FLCE_OK;
 }
@@ -210,8 +224,9 @@ int flce_grad_norm(const void* const* grads, const int64_t* counts, const int* d
     if (!norm) return FLCE_ERR_NULL;
     if (!aligned(norm, 4)) return FLCE_ERR_ALIGN;
     if (norm_type != FLCE_NORM_2 && norm_type != FLCE_NORM_INF) return FLCE_ERR_ARG;
+    if (touches(t, true, norm, sizeof(float))) return FLCE_ERR_ARG;
     double* partial;
-    FLCE_TRY(partial_memory(t, workspace, workspace_bytes, &partial));
+    FLCE_TRY(partial_memory(t, norm, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
     return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, false, partial, 0.0f, norm, s)
                                     : run<GnMax>(t, false, partial, 0.0f, norm, s);
@@ -225,6 +240,7 @@ int flce_grad_clip(const void* const* grads, void* const* outs, const int64_t* c
     if (!aligned(norm, 4)) return FLCE_ERR_ALIGN;
     if (!finite_not_negative(max_norm)) return FLCE_ERR_ARG;
     FLCE_TRY(check_outputs(t));
+    if (touches(t, false, norm, sizeof(float))) return FLCE_ERR_ARG;
     return sweep_scale<GnSumSq>(t, cut_of(t), nullptr, 0, norm, nullptr, max_norm, static_cast<hipStream_t>(stream));
 }
 
@@ -237,8 +253,9 @@ int flce_clip_grad_norm(const void* const* grads, void* const* outs, const int64
     if (!aligned(norm, 4)) return FLCE_ERR_ALIGN;
     if ((norm_type != FLCE_NORM_2 && norm_type != FLCE_NORM_INF) || !finite_not_negative(max_norm)) return FLCE_ERR_ARG;
     FLCE_TRY(check_outputs(t));
+    if (touches(t, true, norm, sizeof(float))) return FLCE_ERR_ARG;
     double* partial;
-    FLCE_TRY(partial_memory(t, workspace, workspace_bytes, &partial));
+    FLCE_TRY(partial_memory(t, norm, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
     return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, true, partial, max_norm, norm, s)
                                     : run<GnMax>(t, true, partial, max_norm, norm, s);

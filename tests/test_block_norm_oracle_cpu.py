@@ -230,6 +230,37 @@ def test_clipping_refuses_bad_arguments():
     del L1
 
 
+def test_clipping_refuses_a_norm_or_workspace_inside_a_tensor():
+    """The norm is written (or read) by one workgroup while others scale the tensors and read the partial results."""
+    buf, a = _memory()
+    L = flce.lib()
+    V2, C2, D2 = ctypes.c_void_p * 2, ctypes.c_int64 * 2, ctypes.c_int * 2
+    # tensors of 16000 and 4000 bytes
+    grads, outs, counts, dtypes = V2(a, a + 16384), V2(a + 20480, a + 36864), C2(4000, 2000), D2(0, 1)
+    ws, size = a + 45056, 16384
+    most = ctypes.c_float(1.0)
+
+    def clip(norm, o=outs, ws=ws):
+        return L.flce_clip_grad_norm(grads, o, counts, dtypes, 2, 0, most, norm, ws, size, None)
+
+    for inside in (a, a + 15996, a + 16384, a + 20380, a + 20480, a + 36864 + 3996):
+        assert clip(inside) == 7
+    for inside in (a, a + 15996, a + 16384):
+        assert clip(inside, o=None) == 7
+        assert L.flce_grad_clip(grads, None, counts, dtypes, 2, inside, most, None) == 7
+        assert L.flce_grad_norm(grads, counts, dtypes, 2, 0, inside, ws, size, None) == 7
+    assert L.flce_grad_clip(grads, outs, counts, dtypes, 2, a + 20480, most, None) == 7
+    big = (ctypes.c_char * (1 << 20))()
+    w = ctypes.addressof(big)
+    w += (-w) % 256
+    counts = C2(100_000, 2000)
+    grads, outs = V2(w, w + 401408), V2(w + 409600, w + 811008)
+    for inside in (w, w + 399872, w + 401408, w + 809472):
+        assert clip(a, ws=inside) == 7
+    assert clip(a + 4096, ws=a) == 7 and L.flce_grad_norm(grads, counts, dtypes, 2, 0, a, a, size, None) == 7
+    assert L.flce_grad_norm(grads, counts, dtypes, 2, 1, a, w + 256, size, None) == 7
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     x = torch.zeros(4, 8)
     with pytest.raises(ValueError):
