@@ -290,7 +290,8 @@ FLCE_API int flce_cross_entropy_inplace_noalloc(void* Z, const int64_t* targets,
  *                   the device's shared workspace; workspace_bytes: flce_block_norm_workspace_bytes
  *                   of the same arguments, or less at the price of fewer workgroups
  *                   (12 H bytes always do; FLCE_ERR_WORKSPACE if not even one serves).  A few
- *                   rows need none (0 bytes), nor does the forward.
+ *                   rows need none (0 bytes), nor does the forward.  What the call uses of it
+ *                   shares no memory with the operands (FLCE_ERR_ARG).
  *
  * Forward: x or y may be NULL (not both; without y there is no gate, gamma_post or h); gate,
  * gamma_post and gamma_pre may be NULL (without gamma_pre there is no n).  Backward: dh may be

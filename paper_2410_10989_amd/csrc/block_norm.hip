@@ -365,6 +365,13 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     if (p.total_bytes > cap) return FLCE_ERR_WORKSPACE;
     char* ws = static_cast<char*>(b.workspace);
     if (!ws && p.total_bytes) FLCE_TRY(shared_workspace(p.total_bytes, &ws));
+    if (p.total_bytes) {   // partial sums are written while the operands are read
+        const Span scratch{ws, p.total_bytes, p.total_bytes, 1};
+        for (const Span& i : in)
+            if (overlap(scratch, i)) return FLCE_ERR_ARG;
+        for (const Span& o : out)
+            if (overlap(scratch, o)) return FLCE_ERR_ARG;
+    }
     float* f = reinterpret_cast<float*>(ws);
     BnArgs a{};
     a.h = h;

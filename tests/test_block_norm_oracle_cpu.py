@@ -191,6 +191,25 @@ def test_h_on_x_excuses_no_other_input():
     assert fwd(rows=1, pre=a) == 7 and fwd(rows=1, post=a) == 7
 
 
+def test_block_norm_backward_refuses_a_workspace_on_its_operands():
+    L = flce.lib()
+    big = (ctypes.c_char * (2 << 20))()
+    w = ctypes.addressof(big)
+    w += (-w) % 256
+    rows, H = 64, 64   # 8 KB per bf16 matrix; more rows than one workgroup takes without partial sums
+    at = [w + 8192 * k for k in range(9)]
+    need = flce.flce_block_norm_workspace_bytes(rows, H, torch.bfloat16)
+    assert 256 < need <= 1 << 20
+
+    def bwd(ws, nbytes=need, **kw):
+        b = _args(rows=rows, H=H, workspace=ws, workspace_bytes=nbytes, **kw)
+        return L.flce_block_norm_bwd(at[0], at[1], at[2], at[3], at[4], at[5], at[5] + 256, ctypes.byref(b), at[6], at[7],
+                                     at[8], at[8] + 256, at[8] + 512, None)
+
+    for operand in (*at[:6], at[5] + 256, *at[6:], at[8] + 256, at[8] + 512):
+        assert bwd(operand) == 7 and bwd(operand - 256 if operand > w else operand) == 7
+
+
 def test_block_norm_workspace_is_bounded():
     need = [flce.flce_block_norm_workspace_bytes(rows, 4096, torch.bfloat16, per)
             for rows in (1, 1000, 10 ** 6, 2 ** 30) for per in (0, 1, 5, 2048)]
