@@ -29,14 +29,21 @@ struct Span {
 Span span(const void* p, int64_t ld, int64_t rows, int64_t H, size_t es) {
     return {static_cast<const char*>(p), (size_t)ld * es, (size_t)H * es, rows};
 }
-// Whether two of them share a byte.  Column windows of one wider buffer (equal pitch) may interleave; with
-// different pitches any common stretch of addresses counts.
+// Whether two of them share a byte.  A single row may lie between the rows of the other, column windows of one wider
+// buffer (equal pitch) may interleave; with different pitches any common stretch of addresses counts.
 bool overlap(const Span& a, const Span& b) {
     if (!a.p || !b.p) return false;
     const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
     const uintptr_t a1 = a0 + (a.rows - 1) * a.pitch + a.width, b1 = b0 + (b.rows - 1) * b.pitch + b.width;
     if (a1 <= b0 || b1 <= a0) return false;
-    if (a.pitch != b.pitch || a.rows == 1 || b.rows == 1) return true;
+    if (a.rows == 1 || b.rows == 1) {
+        const Span &m = a.rows == 1 ? b : a, &v = a.rows == 1 ? a : b;
+        const uintptr_t m0 = reinterpret_cast<uintptr_t>(m.p), v0 = reinterpret_cast<uintptr_t>(v.p);
+        if (v0 <= m0) return true;
+        const size_t off = (v0 - m0) % m.pitch;   // from the row that begins before v
+        return off < m.width || ((int64_t)((v0 - m0) / m.pitch) + 1 < m.rows && off + v.width > m.pitch);
+    }
+    if (a.pitch != b.pitch) return true;
     const size_t off = b0 >= a0 ? (b0 - a0) % a.pitch : (a.pitch - (a0 - b0) % a.pitch) % a.pitch;
     return off < a.width || a.pitch - off < b.width;
 }

@@ -210,6 +210,27 @@ def test_block_norm_backward_refuses_a_workspace_on_its_operands():
         assert bwd(operand) == 7 and bwd(operand - 256 if operand > w else operand) == 7
 
 
+def test_vectors_between_the_rows_of_a_matrix_do_not_overlap_it():
+    """A single row against rows that lie apart: only shared bytes count.  (Refusals behind the overlap check show
+    that a call passed it: a workspace off its alignment.)"""
+    L = flce.lib()
+    big = (ctypes.c_char * (1 << 16))()
+    w = ctypes.addressof(big)
+    w += (-w) % 256
+
+    def bwd(dpre, ldh=64, **kw):   # h: 4 rows of 16 bytes, 128 bytes apart
+        b = _args(rows=4, ldh=ldh, workspace=w + 8194, workspace_bytes=1 << 12, **kw)
+        return L.flce_block_norm_bwd(w + 256, w + 1024, w + 2048, w + 3072, None, None, w + 4096, ctypes.byref(b), w + 5120,
+                                     w + 6144, None, None, dpre, None)
+
+    first = w + 256
+    for dpre in (first + 16, first + 112, first + 128 + 16, first + 2 * 128 + 112, first + 3 * 128 + 16, first - 16):
+        assert bwd(dpre) == 4
+    for dpre in (first - 2, first, first + 14, first + 114, first + 128, first + 128 + 14, first + 3 * 128 + 14, first + 2 * 128 + 114):
+        assert bwd(dpre) == 7
+    assert bwd(first + 3 * 128 - 12, ldh=64) == 7 and bwd(first + 4, ldh=64) == 7
+
+
 def test_block_norm_workspace_is_bounded():
     need = [flce.flce_block_norm_workspace_bytes(rows, 4096, torch.bfloat16, per)
             for rows in (1, 1000, 10 ** 6, 2 ** 30) for per in (0, 1, 5, 2048)]
