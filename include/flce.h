@@ -347,7 +347,8 @@ FLCE_API size_t flce_block_norm_workspace_bytes(const flce_block_norm* args);
  *   workspace     device buffer (256-byte aligned, at least flce_grad_norm_workspace_bytes(n_tensors))
  *                 for the partial results, or NULL for the device's shared workspace; shares no
  *                 memory with the tensors (FLCE_ERR_ARG)
- * Every 120 tensors take a launch for the norm and one for the scaling.
+ * Every 120 tensors take a launch for the norm and one for the scaling; up to 120 tensors of 64 KB
+ * together take one launch in all and no workspace (NULL then allocates nothing).
  */
 enum { FLCE_NORM_2 = 0, FLCE_NORM_INF = 1 };
 FLCE_API int flce_grad_norm(const void* const* grads, const int64_t* counts, const int* dtypes, int n_tensors,

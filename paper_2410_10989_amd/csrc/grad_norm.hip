@@ -127,16 +127,21 @@ GnArgs launch_args(const Tensors& t, int first, const Cut& cut, size_t at, size_
     return a;
 }
 
+// Few elements: one launch of one workgroup, without partial results.
+bool one_workgroup(const Tensors& t, const Cut& cut) { return cut.total <= GN_SMALL_BYTES && t.n <= GN_TENSORS; }
+
 // Memory for the partial results; it may not lie where they or the norm would overwrite what is still read.
-int partial_memory(const Tensors& t, const float* norm, void* workspace, size_t workspace_bytes, double** out) {
+int partial_memory(const Tensors& t, const Cut& cut, const float* norm, void* workspace, size_t workspace_bytes,
+                   double** out) {
     const size_t need = partial_bytes(t.n);
     char* ws = static_cast<char*>(workspace);
     if (workspace) {
         if (!aligned(workspace, 256)) return FLCE_ERR_ALIGN;
         if (workspace_bytes < need) return FLCE_ERR_WORKSPACE;
-    } else {
-        FLCE_TRY(shared_workspace(need, &ws));
     }
+    *out = nullptr;
+    if (one_workgroup(t, cut)) return FLCE_OK;
+    if (!workspace) FLCE_TRY(shared_workspace(need, &ws));
     const char* n = reinterpret_cast<const char*>(norm);
     if (touches(t, true, ws, need) || (n < ws + need && ws < n + sizeof(float))) return FLCE_ERR_ARG;
     *out = reinterpret_cast<double*>(ws);
@@ -188,10 +193,9 @@ int sweep_scale(const Tensors& t, const Cut& cut, const double* partial, int par
 
 // clip: scale too.
 template <typename Op>
-int run(const Tensors& t, bool clip, double* partial, float max_norm, float* norm, hipStream_t s) {
-    const Cut cut = cut_of(t);
+int run(const Tensors& t, const Cut& cut, bool clip, double* partial, float max_norm, float* norm, hipStream_t s) {
     int partials;
-    if (cut.total <= GN_SMALL_BYTES && t.n <= GN_TENSORS) {
+    if (one_workgroup(t, cut)) {
         size_t bytes;
         GnArgs a = launch_args(t, 0, cut, 0, 0, &bytes, &partials);
         a.norm_out = norm;
@@ -225,11 +229,12 @@ int flce_grad_norm(const void* const* grads, const int64_t* counts, const int* d
     if (!aligned(norm, 4)) return FLCE_ERR_ALIGN;
     if (norm_type != FLCE_NORM_2 && norm_type != FLCE_NORM_INF) return FLCE_ERR_ARG;
     if (touches(t, true, norm, sizeof(float))) return FLCE_ERR_ARG;
+    const Cut cut = cut_of(t);
     double* partial;
-    FLCE_TRY(partial_memory(t, norm, workspace, workspace_bytes, &partial));
+    FLCE_TRY(partial_memory(t, cut, norm, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, false, partial, 0.0f, norm, s)
-                                    : run<GnMax>(t, false, partial, 0.0f, norm, s);
+    return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, cut, false, partial, 0.0f, norm, s)
+                                    : run<GnMax>(t, cut, false, partial, 0.0f, norm, s);
 }
 
 int flce_grad_clip(const void* const* grads, void* const* outs, const int64_t* counts, const int* dtypes, int n_tensors,
@@ -254,11 +259,12 @@ int flce_clip_grad_norm(const void* const* grads, void* const* outs, const int64
     if ((norm_type != FLCE_NORM_2 && norm_type != FLCE_NORM_INF) || !finite_not_negative(max_norm)) return FLCE_ERR_ARG;
     FLCE_TRY(check_outputs(t));
     if (touches(t, true, norm, sizeof(float))) return FLCE_ERR_ARG;
+    const Cut cut = cut_of(t);
     double* partial;
-    FLCE_TRY(partial_memory(t, norm, workspace, workspace_bytes, &partial));
+    FLCE_TRY(partial_memory(t, cut, norm, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, true, partial, max_norm, norm, s)
-                                    : run<GnMax>(t, true, partial, max_norm, norm, s);
+    return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, cut, true, partial, max_norm, norm, s)
+                                    : run<GnMax>(t, cut, true, partial, max_norm, norm, s);
 }
 
 }  // extern "C"

@@ -1,0 +1,137 @@
+// The library's host side on a HIP runtime that is stood in for: memory comes from the host (up to a limit that a
+// scenario sets), launches are counted and do nothing.  What a call allocates, frees and launches can so be seen
+// where there is no GPU.  Usage: host_calls <libflce.so> <scenario>; prints "ok" and returns 0, or says what failed.
+#include <dlfcn.h>
+#include <stdio.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include <set>
+#include <vector>
+
+#include "../include/flce.h"
+
+namespace {
+size_t g_limit = (size_t)1 << 40;   // a larger hipMalloc finds too little memory
+bool g_capturing = false;
+int g_mallocs = 0, g_refused = 0, g_frees = 0, g_launches = 0;
+std::set<void*> g_live;
+std::vector<size_t> g_sizes;   // of the allocations that succeeded
+constexpr int OUT_OF_MEMORY = 2;
+}   // namespace
+
+struct Dim3 {
+    unsigned x, y, z;
+};
+extern "C" {
+int hipGetDevice(int* d) { *d = 0; return 0; }
+int hipGetLastError() { return 0; }
+int hipDeviceSynchronize() { return 0; }
+int hipMalloc(void** p, size_t n) {
+    if (n > g_limit) {
+        ++g_refused;
+        return OUT_OF_MEMORY;
+    }
+    ++g_mallocs;
+    g_sizes.push_back(n);
+    *p = aligned_alloc(256, 256);   // (nothing is stored in it)
+    g_live.insert(*p);
+    return 0;
+}
+int hipFree(void* p) {
+    ++g_frees;
+    g_live.erase(p);
+    return 0;   // (kept, so that no two allocations have one address)
+}
+int hipStreamIsCapturing(void*, int* status) { *status = g_capturing ? 1 : 0; return 0; }
+int hipLaunchKernel(const void*, Dim3, Dim3, void**, size_t, void*) { ++g_launches; return 0; }
+int __hipPushCallConfiguration(Dim3, Dim3, size_t, void*) { return 0; }
+int __hipPopCallConfiguration(Dim3* g, Dim3* b, size_t* m, void** s) {
+    *g = *b = {1, 1, 1};
+    *m = 0;
+    *s = nullptr;
+    return 0;
+}
+void** __hipRegisterFatBinary(const void*) { static void* handle; return &handle; }
+void __hipUnregisterFatBinary(void**) {}
+void __hipRegisterFunction(void**, const void*, char*, const char*, unsigned, void*, void*, void*, void*, int*) {}
+void __hipRegisterVar(void**, void*, char*, char*, int, size_t, int, int) {}
+int hipGetSymbolAddress(void** p, const void* s) { *p = const_cast<void*>(s); return 0; }
+int hipEventCreate(void**) { return 0; }
+int hipEventDestroy(void*) { return 0; }
+int hipEventRecord(void*, void*) { return 0; }
+int hipEventSynchronize(void*) { return 0; }
+int hipEventElapsedTime(float* ms, void*, void*) { *ms = 0; return 0; }
+}
+
+namespace {
+#define ENTRY(name) decltype(&::name) name##_;
+struct Library {
+    ENTRY(flce_clip_grad_norm)
+    ENTRY(flce_grad_norm)
+    ENTRY(flce_block_norm_bwd)
+    ENTRY(flce_block_norm_workspace_bytes)
+    ENTRY(flce_cross_entropy_inplace)
+    ENTRY(flce_release_workspace)
+} L;
+#undef ENTRY
+
+int g_failed = 0;
+#define CHECK(cond)                                              \
+    do {                                                         \
+        if (!(cond)) {                                           \
+            printf("line %d: %s does not hold\n", __LINE__, #cond); \
+            ++g_failed;                                          \
+        }                                                        \
+    } while (0)
+
+// Addresses that are never touched: operands of the calls.
+char* operand(int i) { return reinterpret_cast<char*>((uintptr_t)1 << 44) + ((uintptr_t)i << 36); }
+
+int clip(int64_t count, void* stream = nullptr) {
+    const void* grads[1] = {operand(0)};
+    const int dtypes[1] = {FLCE_F32};
+    return L.flce_clip_grad_norm_(grads, nullptr, &count, dtypes, 1, FLCE_NORM_2, 1.0f, reinterpret_cast<float*>(operand(1)),
+                                  nullptr, 0, stream);
+}
+
+// Lists that one workgroup takes leave no partial results and need no memory for them.
+void short_lists() {
+    CHECK(clip(1000) == FLCE_OK && clip(16384) == FLCE_OK);
+    float* norm = reinterpret_cast<float*>(operand(1));
+    CHECK(L.flce_grad_norm_(nullptr, nullptr, nullptr, 0, FLCE_NORM_INF, norm, nullptr, 0, nullptr) == FLCE_OK);
+    CHECK(g_mallocs == 0 && g_launches == 3);
+    CHECK(clip(16385) == FLCE_OK);
+    CHECK(g_mallocs == 1 && g_launches == 5);
+}
+}   // namespace
+
+int main(int argc, char** argv) {
+    if (argc != 3) return 2;
+    void* lib = dlopen(argv[1], RTLD_NOW);
+    if (!lib) {
+        printf("%s\n", dlerror());
+        return 2;
+    }
+#define ENTRY(name) L.name##_ = reinterpret_cast<decltype(L.name##_)>(dlsym(lib, #name));
+    ENTRY(flce_clip_grad_norm)
+    ENTRY(flce_grad_norm)
+    ENTRY(flce_block_norm_bwd)
+    ENTRY(flce_block_norm_workspace_bytes)
+    ENTRY(flce_cross_entropy_inplace)
+    ENTRY(flce_release_workspace)
+#undef ENTRY
+    const struct {
+        const char* name;
+        void (*run)();
+    } scenarios[] = {{"short_lists", short_lists}};
+    for (const auto& s : scenarios)
+        if (!strcmp(s.name, argv[2])) {
+            s.run();
+            printf("%s\n", g_failed ? "failed" : "ok");
+            fflush(stdout);
+            _Exit(g_failed ? 1 : 0);
+        }
+    printf("no such scenario\n");
+    return 2;
+}

@@ -183,6 +183,27 @@ def test_captured_and_replayed():
         assert float(norm) == float(want) and all(torch.equal(a, b) for a, b in zip(outs, mine)), turn
 
 
+def test_a_short_list_is_captured_where_the_library_has_no_workspace():
+    import paper_2410_10989_amd as flce
+    _, grads = make([4000, 77, 0, 1], [F, B], 9)
+    norm = torch.empty((), device="cuda")
+    outs = [torch.empty_like(g) for g in grads]
+    assert flce.lib().flce_release_workspace() == 0
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        flce.flce_clip_grad_norm(grads, 1.0, outs=outs, norm=norm)
+    for turn in range(3):
+        for g in grads:
+            g.mul_(1.5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = host(grads)
+        check_norm(norm, oracle.grad_norm(ref))
+        check_scaled(outs, ref, oracle.clip_factor(oracle.grad_norm(ref), 1.0))
+
+
 def test_a_tensor_of_more_than_2_to_the_31_elements():
     import paper_2410_10989_amd as flce
     n = (1 << 31) + 77
