@@ -368,10 +368,17 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
         if (lent) cap = lent;
     }
     const BnShape shape = bn_shape(b.H, b.dtype, true, gamma_post && gate && !by_row);
-    const BnPlan p = bn_plan(shape, b.rows, b.H, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
-    if (p.total_bytes > cap) return FLCE_ERR_WORKSPACE;
+    BnPlan p;
     char* ws = static_cast<char*>(b.workspace);
-    if (!ws && p.total_bytes) FLCE_TRY(shared_workspace(p.total_bytes, &ws));
+    for (;;) {   // (again with fewer workgroups where the library finds too little memory for this many)
+        p = bn_plan(shape, b.rows, b.H, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
+        if (p.total_bytes > cap) return FLCE_ERR_WORKSPACE;
+        if (ws || !p.total_bytes) break;
+        const int rc = shared_workspace(p.total_bytes, &ws, p.blocks == 1);
+        if (rc == FLCE_OK) break;
+        if (rc != FLCE_ERR_WORKSPACE || p.blocks == 1) return rc;
+        cap = p.total_bytes - 1;
+    }
     if (p.total_bytes) {   // partial sums are written while the operands are read
         const Span scratch{ws, p.total_bytes, p.total_bytes, 1};
         for (const Span& i : in)

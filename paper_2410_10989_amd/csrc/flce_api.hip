@@ -974,7 +974,7 @@ int multihead_fwd_bwd(const Settings& st, const void* X, const void* const* W, c
 
 }  // namespace
 
-int flce::shared_workspace(size_t need, char** out) { return acquire_workspace(need, out); }
+int flce::shared_workspace(size_t need, char** out, bool last) { return acquire_workspace(need, out, last); }
 int flce::shared_workspace_lent(size_t* bytes) { return lent_workspace(bytes); }
 
 extern "C" {

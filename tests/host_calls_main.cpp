@@ -104,6 +104,46 @@ void short_lists() {
     CHECK(clip(16385) == FLCE_OK);
     CHECK(g_mallocs == 1 && g_launches == 5);
 }
+
+int backward(int64_t rows, int64_t H, void* stream = nullptr) {   // both norms, a gate per channel
+    flce_block_norm b{};
+    b.size = sizeof b;
+    b.rows = rows;
+    b.H = H;
+    b.dtype = FLCE_BF16;
+    b.scale = 1.0f;
+    b.eps = 1e-6f;
+    auto at = [](int i) { return static_cast<void*>(operand(2 + i)); };
+    return L.flce_block_norm_bwd_(at(0), at(1), at(2), at(3), at(4), at(5), at(6), &b, at(7), at(8), at(9), at(10), at(11), stream);
+}
+
+// Where the library's own memory cannot grow to the whole plan, the backward runs with fewer workgroups.
+void backward_with_little_memory() {
+    flce_block_norm b{};
+    b.size = sizeof b;
+    b.rows = 8192;
+    b.H = 2048;
+    b.dtype = FLCE_BF16;
+    const size_t need = L.flce_block_norm_workspace_bytes_(&b);
+    CHECK(need > ((size_t)4 << 20));
+    g_limit = need / 3;
+    CHECK(backward(8192, 2048) == FLCE_OK);
+    CHECK(g_mallocs == 1 && g_refused > 0 && g_launches == 2 && g_sizes[0] <= g_limit && g_sizes[0] > need / 8);
+    const int refused = g_refused;   // the next call does not try again
+    CHECK(backward(8192, 2048) == FLCE_OK);
+    CHECK(g_mallocs == 1 && g_refused == refused && g_launches == 4);
+    CHECK(L.flce_release_workspace_() == FLCE_OK);
+    g_limit = need;   // ... but behind a release it does
+    CHECK(backward(8192, 2048) == FLCE_OK);
+    CHECK(g_mallocs == 2 && g_sizes[1] == need && g_launches == 6);
+    CHECK(L.flce_release_workspace_() == FLCE_OK);
+    g_limit = 0;   // one workgroup that holds its rows in registers needs none
+    CHECK(backward(8192, 2048) == FLCE_OK && g_launches == 7);
+    g_launches = 0;
+    CHECK(backward(8192, 20000) == FLCE_ERR_WORKSPACE && g_launches == 0);   // 12 H bytes at the least
+    g_limit = 12 * 20000;
+    CHECK(backward(8192, 20000) == FLCE_OK && g_sizes.back() == 12 * 20000);
+}
 }   // namespace
 
 int main(int argc, char** argv) {
@@ -124,7 +164,7 @@ int main(int argc, char** argv) {
     const struct {
         const char* name;
         void (*run)();
-    } scenarios[] = {{"short_lists", short_lists}};
+    } scenarios[] = {{"short_lists", short_lists}, {"backward_with_little_memory", backward_with_little_memory}};
     for (const auto& s : scenarios)
         if (!strcmp(s.name, argv[2])) {
             s.run();
