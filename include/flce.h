@@ -60,7 +60,10 @@
  *    with a lent buffer) a call consists of kernel launches on `stream` only: no
  *    allocation, no memset, no synchronisation.  It can therefore be recorded
  *    into a HIP graph by stream capture and replayed (not while
- *    flce_timing_enable is on).
+ *    flce_timing_enable is on).  The graph holds the address of the workspace it was
+ *    captured with: the library's own stays allocated for it, also when later calls
+ *    need a larger one, until flce_release_workspace (no replays after that); a lent or
+ *    passed buffer is the caller's to keep.
  */
 #ifndef FLCE_H
 #define FLCE_H
@@ -371,7 +374,8 @@ FLCE_API size_t flce_workspace_bytes_max(int64_t H, int64_t V, int dtype);
  * lent buffer. */
 FLCE_API int flce_set_workspace(void* ws, size_t bytes);
 
-/* Free the library-owned workspace of the current device (synchronises). */
+/* Free the library-owned workspace of the current device, and what captured graphs hold of
+ * it (synchronises). */
 FLCE_API int flce_release_workspace(void);
 
 /* Chunk scheduler (paper section 3.2, FLCE paragraph: chunked logits bound the

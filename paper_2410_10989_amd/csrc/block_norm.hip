@@ -370,11 +370,12 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     const BnShape shape = bn_shape(b.H, b.dtype, true, gamma_post && gate && !by_row);
     BnPlan p;
     char* ws = static_cast<char*>(b.workspace);
+    hipStream_t s = static_cast<hipStream_t>(stream);
     for (;;) {   // (again with fewer workgroups where the library finds too little memory for this many)
         p = bn_plan(shape, b.rows, b.H, gate && !by_row ? per : b.rows, dgamma_pre, dgamma_post, sums, cap);
         if (p.total_bytes > cap) return FLCE_ERR_WORKSPACE;
         if (ws || !p.total_bytes) break;
-        const int rc = shared_workspace(p.total_bytes, &ws, p.blocks == 1);
+        const int rc = shared_workspace(p.total_bytes, &ws, s, p.blocks == 1);
         if (rc == FLCE_OK) break;
         if (rc != FLCE_ERR_WORKSPACE || p.blocks == 1) return rc;
         cap = p.total_bytes - 1;
@@ -423,7 +424,6 @@ int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, const voi
     a.gate_direct = p.direct;
     const bool nt = bn_nontemporal(b, 2 * (h != nullptr) + (dh != nullptr) + (y != nullptr) + (dx != nullptr) +
                                           (dy != nullptr) + by_row + (by_row && dgate));
-    hipStream_t s = static_cast<hipStream_t>(stream);
     if (nt)
         return b.dtype == FLCE_F32 ? run_bwd<float, true>(a, shape, p, dgamma_pre, dgamma_post, s)
                                    : run_bwd<bf16_t, true>(a, shape, p, dgamma_pre, dgamma_post, s);

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <atomic>
 #include <mutex>
+#include <new>
 #include <vector>
 
 #include "../../include/flce.h"
@@ -48,6 +49,8 @@ struct DeviceWorkspace {
     void* own = nullptr;
     size_t own_bytes = 0;
     size_t own_failed = 0;   // an allocation of this size found too little memory, 0 if none did
+    bool captured = false;   // a call on `own` has been captured: a graph holds its address
+    std::vector<void*> kept; // outgrown memory that graphs hold, until flce_release_workspace
 };
 
 std::mutex g_mutex;
@@ -135,11 +138,21 @@ struct ScopedKernelTimer {
     }
 };
 
+// Whether calls on the stream are being recorded into a graph (the null stream's cannot be).
+bool is_captured(hipStream_t s) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (!s) return false;
+    if (hipStreamIsCapturing(s, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+    (void)hipGetLastError();
+    return false;
+}
+
 // The device's shared workspace: the lent buffer, or memory of the library's own that grows as needed.
 // last = false: the caller has a plan that needs less, so an allocation that found too little memory is
 // not tried again on every call (but after flce_release_workspace, or once one as large succeeds).
-// lent: whether it is the lent buffer.
-int acquire_workspace(size_t need, char** out, bool last = true, bool* lent = nullptr) {
+// lent: whether it is the lent buffer.  s: the call's stream; the library's memory that a captured call gets is not
+// freed when a later call needs more, since the graph's replays go on writing to it.
+int acquire_workspace(size_t need, char** out, hipStream_t s, bool last = true, bool* lent = nullptr) {
     int dev = 0;
     HIP_TRY(hipGetDevice(&dev));
     if (dev < 0 || dev >= MAX_DEVICES) return FLCE_ERR_ARG;
@@ -153,22 +166,32 @@ int acquire_workspace(size_t need, char** out, bool last = true, bool* lent = nu
     }
     if (w.own_bytes < need) {
         if (!last && w.own_failed && need >= w.own_failed) return FLCE_ERR_WORKSPACE;
-        if (w.own) {
+        if (w.captured) {
+            try {
+                w.kept.reserve(w.kept.size() + 1);
+            } catch (const std::bad_alloc&) {
+                return FLCE_ERR_WORKSPACE;
+            }
+        } else if (w.own) {
             HIP_TRY(hipDeviceSynchronize());
             HIP_TRY(hipFree(w.own));
             w.own = nullptr;
             w.own_bytes = 0;
         }
-        const hipError_t rc = hipMalloc(&w.own, need);
+        void* grown = nullptr;
+        const hipError_t rc = hipMalloc(&grown, need);
         if (rc != hipSuccess) {
             (void)hipGetLastError();
-            w.own = nullptr;
             if (rc == hipErrorOutOfMemory) w.own_failed = need;   // (not where a stream is being captured)
             return FLCE_ERR_WORKSPACE;
         }
         if (need >= w.own_failed) w.own_failed = 0;
+        if (w.captured) w.kept.push_back(w.own);
+        w.captured = false;
+        w.own = grown;
         w.own_bytes = need;
     }
+    w.captured |= is_captured(s);
     *out = static_cast<char*>(w.own);
     return FLCE_OK;
 }
@@ -795,7 +818,7 @@ int check_launch_limits(const Plan& p, int64_t H, int64_t V) {
 // call's own, the buffer lent to the device or the library's.
 template <typename NeedOf>
 int plan_and_workspace(const Settings& st, int64_t BT, int64_t H, int64_t V, int dtype, NeedOf need_of, Plan* p,
-                       char** ws) {
+                       char** ws, hipStream_t s) {
     for (const Room room : {Room::full, Room::bounded, Room::least}) {
         *p = plan_for(st, BT, H, V, dtype, room);
         if (room == Room::full) {   // (the launches' sizes do not depend on the room)
@@ -803,7 +826,7 @@ int plan_and_workspace(const Settings& st, int64_t BT, int64_t H, int64_t V, int
             if (st.ws && !aligned(st.ws, 256)) return FLCE_ERR_ALIGN;
         }
         auto take = [&](size_t need) -> int {
-            if (!st.ws) return acquire_workspace(need, ws, room == Room::least);
+            if (!st.ws) return acquire_workspace(need, ws, s, room == Room::least);
             *ws = static_cast<char*>(st.ws);
             return st.ws_bytes >= need ? FLCE_OK : FLCE_ERR_WORKSPACE;
         };
@@ -961,8 +984,8 @@ int multihead_fwd_bwd(const Settings& st, const void* X, const void* const* W, c
 
     Plan p;
     char* ws = nullptr;
-    FLCE_TRY(plan_and_workspace(st, BT, H, V, dtype, [](const Plan& q) { return q.total; }, &p, &ws));
     hipStream_t s = static_cast<hipStream_t>(stream);
+    FLCE_TRY(plan_and_workspace(st, BT, H, V, dtype, [](const Plan& q) { return q.total; }, &p, &ws, s));
     if (dtype == FLCE_F32)
         return run_heads<float>(static_cast<const float*>(X), W, targets, weights, n_heads, BT, H, V,
                                 ignore_index, loss, head_losses, static_cast<float*>(dX), dW, flags,
@@ -974,7 +997,7 @@ int multihead_fwd_bwd(const Settings& st, const void* X, const void* const* W, c
 
 }  // namespace
 
-int flce::shared_workspace(size_t need, char** out, bool last) { return acquire_workspace(need, out, last); }
+int flce::shared_workspace(size_t need, char** out, hipStream_t s, bool last) { return acquire_workspace(need, out, s, last); }
 int flce::shared_workspace_lent(size_t* bytes) { return lent_workspace(bytes); }
 
 extern "C" {
@@ -1051,10 +1074,10 @@ int flce_rmsnorm_fwd_bwd(const void* h, const void* gamma, float eps, const void
 
     Plan p;
     char* ws = nullptr;
-    FLCE_TRY(plan_and_workspace(global_settings(), BT, H, V, dtype,
-                                [&](const Plan& q) { return norm_layout(q, H).total; }, &p, &ws));
-    const NormLayout l = norm_layout(p, H);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    FLCE_TRY(plan_and_workspace(global_settings(), BT, H, V, dtype,
+                                [&](const Plan& q) { return norm_layout(q, H).total; }, &p, &ws, s));
+    const NormLayout l = norm_layout(p, H);
     if (dtype == FLCE_F32)
         return run_rmsnorm_head<float>(static_cast<const float*>(h), static_cast<const float*>(gamma),
                                        eps, static_cast<const float*>(W), targets, BT, H, V,
@@ -1096,7 +1119,7 @@ int flce_cross_entropy_inplace(void* Z, const int64_t* targets, int64_t BT, int6
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* ws = nullptr;
     bool lent = false;
-    FLCE_TRY(acquire_workspace(256 + (size_t)step * sizeof(float), &ws, true, &lent));
+    FLCE_TRY(acquire_workspace(256 + (size_t)step * sizeof(float), &ws, s, true, &lent));
     // Calls on different lent buffers may overlap, and a buffer's contents are anybody's: no counters for them.
     done_t* done = nullptr;
     unsigned char* unused;
@@ -1155,6 +1178,11 @@ int flce_release_workspace(void) {
         HIP_TRY(hipFree(w.own));
         w.own = nullptr;
         w.own_bytes = 0;
+        w.captured = false;
+    }
+    for (; !w.kept.empty(); w.kept.pop_back()) {
+        HIP_TRY(hipDeviceSynchronize());
+        HIP_TRY(hipFree(w.kept.back()));
     }
     w.own_failed = 0;
     return FLCE_OK;

@@ -132,7 +132,7 @@ bool one_workgroup(const Tensors& t, const Cut& cut) { return cut.total <= GN_SM
 
 // Memory for the partial results; it may not lie where they or the norm would overwrite what is still read.
 int partial_memory(const Tensors& t, const Cut& cut, const float* norm, void* workspace, size_t workspace_bytes,
-                   double** out) {
+                   hipStream_t s, double** out) {
     const size_t need = partial_bytes(t.n);
     char* ws = static_cast<char*>(workspace);
     if (workspace) {
@@ -141,7 +141,7 @@ int partial_memory(const Tensors& t, const Cut& cut, const float* norm, void* wo
     }
     *out = nullptr;
     if (one_workgroup(t, cut)) return FLCE_OK;
-    if (!workspace) FLCE_TRY(shared_workspace(need, &ws));
+    if (!workspace) FLCE_TRY(shared_workspace(need, &ws, s));
     const char* n = reinterpret_cast<const char*>(norm);
     if (touches(t, true, ws, need) || (n < ws + need && ws < n + sizeof(float))) return FLCE_ERR_ARG;
     *out = reinterpret_cast<double*>(ws);
@@ -231,8 +231,8 @@ int flce_grad_norm(const void* const* grads, const int64_t* counts, const int* d
     if (touches(t, true, norm, sizeof(float))) return FLCE_ERR_ARG;
     const Cut cut = cut_of(t);
     double* partial;
-    FLCE_TRY(partial_memory(t, cut, norm, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
+    FLCE_TRY(partial_memory(t, cut, norm, workspace, workspace_bytes, s, &partial));
     return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, cut, false, partial, 0.0f, norm, s)
                                     : run<GnMax>(t, cut, false, partial, 0.0f, norm, s);
 }
@@ -261,8 +261,8 @@ int flce_clip_grad_norm(const void* const* grads, void* const* outs, const int64
     if (touches(t, true, norm, sizeof(float))) return FLCE_ERR_ARG;
     const Cut cut = cut_of(t);
     double* partial;
-    FLCE_TRY(partial_memory(t, cut, norm, workspace, workspace_bytes, &partial));
     hipStream_t s = static_cast<hipStream_t>(stream);
+    FLCE_TRY(partial_memory(t, cut, norm, workspace, workspace_bytes, s, &partial));
     return norm_type == FLCE_NORM_2 ? run<GnSumSq>(t, cut, true, partial, max_norm, norm, s)
                                     : run<GnMax>(t, cut, true, partial, max_norm, norm, s);
 }

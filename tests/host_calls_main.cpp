@@ -144,6 +144,42 @@ void backward_with_little_memory() {
     g_limit = 12 * 20000;
     CHECK(backward(8192, 20000) == FLCE_OK && g_sizes.back() == 12 * 20000);
 }
+// A captured graph holds the address of the shared workspace: it stays when a later call makes the workspace grow.
+void workspace_of_a_captured_call() {
+    void* const stream = operand(20);
+    auto cross_entropy = [&](int64_t rows) {
+        return L.flce_cross_entropy_inplace_(operand(0), reinterpret_cast<int64_t*>(operand(1)), rows, 512, 512, -100,
+                                             FLCE_BF16, reinterpret_cast<float*>(operand(2)), stream);
+    };
+    // a call that is captured in each of the ways to use the workspace, then a larger one that is not
+    int (*const clip_list)(void*) = [](void* s) { return clip(1 << 20, s); };
+    int (*const norms)(void*) = [](void* s) { return backward(2048, 1024, s); };
+    for (int kind = 0; kind < 3; ++kind) {
+        auto small = [&] { return kind == 0 ? cross_entropy(4) : kind == 1 ? clip_list(stream) : norms(stream); };
+        CHECK(L.flce_release_workspace_() == FLCE_OK && g_live.empty());
+        CHECK(small() == FLCE_OK && g_live.size() == 1);
+        void* const first = *g_live.begin();
+        g_capturing = true;
+        CHECK(small() == FLCE_OK && g_live.size() == 1);
+        g_capturing = false;
+        CHECK(backward(16384, 8192, stream) == FLCE_OK);
+        CHECK(g_live.size() == 2 && g_live.count(first));
+        CHECK(backward(16384, 16000, stream) == FLCE_OK);   // the second one has not been captured: it goes
+        CHECK(g_live.size() == 2 && g_live.count(first));
+        g_capturing = true;
+        CHECK(backward(16384, 16000, stream) == FLCE_OK);
+        g_capturing = false;
+        CHECK(backward(16384, 40000, stream) == FLCE_OK);
+        CHECK(g_live.size() == 3 && g_live.count(first));
+        g_capturing = true;
+        CHECK(backward(16384, 40000, stream) == FLCE_OK);
+        g_capturing = false;
+        g_limit = 0;   // (what could not be outgrown goes on serving, with fewer workgroups)
+        CHECK(backward(16384, 60000, stream) == FLCE_OK && g_live.size() == 3);
+        g_limit = (size_t)1 << 40;
+        CHECK(L.flce_release_workspace_() == FLCE_OK && g_live.empty());
+    }
+}
 }   // namespace
 
 int main(int argc, char** argv) {
@@ -164,7 +200,8 @@ int main(int argc, char** argv) {
     const struct {
         const char* name;
         void (*run)();
-    } scenarios[] = {{"short_lists", short_lists}, {"backward_with_little_memory", backward_with_little_memory}};
+    } scenarios[] = {{"short_lists", short_lists}, {"backward_with_little_memory", backward_with_little_memory},
+                     {"workspace_of_a_captured_call", workspace_of_a_captured_call}};
     for (const auto& s : scenarios)
         if (!strcmp(s.name, argv[2])) {
             s.run();

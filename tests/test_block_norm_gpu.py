@@ -403,6 +403,33 @@ def test_two_captured_graphs_with_workspaces_of_their_own():
             assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
 
 
+def test_a_graph_on_the_shared_workspace_outlives_its_growth():
+    import paper_2410_10989_amd as flce
+    flce.flce_release_workspace()
+    c = make(600, 520, "bf16", 28, post=True, gate="channel", kind="silu")
+    t, kw = {k: _dev(c, k) for k in ("h", "dn", "dh", "y")}, _kw(c)
+    outs = dict(dx=torch.empty_like(t["h"]), dy=torch.empty_like(t["h"]), dgate=torch.empty_like(kw["gate"]),
+                dgamma_post=torch.empty_like(kw["gate"]), dgamma_pre=torch.empty_like(kw["gate"]))
+    flce.flce_block_norm_bwd(**t, **kw, **outs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        flce.flce_block_norm_bwd(**t, **kw, **outs)
+    big = make(2000, 4096, "bf16", 29, post=True)
+    check_backward(big)   # needs more workspace
+    for turn in range(3):
+        t["dn"].mul_(1.25)
+        for o in outs.values():
+            o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = flce.flce_block_norm_bwd(**t, **kw)
+        assert all(torch.equal(a, b) for a, b in zip(outs.values(), want)), turn
+    del graph
+    flce.flce_release_workspace()
+
+
 def test_rows_beyond_32_bit_offsets():
     """1200 rows, 2^21 elements apart: offsets of 5 GB and more than 2^31 elements."""
     import paper_2410_10989_amd as flce

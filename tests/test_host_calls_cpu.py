@@ -20,7 +20,7 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("scenario", ["short_lists", "backward_with_little_memory"])
+@pytest.mark.parametrize("scenario", ["short_lists", "backward_with_little_memory", "workspace_of_a_captured_call"])
 def test_host_calls(program, scenario):
     res = subprocess.run([program, _build.LIB_PATH, scenario], stdout=subprocess.PIPE, text=True, timeout=120)
     assert res.returncode == 0 and res.stdout.endswith("ok\n"), res.stdout
