@@ -439,6 +439,8 @@ def flce_block_norm_bwd(h=None, dn=None, dh=None, y=None, gamma_pre=None, gamma_
         raise ValueError("without y and gamma_pre there is nothing to compute")
 
     def output(given, of, wanted, name, size):   # of: the input it is the gradient of
+        if of is None and given is not None:
+            raise ValueError(f"{name} is the gradient of an input that is not there")
         if of is None or not wanted:
             return None, None, 0
         if given is None:

@@ -487,3 +487,17 @@ def test_binding_refusals():
     with pytest.raises(flce.FlceError) as e:
         flce.flce_block_norm_fwd(x, x.clone(), g, n=x)
     assert e.value.status == 7
+
+
+def test_a_gradient_of_what_there_is_not_is_refused():
+    """The buffer would be left as it was, without a word."""
+    import paper_2410_10989_amd as flce
+    x, g = torch.ones(4, 8, device="cuda"), torch.ones(8, device="cuda")
+    buf, row = torch.empty_like(x), torch.empty_like(g)
+    for kw in (dict(dy=buf), dict(y=x, dgate=row), dict(y=x, dgamma_post=row)):
+        with pytest.raises(ValueError):
+            flce.flce_block_norm_bwd(x, x, x, gamma_pre=g, **kw)
+    with pytest.raises(ValueError):
+        flce.flce_block_norm_bwd(dh=x, y=x, dgamma_pre=row)
+    # what a flag leaves out may be passed all the same, as for the other calls
+    assert flce.flce_block_norm_bwd(x, x, x, gamma_pre=g, dgamma_pre=row, flags=flce.SKIP_DW)[4] is None
