@@ -16,6 +16,7 @@ constexpr int64_t BN_GRID_X = (int64_t)1 << 20;     // workgroups along x, the r
 constexpr int BN_CU_THREADS = 512;                 // threads per CU that the backward is launched for
 constexpr int BN_CUS = 256;
 constexpr int64_t BN_FEW_BLOCKS = 128, BN_ONE_STEPS = 3;
+constexpr int64_t BN_ONE_PER_CU_COLS = 2900;
 constexpr int64_t BN_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
 size_t bn_elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
@@ -150,10 +151,12 @@ BnPlan bn_plan_for(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool 
     p.total_bytes = at * sizeof(float);
     return p;
 }
-// Workgroups of the backward.  Up to two of 256 threads per CU (or one of 512), but one where a row fills nearly all
-// of the (256, 16) form's vectors: their loads a row ahead fill the memory pipes, and every workgroup more costs its
-// partial sums (us, 256 / 512 workgroups: 16384 x 3584 with three sums 135 / 146, 8192 x 4096 70 / 72; but 8192 x 3328
-// 62 / 57, 8192 x 2304 45 / 36, and rows that do not start on 16 bytes 8192 x 3583 93 / 72).  Small batches: few rows
+// Workgroups of the backward.  Up to two of 256 threads per CU (or one of 512), but one where a row fills most of the
+// (256, 16) form's vectors: their loads a row ahead fill the memory pipes, and every workgroup more costs its
+// partial sums (us, 256 / 512 workgroups, inputs not in the cache: 8192 rows with one sum, H = 2304 49.8 / 44.4, 2816
+// 49.2 / 48.6, 3200 53.4 / 54.6, 3584 58.3 / 60.2, 4096 65.7 / 68.1; 16384 rows 2816 89.5 / 88.1, 3200 97.3 / 98.7; 3000
+// rows with two sums 2816 31.2 / 31.1, 3200 32.1 / 34.3.  Three sums, 8192 rows: 2304 69.2 / 74.2, 4096 83.8 / 91.7.  Rows
+// that do not start on 16 bytes, 8192 x 3583: 93 / 72).  Small batches: few rows
 // per workgroup, because sums of few rows cost as much as the rows (512 / 256 / 128 workgroups, H = 4096 with a norm
 // after the block: 256 rows 12.9 / 13.0 / 11.9, 1024 rows 19.8 / 19.2 / 22.8, 4096 x 2048 24.1 / 29.0 / 48.0; below 128
 // rows one each).
@@ -162,7 +165,7 @@ BnPlan bn_plan_for(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool 
 int64_t bn_target(const BnShape& s, int64_t rows, int64_t H) {
     if (s.tpr && rows <= BN_ONE_STEPS * bn_groups(s)) return 1;
     int64_t most = BN_CUS * std::max(1, BN_CU_THREADS / bn_threads(s));
-    if (s.tpr == 256 && s.e == 16 && 8 * H >= 7 * 256 * 16 && H % 8 == 0) most = BN_CUS;
+    if (s.tpr == 256 && s.e == 16 && H >= BN_ONE_PER_CU_COLS && H % 8 == 0) most = BN_CUS;
     return std::min(most, std::max({BN_FEW_BLOCKS, std::min<int64_t>(BN_CUS, rows / 4), rows / 8}));
 }
 // That plan, or the largest power-of-two fraction of it whose sums fit `cap` bytes.
