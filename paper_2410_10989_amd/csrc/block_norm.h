@@ -15,11 +15,13 @@
 // A row belongs to a group of TPR threads that holds it in registers (NV vectors of 16 bytes per thread and
 // stream), so every stream is read once and written once; sums over a row go through the lanes and, for
 // groups of several wavefronts, through LDS.  Rows may start at any element: 16-byte accesses need no
-// alignment (they cost where lines are straddled: backward of 8192 rows of 4096 / 4095 bf16 71 / 98 us).  Rows that
-// are too long for that (`*_long`) are swept several times by a workgroup of 1024 threads.
+// alignment (they cost where lines are straddled: backward of 8192 rows of 4096 / 4095 bf16 67 / 88 us).  Rows that
+// are too long for that (`*_long`) are swept several times by a workgroup of 1024 threads (2048 x 20000 bf16 with both
+// norms and a gate: forward 127 us, backward 619).
 //
-// Bound by HBM.  What streams reach on this chip with nothing to compute: two read and two written, 112 MB each, 7.0
-// TB/s (what is read stays in the memory-side cache from pass to pass), four read and two written 5.6 TB/s.
+// Bound by HBM.  What streams of 117 MB each reach on this chip with nothing to compute, from one set of buffers (of
+// which the memory-side cache keeps some from pass to pass) / from three in turn: two read and two written 7.2 / 6.3
+// TB/s, four read and two written 6.9 / 6.1.
 #pragma once
 #include "flce_device.h"
 #include "rowvec.h"
@@ -196,9 +198,9 @@ __device__ __forceinline__ int bn_group() {
 }
 
 // Forward: a workgroup holds bn_group_count rows.  All loads of a row are issued before the first is used, the
-// occupancy (80 registers with everything on) covers the rest.  us: 8192 x 4096 bf16 with the next block's norm 38
-// (7.0 TB/s), 16384 x 3584 with both norms and a gate 68 (6.9; 85 where nothing read is in the cache yet: 5.5),
-// 2047 x 1000 fp32 with a sigmoid gate per token 10.7, one row of 4096 2.8.
+// occupancy (37 to 106 registers with everything on) covers the rest.  us: 8192 x 4096 bf16 with the next block's norm
+// 38 (7.0 TB/s), 16384 x 3584 with both norms and a gate 67 (7.0; 85 where nothing read is in the cache yet: 5.5),
+// 2047 x 1000 fp32 with a sigmoid gate per token 10.5, one row of 4096 2.8.
 template <typename T, int TPR, int NV, bool POST, bool GATE, bool NT>
 __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a) {
     constexpr int N = RowVec<T>::N, GROUPS = bn_group_count<TPR>;
@@ -387,10 +389,13 @@ struct BnRow {
 // AHEAD: the next row's loads are issued before a row is worked on: registers instead of more workgroups, every one
 // of which costs its partial sums (8192 x 4096 without sums of a second norm 74 -> 69 us).  WIDE: the sums over rows
 // are kept in LDS, where registers do not hold them beside rows of 32 elements per thread; each column belongs to one
-// thread.  2048 x 12000 bf16 83 us, 245 in the long form.
-// us, with the partial sums' launch (4-5): 16384 x 3584 bf16, both norms, a gate per channel 135 (5.2 TB/s; traffic
+// thread.  us, there / in the long form: 2048 x 12000 bf16 with one set of sums 62 / 140, two 84 / 247, three 123 / 356;
+// 2048 x 8200 fp32 72 / 140, 120 / 232, 197 / 307.  Registers spill to scratch memory in the WIDE forms of fp32 but for
+// the one without a norm after the block and a gate (44 to 184 bytes per lane), in those of bf16 with a norm after the
+// block (12 to 84), and in (512, 16) with three sets (fp32 64, bf16 44): 4096 x 8192 bf16 82 us, 56 with one set.
+// us, with the partial sums' launch (4-5): 16384 x 3584 bf16, both norms, a gate per channel 134 (5.3 TB/s; traffic
 // 470 MB read and 246 written, 705 it cannot do without; vector instructions 47 % of the cycles), 8192 x 4096 with
-// the next block's norm 54, 2047 x 1000 fp32 with a silu gate per sequence 17.5.
+// the next block's norm 55, 2047 x 1000 fp32 with a silu gate per sequence 19.
 constexpr int BN_WIDE_COLS = 16384, BN_WIDE_COLS_3 = 13312;   // of up to two and of three sets of sums: 160 KB
 template <typename T, int TPR, int NV, bool POST, int GATE, bool AHEAD, bool WIDE, bool NT>
 __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a) {

@@ -124,7 +124,8 @@ BnPlan bn_plan_for(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool 
         p.parts = std::max<int64_t>(1, std::min(target, (rows + groups - 1) / groups));
     } else if (G < target) {
         // rounds of segments over the workgroups times the steps of one (a step is `groups` rows; writing a
-        // segment's sums counts as one)
+        // segment's sums counts as one).  The search costs the host up to 5 us of a call (2 gate rows; 4: 2, 16:
+        // 0.7).  From G = target on gate rows stay whole, and a last round of few of them is as long as a full one.
         int64_t best = INT64_MAX;
         for (int64_t c = 1; c <= std::min<int64_t>(p.per, 4 * ((target + G - 1) / G)); ++c) {
             const int64_t cost = ((G * c + target - 1) / target) * (((p.per + c - 1) / c + groups - 1) / groups + 1);

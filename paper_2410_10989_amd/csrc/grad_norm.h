@@ -7,9 +7,9 @@
 // among themselves; every workgroup leaves one partial result, and they are added up in the same order everywhere.
 // Squares are summed in fp64: the square of any fp32 or bf16 value is finite there, and two fp64 operations per
 // element cost nothing beside HBM (a plain read of the same bytes takes as long).
-// Bound by HBM.  1.05 GB of bf16: 157-163 us (6.5 TB/s) with nontemporal loads, 196 without (what is read then stays
-// in the memory-side cache, where no later part of the sweep finds it); 390 fp32 gradients of 1.41 GB clipped into
-// other buffers: 722 us for 4.2 GB moved (5.9 TB/s).  32 KB chunks: one round of eight loads per thread; 64 KB chunks
+// Bound by HBM.  1.05 GB of bf16: 157 us (6.7 TB/s) with nontemporal loads, 196 without (what is read then stays
+// in the memory-side cache, where no later part of the sweep finds it); 338 fp32 gradients of 1.41 GB clipped into
+// other buffers: 716 us for 4.2 GB moved (5.9 TB/s).  32 KB chunks: one round of eight loads per thread; 64 KB chunks
 // 6 % slower.
 #pragma once
 #include "flce_device.h"
