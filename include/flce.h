@@ -277,8 +277,9 @@ FLCE_API int flce_cross_entropy_inplace_noalloc(void* Z, const int64_t* targets,
  * in fp64) without atomics, in an order that depends on the shape and the room for partial sums
  * alone; every output is rounded to dtype once.  k rows added up one after the other are off by at
  * most k 2^-24 of the sum of their magnitudes: k is 8 or less below 2048 rows, then about rows / 256
- * (at most twice that), but rows / 16 to rows where the workspace has room for one workgroup only.  A row's sums are fp32: rows whose mean square
- * leaves that type's range give what fp32 arithmetic gives.
+ * (at most twice that), but rows / 16 to rows where the workspace has room for one workgroup only.
+ * A row's sums are fp32: rows whose mean square leaves that type's range give what fp32 arithmetic
+ * gives.
  *
  *   size            must be sizeof(flce_block_norm) (FLCE_ERR_ARG otherwise)
  *   rows, H         1 .. 2^30 and 1 .. 2^24

@@ -49,8 +49,8 @@ struct DeviceWorkspace {
     void* own = nullptr;
     size_t own_bytes = 0;
     size_t own_failed = 0;   // an allocation of this size found too little memory, 0 if none did
-    bool captured = false;   // a call on `own` has been captured: a graph holds its address
-    std::vector<void*> kept; // outgrown memory that graphs hold, until flce_release_workspace
+    bool captured = false;     // a call on `own` has been captured: a graph holds its address
+    std::vector<void*> kept;   // outgrown memory that graphs hold, until flce_release_workspace
 };
 
 std::mutex g_mutex;
@@ -997,7 +997,9 @@ int multihead_fwd_bwd(const Settings& st, const void* X, const void* const* W, c
 
 }  // namespace
 
-int flce::shared_workspace(size_t need, char** out, hipStream_t s, bool last) { return acquire_workspace(need, out, s, last); }
+int flce::shared_workspace(size_t need, char** out, hipStream_t s, bool last) {
+    return acquire_workspace(need, out, s, last);
+}
 int flce::shared_workspace_lent(size_t* bytes) { return lent_workspace(bytes); }
 
 extern "C" {

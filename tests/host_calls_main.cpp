@@ -114,7 +114,8 @@ int backward(int64_t rows, int64_t H, void* stream = nullptr) {   // both norms,
     b.scale = 1.0f;
     b.eps = 1e-6f;
     auto at = [](int i) { return static_cast<void*>(operand(2 + i)); };
-    return L.flce_block_norm_bwd_(at(0), at(1), at(2), at(3), at(4), at(5), at(6), &b, at(7), at(8), at(9), at(10), at(11), stream);
+    return L.flce_block_norm_bwd_(at(0), at(1), at(2), at(3), at(4), at(5), at(6), &b, at(7), at(8), at(9), at(10), at(11),
+                                  stream);
 }
 
 // Where the library's own memory cannot grow to the whole plan, the backward runs with fewer workgroups.

@@ -220,7 +220,7 @@ def test_vectors_between_the_rows_of_a_matrix_do_not_overlap_it():
 
     def bwd(dpre, ldh=64, **kw):   # h: 4 rows of 16 bytes, 128 bytes apart
         b = _args(rows=4, ldh=ldh, workspace=w + 8194, workspace_bytes=1 << 12, **kw)
-        return L.flce_block_norm_bwd(w + 256, w + 1024, w + 2048, w + 3072, None, None, w + 4096, ctypes.byref(b), w + 5120,
+        return L.flce_block_norm_bwd(w + 256, w + 1024, w + 2048, w + 3328, None, None, w + 4096, ctypes.byref(b), w + 5120,
                                      w + 6144, None, None, dpre, None)
 
     first = w + 256
