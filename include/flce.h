@@ -366,6 +366,58 @@ FLCE_API int flce_clip_grad_norm(const void* const* grads, void* const* outs, co
                         void* workspace, size_t workspace_bytes, void* stream);
 FLCE_API size_t flce_grad_norm_workspace_bytes(int n_tensors);
 
+/*
+ * The other end of the model: embedding lookup with scaling, and the gradient of its table.  With
+ * v_i = tokens[i] - first_token, and live rows those with 0 <= v_i < V and tokens[i] != ignore_index,
+ *
+ *     out_i = scale * table[v_i]     for live rows, 0 for all others
+ *     dtable[v] = scale * sum of dout_i over the live rows with v_i = v       (0 where there is none)
+ *     dtable[v] += that                                                       (accumulate = 1)
+ *
+ * The table is a whole embedding (first_token = 0) or a rank's rows of one that is split by tokens: the ranks'
+ * outputs then add up to the whole's, and each rank gets its own rows' gradient.  Any token is taken: what lies
+ * outside [first_token, first_token + V) names no row and reads nothing.  Rows of dout that are not live are
+ * not read.
+ *
+ * accumulate = 1 adds to what dtable holds, e.g. the head's dW of flce_fwd_bwd where the head shares the
+ * table: rows of the table that no live row names are then neither read nor written.
+ *
+ * Every row of the gradient is a sum in the order of i: up to 32 consecutive terms in fp32 (which terms
+ * stand together depends on the tokens), those sums in fp64, scaled in fp32 and rounded to dtype once
+ * (accumulate: added in fp32 first).  No atomics: the same call gives the same bits.
+ *
+ *   size            must be sizeof(flce_embedding) (FLCE_ERR_ARG otherwise)
+ *   rows            number of tokens, 1 .. 2^30
+ *   V, H            rows of the table and their elements, 1 .. 2^30 and 1 .. 2^24
+ *   dtype           of table, out, dout and dtable
+ *   accumulate      0 or 1 (the forward ignores it)
+ *   first_token     the token of the table's first row
+ *   ignore_index    a token that names no row (padding)
+ *   scale           finite
+ *   ldtable, ldrows row strides in elements of table / dtable and of out / dout, 0 = H, else >= H.  Any
+ *                   stride and any pointer that fits its elements is taken (tokens: 8 bytes).
+ *   workspace       the backward's: device buffer (256-byte aligned) of flce_embedding_workspace_bytes of the
+ *                   same arguments, or NULL for the device's shared workspace.  FLCE_ERR_WORKSPACE if it is
+ *                   too small; what the call uses of it shares no memory with the operands (FLCE_ERR_ARG).
+ * An output shares no memory with an input (FLCE_ERR_ARG).
+ */
+typedef struct {
+    size_t size;
+    int64_t rows, V, H;
+    int dtype;
+    int accumulate;
+    int64_t first_token, ignore_index;
+    float scale;
+    int64_t ldtable, ldrows;
+    void* workspace;
+    size_t workspace_bytes;
+} flce_embedding;
+FLCE_API int flce_embedding_fwd(const void* table, const int64_t* tokens, const flce_embedding* args, void* out,
+                       void* stream);
+FLCE_API int flce_embedding_bwd(const void* dout, const int64_t* tokens, const flce_embedding* args, void* dtable,
+                       void* stream);
+FLCE_API size_t flce_embedding_workspace_bytes(const flce_embedding* args);
+
 /* Bytes of device scratch flce_fwd_bwd uses for this problem.  For fixed H, V
  * and dtype it does not grow with BT once BT exceeds one chunk:
  * flce_workspace_bytes(BT, ...) <= flce_workspace_bytes_max(...). */

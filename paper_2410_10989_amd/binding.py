@@ -55,6 +55,9 @@ def lib() -> ctypes.CDLL:
             "flce_grad_clip": ([p, p, p, p, ci, p, ctypes.c_float, p], ci),
             "flce_clip_grad_norm": ([p, p, p, p, ci, ci, ctypes.c_float, p, p, sz, p], ci),
             "flce_grad_norm_workspace_bytes": ([ci], sz),
+            "flce_embedding_fwd": ([p] * 5, ci),
+            "flce_embedding_bwd": ([p] * 5, ci),
+            "flce_embedding_workspace_bytes": ([p], sz),
             "flce_workspace_bytes": ([i64, i64, i64, ci], sz),
             "flce_workspace_bytes_max": ([i64, i64, ci], sz),
             "flce_set_workspace": ([p, sz], ci),
@@ -582,6 +585,84 @@ def flce_clip_grad_norm(grads, max_norm, norm_type=2.0, outs=None, norm=None, wo
                                        *_workspace_args(workspace, norm.device), _stream_handle(stream, norm.device))
     _check(st, "flce_clip_grad_norm")
     return norm
+
+
+class FlceEmbedding(ctypes.Structure):
+    """flce_embedding of include/flce.h."""
+    _fields_ = [("size", ctypes.c_size_t), ("rows", ctypes.c_int64), ("V", ctypes.c_int64), ("H", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("accumulate", ctypes.c_int), ("first_token", ctypes.c_int64),
+                ("ignore_index", ctypes.c_int64), ("scale", ctypes.c_float), ("ldtable", ctypes.c_int64),
+                ("ldrows", ctypes.c_int64), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+_EMBEDDING_BYTES = ctypes.sizeof(FlceEmbedding)
+
+
+def _tokens_ptr(tokens, device):
+    if tokens.dtype != torch.int64:
+        raise TypeError("tokens must be int64")
+    if tokens.device != device:
+        raise ValueError(f"tokens must live on {device}")
+    return _dev_ptr(tokens, "tokens")
+
+
+def flce_embedding_fwd(table, tokens, scale=1.0, ignore_index=-100, first_token=0, out=None, stream=None):
+    """out[i] = scale * table[tokens[i] - first_token]; zeros where that is no row of the table or ignore_index.
+
+    table [V, H] (float32 or bfloat16; rows may be apart), tokens int64 of any shape.  Returns out
+    [*tokens.shape, H]; where it is passed: [tokens.numel(), H], rows may be apart.
+    """
+    code = _dtype_code(table)
+    if table.dim() != 2 or not table.is_cuda:
+        raise ValueError("expected table [V, H] on the GPU")
+    V, H = table.shape
+    rows, device = tokens.numel(), table.device
+    pt = _tokens_ptr(tokens, device)
+    ptab, ldt = _rows_ptr(table, "table", table, table.shape, table.dtype, device.index)
+    if out is None:
+        out = torch.empty((*tokens.shape, H), dtype=table.dtype, device=device)
+        po, ldo = out.data_ptr(), 0
+    else:
+        po, ldo = _rows_ptr(out, "out", table, (rows, H), table.dtype, device.index)
+    args = FlceEmbedding(_EMBEDDING_BYTES, rows, V, H, code, 0, first_token, ignore_index, scale, ldt, ldo)
+    with _OnDevice(device):
+        st = lib().flce_embedding_fwd(ptab, pt, ctypes.byref(args), po, _stream_handle(stream, device))
+    _check(st, "flce_embedding_fwd")
+    return out
+
+
+def flce_embedding_bwd(dout, tokens, V, scale=1.0, ignore_index=-100, first_token=0, dtable=None, accumulate=False,
+                       workspace=None, stream=None):
+    """Gradient [V, H] of flce_embedding_fwd's table from dout [tokens.numel(), H] (rows may be apart) or
+    [*tokens.shape, H] (dense).  accumulate: it is added to what dtable holds (the head's dW, where both share the
+    matrix)."""
+    code = _dtype_code(dout)
+    if not dout.is_cuda or dout.dim() < 2:
+        raise ValueError("expected dout [rows, H] on the GPU")
+    rows, H, device = tokens.numel(), dout.shape[-1], dout.device
+    pt = _tokens_ptr(tokens, device)
+    if dout.dim() > 2 or tokens.dim() != 1:
+        if dout.shape != (*tokens.shape, H) and dout.shape != (rows, H):
+            raise ValueError("expected dout [*tokens.shape, H]")
+        dout = dout.view(rows, H)
+    pd, ldd = _rows_ptr(dout, "dout", dout, (rows, H), dout.dtype, device.index)
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate needs dtable")
+        dtable = torch.empty((V, H), dtype=dout.dtype, device=device)
+    pg, ldg = _rows_ptr(dtable, "dtable", dout, (V, H), dout.dtype, device.index)
+    args = FlceEmbedding(_EMBEDDING_BYTES, rows, V, H, code, 1 if accumulate else 0, first_token, ignore_index, scale, ldg, ldd,
+                         *_workspace_args(workspace, device))
+    with _OnDevice(device):
+        st = lib().flce_embedding_bwd(pd, pt, ctypes.byref(args), pg, _stream_handle(stream, device))
+    _check(st, "flce_embedding_bwd")
+    return dtable
+
+
+def flce_embedding_workspace_bytes(rows, V, H, dtype) -> int:
+    """Bytes of scratch flce_embedding_bwd uses for this shape."""
+    b = FlceEmbedding(size=_EMBEDDING_BYTES, rows=rows, V=V, H=H, dtype=_DTYPES.get(dtype, dtype))
+    return int(lib().flce_embedding_workspace_bytes(ctypes.byref(b)))
 
 
 CE_NOALLOC_MAX_ROWS = 65536

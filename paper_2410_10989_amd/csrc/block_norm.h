@@ -24,6 +24,7 @@
 // TB/s, four read and two written 6.9 / 6.1.
 #pragma once
 #include "flce_device.h"
+#include "rowsums.h"
 #include "rowvec.h"
 
 namespace flce {
@@ -50,62 +51,6 @@ struct BnArgs {
     int gate_direct;   // a segment is all rows of its gate row: dgate is written at once
     void *dpre, *dpost;   // one workgroup has all rows: the gammas' gradients are written at once
 };
-
-typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // at any element
-typedef f32x4 __attribute__((aligned(4))) f32x4_any;
-
-// Vector v of a row: whole for v < nfull; vector nfull has rem elements.
-template <typename T>
-__device__ __forceinline__ u32x4 bn_load(const T* row, int v, int nfull, int rem) {
-    constexpr int N = RowVec<T>::N;
-    u32x4 r = {0u, 0u, 0u, 0u};
-    if (v < nfull) {
-        r = *reinterpret_cast<const u32x4_any*>(row + (int64_t)v * N);
-    } else if (v == nfull && rem) {
-        const T* p = row + (int64_t)v * N;
-        float f[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = e < rem ? to_f32(p[e]) : 0.f;
-        r = RowVec<T>::pack(f);
-    }
-    return r;
-}
-template <typename T, bool NT>
-__device__ __forceinline__ void bn_store(T* row, int v, int nfull, int rem, const float (&f)[RowVec<T>::N]) {
-    constexpr int N = RowVec<T>::N;
-    if (v < nfull) {
-        u32x4_any* p = reinterpret_cast<u32x4_any*>(row + (int64_t)v * N);
-        if constexpr (NT) __builtin_nontemporal_store(RowVec<T>::pack(f), p);
-        else *p = RowVec<T>::pack(f);
-    } else if (v == nfull && rem) {
-        T* p = row + (int64_t)v * N;
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (e < rem) p[e] = from_f32<T>(f[e]);
-    }
-}
-
-// The same for loads that are issued a row ahead (H of at least one vector): putting a partial vector together
-// waits for every load before it, so its place is taken by the 16 bytes that end with the row, and bn_shift_tail
-// moves its elements to the front when the row's turn comes (rows of 4095 bf16: 158 -> 109 us, 8192 of them).
-template <typename T>
-__device__ __forceinline__ u32x4 bn_load_ahead(const T* row, int v, int nvec, int H) {
-    constexpr int N = RowVec<T>::N;
-    u32x4 r = {0u, 0u, 0u, 0u};
-    if (v < nvec) r = *reinterpret_cast<const u32x4_any*>(row + min(v * N, H - N));
-    return r;
-}
-template <typename T>
-__device__ __forceinline__ void bn_shift_tail(u32x4& r, int rem) {
-    const int drop = (RowVec<T>::N - rem) * (int)sizeof(T), words = drop / 4, bits = drop % 4 * 8;
-    const u32x4 from = r;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        auto word = [&](int i) { return i == 0 ? from[0] : i == 1 ? from[1] : i == 2 ? from[2] : i == 3 ? from[3] : 0u; };
-        const uint32_t lo = word(w + words), hi = word(w + words + 1);
-        r[w] = bits ? lo >> bits | hi << (32 - bits) : lo;
-    }
-}
 
 // 1 / (1 + e), e in [0, 1]: the hardware's reciprocal (1 ulp) and one Newton step.
 __device__ __forceinline__ float bn_one_over_1p(float e) {
@@ -137,75 +82,15 @@ __device__ __forceinline__ void bn_act_both(int act, float g, float& a, float& d
     }
 }
 
-template <int CTRL>
-__device__ __forceinline__ float bn_dpp_add(float v) {
-    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-// Sum over the aligned group of 16 or 64 lanes, the same bits in every lane: neighbours within a quad, quads and
-// halves of a row of 16 by mirroring, then rows and halves of the wavefront exchanged.
-template <int LANES>
-__device__ __forceinline__ float bn_lane_sum(float v) {
-    static_assert(LANES == 16 || LANES == 64, "");
-    v = bn_dpp_add<0xB1>(v);    // quad_perm 1 0 3 2
-    v = bn_dpp_add<0x4E>(v);    // quad_perm 2 3 0 1
-    v = bn_dpp_add<0x141>(v);   // row_half_mirror
-    v = bn_dpp_add<0x140>(v);   // row_mirror
-    if constexpr (LANES == 64) {
-        const uint32_t a = __float_as_uint(v);
-        const auto p = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-        const uint32_t b = __float_as_uint(v);
-        const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-        v = __uint_as_float(q[0]) + __uint_as_float(q[1]);
-    }
-    return v;
-}
-
-// K sums over the TPR threads of a row's group, the same values in every one of them.  slot: LDS of these sums
-// alone ([K][TPR / 64]; a group of several wavefronts is a whole workgroup), read until the next barrier.
-template <int TPR, int K>
-__device__ __forceinline__ void bn_sums(float (&v)[K], float* slot) {
-#pragma unroll
-    for (int i = 0; i < K; ++i) v[i] = bn_lane_sum<(TPR < WAVE ? TPR : WAVE)>(v[i]);
-    if constexpr (TPR > WAVE) {
-        constexpr int NW = TPR / WAVE;
-        if ((threadIdx.x & (WAVE - 1)) == 0)
-#pragma unroll
-            for (int i = 0; i < K; ++i) slot[i * NW + threadIdx.x / WAVE] = v[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            v[i] = slot[i * NW];
-#pragma unroll
-            for (int w = 1; w < NW; ++w) v[i] += slot[i * NW + w];
-        }
-    }
-}
-template <int TPR>
-__device__ __forceinline__ float bn_sum(float v, float* slot) {
-    float k[1] = {v};
-    bn_sums<TPR, 1>(k, slot);
-    return k[0];
-}
-// Threads of a workgroup, rows of it, and a thread's row in it (the same in a whole wavefront, if it is).
-template <int TPR> constexpr int bn_block = TPR > WAVE ? TPR : 256;
-template <int TPR> constexpr int bn_group_count = bn_block<TPR> / TPR;
-template <int TPR>
-__device__ __forceinline__ int bn_group() {
-    if constexpr (TPR > WAVE) return 0;
-    if constexpr (TPR == WAVE) return __builtin_amdgcn_readfirstlane((int)threadIdx.x / WAVE);
-    return (int)threadIdx.x / TPR;
-}
-
-// Forward: a workgroup holds bn_group_count rows.  All loads of a row are issued before the first is used, the
+// Forward: a workgroup holds row_groups rows.  All loads of a row are issued before the first is used, the
 // occupancy (37 to 106 registers with everything on) covers the rest.  us: 8192 x 4096 bf16 with the next block's norm
 // 38 (7.0 TB/s), 16384 x 3584 with both norms and a gate 67 (7.0; 85 where nothing read is in the cache yet: 5.5),
 // 2047 x 1000 fp32 with a sigmoid gate per token 10.5, one row of 4096 2.8.
 template <typename T, int TPR, int NV, bool POST, bool GATE, bool NT>
-__global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a) {
-    constexpr int N = RowVec<T>::N, GROUPS = bn_group_count<TPR>;
+__global__ __launch_bounds__(row_block<TPR>) void block_norm_fwd_kernel(BnArgs a) {
+    constexpr int N = RowVec<T>::N, GROUPS = row_groups<TPR>;
     __shared__ float red[2][TPR > WAVE ? TPR / WAVE : 1];
-    const int grp = bn_group<TPR>(), t = threadIdx.x % TPR;
+    const int grp = row_group<TPR>(), t = threadIdx.x % TPR;
     const float inv_H = 1.0f / (float)a.H;
     const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * GROUPS + grp;
     const bool live = row < a.rows;   // (a group past the last row takes part in the barriers)
@@ -215,7 +100,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a)
     auto load = [&](u32x4 (&to)[NV], const void* m, int64_t offset) {
         const T* p = static_cast<const T*>(m) + offset;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) to[k] = bn_load(p, t + k * TPR, nfull, rem);
+        for (int k = 0; k < NV; ++k) to[k] = row_load(p, t + k * TPR, nfull, rem);
     };
     if (a.x) load(xv, a.x, at * a.ldx);
     if (a.y) load(yv, a.y, at * a.ldy);
@@ -233,7 +118,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a)
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < N; ++e) ss += f[k][e] * f[k][e];
-            q = rsqrtf(bn_sum<TPR>(ss, red[0]) * inv_H + a.eps);
+            q = rsqrtf(row_sum<TPR>(ss, red[0]) * inv_H + a.eps);
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -255,7 +140,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a)
         if (a.out_h) {
             T* p = static_cast<T*>(a.out_h) + at * a.ldh;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) bn_store<T, NT>(p, t + k * TPR, nfull, rem, f[k]);
+            for (int k = 0; k < NV; ++k) row_store<T, NT>(p, t + k * TPR, nfull, rem, f[k]);
         }
     } else {
 #pragma unroll
@@ -267,7 +152,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a)
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < N; ++e) ss += f[k][e] * f[k][e];
-        const float r = rsqrtf(bn_sum<TPR>(ss, red[1]) * inv_H + a.eps);
+        const float r = rsqrtf(row_sum<TPR>(ss, red[1]) * inv_H + a.eps);
         T* p = static_cast<T*>(a.out_n) + at * a.ldn;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -275,7 +160,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a)
             RowVec<T>::unpack(nv[k], w);
 #pragma unroll
             for (int e = 0; e < N; ++e) w[e] *= f[k][e] * r;
-            bn_store<T, NT>(p, t + k * TPR, nfull, rem, w);
+            row_store<T, NT>(p, t + k * TPR, nfull, rem, w);
         }
     }
 }
@@ -283,7 +168,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_fwd_kernel(BnArgs a)
 // Sum over a workgroup of BN_LONG_THREADS; the barrier in front frees the LDS of the sum before.
 __device__ __forceinline__ float bn_long_sum(float v, float* red) {
     __syncthreads();
-    return bn_sum<BN_LONG_THREADS>(v, red);
+    return row_sum<BN_LONG_THREADS>(v, red);
 }
 
 // scale a(g) z of one vector of a row (z before the gate comes back too, for the backward).
@@ -292,13 +177,13 @@ __device__ __forceinline__ void bn_long_z(const BnArgs& a, const T* y, const T* 
                                           int rem, float (&z)[RowVec<T>::N], float (&out)[RowVec<T>::N]) {
     constexpr int N = RowVec<T>::N;
     float w[N];
-    RowVec<T>::unpack(bn_load(y, v, nfull, rem), z);
+    RowVec<T>::unpack(row_load(y, v, nfull, rem), z);
     if (a.gpost) {
-        RowVec<T>::unpack(bn_load(static_cast<const T*>(a.gpost), v, nfull, rem), w);
+        RowVec<T>::unpack(row_load(static_cast<const T*>(a.gpost), v, nfull, rem), w);
 #pragma unroll
         for (int e = 0; e < N; ++e) z[e] *= q * w[e];
     }
-    if (gate) RowVec<T>::unpack(bn_load(gate, v, nfull, rem), w);
+    if (gate) RowVec<T>::unpack(row_load(gate, v, nfull, rem), w);
 #pragma unroll
     for (int e = 0; e < N; ++e) out[e] = a.scale * (gate ? z[e] * bn_act(a.act, w[e]) : z[e]);
 }
@@ -309,7 +194,7 @@ __device__ __forceinline__ float bn_long_rstd(const T* row, int nvec, int nfull,
     float ss = 0.f;
     for (int v = threadIdx.x; v < nvec; v += BN_LONG_THREADS) {
         float f[N];
-        RowVec<T>::unpack(bn_load(row, v, nfull, rem), f);
+        RowVec<T>::unpack(row_load(row, v, nfull, rem), f);
 #pragma unroll
         for (int e = 0; e < N; ++e) ss += f[e] * f[e];
     }
@@ -333,7 +218,7 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_fwd_long(BnArgs a)
         float z[N];
         if (y) bn_long_z<T>(a, y, gate, q, v, nfull, rem, z, f);
         if (x) {
-            RowVec<T>::unpack(bn_load(x, v, nfull, rem), z);
+            RowVec<T>::unpack(row_load(x, v, nfull, rem), z);
 #pragma unroll
             for (int e = 0; e < N; ++e) f[e] = y ? z[e] + f[e] : z[e];
         }
@@ -352,13 +237,13 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_fwd_long(BnArgs a)
     for (int v = threadIdx.x; v < nvec; v += BN_LONG_THREADS) {
         float f[N];
         sum_at(v, f);
-        if (a.out_h) bn_store<T, NT>(static_cast<T*>(a.out_h) + row * a.ldh, v, nfull, rem, f);
+        if (a.out_h) row_store<T, NT>(static_cast<T*>(a.out_h) + row * a.ldh, v, nfull, rem, f);
         if (a.gpre) {
             float w[N];
-            RowVec<T>::unpack(bn_load(static_cast<const T*>(a.gpre), v, nfull, rem), w);
+            RowVec<T>::unpack(row_load(static_cast<const T*>(a.gpre), v, nfull, rem), w);
 #pragma unroll
             for (int e = 0; e < N; ++e) w[e] *= f[e] * r;
-            bn_store<T, NT>(static_cast<T*>(a.out_n) + row * a.ldn, v, nfull, rem, w);
+            row_store<T, NT>(static_cast<T*>(a.out_n) + row * a.ldn, v, nfull, rem, w);
         }
     }
 }
@@ -382,7 +267,7 @@ struct BnRow {
 // Backward: workgroup b takes segments b, b + gridDim.x, ...; its GROUPS rows at a time.  The sums over rows
 // stay in registers: the gammas' until the workgroup's last row, a shared gate's until its segment's; then the
 // groups of a workgroup add theirs up in a fixed order.  Sums of several workgroups are left as rows of fp32
-// partial sums for bn_sum_partials_kernel: no atomics, the order of additions depends on the shape and the number
+// partial sums for sum_partials_kernel: no atomics, the order of additions depends on the shape and the number
 // of workgroups alone.  The rows of a segment's parts are dealt side by side, so that all workgroups read
 // neighbouring rows at a time (16384 x 3584: 149 -> 136 us against one stretch of rows each), and the sums are stored
 // in 16-byte pieces (element by element, 32 x 4096 11.3 instead of 8.3 us).
@@ -398,14 +283,14 @@ struct BnRow {
 // the next block's norm 55, 2047 x 1000 fp32 with a silu gate per sequence 19.
 constexpr int BN_WIDE_COLS = 16384, BN_WIDE_COLS_3 = 13312;   // of up to two and of three sets of sums: 160 KB
 template <typename T, int TPR, int NV, bool POST, int GATE, bool AHEAD, bool WIDE, bool NT>
-__global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a) {
-    constexpr int N = RowVec<T>::N, BLOCK = bn_block<TPR>, GROUPS = bn_group_count<TPR>, NW = TPR > WAVE ? TPR / WAVE : 1;
+__global__ __launch_bounds__(row_block<TPR>) void block_norm_bwd_kernel(BnArgs a) {
+    constexpr int N = RowVec<T>::N, BLOCK = row_block<TPR>, GROUPS = row_groups<TPR>, NW = TPR > WAVE ? TPR / WAVE : 1;
     __shared__ float red[3][3 * NW];
     __shared__ __align__(16) float cols[GROUPS > 1 ? BLOCK * NV * N : 4];
     constexpr int SETS = 1 + POST + (GATE == BN_GATE_SUM), COLS = SETS == 3 ? BN_WIDE_COLS_3 : BN_WIDE_COLS;
     constexpr int AT_PRE = 0, AT_POST = COLS, AT_GATE = (1 + POST) * COLS;
     __shared__ __align__(16) float wide[WIDE ? SETS * COLS : 4];
-    const int grp = bn_group<TPR>(), t = threadIdx.x % TPR;
+    const int grp = row_group<TPR>(), t = threadIdx.x % TPR;
     const int nfull_all = a.H / N, rem_all = a.H % N;
     const float inv_H = 1.0f / (float)a.H;
     u32x4 prev[NV], postv[NV];
@@ -442,7 +327,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
     auto load_shared = [&](const void* m, int64_t offset, int v) {   // of what many rows share
         // (WIDE reads it again for every row: kept over the rows it would take the registers of the rows)
         if constexpr (WIDE) asm volatile("" : "+s"(m));
-        return bn_load(static_cast<const T*>(m) + offset, v, nfull_all, rem_all);
+        return row_load(static_cast<const T*>(m) + offset, v, nfull_all, rem_all);
     };
     if (a.gpre && !WIDE)
 #pragma unroll
@@ -478,7 +363,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[e] = WIDE ? wide_at(set, k)[e] : acc[WIDE ? 0 : k][e];
                 if (out) {
-                    bn_store<T, false>(out, at, nfull_all, rem_all, v);
+                    row_store<T, false>(out, at, nfull_all, rem_all, v);
                 } else if (at < nfull_all) {
 #pragma unroll
                     for (int e = 0; e < N; e += 4)
@@ -499,7 +384,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
         auto load = [&](u32x4 (&to)[NV], const void* m, int64_t ld) {
             const T* p = static_cast<const T*>(m) + row * ld;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) to[k] = bn_load_ahead(p, t + k * TPR, nvec, a.H);
+            for (int k = 0; k < NV; ++k) to[k] = row_load_ahead(p, t + k * TPR, nvec, a.H);
         };
         if (a.gpre) {
             load(r.h, a.h, a.ldh);
@@ -548,12 +433,12 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                 for (int k = 0; k < NV; ++k)
                     if (t + k * TPR == nfull) {
                         if (a.gpre) {
-                            bn_shift_tail<T>(in.h[k], rem);
-                            bn_shift_tail<T>(in.dn[k], rem);
+                            row_shift_tail<T>(in.h[k], rem);
+                            row_shift_tail<T>(in.dn[k], rem);
                         }
-                        if (a.y) bn_shift_tail<T>(in.y[k], rem);
-                        if (a.dh) bn_shift_tail<T>(in.dh[k], rem);
-                        if constexpr (GATE == BN_GATE_ROW) bn_shift_tail<T>(in.gate[k], rem);
+                        if (a.y) row_shift_tail<T>(in.y[k], rem);
+                        if (a.dh) row_shift_tail<T>(in.dh[k], rem);
+                        if constexpr (GATE == BN_GATE_ROW) row_shift_tail<T>(in.gate[k], rem);
                     }
             }
             // sum h^2, sum u h and sum y^2 in one exchange
@@ -582,10 +467,10 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                 }
             }
             if constexpr (POST) {
-                bn_sums<TPR, 3>(sums, red[0]);   // (the barrier of the second exchange stands between two of these)
+                row_sums<TPR, 3>(sums, red[0]);   // (the barrier of the second exchange stands between two of these)
             } else if (a.gpre) {
                 float two[2] = {sums[0], sums[1]};
-                bn_sums<TPR, 2>(two, red[turn]);
+                row_sums<TPR, 2>(two, red[turn]);
                 sums[0] = two[0];
                 sums[1] = two[1];
             }
@@ -622,7 +507,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
             if (a.dx) {
                 T* p = static_cast<T*>(a.dx) + row * a.lddx;
 #pragma unroll
-                for (int k = 0; k < NV; ++k) bn_store<T, NT>(p, t + k * TPR, nfull, rem, D[k]);
+                for (int k = 0; k < NV; ++k) row_store<T, NT>(p, t + k * TPR, nfull, rem, D[k]);
             }
             if (!a.y) continue;
             const float q = POST ? rsqrtf(sums[2] * inv_H + a.eps) : 1.0f;
@@ -664,11 +549,11 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
                 if constexpr (WIDE && GATE == BN_GATE_SUM) wide_add(AT_GATE, k, to_gate);
                 if constexpr (WIDE && POST) wide_add(AT_POST, k, to_post);
                 if constexpr (GATE == BN_GATE_ROW) {
-                    if (a.dgate) bn_store<T, NT>(static_cast<T*>(a.dgate) + row * a.lddgate, t + k * TPR, nfull, rem, g);
+                    if (a.dgate) row_store<T, NT>(static_cast<T*>(a.dgate) + row * a.lddgate, t + k * TPR, nfull, rem, g);
                 }
             }
             if constexpr (POST) {
-                bn_sums<TPR, 1>(vy, red[2]);
+                row_sums<TPR, 1>(vy, red[2]);
                 const float yk = -(q * (q * (vy[0] * inv_H)));
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
@@ -681,7 +566,7 @@ __global__ __launch_bounds__(bn_block<TPR>) void block_norm_bwd_kernel(BnArgs a)
             if (a.dy) {
                 T* p = static_cast<T*>(a.dy) + row * a.lddy;
 #pragma unroll
-                for (int k = 0; k < NV; ++k) bn_store<T, NT>(p, t + k * TPR, nfull, rem, D[k]);
+                for (int k = 0; k < NV; ++k) row_store<T, NT>(p, t + k * TPR, nfull, rem, D[k]);
             }
         }
         if constexpr (GATE == BN_GATE_SUM) {
@@ -737,9 +622,9 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
                 float hh = 0.f, uh = 0.f;
                 for (int v = threadIdx.x; v < nvec; v += BN_LONG_THREADS) {
                     float hf[N], u[N], w[N];
-                    RowVec<T>::unpack(bn_load(h, v, nfull, rem), hf);
-                    RowVec<T>::unpack(bn_load(dn, v, nfull, rem), u);
-                    RowVec<T>::unpack(bn_load(gpre, v, nfull, rem), w);
+                    RowVec<T>::unpack(row_load(h, v, nfull, rem), hf);
+                    RowVec<T>::unpack(row_load(dn, v, nfull, rem), u);
+                    RowVec<T>::unpack(row_load(gpre, v, nfull, rem), w);
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
                         hh += hf[e] * hf[e];
@@ -755,19 +640,19 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
             auto grad_h = [&](int v, float (&D)[N]) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) D[e] = 0.f;
-                if (dh) RowVec<T>::unpack(bn_load(dh, v, nfull, rem), D);
+                if (dh) RowVec<T>::unpack(row_load(dh, v, nfull, rem), D);
                 if (h) {
                     float hf[N], u[N], w[N];
-                    RowVec<T>::unpack(bn_load(h, v, nfull, rem), hf);
-                    RowVec<T>::unpack(bn_load(dn, v, nfull, rem), u);
-                    RowVec<T>::unpack(bn_load(gpre, v, nfull, rem), w);
+                    RowVec<T>::unpack(row_load(h, v, nfull, rem), hf);
+                    RowVec<T>::unpack(row_load(dn, v, nfull, rem), u);
+                    RowVec<T>::unpack(row_load(gpre, v, nfull, rem), w);
 #pragma unroll
                     for (int e = 0; e < N; ++e) D[e] += r * (u[e] * w[e] - hf[e] * r * c);
                 }
             };
             auto grad_z = [&](int v, const float (&D)[N], float (&dz)[N]) {
                 float g[N];
-                if (gate) RowVec<T>::unpack(bn_load(gate, v, nfull, rem), g);
+                if (gate) RowVec<T>::unpack(row_load(gate, v, nfull, rem), g);
 #pragma unroll
                 for (int e = 0; e < N; ++e) dz[e] = a.scale * D[e] * (gate ? bn_act(a.act, g[e]) : 1.0f);
             };
@@ -777,8 +662,8 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
                     float D[N], dz[N], yf[N], w[N];
                     grad_h(v, D);
                     grad_z(v, D, dz);
-                    RowVec<T>::unpack(bn_load(y, v, nfull, rem), yf);
-                    RowVec<T>::unpack(bn_load(gpost, v, nfull, rem), w);
+                    RowVec<T>::unpack(row_load(y, v, nfull, rem), yf);
+                    RowVec<T>::unpack(row_load(gpost, v, nfull, rem), w);
 #pragma unroll
                     for (int e = 0; e < N; ++e) vy += dz[e] * w[e] * yf[e] * q;
                 }
@@ -789,8 +674,8 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
                 grad_h(v, D);
                 if (pre) {
                     float hf[N], u[N];
-                    RowVec<T>::unpack(bn_load(h, v, nfull, rem), hf);
-                    RowVec<T>::unpack(bn_load(dn, v, nfull, rem), u);
+                    RowVec<T>::unpack(row_load(h, v, nfull, rem), hf);
+                    RowVec<T>::unpack(row_load(dn, v, nfull, rem), u);
 #pragma unroll
                     for (int e = 0; e < N; ++e)
                         if (v * N + e < a.H) pre[v * N + e] += u[e] * (hf[e] * r);
@@ -798,10 +683,10 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
                 if (y) {
                     float dz[N], yf[N], w[N], g[N], dg[N];
                     grad_z(v, D, dz);
-                    RowVec<T>::unpack(bn_load(y, v, nfull, rem), yf);
-                    if (gpost) RowVec<T>::unpack(bn_load(gpost, v, nfull, rem), w);
+                    RowVec<T>::unpack(row_load(y, v, nfull, rem), yf);
+                    if (gpost) RowVec<T>::unpack(row_load(gpost, v, nfull, rem), w);
                     if (gate) {
-                        RowVec<T>::unpack(bn_load(gate, v, nfull, rem), g);
+                        RowVec<T>::unpack(row_load(gate, v, nfull, rem), g);
 #pragma unroll
                         for (int e = 0; e < N; ++e) {
                             const float z = gpost ? yf[e] * q * w[e] : yf[e];
@@ -811,7 +696,7 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
                             if (gsum && v * N + e < a.H) gsum[v * N + e] += dg[e];
                         }
                         if (a.by_row && a.dgate)
-                            bn_store<T, NT>(static_cast<T*>(a.dgate) + row * a.lddgate, v, nfull, rem, dg);
+                            row_store<T, NT>(static_cast<T*>(a.dgate) + row * a.lddgate, v, nfull, rem, dg);
                     }
                     if (gpost) {
 #pragma unroll
@@ -821,53 +706,15 @@ __global__ __launch_bounds__(BN_LONG_THREADS) void block_norm_bwd_long(BnArgs a)
                             dz[e] = q * (dz[e] * w[e] - yh * cy);
                         }
                     }
-                    if (a.dy) bn_store<T, NT>(static_cast<T*>(a.dy) + row * a.lddy, v, nfull, rem, dz);
+                    if (a.dy) row_store<T, NT>(static_cast<T*>(a.dy) + row * a.lddy, v, nfull, rem, dz);
                 }
-                if (a.dx) bn_store<T, NT>(static_cast<T*>(a.dx) + row * a.lddx, v, nfull, rem, D);
+                if (a.dx) row_store<T, NT>(static_cast<T*>(a.dx) + row * a.lddx, v, nfull, rem, D);
             }
         }
         if (gsum && a.gate_direct) {
             T* out = static_cast<T*>(a.dgate) + (int64_t)seg.g * a.lddgate;
             each(gsum, [&](float* p, int j) { out[j] = from_f32<T>(p[j]); });
         }
-    }
-}
-
-// out[g][j] = sum over p of rows [g * parts + p][j] of fp32 partial sums, for up to three sets of them: the two
-// gammas (one output row each) and the gate.  As in rmsnorm_dgamma_kernel a workgroup owns some columns of an
-// output row (32: lines of 128 bytes), thread (c, q) adds rows q, q + 32, ... of column c, then the 32 sums are added in
-// order; in fp64, which costs nothing here and leaves the fp32 sums of a workgroup's own rows as the only ones.  Bound
-// by the latency of a thread's loads: eight under way at a time, issued without a condition (3-5 us).
-struct BnSums {
-    const float* part[3];
-    void* out[3];
-    int64_t ld[3];
-    int parts[3];
-    int first[4];   // the sets' output rows are rows first[i] .. first[i + 1] of the grid
-};
-constexpr int BN_SUM_COLS = 32, BN_SUM_PARTS = 32;
-template <typename T>
-__global__ __launch_bounds__(BN_SUM_COLS * BN_SUM_PARTS) void bn_sum_partials_kernel(BnSums b, int n) {
-    __shared__ double sums[BN_SUM_PARTS][BN_SUM_COLS];
-    const int c = threadIdx.x % BN_SUM_COLS, q = threadIdx.x / BN_SUM_COLS;
-    const int r = blockIdx.y, j = blockIdx.x * BN_SUM_COLS + c;
-    const int set = r >= b.first[2] ? 2 : r >= b.first[1] ? 1 : 0;
-    const int g = r - b.first[set], parts = b.parts[set];
-    const float* from = b.part[set] + (int64_t)g * parts * n + j;
-    double s = 0.0;
-    if (j < n)
-        for (int p0 = q; p0 < parts; p0 += 8 * BN_SUM_PARTS) {   // (eight loads under way, also where there are fewer)
-            float v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = from[(int64_t)min(p0 + k * BN_SUM_PARTS, parts - 1) * n];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) s += p0 + k * BN_SUM_PARTS < parts ? (double)v[k] : 0.0;
-        }
-    sums[q][c] = s;
-    __syncthreads();
-    if (q == 0 && j < n) {
-        for (int k = 1; k < BN_SUM_PARTS; ++k) s += sums[k][c];
-        (static_cast<T*>(b.out[set]) + (int64_t)g * b.ld[set])[j] = from_f32<T>((float)s);
     }
 }
 

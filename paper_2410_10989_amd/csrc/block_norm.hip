@@ -21,35 +21,6 @@ constexpr int64_t BN_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
 size_t bn_elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
 
-// A strided matrix in memory.
-struct Span {
-    const char* p;
-    size_t pitch, width;   // bytes from row to row, bytes of a row
-    int64_t rows;
-};
-Span span(const void* p, int64_t ld, int64_t rows, int64_t H, size_t es) {
-    return {static_cast<const char*>(p), (size_t)ld * es, (size_t)H * es, rows};
-}
-// Whether two of them share a byte.  A single row may lie between the rows of the other, column windows of one wider
-// buffer (equal pitch) may interleave; with different pitches any common stretch of addresses counts.
-bool overlap(const Span& a, const Span& b) {
-    if (!a.p || !b.p) return false;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-    const uintptr_t a1 = a0 + (a.rows - 1) * a.pitch + a.width, b1 = b0 + (b.rows - 1) * b.pitch + b.width;
-    if (a1 <= b0 || b1 <= a0) return false;
-    if (a.rows == 1 || b.rows == 1) {
-        const Span &m = a.rows == 1 ? b : a, &v = a.rows == 1 ? a : b;
-        const uintptr_t m0 = reinterpret_cast<uintptr_t>(m.p), v0 = reinterpret_cast<uintptr_t>(v.p);
-        if (v0 <= m0) return true;
-        const size_t off = (v0 - m0) % m.pitch;   // from the row that begins before v
-        return off < m.width || ((int64_t)((v0 - m0) / m.pitch) + 1 < m.rows && off + v.width > m.pitch);
-    }
-    if (a.pitch != b.pitch) return true;
-    const size_t off = b0 >= a0 ? (b0 - a0) % a.pitch : (a.pitch - (a0 - b0) % a.pitch) % a.pitch;
-    return off < a.width || a.pitch - off < b.width;
-}
-bool same(const Span& a, const Span& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1); }
-
 struct Strides {
     int64_t x, y, h, n, gate, dx, dy, dh, dn, dgate;
 };
@@ -179,10 +150,10 @@ BnPlan bn_plan(const BnShape& s, int64_t rows, int64_t H, int64_t per, bool pre,
 
 template <typename T, bool NT, int TPR, int E>
 void launch_fwd(const BnArgs& a, hipStream_t s) {
-    constexpr int NV = E / RowVec<T>::N, GROUPS = bn_group_count<TPR>;
+    constexpr int NV = E / RowVec<T>::N, GROUPS = row_groups<TPR>;
     const int64_t blocks = (a.rows + GROUPS - 1) / GROUPS;
     const dim3 grid((unsigned)std::min(blocks, BN_GRID_X), (unsigned)((blocks + BN_GRID_X - 1) / BN_GRID_X));
-    const dim3 block(bn_block<TPR>);
+    const dim3 block(row_block<TPR>);
 #define BN_FWD(POST, GATE) hipLaunchKernelGGL((block_norm_fwd_kernel<T, TPR, NV, POST, GATE, NT>), grid, block, 0, s, a)
     if (a.gpost) {
         if (a.gate) BN_FWD(true, true); else BN_FWD(true, false);
@@ -194,7 +165,7 @@ void launch_fwd(const BnArgs& a, hipStream_t s) {
 template <typename T, bool NT, int TPR, int E>
 void launch_bwd(const BnArgs& a, const dim3& grid, hipStream_t s) {
     constexpr int NV = E / RowVec<T>::N;
-    const dim3 block(bn_block<TPR>);
+    const dim3 block(row_block<TPR>);
 #define BN_BWD(POST, GATE) \
     hipLaunchKernelGGL((block_norm_bwd_kernel<T, TPR, NV, POST, GATE, (NV <= 2), (E == 32), NT>), grid, block, 0, s, a)
 #define BN_BWD_GATE(POST)                             \
@@ -255,7 +226,7 @@ int run_bwd(const BnArgs& a, const BnShape& sh, const BnPlan& p, void* dgamma_pr
         hipLaunchKernelGGL((block_norm_bwd_long<T, NT>), grid, dim3(BN_LONG_THREADS), 0, s, a);
     }
     HIP_TRY(hipGetLastError());
-    BnSums b{};
+    PartialSums b{};
     int set = 0, rows = 0;
     auto add = [&](const float* part, void* out, int64_t ld, int64_t parts, int64_t out_rows) {
         b.part[set] = part;
@@ -271,8 +242,8 @@ int run_bwd(const BnArgs& a, const BnShape& sh, const BnPlan& p, void* dgamma_pr
     if (a.part_gate && !p.direct) add(a.part_gate, a.dgate, a.lddgate, p.parts, p.segments / p.parts);
     if (!rows) return FLCE_OK;
     for (int i = set; i < 4; ++i) b.first[i] = rows;
-    const int col_blocks = (a.H + BN_SUM_COLS - 1) / BN_SUM_COLS;
-    hipLaunchKernelGGL((bn_sum_partials_kernel<T>), dim3((unsigned)col_blocks, (unsigned)rows), dim3(BN_SUM_COLS * BN_SUM_PARTS),
+    const int col_blocks = (a.H + SUM_COLS - 1) / SUM_COLS;
+    hipLaunchKernelGGL((sum_partials_kernel<T>), dim3((unsigned)col_blocks, (unsigned)rows), dim3(SUM_COLS * SUM_PARTS),
                        0, s, b, a.H);
     HIP_TRY(hipGetLastError());
     return FLCE_OK;

@@ -1,0 +1,159 @@
+// C ABI of the embedding lookup and its gradient (see embedding.h): argument checks, workspace, launches.
+#include "embedding.h"
+
+#include <algorithm>
+
+#include "flce_host.h"
+
+using namespace flce;
+
+namespace {
+
+constexpr int64_t EM_MAX_H = (int64_t)1 << 24;      // keeps vector numbers within 32 bits
+constexpr int64_t EM_GRID = (int64_t)1 << 20;       // workgroups of a launch; they go on in strides
+constexpr int EM_CUS = 256, EM_RANGE_MIN = 32;
+constexpr int64_t EM_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
+
+size_t elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
+int64_t align64(int64_t n) { return (n + 63) / 64 * 64; }
+
+int check_common(const flce_embedding* b) {
+    if (!b) return FLCE_ERR_NULL;
+    if (b->size != sizeof(flce_embedding)) return FLCE_ERR_ARG;
+    if (b->dtype != FLCE_F32 && b->dtype != FLCE_BF16) return FLCE_ERR_DTYPE;
+    if (b->rows < 1 || b->rows > MAX_DIM || b->V < 1 || b->V > MAX_DIM || b->H < 1 || b->H > EM_MAX_H) return FLCE_ERR_SHAPE;
+    if (b->scale - b->scale != 0.0f) return FLCE_ERR_ARG;
+    if (b->ldtable && b->V > 1 && (b->ldtable < b->H || b->ldtable > MAX_DIM * 4)) return FLCE_ERR_SHAPE;
+    if (b->ldrows && b->rows > 1 && (b->ldrows < b->H || b->ldrows > MAX_DIM * 4)) return FLCE_ERR_SHAPE;
+    return FLCE_OK;
+}
+int64_t table_stride(const flce_embedding& b) { return b.ldtable && b.V > 1 ? b.ldtable : b.H; }
+int64_t rows_stride(const flce_embedding& b) { return b.ldrows && b.rows > 1 ? b.ldrows : b.H; }
+
+// Where the order and the partial sums lie, in bytes from the workspace's start.
+struct Plan {
+    int64_t slices, pieces;
+    size_t token, row, part, total;
+};
+Plan plan_of(const flce_embedding& b) {
+    const int64_t N = 16 / (int64_t)elem(b.dtype);
+    Plan p{};
+    p.slices = ((b.H + N - 1) / N + WAVE - 1) / WAVE;
+    p.pieces = (b.rows + EM_PIECE - 1) / EM_PIECE;
+    p.token = (size_t)align64(b.V + 1) * sizeof(int);
+    p.row = p.token + (size_t)align64(b.rows) * sizeof(int);
+    p.part = p.row + (size_t)align64(b.rows) * sizeof(int);
+    p.total = p.part + (p.pieces > 1 ? (size_t)p.pieces * 2 * (size_t)(p.slices * WAVE * N) * sizeof(float) : 0);
+    return p;
+}
+
+EmbedArgs args_of(const flce_embedding& b, const int64_t* tokens) {
+    EmbedArgs a{};
+    a.tokens = tokens;
+    a.first = b.first_token;
+    a.ignored = b.ignore_index;
+    a.rows = (int)b.rows;
+    a.V = (int)b.V;
+    a.H = (int)b.H;
+    a.scale = b.scale;
+    return a;
+}
+
+template <typename T, int LPR, int K>
+void launch_fwd(const EmbedArgs& a, bool nt, hipStream_t s) {
+    constexpr int ROWS = 256 / LPR;
+    const dim3 grid((unsigned)std::min<int64_t>(EM_GRID, ((int64_t)a.rows + ROWS - 1) / ROWS));
+    if (nt) hipLaunchKernelGGL((embed_fwd_kernel<T, LPR, K, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((embed_fwd_kernel<T, LPR, K, false>), grid, dim3(256), 0, s, a);
+}
+template <typename T>
+int run_fwd(const EmbedArgs& a, bool nt, hipStream_t s) {
+    const int64_t nvec = ((int64_t)a.H + RowVec<T>::N - 1) / RowVec<T>::N;
+    if (nvec <= 16) launch_fwd<T, 16, 1>(a, nt, s);
+    else if (nvec <= 64) launch_fwd<T, 64, 1>(a, nt, s);
+    else if (nvec <= 256) launch_fwd<T, 64, 4>(a, nt, s);
+    else launch_fwd<T, 64, 8>(a, nt, s);
+    HIP_TRY(hipGetLastError());
+    return FLCE_OK;
+}
+template <typename T, bool NT>
+int run_bwd(const EmbedArgs& a, const Plan& p, hipStream_t s) {
+    const int64_t ranges = ((int64_t)a.V + a.range - 1) / a.range;
+    hipLaunchKernelGGL((embed_sort_kernel<T, NT>), dim3((unsigned)ranges), dim3(EM_SORT_THREADS), 0, s, a);
+    HIP_TRY(hipGetLastError());
+    const int64_t units = p.pieces * p.slices;
+    hipLaunchKernelGGL((embed_sum_kernel<T, NT>), dim3((unsigned)std::min(EM_GRID, (units + 3) / 4)), dim3(256), 0, s, a);
+    HIP_TRY(hipGetLastError());
+    if (p.pieces == 1) return FLCE_OK;
+    hipLaunchKernelGGL((embed_join_kernel<T, NT>), dim3((unsigned)std::min(EM_GRID, units)), dim3(EM_JOIN_THREADS), 0, s, a);
+    HIP_TRY(hipGetLastError());
+    return FLCE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int flce_embedding_fwd(const void* table, const int64_t* tokens, const flce_embedding* args, void* out, void* stream) {
+    FLCE_TRY(check_common(args));
+    const flce_embedding& b = *args;
+    if (!table || !tokens || !out) return FLCE_ERR_NULL;
+    const size_t es = elem(b.dtype);
+    if (!aligned(table, es) || !aligned(out, es) || !aligned(tokens, 8)) return FLCE_ERR_ALIGN;
+    const Span to = span(out, rows_stride(b), b.rows, b.H, es);
+    if (overlap(to, span(table, table_stride(b), b.V, b.H, es)) || overlap(to, span(tokens, b.rows, 1, b.rows, 8)))
+        return FLCE_ERR_ARG;
+    EmbedArgs a = args_of(b, tokens);
+    a.in = table;
+    a.out = out;
+    a.ldin = table_stride(b);
+    a.ldout = rows_stride(b);
+    const bool nt = b.rows * b.H * (int64_t)es > EM_CACHE_BYTES;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return b.dtype == FLCE_F32 ? run_fwd<float>(a, nt, s) : run_fwd<bf16_t>(a, nt, s);
+}
+
+int flce_embedding_bwd(const void* dout, const int64_t* tokens, const flce_embedding* args, void* dtable, void* stream) {
+    FLCE_TRY(check_common(args));
+    const flce_embedding& b = *args;
+    if (!dout || !tokens || !dtable) return FLCE_ERR_NULL;
+    if (b.accumulate != 0 && b.accumulate != 1) return FLCE_ERR_ARG;
+    const size_t es = elem(b.dtype);
+    if (!aligned(dout, es) || !aligned(dtable, es) || !aligned(tokens, 8)) return FLCE_ERR_ALIGN;
+    const Span to = span(dtable, table_stride(b), b.V, b.H, es), from = span(dout, rows_stride(b), b.rows, b.H, es);
+    const Span which = span(tokens, b.rows, 1, b.rows, 8);
+    if (overlap(to, from) || overlap(to, which)) return FLCE_ERR_ARG;
+    const Plan p = plan_of(b);
+    char* ws = static_cast<char*>(b.workspace);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (ws) {
+        if (!aligned(ws, 256)) return FLCE_ERR_ALIGN;
+        if (b.workspace_bytes < p.total) return FLCE_ERR_WORKSPACE;
+    } else {
+        FLCE_TRY(shared_workspace(p.total, &ws, s));
+    }
+    const Span scratch{ws, p.total, p.total, 1};
+    if (overlap(scratch, to) || overlap(scratch, from) || overlap(scratch, which)) return FLCE_ERR_ARG;
+    EmbedArgs a = args_of(b, tokens);
+    a.in = dout;
+    a.out = dtable;
+    a.ldin = rows_stride(b);
+    a.ldout = table_stride(b);
+    a.add = b.accumulate;
+    a.range = EM_RANGE;
+    while (a.range > EM_RANGE_MIN && b.V / a.range < EM_CUS) a.range /= 2;
+    a.begin = reinterpret_cast<int*>(ws);
+    a.token = reinterpret_cast<int*>(ws + p.token);
+    a.row = reinterpret_cast<int*>(ws + p.row);
+    a.part = reinterpret_cast<float*>(ws + p.part);
+    a.slices = (int)p.slices;
+    const bool nt = !b.accumulate && b.V * b.H * (int64_t)es > EM_CACHE_BYTES;
+    if (nt) return b.dtype == FLCE_F32 ? run_bwd<float, true>(a, p, s) : run_bwd<bf16_t, true>(a, p, s);
+    return b.dtype == FLCE_F32 ? run_bwd<float, false>(a, p, s) : run_bwd<bf16_t, false>(a, p, s);
+}
+
+size_t flce_embedding_workspace_bytes(const flce_embedding* args) {
+    return check_common(args) == FLCE_OK ? plan_of(*args).total : 0;
+}
+
+}  // extern "C"

@@ -26,6 +26,35 @@ constexpr int64_t MAX_DIM = (int64_t)1 << 30;   // per-dimension limit, keeps in
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+// A strided matrix in memory.
+struct Span {
+    const char* p;
+    size_t pitch, width;   // bytes from row to row, bytes of a row
+    int64_t rows;
+};
+inline Span span(const void* p, int64_t ld, int64_t rows, int64_t H, size_t es) {
+    return {static_cast<const char*>(p), (size_t)ld * es, (size_t)H * es, rows};
+}
+// Whether two of them share a byte.  A single row may lie between the rows of the other, column windows of one wider
+// buffer (equal pitch) may interleave; with different pitches any common stretch of addresses counts.
+inline bool overlap(const Span& a, const Span& b) {
+    if (!a.p || !b.p) return false;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+    const uintptr_t a1 = a0 + (a.rows - 1) * a.pitch + a.width, b1 = b0 + (b.rows - 1) * b.pitch + b.width;
+    if (a1 <= b0 || b1 <= a0) return false;
+    if (a.rows == 1 || b.rows == 1) {
+        const Span &m = a.rows == 1 ? b : a, &v = a.rows == 1 ? a : b;
+        const uintptr_t m0 = reinterpret_cast<uintptr_t>(m.p), v0 = reinterpret_cast<uintptr_t>(v.p);
+        if (v0 <= m0) return true;
+        const size_t off = (v0 - m0) % m.pitch;   // from the row that begins before v
+        return off < m.width || ((int64_t)((v0 - m0) / m.pitch) + 1 < m.rows && off + v.width > m.pitch);
+    }
+    if (a.pitch != b.pitch) return true;
+    const size_t off = b0 >= a0 ? (b0 - a0) % a.pitch : (a.pitch - (a0 - b0) % a.pitch) % a.pitch;
+    return off < a.width || a.pitch - off < b.width;
+}
+inline bool same(const Span& a, const Span& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1); }
+
 // The current device's shared workspace (see Scratch memory in flce.h), at least `need` bytes of it, for a call on s.
 // last: the caller has no plan that needs less (without one, an allocation that found too little memory is not tried
 // again every call).
