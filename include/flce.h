@@ -327,6 +327,56 @@ FLCE_API int flce_block_norm_bwd(const void* h, const void* dn, const void* dh, 
 FLCE_API size_t flce_block_norm_workspace_bytes(const flce_block_norm* args);
 
 /*
+ * Layer norm, with the residual sum in front of it: what flce_block_norm is to models with RMSNorm, for models that
+ * take the mean off and add a bias.  Row by row of [rows x H] matrices:
+ *
+ *     h = x + y                           (without y: h = x, not written again)
+ *     n = (h - mean h) / sqrt(mean (h - mean h)^2 + eps) * gamma + beta         (gamma, beta: each may be missing)
+ *
+ * n comes from h before it is rounded to dtype.  The backward takes the forward's h (x where there was no y), the
+ * gradient dn of n and, or NULL for zero, dh of h (what flows back along the residual stream), and returns
+ *
+ *     dx = dh + layer-norm backward of dn      (the gradient of x, of y and of all of h)
+ *     dgamma = sum over rows of dn * (h - mean) / sqrt(...)          dbeta = sum over rows of dn
+ *
+ * The mean is taken first and the squares are those of h - mean, so rows that lie far from zero keep their
+ * accuracy; statistics are fp32.  dgamma and dbeta are summed in fp32 within a workgroup and in fp64 over the
+ * workgroups, without atomics, in an order that depends on the shape and the room for partial sums alone; k rows
+ * added up one after the other are off by at most k 2^-24 of the sum of their magnitudes, with k as for
+ * flce_block_norm.  Every output is rounded to dtype once.
+ *
+ *   size            must be sizeof(flce_layer_norm) (FLCE_ERR_ARG otherwise)
+ *   rows, H         1 .. 2^30 and 1 .. 2^24
+ *   dtype           of every matrix and vector
+ *   eps             finite, >= 0
+ *   ldx .. lddn     row strides in elements of the matrices of these names, 0 = H, else >= H.  Any stride and any
+ *                   pointer that fits its elements is taken; gamma, beta and a single row have none.
+ *   workspace       device buffer (256-byte aligned) for the backward's partial sums, or NULL for the device's
+ *                   shared workspace; workspace_bytes: flce_layer_norm_workspace_bytes of the same arguments, or
+ *                   less at the price of fewer workgroups (8 H bytes always do; FLCE_ERR_WORKSPACE if not even one
+ *                   serves).  A few rows need none (0 bytes), nor does the forward.  What the call uses of it
+ *                   shares no memory with the operands (FLCE_ERR_ARG).
+ *
+ * Forward: y, gamma and beta may be NULL; h goes with y.  Backward: dh, gamma (all ones) and outputs that are not
+ * wanted may be NULL, but not all of them; dgamma goes with gamma.  h may lie exactly on x and dx exactly on dh; no
+ * output may share other memory with an input or another output (FLCE_ERR_ARG).
+ */
+typedef struct {
+    size_t size;
+    int64_t rows, H;
+    int dtype;
+    float eps;
+    int64_t ldx, ldy, ldh, ldn, lddx, lddh, lddn;
+    void* workspace;
+    size_t workspace_bytes;
+} flce_layer_norm;
+FLCE_API int flce_layer_norm_fwd(const void* x, const void* y, const void* gamma, const void* beta,
+                        const flce_layer_norm* args, void* h, void* n, void* stream);
+FLCE_API int flce_layer_norm_bwd(const void* h, const void* dn, const void* dh, const void* gamma,
+                        const flce_layer_norm* args, void* dx, void* dgamma, void* dbeta, void* stream);
+FLCE_API size_t flce_layer_norm_workspace_bytes(const flce_layer_norm* args);
+
+/*
  * Global norm of gradients, and clipping by it: the step between the backward calls above (dW of
  * every head, dgammas, ...) and the optimizer's.  Over all elements of n_tensors dense tensors,
  * fp32 and bf16 mixed as they come:

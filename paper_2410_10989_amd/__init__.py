@@ -18,6 +18,7 @@ from .binding import (  # noqa: F401
     flce_block_norm_fwd, flce_block_norm_bwd, flce_block_norm_workspace_bytes, FlceBlockNorm, GATE_ACTS,
     flce_grad_norm, flce_grad_clip, flce_clip_grad_norm, flce_grad_norm_workspace_bytes,
     flce_embedding_fwd, flce_embedding_bwd, flce_embedding_workspace_bytes, FlceEmbedding,
+    flce_layer_norm_fwd, flce_layer_norm_bwd, flce_layer_norm_workspace_bytes, FlceLayerNorm,
     KERNEL_KINDS,
 )
 

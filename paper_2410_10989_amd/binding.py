@@ -55,6 +55,9 @@ def lib() -> ctypes.CDLL:
             "flce_grad_clip": ([p, p, p, p, ci, p, ctypes.c_float, p], ci),
             "flce_clip_grad_norm": ([p, p, p, p, ci, ci, ctypes.c_float, p, p, sz, p], ci),
             "flce_grad_norm_workspace_bytes": ([ci], sz),
+            "flce_layer_norm_fwd": ([p] * 8, ci),
+            "flce_layer_norm_bwd": ([p] * 9, ci),
+            "flce_layer_norm_workspace_bytes": ([p], sz),
             "flce_embedding_fwd": ([p] * 5, ci),
             "flce_embedding_bwd": ([p] * 5, ci),
             "flce_embedding_workspace_bytes": ([p], sz),
@@ -585,6 +588,97 @@ def flce_clip_grad_norm(grads, max_norm, norm_type=2.0, outs=None, norm=None, wo
                                        *_workspace_args(workspace, norm.device), _stream_handle(stream, norm.device))
     _check(st, "flce_clip_grad_norm")
     return norm
+
+
+class FlceLayerNorm(ctypes.Structure):
+    """flce_layer_norm of include/flce.h."""
+    _fields_ = [("size", ctypes.c_size_t), ("rows", ctypes.c_int64), ("H", ctypes.c_int64), ("dtype", ctypes.c_int),
+                ("eps", ctypes.c_float)] + \
+               [(ld, ctypes.c_int64) for ld in ("ldx", "ldy", "ldh", "ldn", "lddx", "lddh", "lddn")] + \
+               [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+_LAYER_NORM_BYTES = ctypes.sizeof(FlceLayerNorm)
+
+
+def flce_layer_norm_fwd(x, y=None, gamma=None, beta=None, eps=1e-5, h=None, n=None, stream=None):
+    """h = x + y and n = (h - mean) / sqrt(var + eps) * gamma + beta, row by row.
+
+    x, y [rows, H] (float32 or bfloat16; rows may be apart), gamma, beta [H] or None.  Returns (h, n), h None without
+    y; outputs are allocated when not passed, h may be x itself.
+    """
+    if not x.is_cuda:
+        raise ValueError("x must live on the GPU")
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError("expected [rows, H]")
+    code, vec, device = _dtype_code(x), shape[1:], x.device
+    dtype, index = x.dtype, device.index
+    if y is not None and h is None:
+        h = torch.empty_like(x)
+    if n is None:
+        n = torch.empty_like(x)
+    px, ldx = _rows_ptr(x, "x", x, shape, dtype, index)
+    py, ldy = _rows_ptr(y, "y", x, shape, dtype, index)
+    ph, ldh = _rows_ptr(h, "h", x, shape, dtype, index)
+    pn, ldn = _rows_ptr(n, "n", x, shape, dtype, index)
+    args = FlceLayerNorm(_LAYER_NORM_BYTES, shape[0], shape[1], code, eps, ldx, ldy, ldh, ldn)
+    with _OnDevice(device):
+        st = lib().flce_layer_norm_fwd(px, py, _rows_ptr(gamma, "gamma", x, vec, dtype, index)[0],
+                                       _rows_ptr(beta, "beta", x, vec, dtype, index)[0], ctypes.byref(args), ph, pn,
+                                       _stream_handle(stream, device))
+    _check(st, "flce_layer_norm_fwd")
+    return h, n
+
+
+def flce_layer_norm_bwd(h, dn, dh=None, gamma=None, bias=True, eps=1e-5, dx=None, dgamma=None, dbeta=None, flags=0,
+                        workspace=None, stream=None):
+    """Gradients of flce_layer_norm_fwd from its h (x where there was no y) and the gradients dn of n, dh of h (None =
+    zero).  bias: the forward had a beta.
+
+    Returns (dx, dgamma, dbeta), None for what there is not.  Outputs are allocated when not passed; dx may be dh
+    itself.  flags: SKIP_DX leaves dx out, SKIP_DW the gradients of gamma and beta.
+    """
+    if not h.is_cuda:
+        raise ValueError("h must live on the GPU")
+    if flags & ~(SKIP_DX | SKIP_DW):
+        raise ValueError("unknown flags")
+    shape = h.shape
+    if len(shape) != 2:
+        raise ValueError("expected [rows, H]")
+    code, vec, device = _dtype_code(h), shape[1:], h.device
+    dtype, index = h.dtype, device.index
+    want_dw = not flags & SKIP_DW
+    if (gamma is None and dgamma is not None) or (not bias and dbeta is not None):
+        raise ValueError("the gradient of an input that is not there")
+
+    def output(given, wanted, name, size):
+        if not wanted:
+            return None, None, 0
+        if given is None:
+            given = torch.empty(size, dtype=dtype, device=device) if len(size) == 1 else torch.empty_like(h)
+            return given, given.data_ptr(), 0
+        return given, *_rows_ptr(given, name, h, size, dtype, index)
+
+    dx, pdx, lddx = output(dx, not flags & SKIP_DX, "dx", shape)
+    dgamma, pdg, _ = output(dgamma, gamma is not None and want_dw, "dgamma", vec)
+    dbeta, pdb, _ = output(dbeta, bias and want_dw, "dbeta", vec)
+    ph, ldh = _rows_ptr(h, "h", h, shape, dtype, index)
+    pdn, lddn = _rows_ptr(dn, "dn", h, shape, dtype, index)
+    pdh, lddh = _rows_ptr(dh, "dh", h, shape, dtype, index)
+    args = FlceLayerNorm(_LAYER_NORM_BYTES, shape[0], shape[1], code, eps, 0, 0, ldh, 0, lddx, lddh, lddn,
+                         *_workspace_args(workspace, device))
+    with _OnDevice(device):
+        st = lib().flce_layer_norm_bwd(ph, pdn, pdh, _rows_ptr(gamma, "gamma", h, vec, dtype, index)[0], ctypes.byref(args),
+                                       pdx, pdg, pdb, _stream_handle(stream, device))
+    _check(st, "flce_layer_norm_bwd")
+    return dx, dgamma, dbeta
+
+
+def flce_layer_norm_workspace_bytes(rows, H, dtype) -> int:
+    """Bytes flce_layer_norm_bwd uses at most for this shape."""
+    b = FlceLayerNorm(size=_LAYER_NORM_BYTES, rows=rows, H=H, dtype=_DTYPES.get(dtype, dtype))
+    return int(lib().flce_layer_norm_workspace_bytes(ctypes.byref(b)))
 
 
 class FlceEmbedding(ctypes.Structure):

@@ -1,0 +1,393 @@
+// Layer norm with the residual sum in front of it.  Row i, in fp32 on values widened from the storage type:
+//
+//     h = x + y  (or x)      m = mean h,  d = h - m,  r = 1 / sqrt(mean d^2 + eps)      n = d r gamma + beta
+//
+// and backward, from the stored h alone (m and r are computed again):
+//
+//     u = dn gamma      dx = dh + r (u - mean u - d r mean(u d r))      dgamma = sum_i dn d r      dbeta = sum_i dn
+//
+// The mean is taken first and the squares are those of d: their sum does not cancel, however far a row lies from
+// zero.  A row lies in the registers of a group of TPR threads (see block_norm.h), so the second pass over it reads
+// nothing; what it costs is a second exchange between the threads, in which the backward takes its other sums along.
+//
+// Bound by HBM.
+#pragma once
+#include "rowsums.h"
+#include "rowvec.h"
+
+namespace flce {
+
+struct LnArgs {
+    const void *x, *y, *gamma, *beta;      // forward
+    void *out_h, *out_n;
+    const void *h, *dn, *dh;               // backward
+    void* dx;
+    float *part_gamma, *part_beta;         // fp32 sums, a row per workgroup, or null
+    void *dgamma, *dbeta;                  // one workgroup has all rows: written at once
+    int64_t ldx, ldy, ldh, ldn, lddx, lddh, lddn;
+    int rows, H;
+    float eps;
+};
+
+constexpr int LN_LONG_THREADS = 1024;
+
+// Elements of vector v that belong to the row.
+template <typename T>
+__device__ __forceinline__ int ln_live(int v, int nfull, int rem) {
+    return v < nfull ? RowVec<T>::N : v == nfull ? rem : 0;
+}
+
+// The last vectors of a group may be partial or not there: what they hold is zero, and d of it is set to zero.
+template <typename T, int TPR, int NV, bool NT>
+__global__ __launch_bounds__(row_block<TPR>) void layer_norm_fwd_kernel(LnArgs a) {
+    constexpr int N = RowVec<T>::N, GROUPS = row_groups<TPR>;
+    __shared__ float red[2][TPR > WAVE ? TPR / WAVE : 1];
+    const int grp = row_group<TPR>(), t = threadIdx.x % TPR;
+    const float inv_H = 1.0f / (float)a.H;
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * GROUPS + grp;
+    const bool live = row < a.rows;   // (a group past the last row takes part in the barriers)
+    const int nfull = live ? a.H / N : 0, rem = live ? a.H % N : 0;
+    const int64_t at = live ? row : 0;
+    u32x4 xv[NV], yv[NV], gv[NV], bv[NV];
+    auto load = [&](u32x4 (&to)[NV], const void* m, int64_t offset) {
+        const T* p = static_cast<const T*>(m) + offset;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) to[k] = row_load(p, t + k * TPR, nfull, rem);
+    };
+    load(xv, a.x, at * a.ldx);
+    if (a.y) load(yv, a.y, at * a.ldy);
+    if (a.gamma) load(gv, a.gamma, 0);
+    if (a.beta) load(bv, a.beta, 0);
+    float f[NV][N];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        RowVec<T>::unpack(xv[k], f[k]);
+        if (a.y) {
+            float w[N];
+            RowVec<T>::unpack(yv[k], w);
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[k][e] += w[e];
+        }
+    }
+    if (a.out_h) {
+        T* p = static_cast<T*>(a.out_h) + at * a.ldh;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) row_store<T, NT>(p, t + k * TPR, nfull, rem, f[k]);
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) s += f[k][e];
+    const float mean = row_sum<TPR>(s, red[0]) / (float)a.H;   // (rows of equal elements have d = 0)
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int n = ln_live<T>(t + k * TPR, nfull, rem);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            f[k][e] = e < n ? f[k][e] - mean : 0.f;
+            s = fmaf(f[k][e], f[k][e], s);
+        }
+    }
+    const float r = rsqrtf(row_sum<TPR>(s, red[1]) * inv_H + a.eps);
+    T* p = static_cast<T*>(a.out_n) + at * a.ldn;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        float g[N], b[N];
+        if (a.gamma) RowVec<T>::unpack(gv[k], g);
+        if (a.beta) RowVec<T>::unpack(bv[k], b);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            f[k][e] *= r;
+            if (a.gamma) f[k][e] *= g[e];
+            if (a.beta) f[k][e] += b[e];
+        }
+        row_store<T, NT>(p, t + k * TPR, nfull, rem, f[k]);
+    }
+}
+
+// Sum over a workgroup of LN_LONG_THREADS; the barrier in front frees the LDS of the sum before.
+template <int K>
+__device__ __forceinline__ void ln_long_sums(float (&v)[K], float* red) {
+    __syncthreads();
+    row_sums<LN_LONG_THREADS, K>(v, red);
+}
+
+// Rows beyond the register forms: a workgroup per row, swept three times; the last sweep alone writes, and a thread
+// writes only where it has read.
+template <typename T, bool NT>
+__global__ __launch_bounds__(LN_LONG_THREADS) void layer_norm_fwd_long(LnArgs a) {
+    constexpr int N = RowVec<T>::N;
+    __shared__ float red[LN_LONG_THREADS / WAVE];
+    const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (row >= a.rows) return;
+    const int nfull = a.H / N, rem = a.H % N, nvec = nfull + (rem ? 1 : 0);
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* y = a.y ? static_cast<const T*>(a.y) + row * a.ldy : nullptr;
+    auto sum_at = [&](int v, float (&f)[N]) {
+        RowVec<T>::unpack(row_load(x, v, nfull, rem), f);
+        if (y) {
+            float w[N];
+            RowVec<T>::unpack(row_load(y, v, nfull, rem), w);
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[e] += w[e];
+        }
+    };
+    float s[1] = {0.f};
+    for (int v = threadIdx.x; v < nvec; v += LN_LONG_THREADS) {
+        float f[N];
+        sum_at(v, f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[0] += f[e];
+    }
+    ln_long_sums(s, red);
+    const float mean = s[0] / (float)a.H;
+    s[0] = 0.f;
+    for (int v = threadIdx.x; v < nvec; v += LN_LONG_THREADS) {
+        float f[N];
+        sum_at(v, f);
+        const int n = ln_live<T>(v, nfull, rem);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float d = e < n ? f[e] - mean : 0.f;
+            s[0] = fmaf(d, d, s[0]);
+        }
+    }
+    ln_long_sums(s, red);
+    const float r = 1.0f / sqrtf(s[0] / (float)a.H + a.eps);
+    for (int v = threadIdx.x; v < nvec; v += LN_LONG_THREADS) {
+        float f[N], w[N];
+        sum_at(v, f);
+        if (a.out_h) row_store<T, NT>(static_cast<T*>(a.out_h) + row * a.ldh, v, nfull, rem, f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = (f[e] - mean) * r;
+        if (a.gamma) {
+            RowVec<T>::unpack(row_load(static_cast<const T*>(a.gamma), v, nfull, rem), w);
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[e] *= w[e];
+        }
+        if (a.beta) {
+            RowVec<T>::unpack(row_load(static_cast<const T*>(a.beta), v, nfull, rem), w);
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[e] += w[e];
+        }
+        row_store<T, NT>(static_cast<T*>(a.out_n) + row * a.ldn, v, nfull, rem, f);
+    }
+}
+
+// Backward: workgroup b takes rows b * GROUPS, (b + gridDim.x) * GROUPS, ...: all workgroups read neighbouring rows at
+// a time.  The sums over rows stay in registers until the workgroup's last row and are left as one row of fp32
+// partial sums (sum_partials_kernel adds them up in fp64): no atomics, the order depends on the shape and the number
+// of workgroups alone.  AHEAD: the next row's loads are issued before a row is worked on.
+template <typename T, int TPR, int NV, bool AHEAD, bool NT>
+__global__ __launch_bounds__(row_block<TPR>) void layer_norm_bwd_kernel(LnArgs a) {
+    constexpr int N = RowVec<T>::N, BLOCK = row_block<TPR>, GROUPS = row_groups<TPR>, NW = TPR > WAVE ? TPR / WAVE : 1;
+    __shared__ float red[2][2][3 * NW];
+    __shared__ __align__(16) float cols[GROUPS > 1 ? BLOCK * NV * N : 4];
+    const int grp = row_group<TPR>(), t = threadIdx.x % TPR;
+    const int nfull = a.H / N, rem = a.H % N, nvec = nfull + (rem ? 1 : 0);
+    const float inv_H = 1.0f / (float)a.H;
+    u32x4 gv[NV];
+    if (a.gamma)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) gv[k] = row_load(static_cast<const T*>(a.gamma), t + k * TPR, nfull, rem);
+    float acc_gamma[NV][N], acc_beta[NV][N];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc_gamma[k][e] = acc_beta[k][e] = 0.f;
+
+    struct Row {
+        u32x4 h[NV], dn[NV], dh[NV];
+    };
+    auto load_row = [&](Row& r, int64_t base) {
+        const bool live = base + grp < a.rows;   // (a group past the last row loads nothing)
+        const int64_t row = live ? base + grp : base;
+        auto load = [&](u32x4 (&to)[NV], const void* m, int64_t ld) {
+            const T* p = static_cast<const T*>(m) + row * ld;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) to[k] = row_load_ahead(p, t + k * TPR, live ? nvec : 0, a.H);
+        };
+        load(r.h, a.h, a.ldh);
+        load(r.dn, a.dn, a.lddn);
+        if (a.dh) load(r.dh, a.dh, a.lddh);
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t base = (int64_t)blockIdx.x * GROUPS;
+    Row next;
+    if (AHEAD && base < a.rows) load_row(next, base);
+    for (int turn = 0; base < a.rows; base += step, turn ^= 1) {
+        if (GROUPS > 1 && base + grp >= a.rows) break;   // (at most a wavefront: no barrier in here is meant for it)
+        Row in;
+        if constexpr (AHEAD) {
+            in = next;
+            if (base + step < a.rows) load_row(next, base + step);
+        } else {
+            load_row(in, base);
+        }
+        if (rem) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (t + k * TPR == nfull) {
+                    row_shift_tail<T>(in.h[k], rem);
+                    row_shift_tail<T>(in.dn[k], rem);
+                    if (a.dh) row_shift_tail<T>(in.dh[k], rem);
+                }
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float h[N];
+            RowVec<T>::unpack(in.h[k], h);
+#pragma unroll
+            for (int e = 0; e < N; ++e) s += h[e];
+        }
+        const float mean = row_sum<TPR>(s, red[turn][0]) / (float)a.H;
+        // sum d^2, sum u, sum u d in one exchange
+        float sums[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float h[N], u[N], g[N];
+            RowVec<T>::unpack(in.h[k], h);
+            RowVec<T>::unpack(in.dn[k], u);
+            if (a.gamma) RowVec<T>::unpack(gv[k], g);
+            const int n = ln_live<T>(t + k * TPR, nfull, rem);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float d = e < n ? h[e] - mean : 0.f;
+                if (a.gamma) u[e] *= g[e];
+                sums[0] = fmaf(d, d, sums[0]);
+                sums[1] += u[e];
+                sums[2] = fmaf(u[e], d, sums[2]);
+            }
+        }
+        row_sums<TPR, 3>(sums, red[turn][1]);
+        const float r = rsqrtf(sums[0] * inv_H + a.eps), mu = sums[1] * inv_H, mx = sums[2] * r * inv_H;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float h[N], dn[N], g[N], D[N];
+            RowVec<T>::unpack(in.h[k], h);
+            RowVec<T>::unpack(in.dn[k], dn);
+            if (a.gamma) RowVec<T>::unpack(gv[k], g);
+            if (a.dh) RowVec<T>::unpack(in.dh[k], D);
+            const int n = ln_live<T>(t + k * TPR, nfull, rem);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float xh = e < n ? (h[e] - mean) * r : 0.f;
+                const float u = a.gamma ? dn[e] * g[e] : dn[e];
+                acc_gamma[k][e] = fmaf(dn[e], xh, acc_gamma[k][e]);
+                acc_beta[k][e] += dn[e];
+                const float v = r * (u - mu - xh * mx);
+                D[e] = a.dh ? D[e] + v : v;
+            }
+            if (a.dx) row_store<T, NT>(static_cast<T*>(a.dx) + (base + grp) * a.lddx, t + k * TPR, nfull, rem, D);
+        }
+    }
+
+    // The workgroup's row of sums (over its groups, in order), rounded to `out` or as it is to `part`.
+    auto put_sums = [&](float (&acc)[NV][N], T* out, float* part) {
+        if constexpr (GROUPS > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < N; e += 4)
+                    *reinterpret_cast<f32x4*>(&cols[grp * (TPR * NV * N) + (t + k * TPR) * N + e]) =
+                        f32x4{acc[k][e], acc[k][e + 1], acc[k][e + 2], acc[k][e + 3]};
+            __syncthreads();
+            for (int j = threadIdx.x; j < TPR * NV * N && j < a.H; j += BLOCK) {
+                float s = cols[j];
+                for (int q = 1; q < GROUPS; ++q) s += cols[q * (TPR * NV * N) + j];
+                if (out) out[j] = from_f32<T>(s); else part[j] = s;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int at = t + k * TPR;
+                if (out) {
+                    row_store<T, false>(out, at, nfull, rem, acc[k]);
+                } else if (at < nfull) {
+#pragma unroll
+                    for (int e = 0; e < N; e += 4)
+                        *reinterpret_cast<f32x4_any*>(part + at * N + e) = f32x4{acc[k][e], acc[k][e + 1], acc[k][e + 2], acc[k][e + 3]};
+                } else if (at == nfull) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (e < rem) part[at * N + e] = acc[k][e];
+                }
+            }
+        }
+    };
+    if (a.dgamma) put_sums(acc_gamma, static_cast<T*>(a.dgamma), nullptr);
+    else if (a.part_gamma) put_sums(acc_gamma, nullptr, a.part_gamma + (int64_t)blockIdx.x * a.H);
+    if (a.dbeta) put_sums(acc_beta, static_cast<T*>(a.dbeta), nullptr);
+    else if (a.part_beta) put_sums(acc_beta, nullptr, a.part_beta + (int64_t)blockIdx.x * a.H);
+}
+
+// Rows beyond the register forms, and rows of less than a vector.  The sums over rows live in the partial sums'
+// memory; a column always belongs to the same thread.
+template <typename T, bool NT>
+__global__ __launch_bounds__(LN_LONG_THREADS) void layer_norm_bwd_long(LnArgs a) {
+    constexpr int N = RowVec<T>::N;
+    __shared__ float red[3 * LN_LONG_THREADS / WAVE];
+    const int nfull = a.H / N, rem = a.H % N, nvec = nfull + (rem ? 1 : 0);
+    float* pg = a.part_gamma ? a.part_gamma + (int64_t)blockIdx.x * a.H : nullptr;
+    float* pb = a.part_beta ? a.part_beta + (int64_t)blockIdx.x * a.H : nullptr;
+    const T* gamma = static_cast<const T*>(a.gamma);
+    bool first = true;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, first = false) {
+        const T* h = static_cast<const T*>(a.h) + row * a.ldh;
+        const T* dn = static_cast<const T*>(a.dn) + row * a.lddn;
+        float s[1] = {0.f};
+        for (int v = threadIdx.x; v < nvec; v += LN_LONG_THREADS) {
+            float f[N];
+            RowVec<T>::unpack(row_load(h, v, nfull, rem), f);
+#pragma unroll
+            for (int e = 0; e < N; ++e) s[0] += f[e];
+        }
+        ln_long_sums(s, red);
+        const float mean = s[0] / (float)a.H;
+        float sums[3] = {0.f, 0.f, 0.f};
+        auto centered = [&](int v, float (&d)[N], float (&u)[N], float (&g)[N]) {   // h - mean, dn, gamma
+            RowVec<T>::unpack(row_load(h, v, nfull, rem), d);
+            RowVec<T>::unpack(row_load(dn, v, nfull, rem), u);
+            if (gamma) RowVec<T>::unpack(row_load(gamma, v, nfull, rem), g);
+            const int n = ln_live<T>(v, nfull, rem);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                d[e] = e < n ? d[e] - mean : 0.f;
+                if (!gamma) g[e] = 1.0f;
+            }
+        };
+        for (int v = threadIdx.x; v < nvec; v += LN_LONG_THREADS) {
+            float d[N], u[N], g[N];
+            centered(v, d, u, g);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                sums[0] = fmaf(d[e], d[e], sums[0]);
+                sums[1] = fmaf(u[e], g[e], sums[1]);
+                sums[2] = fmaf(u[e] * g[e], d[e], sums[2]);
+            }
+        }
+        ln_long_sums(sums, red);
+        const float r = 1.0f / sqrtf(sums[0] / (float)a.H + a.eps), mu = sums[1] / (float)a.H, mx = sums[2] * r / (float)a.H;
+        for (int v = threadIdx.x; v < nvec; v += LN_LONG_THREADS) {
+            float d[N], u[N], g[N], D[N];
+            centered(v, d, u, g);
+            if (a.dh) RowVec<T>::unpack(row_load(static_cast<const T*>(a.dh) + row * a.lddh, v, nfull, rem), D);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float xh = d[e] * r, w = r * (u[e] * g[e] - mu - xh * mx);
+                D[e] = a.dh ? D[e] + w : w;
+                if (v * N + e < a.H) {
+                    if (pg) pg[v * N + e] = first ? u[e] * xh : fmaf(u[e], xh, pg[v * N + e]);
+                    if (pb) pb[v * N + e] = first ? u[e] : u[e] + pb[v * N + e];
+                }
+            }
+            if (a.dx) row_store<T, NT>(static_cast<T*>(a.dx) + row * a.lddx, v, nfull, rem, D);
+        }
+    }
+}
+
+}  // namespace flce

@@ -9,40 +9,13 @@ import numpy as np
 import pytest
 import torch
 
+from matrices import DT, Matrix, half, rounded
 from oracle import step_oracle as oracle
 
 pytestmark = pytest.mark.gpu
 
-DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 IGNORE = -100
 TINY = 2.0 ** -126
-MARK = 77.0
-
-
-def half(dtype):
-    return torch.finfo(DT[dtype]).eps / 2
-
-
-class Matrix:
-    """A [rows, H] matrix inside a wider buffer whose rest is filled with a mark."""
-
-    def __init__(self, rows, H, dtype, pad=0, front=0, data=None):
-        self.buf = torch.full((front + rows * (H + pad) + 3,), MARK, dtype=DT[dtype], device="cuda")
-        self.view = self.buf[front:front + rows * (H + pad)].view(rows, H + pad)[:, :H]
-        if data is None:
-            self.view.fill_(float("nan"))   # outputs must be overwritten
-        else:
-            self.view.copy_(torch.from_numpy(data))
-
-    def assert_around_untouched(self):
-        inside = self.view.clone()
-        self.view.fill_(MARK)
-        assert (self.buf == MARK).all(), "written outside the rows"
-        self.view.copy_(inside)
-
-
-def rounded(a, dtype):
-    return torch.from_numpy(a).to(DT[dtype]).double().numpy()
 
 
 def make_tokens(g, rows, V, kind):

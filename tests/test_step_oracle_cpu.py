@@ -92,3 +92,92 @@ def test_embedding_binding_refusals():
         flce.flce_embedding_fwd(t.half(), torch.zeros(3, dtype=torch.int64))
     with pytest.raises(ValueError):
         flce.flce_embedding_bwd(t, torch.zeros(4, dtype=torch.int64), 9)
+
+
+# ---- layer norm ----
+
+@pytest.mark.parametrize("y,gamma,beta,dh", [(True, True, True, True), (False, True, False, True), (True, False, True, False),
+                                             (False, False, False, False)])
+def test_layer_norm_gradient_is_the_derivative_of_the_forward(y, gamma, beta, dh):
+    g = rng(3, 4)
+    x, dn = g.standard_normal((4, 7)) + 2, g.standard_normal((4, 7))
+    y = g.standard_normal((4, 7)) if y else None
+    gamma, beta = g.standard_normal(7) if gamma else None, g.standard_normal(7) if beta else None
+    dh = g.standard_normal((4, 7)) if dh else None
+    f = oracle.layer_norm(x, y, gamma, beta, 1e-3)
+    leaf = lambda a: None if a is None else torch.from_numpy(a).requires_grad_()
+    X, G, B = leaf(x), leaf(gamma), leaf(beta)
+    h = X if y is None else X + torch.from_numpy(y)
+    n = torch.nn.functional.layer_norm(h, (7,), G, B, 1e-3)
+    np.testing.assert_allclose(f["n"], n.detach().numpy(), rtol=1e-12, atol=1e-13)
+    np.testing.assert_allclose(f["h"], h.detach().numpy())
+    loss = (n * torch.from_numpy(dn)).sum() + (0 if dh is None else (h * torch.from_numpy(dh)).sum())
+    loss.backward()
+    b = oracle.layer_norm_grad(f["h"], dn, dh, gamma, 1e-3)
+    np.testing.assert_allclose(b["dx"], X.grad.numpy(), rtol=1e-10, atol=1e-12)
+    if gamma is not None:
+        np.testing.assert_allclose(b["dgamma"], G.grad.numpy(), rtol=1e-11, atol=1e-12)
+    if beta is not None:
+        np.testing.assert_allclose(b["dbeta"], B.grad.numpy(), rtol=1e-11, atol=1e-12)
+    assert all((b[k + "_mag"] >= np.abs(b[k]) - 1e-12).all() for k in ("dx", "dgamma", "dbeta"))
+
+
+def layer_norm_args(**kw):
+    d = dict(size=ctypes.sizeof(flce.FlceLayerNorm), rows=6, H=8, dtype=flce.FLCE_F32, eps=1e-5)
+    d.update(kw)
+    return flce.FlceLayerNorm(**d)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(size=8), 7), (dict(rows=0), 2), (dict(rows=(1 << 30) + 1), 2), (dict(H=0), 2), (dict(H=(1 << 24) + 1), 2), (dict(dtype=5), 3),
+    (dict(eps=-1.0), 7), (dict(eps=float("nan")), 7), (dict(eps=float("inf")), 7), (dict(ldx=7), 2), (dict(ldn=-8), 2), (dict(lddx=3), 2)])
+def test_layer_norm_refuses_bad_arguments(kw, status):
+    a, L = layer_norm_args(**kw), flce.lib()
+    assert L.flce_layer_norm_fwd(A, None, None, None, ctypes.byref(a), None, 2 * A, None) == status
+    assert L.flce_layer_norm_bwd(A, 2 * A, None, None, ctypes.byref(a), 3 * A, None, None, None) == status
+    assert flce.lib().flce_layer_norm_workspace_bytes(ctypes.byref(a)) == 0
+
+
+def test_layer_norm_refuses_bad_pointers():
+    L, a = flce.lib(), ctypes.byref(layer_norm_args())
+    row = 6 * 8 * 4
+
+    def fwd(x=A, y=2 * A, gamma=3 * A, beta=4 * A, h=5 * A, n=6 * A, args=a):
+        return L.flce_layer_norm_fwd(x, y, gamma, beta, args, h, n, None)
+
+    assert fwd(args=None) == 1 and fwd(x=None) == 1 and fwd(n=None) == 1 and fwd(h=None) == 1
+    assert fwd(y=None) == 7                                       # h without y
+    for k in ("x", "y", "gamma", "beta", "h", "n"):
+        assert fwd(**{k: 7 * A + 2}) == 4
+    assert fwd(h=6 * A) == 7 and fwd(h=6 * A + row - 4) == 7      # h and n
+    assert fwd(n=A) == 7 and fwd(n=2 * A) == 7 and fwd(n=3 * A - row + 4) == 7 and fwd(n=4 * A) == 7
+    assert fwd(h=A + 4) == 7 and fwd(h=2 * A) == 7 and fwd(h=3 * A) == 7
+
+    def bwd(h=A, dn=2 * A, dh=3 * A, gamma=4 * A, dx=5 * A, dgamma=6 * A, dbeta=7 * A, args=a):
+        return L.flce_layer_norm_bwd(h, dn, dh, gamma, args, dx, dgamma, dbeta, None)
+
+    assert bwd(args=None) == 1 and bwd(h=None) == 1 and bwd(dn=None) == 1
+    assert bwd(gamma=None) == 7 and bwd(dx=None, dgamma=None, dbeta=None) == 7
+    for k in ("h", "dn", "dh", "gamma", "dx", "dgamma", "dbeta"):
+        assert bwd(**{k: 8 * A + 1}) == 4
+    for at in (A, 2 * A, 4 * A, 6 * A, 7 * A, 3 * A + 4, 3 * A - 4):
+        assert bwd(dx=at) == 7
+    for at in (A, 2 * A, 3 * A, 4 * A, 7 * A):
+        assert bwd(dgamma=at) == 7
+    # a workspace that lies on an operand, is too small, misaligned
+    big = dict(rows=4000, H=8)
+    need = flce.flce_layer_norm_workspace_bytes(4000, 8, torch.float32)
+    assert need > 0
+    for at in (A, 2 * A, 3 * A, 4 * A, 5 * A, 6 * A, 7 * A):
+        assert bwd(args=ctypes.byref(layer_norm_args(workspace=at, workspace_bytes=need, **big))) == 7
+    assert bwd(args=ctypes.byref(layer_norm_args(workspace=9 * A + 4, workspace_bytes=need, **big))) == 4
+    long = dict(rows=6, H=20000)
+    assert bwd(args=ctypes.byref(layer_norm_args(workspace=9 * A, workspace_bytes=8 * 20000 - 4, **long))) == 5
+
+
+def test_layer_norm_binding_refusals():
+    t = torch.zeros(4, 8)
+    with pytest.raises(ValueError):
+        flce.flce_layer_norm_fwd(t)
+    with pytest.raises(ValueError):
+        flce.flce_layer_norm_bwd(t, t)
