@@ -417,6 +417,58 @@ FLCE_API int flce_clip_grad_norm(const void* const* grads, void* const* outs, co
 FLCE_API size_t flce_grad_norm_workspace_bytes(int n_tensors);
 
 /*
+ * Orthogonalising updates, as the Muon optimizer does: the step between the clipped gradients (or their momentum)
+ * and the weights for matrices.  For each of n_matrices matrices G of the same shape, with (a, b, c) the step's
+ * coefficients,
+ *
+ *     X = G / (|G|_F + eps)                          (its transpose where rows > cols)
+ *     X <- a X + (b A + c A A) X,  A = X X^T         `steps` times
+ *     out = scale * X                                (transposed back)
+ *
+ * which keeps the singular vectors and drives the singular values towards 1.
+ *
+ * Products are taken in the matrix cores on fp16 operands scaled by powers of two, accumulated in fp32, the X that is
+ * carried over in 22 bits.  bf16 matrices: operands of 11 bits; what the result is off by, relative to
+ * its norm, is about 1e-3 (its rounding to bf16: 1.7e-3).  fp32 matrices: operands of 22 bits, three products for
+ * one, about 5e-7 (fp32 arithmetic: 2e-6).  Both are for the usual coefficients; small singular values and the
+ * errors in their directions grow by a factor a per step.  The norm is summed in fp64.  No atomics: the same call
+ * gives the same bits.  A matrix that holds infinities or NaN gives NaN, and leaves the others of the list alone;
+ * zeros give zeros.
+ *
+ *   in, out       HOST arrays of n_matrices DEVICE pointers to dense row-major rows x cols matrices, aligned to
+ *                 their elements; read before the call returns.  out == NULL, or out[i] == in[i]: in place.  No
+ *                 two outs may share memory, nor an out and an in other than its own (FLCE_ERR_ARG).
+ *   n_matrices    >= 0
+ *   size          must be sizeof(flce_orthogonalize_args) (FLCE_ERR_ARG otherwise)
+ *   rows, cols    1 .. 2^20, their product, each rounded up to 64, at most 2^28
+ *   dtype         of all matrices
+ *   steps         1 .. 32
+ *   coefficients  HOST array of 3 floats for all steps (per_step = 0) or 3 * steps (per_step = 1), or NULL: 3.4445,
+ *                 -4.7750, 2.0315.  Finite, and such that no singular value in [0, 1] can exceed 1024 on the
+ *                 way (FLCE_ERR_ARG).
+ *   scale, eps    finite, eps >= 0
+ *   workspace     device buffer (256-byte aligned), or NULL for the device's shared workspace; workspace_bytes:
+ *                 flce_orthogonalize_workspace_bytes of the same arguments, or less (what one matrix takes at the
+ *                 least, FLCE_ERR_WORKSPACE otherwise) at the price of fewer matrices at a time.  What the call uses
+ *                 of it shares no memory with the matrices (FLCE_ERR_ARG).
+ * The matrices of a list share their launches (up to 120 of them), which small ones need to fill the chip.
+ */
+typedef struct {
+    size_t size;
+    int64_t rows, cols;
+    int dtype;
+    int steps;
+    const float* coefficients;
+    int per_step;
+    float scale, eps;
+    void* workspace;
+    size_t workspace_bytes;
+} flce_orthogonalize_args;
+FLCE_API int flce_orthogonalize(const void* const* in, void* const* out, int n_matrices,
+                       const flce_orthogonalize_args* args, void* stream);
+FLCE_API size_t flce_orthogonalize_workspace_bytes(int n_matrices, const flce_orthogonalize_args* args);
+
+/*
  * The other end of the model: embedding lookup with scaling, and the gradient of its table.  With
  * v_i = tokens[i] - first_token, and live rows those with 0 <= v_i < V and tokens[i] != ignore_index,
  *

@@ -73,3 +73,32 @@ def orthogonalize(G, steps=5, coefficients=COEFFICIENTS, scale=1.0, eps=1e-7):
         X = a * X + (b * A + q * (A @ A)) @ X
     X = X.T if tall else X
     return scale * X
+
+
+def orthogonalize_rounded(G, planes, steps=5, coefficients=COEFFICIENTS, scale=1.0, eps=1e-7):
+    """The same with the roundings of a computation on fp16 operands, for the size of the error they make: X in two fp16
+    planes, A and B in `planes`, products of the first planes (planes = 1) or hi hi + hi lo + lo hi (2), sums in
+    fp32.  Scaled by 2^13, which keeps what is rounded in the type's normal range."""
+    S = 2.0 ** 13
+    c = np.broadcast_to(np.asarray(coefficients, dtype=np.float64), (steps, 3))
+
+    def split(v):
+        hi = (v.astype(np.float32) * np.float32(S)).astype(np.float16)
+        lo = (v.astype(np.float32) * np.float32(S) - hi.astype(np.float32)).astype(np.float16)
+        return hi.astype(np.float32) / np.float32(S), lo.astype(np.float32) / np.float32(S)
+
+    def product(p, q):
+        r = p[0] @ q[0]
+        return r if planes == 1 else r + (p[0] @ q[1] + p[1] @ q[0])
+
+    X = G / (np.sqrt((G * G).sum()) + eps)
+    tall = X.shape[0] > X.shape[1]
+    X = split(X.T if tall else X)
+    for a, b, q in c.astype(np.float32):
+        A = split(product(X, (X[0].T, X[1].T)))
+        A = A if planes == 2 else (A[0], np.zeros_like(A[1]))
+        B = split(b * (A[0] + A[1]) + q * product(A, A))
+        X = a * (X[0] + X[1]) + product(B, X)
+        last, X = X, split(X)
+    last = last.T if tall else last
+    return scale * last.astype(np.float64)

@@ -19,6 +19,7 @@ from .binding import (  # noqa: F401
     flce_grad_norm, flce_grad_clip, flce_clip_grad_norm, flce_grad_norm_workspace_bytes,
     flce_embedding_fwd, flce_embedding_bwd, flce_embedding_workspace_bytes, FlceEmbedding,
     flce_layer_norm_fwd, flce_layer_norm_bwd, flce_layer_norm_workspace_bytes, FlceLayerNorm,
+    flce_orthogonalize, flce_orthogonalize_workspace_bytes, FlceOrthogonalizeArgs,
     KERNEL_KINDS,
 )
 

@@ -58,6 +58,8 @@ def lib() -> ctypes.CDLL:
             "flce_layer_norm_fwd": ([p] * 8, ci),
             "flce_layer_norm_bwd": ([p] * 9, ci),
             "flce_layer_norm_workspace_bytes": ([p], sz),
+            "flce_orthogonalize": ([p, p, ci, p, p], ci),
+            "flce_orthogonalize_workspace_bytes": ([ci, p], sz),
             "flce_embedding_fwd": ([p] * 5, ci),
             "flce_embedding_bwd": ([p] * 5, ci),
             "flce_embedding_workspace_bytes": ([p], sz),
@@ -679,6 +681,59 @@ def flce_layer_norm_workspace_bytes(rows, H, dtype) -> int:
     """Bytes flce_layer_norm_bwd uses at most for this shape."""
     b = FlceLayerNorm(size=_LAYER_NORM_BYTES, rows=rows, H=H, dtype=_DTYPES.get(dtype, dtype))
     return int(lib().flce_layer_norm_workspace_bytes(ctypes.byref(b)))
+
+
+class FlceOrthogonalizeArgs(ctypes.Structure):
+    """flce_orthogonalize_args of include/flce.h."""
+    _fields_ = [("size", ctypes.c_size_t), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("dtype", ctypes.c_int),
+                ("steps", ctypes.c_int), ("coefficients", ctypes.c_void_p), ("per_step", ctypes.c_int),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+def _orthogonalize_args(rows, cols, code, steps, coefficients, scale, eps) -> FlceOrthogonalizeArgs:
+    args = FlceOrthogonalizeArgs(ctypes.sizeof(FlceOrthogonalizeArgs), rows, cols, code, steps, None, 0, scale, eps)
+    if coefficients is not None:
+        triples = list(coefficients)
+        args.per_step = 0 if not hasattr(triples[0], "__len__") else 1
+        flat = [float(x) for t in triples for x in t] if args.per_step else [float(x) for x in triples]
+        if len(flat) != 3 * (steps if args.per_step else 1):
+            raise ValueError("coefficients must be three numbers, or three for each step")
+        args._coefficients = (ctypes.c_float * len(flat))(*flat)   # (kept alive by the struct)
+        args.coefficients = ctypes.addressof(args._coefficients)
+    return args
+
+
+def flce_orthogonalize(updates, outs=None, steps=5, coefficients=None, scale=1.0, eps=1e-7, workspace=None, stream=None):
+    """scale * (each matrix of the list with its singular values driven towards 1 by `steps` Newton-Schulz steps).
+
+    updates: dense [rows, cols] tensors of one shape and dtype (float32 or bfloat16) on one GPU; outs: as many, or
+    None for in place.  coefficients: (a, b, c), a triple for each step, or None for (3.4445, -4.7750, 2.0315).
+    Returns outs.
+    """
+    updates = list(updates)
+    if not updates:
+        return []
+    first = updates[0]
+    if first.dim() != 2 or any(t.shape != first.shape or t.dtype != first.dtype for t in updates):
+        raise ValueError("updates must be matrices of one shape and dtype")
+    outs = updates if outs is None else list(outs)
+    if any(t.shape != first.shape for t in outs):
+        raise ValueError("outs must hold one tensor per update, of its size and dtype and on its GPU")
+    device, ptrs, counts, dtypes = _tensor_list(updates)
+    to = None if outs is updates else _out_list(outs, device, counts, dtypes)
+    args = _orthogonalize_args(first.shape[0], first.shape[1], _dtype_code(first), int(steps), coefficients, scale, eps)
+    args.workspace, args.workspace_bytes = _workspace_args(workspace, device)
+    with _OnDevice(device):
+        st = lib().flce_orthogonalize(_at(ptrs), _at(to), len(updates), ctypes.byref(args), _stream_handle(stream, device))
+    _check(st, "flce_orthogonalize")
+    return outs
+
+
+def flce_orthogonalize_workspace_bytes(n_matrices, rows, cols, dtype) -> int:
+    """Bytes flce_orthogonalize uses at most for a list of that many matrices."""
+    args = _orthogonalize_args(rows, cols, _DTYPES.get(dtype, dtype), 1, None, 1.0, 0.0)
+    return int(lib().flce_orthogonalize_workspace_bytes(int(n_matrices), ctypes.byref(args)))
 
 
 class FlceEmbedding(ctypes.Structure):

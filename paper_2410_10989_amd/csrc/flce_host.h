@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/flce.h"
 
 #define HIP_TRY(expr)                          \
@@ -54,6 +56,23 @@ inline bool overlap(const Span& a, const Span& b) {
     return off < a.width || a.pitch - off < b.width;
 }
 inline bool same(const Span& a, const Span& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1); }
+
+// Stretches of memory that a call reads or writes; whether one that is written shares a byte with any other.
+struct Piece {
+    uintptr_t begin, end;
+    bool write;
+};
+inline bool written_twice(Piece* pieces, size_t n) {
+    std::sort(pieces, pieces + n, [](const Piece& a, const Piece& b) { return a.begin < b.begin; });
+    uintptr_t any_end = 0, write_end = 0;   // of the pieces so far
+    bool found = false;
+    for (size_t i = 0; i < n; ++i) {
+        if (pieces[i].begin < (pieces[i].write ? any_end : write_end)) found = true;
+        any_end = std::max(any_end, pieces[i].end);
+        if (pieces[i].write) write_end = std::max(write_end, pieces[i].end);
+    }
+    return found;
+}
 
 // The current device's shared workspace (see Scratch memory in flce.h), at least `need` bytes of it, for a call on s.
 // last: the caller has no plan that needs less (without one, an allocation that found too little memory is not tried

@@ -50,10 +50,6 @@ int check_tensors(const Tensors& t) {
 
 // No two outputs may share memory, and an output may only lie on an input that is its own, exactly.
 int check_outputs(const Tensors& t) {
-    struct Piece {
-        uintptr_t begin, end;
-        bool write;
-    };
     Piece* pieces = new (std::nothrow) Piece[2 * (size_t)t.n + 1];
     if (!pieces) return FLCE_ERR_WORKSPACE;
     size_t k = 0;
@@ -64,14 +60,7 @@ int check_outputs(const Tensors& t) {
         pieces[k++] = {w, w + bytes_of(t, i), true};
         if (r != w) pieces[k++] = {r, r + bytes_of(t, i), false};
     }
-    std::sort(pieces, pieces + k, [](const Piece& a, const Piece& b) { return a.begin < b.begin; });
-    uintptr_t any_end = 0, write_end = 0;   // of the pieces so far
-    int rc = FLCE_OK;
-    for (size_t i = 0; i < k; ++i) {
-        if (pieces[i].begin < (pieces[i].write ? any_end : write_end)) rc = FLCE_ERR_ARG;
-        any_end = std::max(any_end, pieces[i].end);
-        if (pieces[i].write) write_end = std::max(write_end, pieces[i].end);
-    }
+    const int rc = written_twice(pieces, k) ? FLCE_ERR_ARG : FLCE_OK;
     delete[] pieces;
     return rc;
 }

@@ -1,0 +1,493 @@
+// Orthogonalising matrices by Newton-Schulz products.  For a matrix G of min(rows, cols) = m and max(rows, cols) = n
+// (transposed where it has more rows than columns)
+//
+//     X = G / (|G|_F + eps),      then per step    A = X X^T,   B = b A + c A A,   X <- a X + B X        out = s X
+//
+// drives every singular value of X towards 1 and keeps its singular vectors.  Per step 2 m^2 n + 2 m^3 + 2 m^2 n
+// operations; A and B are symmetric, so only the tiles on and below the diagonal are computed, the others mirrored.
+//
+// Numbers.  The iteration multiplies the smallest singular values by a^steps (485 for five of the usual steps), and any
+// error in their directions with them.  The operands of the products are fp16, scaled by powers of two that keep them
+// in range: 11 bits where bf16 has 8, at the same rate (relative error of the result 1.2e-3 instead of 1e-2 for a
+// matrix of noise).  X is held as the sum of two fp16 planes, hi and lo, 22 bits: what a X carries over is not rounded
+// to 11 bits (for a matrix of low rank and a little noise 2.4e-4; with X in one plane 2e-2, in bf16 0.14).  For
+// bf16 matrices the products take the hi planes alone; for fp32 matrices A and B have two planes as well and every
+// product is hi lo + lo hi + hi hi.  Sums are fp32 in the matrix cores, the norm fp64.  The cores cut a sum off where
+// it leaves fp32: each 16 terms added to a sum of S take up to 2^-23 S from it, always towards zero, so the small
+// products come first (16 x 4099: 7.2e-6 with hi hi first).
+#pragma once
+#include "mfma_tiles.h"
+#include "rowvec.h"
+
+namespace flce {
+
+typedef _Float16 f16_t;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int OR_MATRICES = 120;   // a launch's arguments stay below 4 KB
+constexpr int OR_PAD = 64;         // rows and columns are padded with zeros to whole K steps
+constexpr int OR_NORM_BLOCKS = 32; // workgroups that add up a matrix's squares
+
+enum { OR_GRAM = 0, OR_POLY = 1, OR_APPLY = 2, OR_LAST = 3 };   // A = X X^T, B = b A + c A A, X <- a X + B X, out = s X
+
+struct OrArgs {
+    const f16_t *X, *A, *B;      // planes, of the first matrix; X: rows of [hi np | lo np], A and B of [hi mp (| lo mp)]
+    f16_t* to;                   // the product's, unless OR_LAST
+    int64_t stride_x, stride_a;  // elements from one matrix to the next
+    int mp, np;                  // m and n, padded
+    int count;
+    int tiles_m, tiles_n, tiles;   // of a matrix
+    float alpha, beta;           // alpha * (the accumulated product) + beta * (A or X)
+    int rows, cols;              // OR_LAST: of out
+    void* out[OR_MATRICES];
+};
+struct OrLoadArgs {
+    const void* in[OR_MATRICES];
+    double* partial;             // OR_NORM_BLOCKS per matrix
+    f16_t* X;
+    int64_t stride_x;
+    int rows, cols, mp, np;
+    double scale, eps;           // of the first X
+};
+
+__device__ __forceinline__ f32x16 or_mfma(bf16x8 b, bf16x8 a, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+}
+
+// 8 values as two planes: hi, and what it leaves of them.
+__device__ __forceinline__ void or_split(const float (&v)[8], u32x4& hi, u32x4& lo) {
+    f16x8 h, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        h[e] = (f16_t)v[e];
+        l[e] = (f16_t)(v[e] - (float)h[e]);
+    }
+    hi = __builtin_bit_cast(u32x4, h);
+    lo = __builtin_bit_cast(u32x4, l);
+}
+
+// Squares of a matrix, in fp64; workgroup (p, matrix) adds up its share.
+template <typename T>
+__global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
+    constexpr int N = RowVec<T>::N;
+    __shared__ double red[4];
+    const T* in = static_cast<const T*>(a.in[blockIdx.y]);
+    const int64_t all = (int64_t)a.rows * a.cols;
+    const int nfull = (int)(all / N), rem = (int)(all % N), nvec = nfull + (rem ? 1 : 0);
+    const int v0 = (int)((int64_t)nvec * blockIdx.x / OR_NORM_BLOCKS), v1 = (int)((int64_t)nvec * (blockIdx.x + 1) / OR_NORM_BLOCKS);
+    double s = 0.0;
+    for (int v = v0 + (int)threadIdx.x; v < v1; v += 4 * 256) {
+        u32x4 raw[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) raw[k] = row_load(in, v + k * 256, min(nfull, v1), v1 > nfull ? rem : 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float f[N];
+            RowVec<T>::unpack(raw[k], f);
+#pragma unroll
+            for (int e = 0; e < N; ++e) s = fma((double)f[e], (double)f[e], s);
+        }
+    }
+    s = wave_sum(s);
+    if (threadIdx.x % WAVE == 0) red[threadIdx.x / WAVE] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) a.partial[(int64_t)blockIdx.y * OR_NORM_BLOCKS + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+// The first X: a workgroup writes 64 x 64 of its elements, both planes, zeros where the matrix ends.  TALL: it is
+// turned around in LDS.
+template <typename T, bool TALL>
+__global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
+    constexpr int N = RowVec<T>::N, LANES = 64 / N;   // lanes per row of the tile
+    __shared__ float tile[64][65];
+    const int tn = a.np / 64, m0 = (int)blockIdx.x / tn * 64, n0 = (int)blockIdx.x % tn * 64, matrix = blockIdx.y;
+    const T* in = static_cast<const T*>(a.in[matrix]);
+    double ss = 0.0;
+    for (int p = 0; p < OR_NORM_BLOCKS; ++p) ss += a.partial[(int64_t)matrix * OR_NORM_BLOCKS + p];
+    const double factor = a.scale / (sqrt(ss) + a.eps);
+    const int r0 = TALL ? n0 : m0, c0 = TALL ? m0 : n0;   // the tile's origin in the matrix
+    for (int i = threadIdx.x; i < 64 * LANES; i += 256) {
+        const int r = i / LANES, c = i % LANES * N;
+        float f[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = 0.f;
+        if (r0 + r < a.rows) {
+            const int left = a.cols - c0 - c;
+            RowVec<T>::unpack(row_load(in + (int64_t)(r0 + r) * a.cols + c0 + c, 0, left >= N ? 1 : 0, left > 0 ? left : 0), f);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) tile[r][c + e] = (float)((double)f[e] * factor);
+    }
+    __syncthreads();
+    f16_t* X = a.X + matrix * a.stride_x;
+#pragma unroll
+    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+        const int r = i / 8, c = i % 8 * 8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = TALL ? tile[c + e][r] : tile[r][c + e];
+        u32x4 hi, lo;
+        or_split(v, hi, lo);
+        f16_t* to = X + (int64_t)(m0 + r) * 2 * a.np + n0 + c;
+        *reinterpret_cast<u32x4*>(to) = hi;
+        *reinterpret_cast<u32x4*>(to + a.np) = lo;
+    }
+}
+
+// A workgroup's K loop over nk K steps, from the first loads on, up to the last step's last sub-step, whose fragments are
+// left in raw_a[1], raw_b[1] (or_last_quarter multiplies them; loads past the end are still under way: or_drain).  The
+// loop of fg_product (gemm_bf16_nt.h), which stays as it is there: as a function that both call it compiled to other
+// code for those products.  acc: zeros.  smem: fg_lds_bytes(TILE) of LDS.
+template <bool A_KM, bool B_KM, int TILE, int ORDER, int W>
+__device__ __forceinline__ void or_k_loop(FgOperand<A_KM, TILE, ORDER>& opa, FgOperand<B_KM, TILE, ORDER>& opb, int nk,
+                                          unsigned char* smem, int uwave, f32x16 (&acc)[W][W], FgRaw<A_KM> (&raw_a)[2][W],
+                                          FgRaw<B_KM> (&raw_b)[2][W]) {
+    static_assert(W == TILE / 64, "32 x 32 MFMA tiles per wavefront and direction");
+    constexpr int SLOT = fg_slot_bytes(TILE);
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+
+    // Workgroup barrier of the pipeline.  Loads complete in order and every
+    // wavefront issues NL = TILE / 32 per slot, so "at most NL outstanding" means everything
+    // but the youngest slot (the A tile two steps ahead) has landed.  All LDS
+    // reads of the step are complete as well, so its two slots can be refilled.
+    auto pipeline_barrier = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(TILE / 32) : "memory");
+    };
+
+    // One quarter of a K step: the 16 MFMAs of one K=16 sub-step on the fragments in
+    // register buffer MB (TILE 256; 4 for TILE 128), interleaved with the 8 (4) fragment reads of sub-step KK of the
+    // tile in slots (SA, SB) into buffer 1-MB (one fragment per MFMA, in the order
+    // a0 b0 b1 b2 b3 a1 a2 a3 in which the next quarter consumes them), and with 4 of
+    // the 16 loads of the step, one behind every fourth MFMA (DMA = 1: loads R0..R0+3
+    // of the B tile of step kt into slot SD, DMA = 2: of the A tile).  Loads issued in
+    // bursts fill the memory pipe's queue and stall the wavefront, and with it the
+    // matrix pipe: measured 500 extra cycles for 8 back-to-back loads.
+    auto quarter = [&](auto mb_, auto kk_, auto sa_, auto sb_, auto dma_, auto sd_, auto r0_, int kt) {
+        constexpr int MB = decltype(mb_)::value, RB = 1 - MB, KK = decltype(kk_)::value;
+        constexpr int SA = decltype(sa_)::value, SB = decltype(sb_)::value;
+        constexpr int DMA = decltype(dma_)::value, SD = decltype(sd_)::value, R0 = decltype(r0_)::value;
+        if constexpr (DMA == 1 && R0 == 0) opb.before_step(kt);
+        if constexpr (DMA == 2 && R0 == 0) opa.before_step(kt);
+        fg_wait(raw_a[MB], raw_b[MB]);
+        bf16x8 fa[W], fb[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            fa[i] = fg_value(raw_a[MB][i]);
+            fb[i] = fg_value(raw_b[MB][i]);
+        }
+        const unsigned sa_addr = lds0 + SA * SLOT, sb_addr = lds0 + SB * SLOT;
+        __builtin_amdgcn_sched_barrier(0);
+#define FG_MFMA(q) \
+        acc[(q) / W][(q) % W] = or_mfma(fb[(q) % W], fa[(q) / W], acc[(q) / W][(q) % W])
+#define FG_DMA(n)                                                          \
+        if constexpr (DMA == 1) opb.load_one(smem, SD, kt, uwave, R0 + (n));   \
+        if constexpr (DMA == 2) opa.load_one(smem, SD, kt, uwave, R0 + (n))
+#define FG_END __builtin_amdgcn_sched_barrier(0)
+        if constexpr (W == 2) {
+            FG_MFMA(0); fg_issue<KK, 0>(raw_a[RB][0], opa, sa_addr); fg_issue<KK, 0>(raw_b[RB][0], opb, sb_addr); FG_END;
+            FG_MFMA(1); fg_issue<KK, 1>(raw_b[RB][1], opb, sb_addr); FG_DMA(0); FG_END;
+            FG_MFMA(2); fg_issue<KK, 1>(raw_a[RB][1], opa, sa_addr); FG_END;
+            FG_MFMA(3); FG_DMA(1); FG_END;
+        } else {
+        FG_MFMA(0);  fg_issue<KK, 0>(raw_a[RB][0], opa, sa_addr); FG_END;
+        FG_MFMA(1);  fg_issue<KK, 0>(raw_b[RB][0], opb, sb_addr); FG_END;
+        FG_MFMA(2);  fg_issue<KK, 1>(raw_b[RB][1], opb, sb_addr); FG_DMA(0); FG_END;
+        FG_MFMA(3);  fg_issue<KK, 2>(raw_b[RB][2], opb, sb_addr); FG_END;
+        FG_MFMA(4);  fg_issue<KK, 3>(raw_b[RB][3], opb, sb_addr); FG_END;
+        FG_MFMA(5);  fg_issue<KK, 1>(raw_a[RB][1], opa, sa_addr); FG_END;
+        FG_MFMA(6);  fg_issue<KK, 2>(raw_a[RB][2], opa, sa_addr); FG_DMA(1); FG_END;
+        FG_MFMA(7);  fg_issue<KK, 3>(raw_a[RB][3], opa, sa_addr); FG_END;
+        FG_MFMA(8);  FG_END;
+        FG_MFMA(9);  FG_END;
+        FG_MFMA(10); FG_DMA(2); FG_END;
+        FG_MFMA(11); FG_END;
+        FG_MFMA(12); FG_END;
+        FG_MFMA(13); FG_END;
+        FG_MFMA(14); FG_DMA(3); FG_END;
+        FG_MFMA(15); FG_END;
+        }
+#undef FG_MFMA
+#undef FG_DMA
+#undef FG_END
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+
+    // One K step.  PH = t % 5 fixes the slots: A(t) in (2 PH) % 5, B(t) in
+    // (2 PH + 1) % 5; B(t+1) refills the slot A(t-1) left, A(t+2) the slot B(t-1)
+    // left.  The fourth K=16 sub-step of a tile is multiplied in the first quarter
+    // of the next step, behind the barrier, while the new fragments arrive.  Tiles
+    // past the end are loaded but never consumed (the descriptor returns zeros
+    // past its range), which keeps the steady state free of branches.
+    auto step = [&](auto phase, int t) {
+        constexpr int PH = decltype(phase)::value;
+        using SA = std::integral_constant<int, (2 * PH) % 5>;
+        using SB = std::integral_constant<int, (2 * PH + 1) % 5>;
+        using SB1 = std::integral_constant<int, (2 * PH + 3) % 5>;
+        using SA2 = std::integral_constant<int, (2 * PH + 4) % 5>;
+        using I4 = std::integral_constant<int, TILE / 64>;   // half of a tile's loads
+        quarter(I1{}, I0{}, SA{}, SB{}, I1{}, SB1{}, I0{}, t + 1);   // MFMA: sub-step 3 of tile t-1
+        quarter(I0{}, I1{}, SA{}, SB{}, I1{}, SB1{}, I4{}, t + 1);   // MFMA: sub-step 0
+        quarter(I1{}, I2{}, SA{}, SB{}, I2{}, SA2{}, I0{}, t + 2);   // MFMA: sub-step 1
+        quarter(I0{}, I3{}, SA{}, SB{}, I2{}, SA2{}, I4{}, t + 2);   // MFMA: sub-step 2
+        pipeline_barrier();
+    };
+
+    opa.load(smem, 0, 0, uwave);
+    opb.load(smem, 1, 0, uwave);
+    opa.load(smem, 2, 1, uwave);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {        // the first step has no previous sub-step: add zero
+        fg_zero(raw_a[1][i]);
+        fg_zero(raw_b[1][i]);
+    }
+    pipeline_barrier();
+    int t = 0;
+    for (; t + 5 <= nk; t += 5) {
+        step(std::integral_constant<int, 0>{}, t);
+        step(std::integral_constant<int, 1>{}, t + 1);
+        step(std::integral_constant<int, 2>{}, t + 2);
+        step(std::integral_constant<int, 3>{}, t + 3);
+        step(std::integral_constant<int, 4>{}, t + 4);
+    }
+    if (t < nk) step(std::integral_constant<int, 0>{}, t++);
+    if (t < nk) step(std::integral_constant<int, 1>{}, t++);
+    if (t < nk) step(std::integral_constant<int, 2>{}, t++);
+    if (t < nk) step(std::integral_constant<int, 3>{}, t++);
+}
+
+// Sub-step 3 of the last K step.
+template <bool A_KM, bool B_KM, int W>
+__device__ __forceinline__ void or_last_quarter(f32x16 (&acc)[W][W], FgRaw<A_KM> (&raw_a)[2][W], FgRaw<B_KM> (&raw_b)[2][W]) {
+    fg_wait(raw_a[1], raw_b[1]);
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+        for (int j = 0; j < W; ++j) acc[i][j] = or_mfma(fg_value(raw_b[1][j]), fg_value(raw_a[1][i]), acc[i][j]);
+}
+
+// The loads of the tiles past the end still target LDS: let them land, for every
+// wavefront of the workgroup, before LDS is reused (and before the workgroup can
+// retire and its LDS be handed to another one).
+__device__ __forceinline__ void or_drain() { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Writes a wavefront's part of a tile out, 32 rows at a time through LDS (see FgOut in gemm_bf16_nt.h for the layout of
+// the accumulators): v = alpha * acc + beta * (the addend's planes), as planes of 8 values per lane, the mirrored tile
+// too; or (OR_LAST) rounded to out, whose rows are the tile's columns where the matrix is tall.
+template <int PRODUCT, int PLANES, int TILE, typename OutT, bool TALL>
+struct OrOut {
+    static constexpr int WN = TILE / 2, W = TILE / 64;
+    static constexpr int LANES = WN / 8, ROWS = 64 / LANES, NACC = 32 / ROWS;   // lanes per row, rows and accesses per pass
+    static constexpr int PITCH = WN + 4;
+    static constexpr bool LAST = PRODUCT == OR_LAST, TURN = LAST && TALL, MIRROR = PRODUCT <= OR_POLY;
+    static constexpr int IN = PRODUCT == OR_GRAM ? 0 : PRODUCT == OR_POLY ? PLANES : 2;   // planes of the addend
+    static constexpr int OUT = PRODUCT <= OR_POLY ? PLANES : 2;
+
+    __amdgpu_buffer_rsrc_t rsrc_in, rsrc_out;
+    int ld;          // columns of a plane, of the addend and of the output
+    int rows_all;    // their rows
+    int row0, col0;  // of the wavefront's part
+    int lane;
+    float* stage;
+    u32x4 addend[IN ? 2 : 1][NACC][IN ? IN : 1];
+
+    __device__ __forceinline__ void init(const f16_t* in, f16_t* to, int ld_, int rows_, int r0, int c0, unsigned char* smem, int lane_, int uwave) {
+        ld = ld_;
+        rows_all = rows_;
+        row0 = r0;
+        col0 = c0;
+        lane = lane_;
+        stage = reinterpret_cast<float*>(smem + uwave * (fg_lds_bytes(TILE) / 4));
+        if constexpr (IN > 0) rsrc_in = fg_make_rsrc(in, (uint32_t)rows_all * (uint32_t)ld * (2u * IN));
+        if constexpr (!LAST) rsrc_out = fg_make_rsrc(to, (uint32_t)rows_all * (uint32_t)ld * (2u * OUT));
+    }
+    // byte offset of 8 values in a matrix of P planes, or one past its end
+    template <int P>
+    __device__ __forceinline__ int at(int row, int col) const {
+        return row < rows_all && col < ld ? (row * (P * ld) + col) * 2 : 0x7fffffff;
+    }
+    __device__ __forceinline__ int lane_row(int k) const { return k * ROWS + lane / LANES; }
+    __device__ __forceinline__ int lane_col() const { return lane % LANES * 8; }
+
+    template <int BUF>
+    __device__ __forceinline__ void load_addend(int pass) {
+        if constexpr (IN > 0) {
+#pragma unroll
+            for (int k = 0; k < NACC; ++k) {
+                const int off = at<IN>(row0 + pass * 32 + lane_row(k), col0 + lane_col());
+#pragma unroll
+                for (int p = 0; p < IN; ++p)
+                    addend[BUF][k][p] = __builtin_amdgcn_raw_buffer_load_b128(rsrc_in, off, p * ld * 2, 0);
+            }
+        }
+    }
+    __device__ __forceinline__ void put_planes(int row, int col, const float (&v)[8]) {
+        u32x4 hi, lo;
+        or_split(v, hi, lo);
+        const int off = at<OUT>(row, col);
+        __builtin_amdgcn_raw_buffer_store_b128(hi, rsrc_out, off, 0, 0);
+        if constexpr (OUT == 2) __builtin_amdgcn_raw_buffer_store_b128(lo, rsrc_out, off, ld * 2, 0);
+    }
+    static __device__ __forceinline__ void put_out(OutT* out, int rows, int cols, int row, int col, const float (&v)[8]) {
+        if (row >= rows || col >= cols) return;
+        OutT* to = out + (int64_t)row * cols + col;
+        constexpr int N = RowVec<OutT>::N;
+        if (col + 8 <= cols) {
+#pragma unroll
+            for (int g = 0; g < 8 / N; ++g) {
+                float w[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) w[e] = v[g * N + e];
+                *reinterpret_cast<u32x4_any*>(to + g * N) = RowVec<OutT>::pack(w);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < cols) to[e] = from_f32<OutT>(v[e]);
+        }
+    }
+
+    // The passes; load_addend<0>(0) has been issued before.
+    __device__ __forceinline__ void write(f32x16 (&acc)[W][W], const OrArgs& a, int matrix, bool mirror) {
+        const int frow = lane & 31, fhalf = lane >> 5;
+        OutT* out = LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if (i + 1 < W) {
+                if (i % 2 == 0) load_addend<IN ? 1 : 0>(i + 1); else load_addend<0>(i + 1);
+            }
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float v0 = acc[i][j][4 * g], v1 = acc[i][j][4 * g + 1], v2 = acc[i][j][4 * g + 2], v3 = acc[i][j][4 * g + 3];
+                    *reinterpret_cast<f32x4*>(stage + frow * PITCH + 32 * j + 8 * g + 4 * fhalf) = f32x4{v0, v1, v2, v3};
+                }
+            // (the region is the wavefront's own, and LDS executes its accesses in order)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int k = 0; k < NACC; ++k) {
+                float* src = stage + lane_row(k) * PITCH + lane_col();
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    const f32x4 q = *reinterpret_cast<const f32x4*>(src + e);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[e + u] = a.alpha * q[u];
+                }
+                if constexpr (IN > 0) {
+#pragma unroll
+                    for (int p = IN - 1; p >= 0; --p) {
+                        const f16x8 w = __builtin_bit_cast(f16x8, addend[i % 2][k][p]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = fmaf(a.beta, (float)w[e], v[e]);
+                    }
+                }
+                const int row = row0 + 32 * i + lane_row(k), col = col0 + lane_col();
+                if constexpr (!LAST) put_planes(row, col, v);
+                else if constexpr (!TALL) put_out(out, a.rows, a.cols, row, col, v);
+                if constexpr (TURN || MIRROR) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4*>(src + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if ((MIRROR && mirror) || TURN) {
+                // lane: column lane / 4 + 16 k, rows 8 (lane % 4) .. + 7 of the pass
+#pragma unroll
+                for (int k = 0; k < WN / 16; ++k) {
+                    const int c = lane / 4 + 16 * k, r = lane % 4 * 8;
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = stage[(r + e) * PITCH + c];
+                    if constexpr (TURN) put_out(out, a.rows, a.cols, col0 + c, row0 + 32 * i + r, v);
+                    else put_planes(col0 + c, row0 + 32 * i + r, v);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+        }
+    }
+};
+
+// Tile t of a matrix: of a symmetric product, row by row on and below the diagonal; else OR_GROUP rows at a time, column
+// by column among them.
+constexpr int OR_GROUP = 4;
+template <bool SYMMETRIC>
+__device__ __forceinline__ void or_tile(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
+    if constexpr (SYMMETRIC) {
+        tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+        while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;   // (the root may be off by a rounding)
+        while (tm * (tm + 1) / 2 > t) --tm;
+        tn = t - tm * (tm + 1) / 2;
+    } else {
+        const int grp = t / (OR_GROUP * tiles_n), first = grp * OR_GROUP, g = min(OR_GROUP, tiles_m - first);
+        const int rem = t - grp * OR_GROUP * tiles_n;
+        tm = first + rem % g;
+        tn = rem / g;
+    }
+}
+
+// One workgroup per tile of a matrix, 256 x 256, or 128 x 128 and two workgroups per CU.
+template <int PRODUCT, int PLANES, int TILE, typename OutT, bool TALL>
+__global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_kernel(OrArgs a) {
+    constexpr bool SYMMETRIC = PRODUCT <= OR_POLY, B_KM = !SYMMETRIC;
+    constexpr int ORDER = PLANES == 2 ? FG_PLANES : FG_PLAIN, W = TILE / 64;
+    __shared__ __attribute__((aligned(16))) unsigned char smem[fg_lds_bytes(TILE)];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int wm = wave >> 1, wn = wave & 1;
+    // workgroups go round-robin to the XCDs: each gets a stretch of tiles
+    const int total = a.tiles * a.count, per_xcd = (total + FG_XCDS - 1) / FG_XCDS;
+    const int seq = (int)blockIdx.x % FG_XCDS * per_xcd + (int)blockIdx.x / FG_XCDS;
+    if ((int)blockIdx.x / FG_XCDS >= per_xcd || seq >= total) return;
+    const int matrix = seq / a.tiles;
+    int tm, tn;
+    or_tile<SYMMETRIC>(seq - matrix * a.tiles, a.tiles_m, a.tiles_n, tm, tn);
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
+    const int m0 = tm * TILE, n0 = tn * TILE;
+
+    // operands: X X^T, A A (A is symmetric), B X
+    const f16_t* X = a.X + matrix * a.stride_x;
+    const f16_t* left = PRODUCT == OR_GRAM ? X : (PRODUCT == OR_POLY ? a.A : a.B) + matrix * a.stride_a;
+    const f16_t* right = PRODUCT == OR_POLY ? left : X;
+    const int ldl = PRODUCT == OR_GRAM ? 2 * a.np : PLANES * a.mp, ldr = PRODUCT == OR_POLY ? PLANES * a.mp : 2 * a.np;
+    const int K = PRODUCT == OR_GRAM ? a.np : a.mp, N = SYMMETRIC ? a.mp : a.np;
+    FgOperand<false, TILE, ORDER> opa;
+    FgOperand<B_KM, TILE, ORDER> opb;
+    opa.init(reinterpret_cast<const bf16_t*>(left), ldl, m0, a.mp, K, tid, wm);
+    opb.init(reinterpret_cast<const bf16_t*>(right), ldr, n0, N, K, tid, wn);
+    opa.start_at(0);
+    opb.start_at(0);
+    int nk = K / FG_BK;
+    if constexpr (PLANES == 2) {
+        opa.plane_steps = opb.plane_steps = nk;
+        opa.plane_bytes = (PRODUCT == OR_GRAM ? a.np : a.mp) * 2;
+        opb.plane_bytes = (PRODUCT == OR_POLY ? a.mp : a.np) * 2;
+        opa.lo_part = 1;
+        opb.lo_part = 0;
+        nk *= 3;
+    }
+    const int uwave = __builtin_amdgcn_readfirstlane(wave);
+    f32x16 acc[W][W];
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int g = 0; g < 16; ++g) acc[i][j][g] = 0.f;
+    FgRaw<false> raw_a[2][W];
+    FgRaw<B_KM> raw_b[2][W];
+    or_k_loop(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
+    OrOut<PRODUCT, PLANES, TILE, OutT, TALL> out;
+    const f16_t* addend = PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X;
+    out.init(addend, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N, a.mp,
+             m0 + __builtin_amdgcn_readfirstlane(wm) * (TILE / 2), n0 + __builtin_amdgcn_readfirstlane(wn) * (TILE / 2), smem, lane, uwave);
+    out.template load_addend<0>(0);
+    or_last_quarter(acc, raw_a, raw_b);
+    or_drain();
+    out.write(acc, a, matrix, tm != tn);
+}
+
+}  // namespace flce

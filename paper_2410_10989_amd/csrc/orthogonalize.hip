@@ -1,0 +1,241 @@
+// C ABI of the orthogonalisation (see orthogonalize.h): argument checks, the powers of two that keep the iterates in
+// fp16's range, workspace, launches.
+#include "orthogonalize.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+#include <type_traits>
+
+#include "flce_host.h"
+
+using namespace flce;
+
+namespace {
+
+constexpr int64_t OR_MAX_DIM = (int64_t)1 << 20;         // a tile's rows stay below 2^31 bytes apart
+constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: its planes stay below 2^30 bytes
+constexpr int OR_MAX_STEPS = 32;
+constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
+constexpr int64_t OR_TILES_256 = 128;                    // fewest tiles of 256 that a launch takes those for
+constexpr int64_t OR_ROUNDS = 1024;                      // tiles of a launch that more matrices would not fill better
+constexpr float OR_USUAL[3] = {3.4445f, -4.7750f, 2.0315f};
+
+size_t elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
+int64_t padded(int64_t v) { return (v + OR_PAD - 1) / OR_PAD * OR_PAD; }
+size_t aligned_bytes(size_t n) { return (n + 255) / 256 * 256; }
+
+struct OrStep {
+    float a, b, c;
+    int e_x, e_a, e_b;   // X, A and B are held times 2 to these
+};
+struct OrPlan {
+    int64_t mp, np;
+    int planes;                       // of A and B
+    int64_t group;                    // matrices at a time
+    size_t x_bytes, a_bytes, bytes;   // of one matrix: X (there are two), A (and B); all of them, and its partial sums
+    OrStep steps[OR_MAX_STEPS];
+};
+
+// The exponent that brings values of up to `most` below 2^14.
+int exponent_for(double most) { return 14 - (int)ceil(log2(std::max(most, 0x1p-40))); }
+
+// Singular values of X_k lie in [0, s]; every step's polynomial says where those of X_{k+1} do.
+int steps_of(const flce_orthogonalize_args& b, OrStep* to) {
+    double s = 1.0;
+    for (int k = 0; k < b.steps; ++k) {
+        const float* p = !b.coefficients ? OR_USUAL : b.coefficients + (b.per_step ? 3 * k : 0);
+        for (int i = 0; i < 3; ++i)
+            if (p[i] - p[i] != 0.0f) return FLCE_ERR_ARG;
+        const double A = p[0], B = p[1], C = p[2], l1 = s * s;
+        auto poly = [&](double l) { return fabs(B * l + C * l * l); };
+        auto next = [&](double l) { return fabs(sqrt(l) * (A + B * l + C * l * l)); };
+        double most_b = poly(l1), most_x = next(l1);
+        auto at = [&](double l, auto f, double& most) {
+            if (l > 0.0 && l < l1) most = std::max(most, f(l));
+        };
+        if (C != 0.0) {
+            at(-B / (2.0 * C), poly, most_b);
+            const double disc = 9.0 * B * B - 20.0 * A * C;
+            if (disc >= 0.0) {
+                at((-3.0 * B + sqrt(disc)) / (10.0 * C), next, most_x);
+                at((-3.0 * B - sqrt(disc)) / (10.0 * C), next, most_x);
+            }
+        } else if (B != 0.0) {
+            at(-A / (3.0 * B), next, most_x);
+        }
+        to[k] = {p[0], p[1], p[2], exponent_for(s), exponent_for(l1), exponent_for(most_b)};
+        s = std::max(most_x, 0x1p-20) * 1.01;   // (what rounding may add)
+        if (!(s <= OR_MAX_NORM)) return FLCE_ERR_ARG;
+    }
+    return FLCE_OK;
+}
+
+int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
+    if (!args) return FLCE_ERR_NULL;
+    const flce_orthogonalize_args& b = *args;
+    if (b.size != sizeof(flce_orthogonalize_args) || n < 0) return FLCE_ERR_ARG;
+    if (b.dtype != FLCE_F32 && b.dtype != FLCE_BF16) return FLCE_ERR_DTYPE;
+    if (b.rows < 1 || b.rows > OR_MAX_DIM || b.cols < 1 || b.cols > OR_MAX_DIM) return FLCE_ERR_SHAPE;
+    if (b.steps < 1 || b.steps > OR_MAX_STEPS || (b.per_step != 0 && b.per_step != 1)) return FLCE_ERR_ARG;
+    if (b.scale - b.scale != 0.0f || !(b.eps >= 0.0f) || b.eps - b.eps != 0.0f) return FLCE_ERR_ARG;
+    p->mp = padded(std::min(b.rows, b.cols));
+    p->np = padded(std::max(b.rows, b.cols));
+    if (p->mp * p->np > OR_MAX_ELEMENTS) return FLCE_ERR_SHAPE;
+    FLCE_TRY(steps_of(b, p->steps));
+    p->planes = b.dtype == FLCE_F32 ? 2 : 1;
+    p->x_bytes = aligned_bytes((size_t)(p->mp * p->np) * 2 * sizeof(f16_t));
+    p->a_bytes = aligned_bytes((size_t)(p->mp * p->mp) * p->planes * sizeof(f16_t));
+    p->bytes = 2 * p->x_bytes + 2 * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double));
+    // Matrices at a time: until the launch with the fewest tiles has several rounds of them.
+    const int64_t t = (p->mp + 255) / 256, tiles = t * (t + 1) / 2;
+    p->group = std::max<int64_t>(1, std::min<int64_t>({n, OR_MATRICES, (OR_ROUNDS + tiles - 1) / tiles}));
+    return FLCE_OK;
+}
+
+template <int PRODUCT, int PLANES, typename OutT, bool TALL>
+int launch_product(OrArgs& a, hipStream_t s) {
+    constexpr bool SYMMETRIC = PRODUCT <= OR_POLY;
+    auto tiles_of = [&](int64_t tile) {
+        a.tiles_m = (int)((a.mp + tile - 1) / tile);
+        a.tiles_n = SYMMETRIC ? a.tiles_m : (int)((a.np + tile - 1) / tile);
+        const int64_t tiles = SYMMETRIC ? (int64_t)a.tiles_m * (a.tiles_m + 1) / 2 : (int64_t)a.tiles_m * a.tiles_n;
+        a.tiles = (int)tiles;
+        return tiles * a.count;
+    };
+    int64_t total = tiles_of(256);
+    const bool large = total >= OR_TILES_256;
+    if (!large) total = tiles_of(128);
+    const dim3 grid((unsigned)((total + FG_XCDS - 1) / FG_XCDS * FG_XCDS));
+    if (large) hipLaunchKernelGGL((or_product_kernel<PRODUCT, PLANES, 256, OutT, TALL>), grid, dim3(FG_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((or_product_kernel<PRODUCT, PLANES, 128, OutT, TALL>), grid, dim3(FG_THREADS), 0, s, a);
+    HIP_TRY(hipGetLastError());
+    return FLCE_OK;
+}
+
+// `count` matrices, in the workspace from ws on.
+template <typename T>
+int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* const* in, void* const* out, int count, char* ws, hipStream_t s) {
+    constexpr int PLANES = std::is_same<T, float>::value ? 2 : 1;
+    const bool tall = b.rows > b.cols;
+    f16_t* X[2] = {reinterpret_cast<f16_t*>(ws), reinterpret_cast<f16_t*>(ws + count * p.x_bytes)};
+    f16_t* A = reinterpret_cast<f16_t*>(ws + 2 * count * p.x_bytes);
+    f16_t* B = reinterpret_cast<f16_t*>(ws + count * (2 * p.x_bytes + p.a_bytes));
+    OrLoadArgs l{};
+    l.partial = reinterpret_cast<double*>(ws + count * (2 * p.x_bytes + 2 * p.a_bytes));
+    l.X = X[0];
+    l.stride_x = (int64_t)(p.x_bytes / sizeof(f16_t));
+    l.rows = (int)b.rows;
+    l.cols = (int)b.cols;
+    l.mp = (int)p.mp;
+    l.np = (int)p.np;
+    l.scale = ldexp(1.0, p.steps[0].e_x);
+    l.eps = b.eps;
+    for (int i = 0; i < count; ++i) l.in[i] = in[i];
+    hipLaunchKernelGGL((or_norm_kernel<T>), dim3(OR_NORM_BLOCKS, (unsigned)count), dim3(256), 0, s, l);
+    HIP_TRY(hipGetLastError());
+    const dim3 blocks((unsigned)(p.mp / 64 * (p.np / 64)), (unsigned)count);
+    if (tall) hipLaunchKernelGGL((or_load_kernel<T, true>), blocks, dim3(256), 0, s, l);
+    else hipLaunchKernelGGL((or_load_kernel<T, false>), blocks, dim3(256), 0, s, l);
+    HIP_TRY(hipGetLastError());
+    OrArgs a{};
+    a.A = A;
+    a.B = B;
+    a.stride_x = l.stride_x;
+    a.stride_a = (int64_t)(p.a_bytes / sizeof(f16_t));
+    a.mp = l.mp;
+    a.np = l.np;
+    a.count = count;
+    a.rows = l.rows;
+    a.cols = l.cols;
+    for (int i = 0; i < count; ++i) a.out[i] = out[i];
+    for (int k = 0; k < b.steps; ++k) {
+        const OrStep& st = p.steps[k];
+        a.X = X[k % 2];
+        a.to = A;
+        a.alpha = ldexpf(1.0f, st.e_a - 2 * st.e_x);
+        a.beta = 0.0f;
+        FLCE_TRY((launch_product<OR_GRAM, PLANES, float, false>(a, s)));
+        a.to = B;
+        a.alpha = ldexpf(st.c, st.e_b - 2 * st.e_a);
+        a.beta = ldexpf(st.b, st.e_b - st.e_a);
+        FLCE_TRY((launch_product<OR_POLY, PLANES, float, false>(a, s)));
+        a.to = X[(k + 1) % 2];
+        if (k + 1 < b.steps) {
+            const int e = p.steps[k + 1].e_x;
+            a.alpha = ldexpf(1.0f, e - st.e_b - st.e_x);
+            a.beta = ldexpf(st.a, e - st.e_x);
+            FLCE_TRY((launch_product<OR_APPLY, PLANES, float, false>(a, s)));
+        } else {
+            a.alpha = ldexpf(b.scale, -st.e_b - st.e_x);
+            a.beta = ldexpf(b.scale * st.a, -st.e_x);
+            if (tall) FLCE_TRY((launch_product<OR_LAST, PLANES, T, true>(a, s)));
+            else FLCE_TRY((launch_product<OR_LAST, PLANES, T, false>(a, s)));
+        }
+    }
+    return FLCE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int flce_orthogonalize(const void* const* in, void* const* out, int n_matrices, const flce_orthogonalize_args* args, void* stream) {
+    OrPlan p;
+    FLCE_TRY(or_plan(args, n_matrices, &p));
+    const flce_orthogonalize_args& b = *args;
+    if (!n_matrices) return FLCE_OK;
+    if (!in) return FLCE_ERR_NULL;
+    if (!out) out = const_cast<void* const*>(in);
+    const size_t es = elem(b.dtype), bytes = (size_t)b.rows * (size_t)b.cols * es;
+    for (int i = 0; i < n_matrices; ++i) {
+        if (!in[i] || !out[i]) return FLCE_ERR_NULL;
+        if (!aligned(in[i], es) || !aligned(out[i], es)) return FLCE_ERR_ALIGN;
+    }
+    if (b.workspace && !aligned(b.workspace, 256)) return FLCE_ERR_ALIGN;
+    // the workspace: for a group, or for as many of its matrices as there is room for
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(b.workspace);
+    size_t cap = SIZE_MAX;
+    if (ws) {
+        cap = b.workspace_bytes;
+    } else {
+        size_t lent = 0;
+        FLCE_TRY(shared_workspace_lent(&lent));
+        if (lent) cap = lent;
+    }
+    p.group = (int64_t)std::min<size_t>((size_t)p.group, cap / p.bytes);
+    if (p.group < 1) return FLCE_ERR_WORKSPACE;
+    while (!ws) {
+        const int rc = shared_workspace((size_t)p.group * p.bytes, &ws, s, p.group == 1);
+        if (rc == FLCE_OK) break;
+        if (rc != FLCE_ERR_WORKSPACE || p.group == 1) return rc;
+        p.group = (p.group + 1) / 2;
+    }
+    Piece* pieces = new (std::nothrow) Piece[2 * (size_t)n_matrices + 1];
+    if (!pieces) return FLCE_ERR_WORKSPACE;
+    size_t k = 0;
+    for (int i = 0; i < n_matrices; ++i) {
+        const uintptr_t w = reinterpret_cast<uintptr_t>(out[i]), r = reinterpret_cast<uintptr_t>(in[i]);
+        pieces[k++] = {w, w + bytes, true};
+        if (r != w) pieces[k++] = {r, r + bytes, false};
+    }
+    pieces[k++] = {reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + (size_t)p.group * p.bytes, true};
+    const bool shared = written_twice(pieces, k);
+    delete[] pieces;
+    if (shared) return FLCE_ERR_ARG;
+    for (int i = 0; i < n_matrices; i += (int)p.group) {
+        const int count = (int)std::min<int64_t>(p.group, n_matrices - i);
+        FLCE_TRY(b.dtype == FLCE_F32 ? run_group<float>(b, p, in + i, out + i, count, ws, s)
+                                     : run_group<bf16_t>(b, p, in + i, out + i, count, ws, s));
+    }
+    return FLCE_OK;
+}
+
+size_t flce_orthogonalize_workspace_bytes(int n_matrices, const flce_orthogonalize_args* args) {
+    OrPlan p;
+    return or_plan(args, n_matrices, &p) == FLCE_OK && n_matrices ? (size_t)p.group * p.bytes : 0;
+}
+
+}  // extern "C"

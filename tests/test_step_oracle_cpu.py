@@ -181,3 +181,95 @@ def test_layer_norm_binding_refusals():
         flce.flce_layer_norm_fwd(t)
     with pytest.raises(ValueError):
         flce.flce_layer_norm_bwd(t, t)
+
+
+# ---- orthogonalisation ----
+
+@pytest.mark.parametrize("rows,cols", [(6, 9), (9, 6), (1, 4), (5, 5)])
+def test_orthogonalisation_acts_on_the_singular_values(rows, cols):
+    g = rng(5, rows)
+    G = g.standard_normal((rows, cols))
+    got = oracle.orthogonalize(G, scale=1.5)
+    U, s, Vt = np.linalg.svd(G, full_matrices=False)
+    s = s / (np.linalg.norm(G) + 1e-7)
+    for _ in range(5):
+        s = 3.4445 * s - 4.7750 * s ** 3 + 2.0315 * s ** 5
+    np.testing.assert_allclose(got, 1.5 * (U * s) @ Vt, rtol=1e-9, atol=1e-10)
+    # the cubic that converges: U V^T itself
+    np.testing.assert_allclose(oracle.orthogonalize(G, 60, (1.5, -0.5, 0.0)), U @ Vt, atol=1e-9)
+
+
+def test_rounded_orthogonalisation_is_near_the_exact_one():
+    G = rng(6, 7).standard_normal((60, 90))
+    ref = oracle.orthogonalize(G)
+    err = [np.linalg.norm(oracle.orthogonalize_rounded(G, p) - ref) / np.linalg.norm(ref) for p in (1, 2)]
+    assert 1e-5 < err[0] < 5e-3 and err[1] < 5e-6
+
+
+def ortho_args(**kw):
+    d = dict(size=ctypes.sizeof(flce.FlceOrthogonalizeArgs), rows=70, cols=90, dtype=flce.FLCE_F32, steps=5, coefficients=None, per_step=0,
+             scale=1.0, eps=1e-7)
+    d.update(kw)
+    c = d.pop("coefficients")
+    a = flce.FlceOrthogonalizeArgs(**d)
+    if c is not None:
+        a._keep = (ctypes.c_float * len(c))(*c)
+        a.coefficients = ctypes.addressof(a._keep)
+    return a
+
+
+def ortho(a, ins=(A, 2 * A), outs=(3 * A, 4 * A), n=None):
+    P = ctypes.c_void_p * 2
+    return flce.lib().flce_orthogonalize(P(*ins) if ins else None, P(*outs) if outs else None, len(ins) if n is None else n,
+                                         ctypes.byref(a) if a else None, None)
+
+
+INF = float("inf")
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(size=4), 7), (dict(rows=0), 2), (dict(cols=0), 2), (dict(rows=(1 << 20) + 1), 2), (dict(cols=(1 << 20) + 1), 2),
+    (dict(rows=1 << 15, cols=(1 << 13) + 1), 2), (dict(dtype=7), 3), (dict(steps=0), 7), (dict(steps=33), 7), (dict(per_step=2), 7),
+    (dict(scale=INF), 7), (dict(eps=-1e-9), 7), (dict(eps=float("nan")), 7), (dict(coefficients=[1.0, INF, 0.0]), 7),
+    (dict(coefficients=[12.0, 0.0, 0.0]), 7),                                       # 12^3 > 1024
+    (dict(coefficients=[3.0, 2.0, 1.0]), 7), (dict(steps=1, coefficients=[0.0, 0.0, 1025.0]), 7)])
+def test_orthogonalisation_refuses_bad_arguments(kw, status):
+    a = ortho_args(**kw)
+    assert ortho(a) == status
+    assert flce.lib().flce_orthogonalize_workspace_bytes(2, ctypes.byref(a)) == 0
+
+
+def test_orthogonalisation_refuses_bad_pointers():
+    size = 70 * 90 * 4
+    need = flce.flce_orthogonalize_workspace_bytes(2, 70, 90, torch.float32)
+    assert need > 0
+    with_ws = lambda at=9 * A, n=need: ortho_args(workspace=at, workspace_bytes=n)
+    assert ortho(None) == 1 and ortho(ortho_args(), ins=None, n=2) == 1
+    assert ortho(ortho_args(), n=-1) == 7 and ortho(ortho_args(), n=0) == 0
+    assert ortho(with_ws(), ins=(A, 0)) == 1 and ortho(with_ws(), outs=(0, A)) == 1
+    assert ortho(with_ws(), ins=(A, 2 * A + 2)) == 4 and ortho(with_ws(), outs=(3 * A + 1, 4 * A)) == 4
+    assert ortho(with_ws(at=9 * A + 64)) == 4
+    assert ortho(with_ws(n=flce.flce_orthogonalize_workspace_bytes(1, 70, 90, torch.float32) - 1)) == 5
+    assert ortho(with_ws(), outs=(3 * A, 3 * A)) == 7                       # two outs
+    assert ortho(with_ws(), outs=(3 * A, 3 * A + size - 4)) == 7
+    assert ortho(with_ws(), outs=(2 * A, A)) == 7                           # an out on another's in
+    assert ortho(with_ws(), outs=(A + 4, 4 * A)) == 7                       # shifted on its own
+    assert ortho(with_ws(), ins=(A, A), outs=None) == 7                     # the same matrix twice, in place
+    for at in (A, 2 * A, 3 * A, 4 * A):
+        assert ortho(with_ws(at=at)) == 7                                   # the workspace on a matrix
+
+
+def test_orthogonalisation_accepts_what_stays_in_range():
+    big = lambda **kw: flce.lib().flce_orthogonalize_workspace_bytes(1, ctypes.byref(ortho_args(**kw))) > 0
+    assert big() and big(steps=32) and big(coefficients=[2.0, -1.5, 0.5], steps=32) and big(coefficients=[0.0, 0.0, 0.0])
+    assert big(steps=1, coefficients=[1000.0, 0.0, 0.0]) and big(rows=1 << 15, cols=1 << 13) and big(rows=1 << 20, cols=1)
+    assert big(steps=2, per_step=1, coefficients=[8.0, -22.0, 16.0, 4.0, -3.0, 0.5])
+
+
+def test_orthogonalisation_binding_refusals():
+    t = torch.zeros(4, 8)
+    with pytest.raises(ValueError):
+        flce.flce_orthogonalize([t])
+    with pytest.raises(ValueError):
+        flce.flce_orthogonalize([t, torch.zeros(8, 4)])
+    assert flce.flce_orthogonalize([]) == []
