@@ -1,7 +1,7 @@
 // Orthogonalising matrices by Newton-Schulz products.  For a matrix G of min(rows, cols) = m and max(rows, cols) = n
 // (transposed where it has more rows than columns)
 //
-//     X = G / (|G|_F + eps),      then per step    A = X X^T,   B = b A + c A A,   X <- a X + B X        out = s X
+//     X = G / (|G|_F + eps),      then per step    A = X X^T,   B = a I + b A + c A A,   X <- B X        out = s X
 //
 // drives every singular value of X towards 1 and keeps its singular vectors.  Per step 2 m^2 n + 2 m^3 + 2 m^2 n
 // operations; A and B are symmetric, so only the tiles on and below the diagonal are computed, the others mirrored.
@@ -9,12 +9,17 @@
 // Numbers.  The iteration multiplies the smallest singular values by a^steps (485 for five of the usual steps), and any
 // error in their directions with them.  The operands of the products are fp16, scaled by powers of two that keep them
 // in range: 11 bits where bf16 has 8, at the same rate (relative error of the result 1.2e-3 instead of 1e-2 for a
-// matrix of noise).  X is held as the sum of two fp16 planes, hi and lo, 22 bits: what a X carries over is not rounded
-// to 11 bits (for a matrix of low rank and a little noise 2.4e-4; with X in one plane 2e-2, in bf16 0.14).  For
-// bf16 matrices the products take the hi planes alone; for fp32 matrices A and B have two planes as well and every
-// product is hi lo + lo hi + hi hi.  Sums are fp32 in the matrix cores, the norm fp64.  The cores cut a sum off where
-// it leaves fp32: each 16 terms added to a sum of S take up to 2^-23 S from it, always towards zero, so the small
-// products come first (16 x 4099: 7.2e-6 with hi hi first).
+// matrix of noise).  X can be held as the sum of two fp16 planes, hi and lo, 22 bits.
+//   bf16 matrices: the first X is G times a power of two, exact in one plane (the rest of the norm goes into the first
+//   step's factors).  The products take the hi planes; while what follows may multiply an error by more than
+//   OR_CARRY, X is stored in both planes and X <- B hi + a lo, so that what is carried over is not rounded to 11
+//   bits (a matrix of low rank and a little noise: 4e-4; with every X in one plane 3e-3, in bf16 0.14).  Up to
+//   m = OR_SMALL, where A and B cost little, they have two planes, too (64 x 512: 1.75e-3 instead of 2.4e-3 with the
+//   1.66e-3 of rounding the result to bf16).
+//   fp32 matrices: two planes everywhere, every product is hi lo + lo hi + hi hi.
+// Sums are fp32 in the matrix cores, the norm fp64.  The cores cut a sum off where it leaves fp32: each 16 terms added
+// to a sum of S take up to 2^-23 S from it, always towards zero, so the small products come first (16 x 4099 fp32:
+// 7.2e-6 with hi hi first).
 #pragma once
 #include "mfma_tiles.h"
 #include "rowvec.h"
@@ -28,7 +33,12 @@ constexpr int OR_MATRICES = 120;   // a launch's arguments stay below 4 KB
 constexpr int OR_PAD = 64;         // rows and columns are padded with zeros to whole K steps
 constexpr int OR_NORM_BLOCKS = 32; // workgroups that add up a matrix's squares
 
-enum { OR_GRAM = 0, OR_POLY = 1, OR_APPLY = 2, OR_LAST = 3 };   // A = X X^T, B = b A + c A A, X <- a X + B X, out = s X
+constexpr int OR_SMALL = 256;      // bf16: A and B in two planes up to this many (padded) rows
+constexpr float OR_CARRY = 16.0f;
+
+enum { OR_GRAM = 0, OR_POLY = 1, OR_APPLY = 2, OR_LAST = 3 };   // A = X X^T, B = a I + b A + c A A, X <- B X, out = s B X
+// A launch does whole products, or K ranges of them whose sums it leaves, or adds those up and writes the results.
+enum { OR_WHOLE = 0, OR_RANGES = 1, OR_JOIN = 2 };
 
 struct OrArgs {
     const f16_t *X, *A, *B;      // planes, of the first matrix; X: rows of [hi np | lo np], A and B of [hi mp (| lo mp)]
@@ -37,30 +47,41 @@ struct OrArgs {
     int mp, np;                  // m and n, padded
     int count;
     int tiles_m, tiles_n, tiles;   // of a matrix
-    float alpha, beta;           // alpha * (the accumulated product) + beta * (A or X)
+    // to = alpha * (the accumulated product) + beta * A (OR_POLY), beta * X's lo plane (add_lo), diagonal (OR_POLY)
+    float alpha, beta, diagonal;
+    int add_lo, put_lo;          // OR_APPLY, OR_LAST: X's lo plane is added; the result has one
+    const float* factor;         // the first step: of each matrix, what its X is to be multiplied by; or null
+    int ranges;                  // of K
+    float* part;                 // the ranges' sums
     int rows, cols;              // OR_LAST: of out
     void* out[OR_MATRICES];
 };
 struct OrLoadArgs {
     const void* in[OR_MATRICES];
     double* partial;             // OR_NORM_BLOCKS per matrix
+    float* factor;               // of each matrix
     f16_t* X;
     int64_t stride_x;
     int rows, cols, mp, np;
-    double scale, eps;           // of the first X
+    int planes;                  // of X that are read
+    int exponent;                // the largest element of the first X may be 2 to this
+    double eps;
 };
 
 __device__ __forceinline__ f32x16 or_mfma(bf16x8 b, bf16x8 a, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
 }
 
-// 8 values as two planes: hi, and what it leaves of them.
+// 8 values as two planes: hi, and what it leaves of them.  (Each value is made to be an fp32 number first: a product that
+// the compiler rounds to fp16 at once for the one plane and by way of fp32 for the other gives two his now and then.)
 __device__ __forceinline__ void or_split(const float (&v)[8], u32x4& hi, u32x4& lo) {
     f16x8 h, l;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        h[e] = (f16_t)v[e];
-        l[e] = (f16_t)(v[e] - (float)h[e]);
+        float x = v[e];
+        asm("" : "+v"(x));
+        h[e] = (f16_t)x;
+        l[e] = (f16_t)(x - (float)h[e]);
     }
     hi = __builtin_bit_cast(u32x4, h);
     lo = __builtin_bit_cast(u32x4, l);
@@ -94,8 +115,9 @@ __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
     if (threadIdx.x == 0) a.partial[(int64_t)blockIdx.y * OR_NORM_BLOCKS + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
 
-// The first X: a workgroup writes 64 x 64 of its elements, both planes, zeros where the matrix ends.  TALL: it is
-// turned around in LDS.
+// The first X: a workgroup writes 64 x 64 elements of G times the power of two that brings its norm to 2^exponent, zeros
+// where the matrix ends.  TALL: it is turned around in LDS.  The factor that is left, norm / (norm + eps) up to a power
+// of two: see OrArgs.
 template <typename T, bool TALL>
 __global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
     constexpr int N = RowVec<T>::N, LANES = 64 / N;   // lanes per row of the tile
@@ -104,33 +126,37 @@ __global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
     const T* in = static_cast<const T*>(a.in[matrix]);
     double ss = 0.0;
     for (int p = 0; p < OR_NORM_BLOCKS; ++p) ss += a.partial[(int64_t)matrix * OR_NORM_BLOCKS + p];
-    const double factor = a.scale / (sqrt(ss) + a.eps);
+    const double norm = sqrt(ss);
+    const bool usual = norm > 0.0 && norm - norm == 0.0;
+    const int e = usual ? ilogb(norm) + 1 : 0;   // norm <= 2^e
+    const double scale = ldexp(1.0, a.exponent - e);
+    if (blockIdx.x == 0 && threadIdx.x == 0)   // (zeros stay zeros; infinities and NaN make all of the result NaN)
+        a.factor[matrix] = usual ? (float)(ldexp(1.0, e) / (norm + a.eps)) : norm == 0.0 ? 1.0f : __builtin_nanf("");
     const int r0 = TALL ? n0 : m0, c0 = TALL ? m0 : n0;   // the tile's origin in the matrix
     for (int i = threadIdx.x; i < 64 * LANES; i += 256) {
         const int r = i / LANES, c = i % LANES * N;
         float f[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = 0.f;
+        for (int k = 0; k < N; ++k) f[k] = 0.f;
         if (r0 + r < a.rows) {
             const int left = a.cols - c0 - c;
             RowVec<T>::unpack(row_load(in + (int64_t)(r0 + r) * a.cols + c0 + c, 0, left >= N ? 1 : 0, left > 0 ? left : 0), f);
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) tile[r][c + e] = (float)((double)f[e] * factor);
+        for (int k = 0; k < N; ++k) tile[r][c + k] = (float)((double)f[k] * scale);
     }
     __syncthreads();
     f16_t* X = a.X + matrix * a.stride_x;
-#pragma unroll
     for (int i = threadIdx.x; i < 64 * 8; i += 256) {
         const int r = i / 8, c = i % 8 * 8;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = TALL ? tile[c + e][r] : tile[r][c + e];
+        for (int k = 0; k < 8; ++k) v[k] = TALL ? tile[c + k][r] : tile[r][c + k];
         u32x4 hi, lo;
         or_split(v, hi, lo);
         f16_t* to = X + (int64_t)(m0 + r) * 2 * a.np + n0 + c;
         *reinterpret_cast<u32x4*>(to) = hi;
-        *reinterpret_cast<u32x4*>(to + a.np) = lo;
+        if (a.planes == 2) *reinterpret_cast<u32x4*>(to + a.np) = lo;
     }
 }
 
@@ -274,16 +300,16 @@ __device__ __forceinline__ void or_last_quarter(f32x16 (&acc)[W][W], FgRaw<A_KM>
 __device__ __forceinline__ void or_drain() { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Writes a wavefront's part of a tile out, 32 rows at a time through LDS (see FgOut in gemm_bf16_nt.h for the layout of
-// the accumulators): v = alpha * acc + beta * (the addend's planes), as planes of 8 values per lane, the mirrored tile
-// too; or (OR_LAST) rounded to out, whose rows are the tile's columns where the matrix is tall.
-template <int PRODUCT, int PLANES, int TILE, typename OutT, bool TALL>
+// the accumulators), as planes of 8 values per lane, the mirrored tile too; or (OR_LAST) rounded to out, whose rows are
+// the tile's columns where the matrix is tall.  PL: planes that are multiplied, OUT: of A.
+template <int PRODUCT, int PL, int OUT, int TILE, typename OutT, bool TALL>
 struct OrOut {
     static constexpr int WN = TILE / 2, W = TILE / 64;
     static constexpr int LANES = WN / 8, ROWS = 64 / LANES, NACC = 32 / ROWS;   // lanes per row, rows and accesses per pass
     static constexpr int PITCH = WN + 4;
     static constexpr bool LAST = PRODUCT == OR_LAST, TURN = LAST && TALL, MIRROR = PRODUCT <= OR_POLY;
-    static constexpr int IN = PRODUCT == OR_GRAM ? 0 : PRODUCT == OR_POLY ? PLANES : 2;   // planes of the addend
-    static constexpr int OUT = PRODUCT <= OR_POLY ? PLANES : 2;
+    static constexpr int IN = PRODUCT == OR_POLY ? PL : PRODUCT >= OR_APPLY && PL == 1 ? 1 : 0;   // planes of the addend: A, X's lo
+    static constexpr bool LO_ONLY = PRODUCT >= OR_APPLY;
 
     __amdgpu_buffer_rsrc_t rsrc_in, rsrc_out;
     int ld;          // columns of a plane, of the addend and of the output
@@ -293,14 +319,16 @@ struct OrOut {
     float* stage;
     u32x4 addend[IN ? 2 : 1][NACC][IN ? IN : 1];
 
-    __device__ __forceinline__ void init(const f16_t* in, f16_t* to, int ld_, int rows_, int r0, int c0, unsigned char* smem, int lane_, int uwave) {
+    __device__ __forceinline__ void init(const f16_t* in, f16_t* to, int ld_, int rows_, bool add, int r0, int c0, unsigned char* smem,
+                                         int lane_, int uwave) {
         ld = ld_;
         rows_all = rows_;
         row0 = r0;
         col0 = c0;
         lane = lane_;
         stage = reinterpret_cast<float*>(smem + uwave * (fg_lds_bytes(TILE) / 4));
-        if constexpr (IN > 0) rsrc_in = fg_make_rsrc(in, (uint32_t)rows_all * (uint32_t)ld * (2u * IN));
+        // (a range of zero bytes makes every load return zero without touching memory)
+        if constexpr (IN > 0) rsrc_in = fg_make_rsrc(in, add ? (uint32_t)rows_all * (uint32_t)ld * (LO_ONLY ? 4u : 2u * IN) : 0u);
         if constexpr (!LAST) rsrc_out = fg_make_rsrc(to, (uint32_t)rows_all * (uint32_t)ld * (2u * OUT));
     }
     // byte offset of 8 values in a matrix of P planes, or one past its end
@@ -316,19 +344,19 @@ struct OrOut {
         if constexpr (IN > 0) {
 #pragma unroll
             for (int k = 0; k < NACC; ++k) {
-                const int off = at<IN>(row0 + pass * 32 + lane_row(k), col0 + lane_col());
+                const int off = at<LO_ONLY ? 2 : IN>(row0 + pass * 32 + lane_row(k), col0 + lane_col());
 #pragma unroll
                 for (int p = 0; p < IN; ++p)
-                    addend[BUF][k][p] = __builtin_amdgcn_raw_buffer_load_b128(rsrc_in, off, p * ld * 2, 0);
+                    addend[BUF][k][p] = __builtin_amdgcn_raw_buffer_load_b128(rsrc_in, off, (LO_ONLY ? 1 : p) * ld * 2, 0);
             }
         }
     }
-    __device__ __forceinline__ void put_planes(int row, int col, const float (&v)[8]) {
+    __device__ __forceinline__ void put_planes(int row, int col, const float (&v)[8], bool put_lo) {
         u32x4 hi, lo;
         or_split(v, hi, lo);
         const int off = at<OUT>(row, col);
         __builtin_amdgcn_raw_buffer_store_b128(hi, rsrc_out, off, 0, 0);
-        if constexpr (OUT == 2) __builtin_amdgcn_raw_buffer_store_b128(lo, rsrc_out, off, ld * 2, 0);
+        if (OUT == 2 && put_lo) __builtin_amdgcn_raw_buffer_store_b128(lo, rsrc_out, off, ld * 2, 0);
     }
     static __device__ __forceinline__ void put_out(OutT* out, int rows, int cols, int row, int col, const float (&v)[8]) {
         if (row >= rows || col >= cols) return;
@@ -349,10 +377,11 @@ struct OrOut {
         }
     }
 
-    // The passes; load_addend<0>(0) has been issued before.
-    __device__ __forceinline__ void write(f32x16 (&acc)[W][W], const OrArgs& a, int matrix, bool mirror) {
+    // The passes; load_addend<0>(0) has been issued before.  alpha: with the matrix's factor.
+    __device__ __forceinline__ void write(f32x16 (&acc)[W][W], const OrArgs& a, float alpha, int matrix, bool mirror) {
         const int frow = lane & 31, fhalf = lane >> 5;
         OutT* out = LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
+        const bool put_lo = PRODUCT != OR_APPLY || PL == 2 || a.put_lo;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             if (i + 1 < W) {
@@ -375,7 +404,7 @@ struct OrOut {
                 for (int e = 0; e < 8; e += 4) {
                     const f32x4 q = *reinterpret_cast<const f32x4*>(src + e);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) v[e + u] = a.alpha * q[u];
+                    for (int u = 0; u < 4; ++u) v[e + u] = alpha * q[u];
                 }
                 if constexpr (IN > 0) {
 #pragma unroll
@@ -386,7 +415,11 @@ struct OrOut {
                     }
                 }
                 const int row = row0 + 32 * i + lane_row(k), col = col0 + lane_col();
-                if constexpr (!LAST) put_planes(row, col, v);
+                if constexpr (PRODUCT == OR_POLY) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += row == col + e ? a.diagonal : 0.f;
+                }
+                if constexpr (!LAST) put_planes(row, col, v, put_lo);
                 else if constexpr (!TALL) put_out(out, a.rows, a.cols, row, col, v);
                 if constexpr (TURN || MIRROR) {
 #pragma unroll
@@ -403,7 +436,7 @@ struct OrOut {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = stage[(r + e) * PITCH + c];
                     if constexpr (TURN) put_out(out, a.rows, a.cols, col0 + c, row0 + 32 * i + r, v);
-                    else put_planes(col0 + c, row0 + 32 * i + r, v);
+                    else put_planes(col0 + c, row0 + 32 * i + r, v, put_lo);
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
@@ -429,47 +462,32 @@ __device__ __forceinline__ void or_tile(int t, int tiles_m, int tiles_n, int& tm
     }
 }
 
-// One workgroup per tile of a matrix, 256 x 256, or 128 x 128 and two workgroups per CU.
-template <int PRODUCT, int PLANES, int TILE, typename OutT, bool TALL>
+// One workgroup per tile of a matrix (and K range of it), 256 x 256, or 128 x 128 and two workgroups per CU.
+template <int PRODUCT, int PL, int OUT, int TILE, typename OutT, bool TALL, int PART>
 __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_kernel(OrArgs a) {
     constexpr bool SYMMETRIC = PRODUCT <= OR_POLY, B_KM = !SYMMETRIC;
-    constexpr int ORDER = PLANES == 2 ? FG_PLANES : FG_PLAIN, W = TILE / 64;
+    constexpr int ORDER = PL == 2 ? FG_PLANES : FG_PLAIN, W = TILE / 64;
+    // planes of the matrices' rows: X 2; A and B what the Gram product stores
+    constexpr int PA = PRODUCT == OR_GRAM ? OUT : PL;
     __shared__ __attribute__((aligned(16))) unsigned char smem[fg_lds_bytes(TILE)];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave >> 1, wn = wave & 1;
-    // workgroups go round-robin to the XCDs: each gets a stretch of tiles
-    const int total = a.tiles * a.count, per_xcd = (total + FG_XCDS - 1) / FG_XCDS;
-    const int seq = (int)blockIdx.x % FG_XCDS * per_xcd + (int)blockIdx.x / FG_XCDS;
+    // workgroups go round-robin to the XCDs: each gets a stretch of tiles, range by range
+    const int all = a.tiles * a.count, total = PART == OR_RANGES ? all * a.ranges : all, per_xcd = (total + FG_XCDS - 1) / FG_XCDS;
+    int seq = (int)blockIdx.x % FG_XCDS * per_xcd + (int)blockIdx.x / FG_XCDS;
     if ((int)blockIdx.x / FG_XCDS >= per_xcd || seq >= total) return;
+    const int range = PART == OR_RANGES ? seq / all : 0;
+    seq -= range * all;
     const int matrix = seq / a.tiles;
     int tm, tn;
     or_tile<SYMMETRIC>(seq - matrix * a.tiles, a.tiles_m, a.tiles_n, tm, tn);
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
     const int m0 = tm * TILE, n0 = tn * TILE;
-
-    // operands: X X^T, A A (A is symmetric), B X
-    const f16_t* X = a.X + matrix * a.stride_x;
-    const f16_t* left = PRODUCT == OR_GRAM ? X : (PRODUCT == OR_POLY ? a.A : a.B) + matrix * a.stride_a;
-    const f16_t* right = PRODUCT == OR_POLY ? left : X;
-    const int ldl = PRODUCT == OR_GRAM ? 2 * a.np : PLANES * a.mp, ldr = PRODUCT == OR_POLY ? PLANES * a.mp : 2 * a.np;
-    const int K = PRODUCT == OR_GRAM ? a.np : a.mp, N = SYMMETRIC ? a.mp : a.np;
-    FgOperand<false, TILE, ORDER> opa;
-    FgOperand<B_KM, TILE, ORDER> opb;
-    opa.init(reinterpret_cast<const bf16_t*>(left), ldl, m0, a.mp, K, tid, wm);
-    opb.init(reinterpret_cast<const bf16_t*>(right), ldr, n0, N, K, tid, wn);
-    opa.start_at(0);
-    opb.start_at(0);
-    int nk = K / FG_BK;
-    if constexpr (PLANES == 2) {
-        opa.plane_steps = opb.plane_steps = nk;
-        opa.plane_bytes = (PRODUCT == OR_GRAM ? a.np : a.mp) * 2;
-        opb.plane_bytes = (PRODUCT == OR_POLY ? a.mp : a.np) * 2;
-        opa.lo_part = 1;
-        opb.lo_part = 0;
-        nk *= 3;
-    }
     const int uwave = __builtin_amdgcn_readfirstlane(wave);
+
+    const f16_t* X = a.X + matrix * a.stride_x;
+    const int K = PRODUCT == OR_GRAM ? a.np : a.mp, N = SYMMETRIC ? a.mp : a.np;
     f32x16 acc[W][W];
 #pragma unroll
     for (int i = 0; i < W; ++i)
@@ -477,17 +495,79 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
         for (int j = 0; j < W; ++j)
 #pragma unroll
             for (int g = 0; g < 16; ++g) acc[i][j][g] = 0.f;
-    FgRaw<false> raw_a[2][W];
-    FgRaw<B_KM> raw_b[2][W];
-    or_k_loop(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
-    OrOut<PRODUCT, PLANES, TILE, OutT, TALL> out;
-    const f16_t* addend = PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X;
-    out.init(addend, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N, a.mp,
-             m0 + __builtin_amdgcn_readfirstlane(wm) * (TILE / 2), n0 + __builtin_amdgcn_readfirstlane(wn) * (TILE / 2), smem, lane, uwave);
-    out.template load_addend<0>(0);
-    or_last_quarter(acc, raw_a, raw_b);
-    or_drain();
-    out.write(acc, a, matrix, tm != tn);
+    // The sums of a range: accumulators as they lie, 16 bytes per lane.
+    constexpr int64_t TILE_FLOATS = (int64_t)TILE * TILE;
+    auto part_at = [&](int r, int i, int j, int g) {
+        return reinterpret_cast<f32x4*>(a.part + ((int64_t)r * all + seq) * TILE_FLOATS + (((i * W + j) * 4 + g) * FG_THREADS + tid) * 4);
+    };
+    OrOut<PRODUCT, PL, OUT, TILE, OutT, TALL> out;
+    auto begin_out = [&]() {
+        out.init(PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N, a.mp,
+                 PRODUCT == OR_POLY || a.add_lo, m0 + __builtin_amdgcn_readfirstlane(wm) * (TILE / 2),
+                 n0 + __builtin_amdgcn_readfirstlane(wn) * (TILE / 2), smem, lane, uwave);
+        out.template load_addend<0>(0);
+    };
+    if constexpr (PART != OR_JOIN) {
+        // operands: X X^T, A A (A is symmetric), B X
+        const f16_t* left = PRODUCT == OR_GRAM ? X : (PRODUCT == OR_POLY ? a.A : a.B) + matrix * a.stride_a;
+        const f16_t* right = PRODUCT == OR_POLY ? left : X;
+        const int ldl = PRODUCT == OR_GRAM ? 2 * a.np : PA * a.mp, ldr = PRODUCT == OR_POLY ? PA * a.mp : 2 * a.np;
+        FgOperand<false, TILE, ORDER> opa;
+        FgOperand<B_KM, TILE, ORDER> opb;
+        opa.init(reinterpret_cast<const bf16_t*>(left), ldl, m0, a.mp, K, tid, wm);
+        opb.init(reinterpret_cast<const bf16_t*>(right), ldr, n0, N, K, tid, wn);
+        const int steps = K / FG_BK;
+        int k0 = 0, nk = steps;
+        if constexpr (PART == OR_RANGES) {
+            k0 = (int)((int64_t)steps * range / a.ranges);
+            nk = (int)((int64_t)steps * (range + 1) / a.ranges) - k0;
+        }
+        opa.start_at(k0);
+        opb.start_at(k0);
+        if constexpr (PL == 2) {
+            opa.plane_steps = opb.plane_steps = nk;
+            opa.plane_bytes = (PRODUCT == OR_GRAM ? a.np : a.mp) * 2;
+            opb.plane_bytes = (PRODUCT == OR_POLY ? a.mp : a.np) * 2;
+            opa.lo_part = 1;
+            opb.lo_part = 0;
+            nk *= 3;
+        }
+        FgRaw<false> raw_a[2][W];
+        FgRaw<B_KM> raw_b[2][W];
+        or_k_loop(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
+        if constexpr (PART == OR_WHOLE) begin_out();
+        or_last_quarter(acc, raw_a, raw_b);
+        or_drain();
+    }
+    if constexpr (PART == OR_RANGES) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float v0 = acc[i][j][4 * g], v1 = acc[i][j][4 * g + 1], v2 = acc[i][j][4 * g + 2], v3 = acc[i][j][4 * g + 3];
+                    *part_at(range, i, j, g) = f32x4{v0, v1, v2, v3};
+                }
+    } else {
+        if constexpr (PART == OR_JOIN) {
+            begin_out();
+            for (int r = 0; r < a.ranges; ++r)
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const f32x4 v = *part_at(r, i, j, g);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += v[e];
+                        }
+        }
+        float alpha = a.alpha;
+        if (a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : PRODUCT >= OR_APPLY ? a.factor[matrix] : 1.0f;
+        out.write(acc, a, alpha, matrix, tm != tn);
+    }
 }
 
 }  // namespace flce

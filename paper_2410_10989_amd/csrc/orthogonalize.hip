@@ -19,6 +19,8 @@ constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: 
 constexpr int OR_MAX_STEPS = 32;
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
 constexpr int64_t OR_TILES_256 = 128;                    // fewest tiles of 256 that a launch takes those for
+constexpr int64_t OR_SLOTS_128 = 512;                    // workgroups of 128-tiles that run at a time
+constexpr int64_t OR_RANGE_STEPS = 4, OR_MAX_RANGES = 16;   // fewest K steps of a range, most ranges
 constexpr int64_t OR_ROUNDS = 1024;                      // tiles of a launch that more matrices would not fill better
 constexpr float OR_USUAL[3] = {3.4445f, -4.7750f, 2.0315f};
 
@@ -29,12 +31,15 @@ size_t aligned_bytes(size_t n) { return (n + 255) / 256 * 256; }
 struct OrStep {
     float a, b, c;
     int e_x, e_a, e_b;   // X, A and B are held times 2 to these
+    bool lo;             // X is needed in two planes
 };
 struct OrPlan {
     int64_t mp, np;
-    int planes;                       // of A and B
+    int planes;                       // that POLY and APPLY multiply, and of A and B
+    int gram_planes;                  // that GRAM multiplies
     int64_t group;                    // matrices at a time
     size_t x_bytes, a_bytes, bytes;   // of one matrix: X (there are two), A (and B); all of them, and its partial sums
+    size_t part_bytes;                // K ranges' sums, of all matrices
     OrStep steps[OR_MAX_STEPS];
 };
 
@@ -49,9 +54,9 @@ int steps_of(const flce_orthogonalize_args& b, OrStep* to) {
         for (int i = 0; i < 3; ++i)
             if (p[i] - p[i] != 0.0f) return FLCE_ERR_ARG;
         const double A = p[0], B = p[1], C = p[2], l1 = s * s;
-        auto poly = [&](double l) { return fabs(B * l + C * l * l); };
-        auto next = [&](double l) { return fabs(sqrt(l) * (A + B * l + C * l * l)); };
-        double most_b = poly(l1), most_x = next(l1);
+        auto poly = [&](double l) { return fabs(A + B * l + C * l * l); };
+        auto next = [&](double l) { return sqrt(l) * poly(l); };
+        double most_b = std::max(poly(0.0), poly(l1)), most_x = next(l1);
         auto at = [&](double l, auto f, double& most) {
             if (l > 0.0 && l < l1) most = std::max(most, f(l));
         };
@@ -65,9 +70,14 @@ int steps_of(const flce_orthogonalize_args& b, OrStep* to) {
         } else if (B != 0.0) {
             at(-A / (3.0 * B), next, most_x);
         }
-        to[k] = {p[0], p[1], p[2], exponent_for(s), exponent_for(l1), exponent_for(most_b)};
+        to[k] = {p[0], p[1], p[2], exponent_for(s), exponent_for(l1), exponent_for(most_b), false};
         s = std::max(most_x, 0x1p-20) * 1.01;   // (what rounding may add)
         if (!(s <= OR_MAX_NORM)) return FLCE_ERR_ARG;
+    }
+    float grows = 1.0f;   // what an error of X_k may be multiplied by in what follows
+    for (int k = b.steps - 1; k >= 0; --k) {
+        grows = std::min(grows * std::max(1.0f, fabsf(to[k].a)), 1e30f);
+        to[k].lo = k > 0 && grows > OR_CARRY;
     }
     return FLCE_OK;
 }
@@ -84,17 +94,21 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     p->np = padded(std::max(b.rows, b.cols));
     if (p->mp * p->np > OR_MAX_ELEMENTS) return FLCE_ERR_SHAPE;
     FLCE_TRY(steps_of(b, p->steps));
-    p->planes = b.dtype == FLCE_F32 ? 2 : 1;
+    p->gram_planes = b.dtype == FLCE_F32 ? 2 : 1;
+    p->planes = b.dtype == FLCE_F32 || p->mp <= OR_SMALL ? 2 : 1;
     p->x_bytes = aligned_bytes((size_t)(p->mp * p->np) * 2 * sizeof(f16_t));
     p->a_bytes = aligned_bytes((size_t)(p->mp * p->mp) * p->planes * sizeof(f16_t));
-    p->bytes = 2 * p->x_bytes + 2 * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double));
+    p->bytes = 2 * p->x_bytes + 2 * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) + 256;
+    p->part_bytes = OR_SLOTS_128 * 128 * 128 * sizeof(float);
     // Matrices at a time: until the launch with the fewest tiles has several rounds of them.
     const int64_t t = (p->mp + 255) / 256, tiles = t * (t + 1) / 2;
     p->group = std::max<int64_t>(1, std::min<int64_t>({n, OR_MATRICES, (OR_ROUNDS + tiles - 1) / tiles}));
     return FLCE_OK;
 }
 
-template <int PRODUCT, int PLANES, typename OutT, bool TALL>
+// A product of all matrices of a group.  Tiles of 128 that leave CUs idle are cut into ranges of K, at most as many as
+// run at a time.
+template <int PRODUCT, int PL, int OUT, typename OutT, bool TALL>
 int launch_product(OrArgs& a, hipStream_t s) {
     constexpr bool SYMMETRIC = PRODUCT <= OR_POLY;
     auto tiles_of = [&](int64_t tile) {
@@ -104,33 +118,52 @@ int launch_product(OrArgs& a, hipStream_t s) {
         a.tiles = (int)tiles;
         return tiles * a.count;
     };
-    int64_t total = tiles_of(256);
-    const bool large = total >= OR_TILES_256;
-    if (!large) total = tiles_of(128);
-    const dim3 grid((unsigned)((total + FG_XCDS - 1) / FG_XCDS * FG_XCDS));
-    if (large) hipLaunchKernelGGL((or_product_kernel<PRODUCT, PLANES, 256, OutT, TALL>), grid, dim3(FG_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((or_product_kernel<PRODUCT, PLANES, 128, OutT, TALL>), grid, dim3(FG_THREADS), 0, s, a);
+    auto grid = [](int64_t total) { return dim3((unsigned)((total + FG_XCDS - 1) / FG_XCDS * FG_XCDS)); };
+    const int64_t large = tiles_of(256);
+    if (large >= OR_TILES_256) {
+        hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 256, OutT, TALL, OR_WHOLE>), grid(large), dim3(FG_THREADS), 0, s, a);
+        HIP_TRY(hipGetLastError());
+        return FLCE_OK;
+    }
+    const int64_t total = tiles_of(128), steps = (PRODUCT == OR_GRAM ? a.np : a.mp) / FG_BK;
+    a.ranges = (int)std::min({OR_MAX_RANGES, OR_SLOTS_128 / total, steps * (PL == 2 ? 3 : 1) / OR_RANGE_STEPS, steps});
+    if (a.ranges <= 1) {
+        hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_WHOLE>), grid(total), dim3(FG_THREADS), 0, s, a);
+        HIP_TRY(hipGetLastError());
+        return FLCE_OK;
+    }
+    hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_RANGES>), grid(total * a.ranges), dim3(FG_THREADS), 0, s, a);
+    HIP_TRY(hipGetLastError());
+    hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_JOIN>), grid(total), dim3(FG_THREADS), 0, s, a);
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
 }
 
-// `count` matrices, in the workspace from ws on.
-template <typename T>
+// `count` matrices, in the workspace from ws on.  GP: planes that GRAM multiplies, PL: that the others do.
+template <typename T, int GP, int PL>
 int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* const* in, void* const* out, int count, char* ws, hipStream_t s) {
-    constexpr int PLANES = std::is_same<T, float>::value ? 2 : 1;
     const bool tall = b.rows > b.cols;
-    f16_t* X[2] = {reinterpret_cast<f16_t*>(ws), reinterpret_cast<f16_t*>(ws + count * p.x_bytes)};
-    f16_t* A = reinterpret_cast<f16_t*>(ws + 2 * count * p.x_bytes);
-    f16_t* B = reinterpret_cast<f16_t*>(ws + count * (2 * p.x_bytes + p.a_bytes));
+    size_t at = p.part_bytes;
+    auto take = [&](size_t bytes) {
+        char* here = ws + at;
+        at += aligned_bytes(bytes);
+        return here;
+    };
+    f16_t* X[2];
+    for (f16_t*& x : X) x = reinterpret_cast<f16_t*>(take(count * p.x_bytes));
+    f16_t* A = reinterpret_cast<f16_t*>(take(count * p.a_bytes));
+    f16_t* B = reinterpret_cast<f16_t*>(take(count * p.a_bytes));
     OrLoadArgs l{};
-    l.partial = reinterpret_cast<double*>(ws + count * (2 * p.x_bytes + 2 * p.a_bytes));
+    l.partial = reinterpret_cast<double*>(take(count * OR_NORM_BLOCKS * sizeof(double)));
+    l.factor = reinterpret_cast<float*>(take(count * sizeof(float)));
     l.X = X[0];
     l.stride_x = (int64_t)(p.x_bytes / sizeof(f16_t));
     l.rows = (int)b.rows;
     l.cols = (int)b.cols;
     l.mp = (int)p.mp;
     l.np = (int)p.np;
-    l.scale = ldexp(1.0, p.steps[0].e_x);
+    l.planes = PL;
+    l.exponent = p.steps[0].e_x;
     l.eps = b.eps;
     for (int i = 0; i < count; ++i) l.in[i] = in[i];
     hipLaunchKernelGGL((or_norm_kernel<T>), dim3(OR_NORM_BLOCKS, (unsigned)count), dim3(256), 0, s, l);
@@ -149,30 +182,32 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     a.count = count;
     a.rows = l.rows;
     a.cols = l.cols;
+    a.part = reinterpret_cast<float*>(ws);
     for (int i = 0; i < count; ++i) a.out[i] = out[i];
     for (int k = 0; k < b.steps; ++k) {
         const OrStep& st = p.steps[k];
+        a.factor = k == 0 ? l.factor : nullptr;
         a.X = X[k % 2];
         a.to = A;
         a.alpha = ldexpf(1.0f, st.e_a - 2 * st.e_x);
         a.beta = 0.0f;
-        FLCE_TRY((launch_product<OR_GRAM, PLANES, float, false>(a, s)));
+        a.add_lo = 0;
+        FLCE_TRY((launch_product<OR_GRAM, GP, PL, float, false>(a, s)));
         a.to = B;
         a.alpha = ldexpf(st.c, st.e_b - 2 * st.e_a);
         a.beta = ldexpf(st.b, st.e_b - st.e_a);
-        FLCE_TRY((launch_product<OR_POLY, PLANES, float, false>(a, s)));
+        a.diagonal = ldexpf(st.a, st.e_b);
+        FLCE_TRY((launch_product<OR_POLY, PL, PL, float, false>(a, s)));
+        const bool last = k + 1 == b.steps;
+        const float scale = last ? b.scale : ldexpf(1.0f, p.steps[k + 1].e_x);
         a.to = X[(k + 1) % 2];
-        if (k + 1 < b.steps) {
-            const int e = p.steps[k + 1].e_x;
-            a.alpha = ldexpf(1.0f, e - st.e_b - st.e_x);
-            a.beta = ldexpf(st.a, e - st.e_x);
-            FLCE_TRY((launch_product<OR_APPLY, PLANES, float, false>(a, s)));
-        } else {
-            a.alpha = ldexpf(b.scale, -st.e_b - st.e_x);
-            a.beta = ldexpf(b.scale * st.a, -st.e_x);
-            if (tall) FLCE_TRY((launch_product<OR_LAST, PLANES, T, true>(a, s)));
-            else FLCE_TRY((launch_product<OR_LAST, PLANES, T, false>(a, s)));
-        }
+        a.alpha = ldexpf(scale, -st.e_b - st.e_x);
+        a.beta = ldexpf(scale * st.a, -st.e_x);
+        a.add_lo = PL == 1 && st.lo;
+        a.put_lo = !last && p.steps[k + 1].lo;
+        if (!last) FLCE_TRY((launch_product<OR_APPLY, PL, 2, float, false>(a, s)));
+        else if (tall) FLCE_TRY((launch_product<OR_LAST, PL, 2, T, true>(a, s)));
+        else FLCE_TRY((launch_product<OR_LAST, PL, 2, T, false>(a, s)));
     }
     return FLCE_OK;
 }
@@ -205,10 +240,10 @@ int flce_orthogonalize(const void* const* in, void* const* out, int n_matrices, 
         FLCE_TRY(shared_workspace_lent(&lent));
         if (lent) cap = lent;
     }
-    p.group = (int64_t)std::min<size_t>((size_t)p.group, cap / p.bytes);
-    if (p.group < 1) return FLCE_ERR_WORKSPACE;
+    if (cap < p.part_bytes + p.bytes) return FLCE_ERR_WORKSPACE;
+    p.group = (int64_t)std::min<size_t>((size_t)p.group, (cap - p.part_bytes) / p.bytes);
     while (!ws) {
-        const int rc = shared_workspace((size_t)p.group * p.bytes, &ws, s, p.group == 1);
+        const int rc = shared_workspace(p.part_bytes + (size_t)p.group * p.bytes, &ws, s, p.group == 1);
         if (rc == FLCE_OK) break;
         if (rc != FLCE_ERR_WORKSPACE || p.group == 1) return rc;
         p.group = (p.group + 1) / 2;
@@ -221,21 +256,22 @@ int flce_orthogonalize(const void* const* in, void* const* out, int n_matrices, 
         pieces[k++] = {w, w + bytes, true};
         if (r != w) pieces[k++] = {r, r + bytes, false};
     }
-    pieces[k++] = {reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + (size_t)p.group * p.bytes, true};
+    pieces[k++] = {reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + p.part_bytes + (size_t)p.group * p.bytes, true};
     const bool shared = written_twice(pieces, k);
     delete[] pieces;
     if (shared) return FLCE_ERR_ARG;
     for (int i = 0; i < n_matrices; i += (int)p.group) {
         const int count = (int)std::min<int64_t>(p.group, n_matrices - i);
-        FLCE_TRY(b.dtype == FLCE_F32 ? run_group<float>(b, p, in + i, out + i, count, ws, s)
-                                     : run_group<bf16_t>(b, p, in + i, out + i, count, ws, s));
+        FLCE_TRY(p.gram_planes == 2 ? (run_group<float, 2, 2>(b, p, in + i, out + i, count, ws, s))
+                 : p.planes == 2    ? (run_group<bf16_t, 1, 2>(b, p, in + i, out + i, count, ws, s))
+                                    : (run_group<bf16_t, 1, 1>(b, p, in + i, out + i, count, ws, s)));
     }
     return FLCE_OK;
 }
 
 size_t flce_orthogonalize_workspace_bytes(int n_matrices, const flce_orthogonalize_args* args) {
     OrPlan p;
-    return or_plan(args, n_matrices, &p) == FLCE_OK && n_matrices ? (size_t)p.group * p.bytes : 0;
+    return or_plan(args, n_matrices, &p) == FLCE_OK && n_matrices ? p.part_bytes + (size_t)p.group * p.bytes : 0;
 }
 
 }  // extern "C"
