@@ -31,7 +31,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int OR_MATRICES = 120;   // a launch's arguments stay below 4 KB
 constexpr int OR_PAD = 64;         // rows and columns are padded with zeros to whole K steps
-constexpr int OR_NORM_BLOCKS = 32; // workgroups that add up a matrix's squares
+constexpr int OR_NORM_BLOCKS = 64; // workgroups that add up a matrix's squares
 
 constexpr int OR_SMALL = 256;      // bf16: A and B in two planes up to this many (padded) rows
 constexpr float OR_CARRY = 16.0f;
@@ -90,19 +90,19 @@ __device__ __forceinline__ void or_split(const float (&v)[8], u32x4& hi, u32x4& 
 // Squares of a matrix, in fp64; workgroup (p, matrix) adds up its share.
 template <typename T>
 __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
-    constexpr int N = RowVec<T>::N;
+    constexpr int N = RowVec<T>::N, AHEAD = 8;
     __shared__ double red[4];
     const T* in = static_cast<const T*>(a.in[blockIdx.y]);
     const int64_t all = (int64_t)a.rows * a.cols;
     const int nfull = (int)(all / N), rem = (int)(all % N), nvec = nfull + (rem ? 1 : 0);
     const int v0 = (int)((int64_t)nvec * blockIdx.x / OR_NORM_BLOCKS), v1 = (int)((int64_t)nvec * (blockIdx.x + 1) / OR_NORM_BLOCKS);
     double s = 0.0;
-    for (int v = v0 + (int)threadIdx.x; v < v1; v += 4 * 256) {
-        u32x4 raw[4];
+    for (int v = v0 + (int)threadIdx.x; v < v1; v += AHEAD * 256) {
+        u32x4 raw[AHEAD];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) raw[k] = row_load(in, v + k * 256, min(nfull, v1), v1 > nfull ? rem : 0);
+        for (int k = 0; k < AHEAD; ++k) raw[k] = row_load(in, v + k * 256, min(nfull, v1), v1 > nfull ? rem : 0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < AHEAD; ++k) {
             float f[N];
             RowVec<T>::unpack(raw[k], f);
 #pragma unroll
@@ -318,6 +318,7 @@ struct OrOut {
     int lane;
     float* stage;
     u32x4 addend[IN ? 2 : 1][NACC][IN ? IN : 1];
+    static_assert(64 * PITCH * 4 <= fg_lds_bytes(TILE) / 4, "two passes fit a wavefront's share of LDS");
 
     __device__ __forceinline__ void init(const f16_t* in, f16_t* to, int ld_, int rows_, bool add, int r0, int c0, unsigned char* smem,
                                          int lane_, int uwave) {
@@ -351,12 +352,15 @@ struct OrOut {
             }
         }
     }
+    // (Both stores have their whole offset in a vector register.  With part of it in a scalar one the compiler takes the
+    // data for read at once and may let the very next instruction overwrite it; on this chip the store then wrote some of
+    // the new values: one lo plane in 10^5, more where the memory pipe was full.)
     __device__ __forceinline__ void put_planes(int row, int col, const float (&v)[8], bool put_lo) {
         u32x4 hi, lo;
         or_split(v, hi, lo);
-        const int off = at<OUT>(row, col);
-        __builtin_amdgcn_raw_buffer_store_b128(hi, rsrc_out, off, 0, 0);
-        if (OUT == 2 && put_lo) __builtin_amdgcn_raw_buffer_store_b128(lo, rsrc_out, off, ld * 2, 0);
+        const uint32_t off = (uint32_t)at<OUT>(row, col);
+        __builtin_amdgcn_raw_buffer_store_b128(hi, rsrc_out, (int)off, 0, 0);
+        if (OUT == 2 && put_lo) __builtin_amdgcn_raw_buffer_store_b128(lo, rsrc_out, (int)(off + 2u * (uint32_t)ld), 0, 0);
     }
     static __device__ __forceinline__ void put_out(OutT* out, int rows, int cols, int row, int col, const float (&v)[8]) {
         if (row >= rows || col >= cols) return;
@@ -377,69 +381,85 @@ struct OrOut {
         }
     }
 
-    // The passes; load_addend<0>(0) has been issued before.  alpha: with the matrix's factor.
-    __device__ __forceinline__ void write(f32x16 (&acc)[W][W], const OrArgs& a, float alpha, int matrix, bool mirror) {
+    // 4 values of a row of the stage.  Groups of 8 rows have them in another order each: what turned() reads at a time, 8
+    // columns of 8 rows that are 8 apart, lies in 64 banks.
+    __device__ __forceinline__ f32x4* staged(int row, int group) const {
+        return reinterpret_cast<f32x4*>(stage + row * PITCH + (group ^ ((row >> 3) & 7)) * 4);
+    }
+    // Rows 32 i .. of the wavefront's part, from its accumulators of them; their addend is in buffer BUF.  TURN, MIRROR:
+    // they are left in half H of the stage, for turned().
+    template <int BUF, int H>
+    __device__ __forceinline__ void pass(f32x16 (&acc)[W], const OrArgs& a, float alpha, OutT* out, int i) {
         const int frow = lane & 31, fhalf = lane >> 5;
-        OutT* out = LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
         const bool put_lo = PRODUCT != OR_APPLY || PL == 2 || a.put_lo;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if (i + 1 < W) {
-                if (i % 2 == 0) load_addend<IN ? 1 : 0>(i + 1); else load_addend<0>(i + 1);
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float v0 = acc[j][4 * g], v1 = acc[j][4 * g + 1], v2 = acc[j][4 * g + 2], v3 = acc[j][4 * g + 3];
+                *staged(H * 32 + frow, 8 * j + 2 * g + fhalf) = f32x4{v0, v1, v2, v3};
             }
+        // (the region is the wavefront's own, and LDS executes its accesses in order)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-            for (int j = 0; j < W; ++j)
+        for (int k = 0; k < NACC; ++k) {
+            float v[8];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float v0 = acc[i][j][4 * g], v1 = acc[i][j][4 * g + 1], v2 = acc[i][j][4 * g + 2], v3 = acc[i][j][4 * g + 3];
-                    *reinterpret_cast<f32x4*>(stage + frow * PITCH + 32 * j + 8 * g + 4 * fhalf) = f32x4{v0, v1, v2, v3};
-                }
-            // (the region is the wavefront's own, and LDS executes its accesses in order)
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            for (int e = 0; e < 8; e += 4) {
+                const f32x4 q = *staged(H * 32 + lane_row(k), (lane_col() + e) / 4);
 #pragma unroll
-            for (int k = 0; k < NACC; ++k) {
-                float* src = stage + lane_row(k) * PITCH + lane_col();
-                float v[8];
+                for (int u = 0; u < 4; ++u) v[e + u] = alpha * q[u];
+            }
+            if constexpr (IN > 0) {
 #pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    const f32x4 q = *reinterpret_cast<const f32x4*>(src + e);
+                for (int p = IN - 1; p >= 0; --p) {
+                    const f16x8 w = __builtin_bit_cast(f16x8, addend[BUF][k][p]);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) v[e + u] = alpha * q[u];
-                }
-                if constexpr (IN > 0) {
-#pragma unroll
-                    for (int p = IN - 1; p >= 0; --p) {
-                        const f16x8 w = __builtin_bit_cast(f16x8, addend[i % 2][k][p]);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = fmaf(a.beta, (float)w[e], v[e]);
-                    }
-                }
-                const int row = row0 + 32 * i + lane_row(k), col = col0 + lane_col();
-                if constexpr (PRODUCT == OR_POLY) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += row == col + e ? a.diagonal : 0.f;
-                }
-                if constexpr (!LAST) put_planes(row, col, v, put_lo);
-                else if constexpr (!TALL) put_out(out, a.rows, a.cols, row, col, v);
-                if constexpr (TURN || MIRROR) {
-#pragma unroll
-                    for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4*>(src + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(a.beta, (float)w[e], v[e]);
                 }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if ((MIRROR && mirror) || TURN) {
-                // lane: column lane / 4 + 16 k, rows 8 (lane % 4) .. + 7 of the pass
+            const int row = row0 + 32 * i + lane_row(k), col = col0 + lane_col();
+            if constexpr (PRODUCT == OR_POLY) {
 #pragma unroll
-                for (int k = 0; k < WN / 16; ++k) {
-                    const int c = lane / 4 + 16 * k, r = lane % 4 * 8;
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = stage[(r + e) * PITCH + c];
-                    if constexpr (TURN) put_out(out, a.rows, a.cols, col0 + c, row0 + 32 * i + r, v);
-                    else put_planes(col0 + c, row0 + 32 * i + r, v, put_lo);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                for (int e = 0; e < 8; ++e) v[e] += row == col + e ? a.diagonal : 0.f;
             }
+            if constexpr (!LAST) put_planes(row, col, v, put_lo);
+            else if constexpr (!TALL) put_out(out, a.rows, a.cols, row, col, v);
+            if constexpr (TURN || MIRROR) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 4)
+                    *staged(H * 32 + lane_row(k), (lane_col() + e) / 4) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    // The 64 rows (PASSES = 2) or 32 in the stage, whose first is row 32 i, as columns: whole lines of 128 bytes of 16-bit
+    // values.
+    template <int PASSES>
+    __device__ __forceinline__ void turned(const OrArgs& a, OutT* out, int i) {
+        constexpr int LPC = 4 * PASSES;   // lanes per column
+        const bool put_lo = PRODUCT != OR_APPLY || PL == 2 || a.put_lo;
+#pragma unroll
+        for (int k = 0; k < WN * LPC / 64; ++k) {
+            const int c = lane / LPC + 64 / LPC * k, r = lane % LPC * 8;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const float*>(staged(r + e, c / 4))[c % 4];
+            if constexpr (TURN) put_out(out, a.rows, a.cols, col0 + c, row0 + 32 * i + r, v);
+            else put_planes(col0 + c, row0 + 32 * i + r, v, put_lo);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    // All of it; load_addend<0>(0) has been issued before.  alpha: with the matrix's factor.
+    __device__ __forceinline__ void write(f32x16 (&acc)[W][W], const OrArgs& a, float alpha, int matrix, bool mirror) {
+        OutT* out = LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
+#pragma unroll
+        for (int i = 0; i < W; i += 2) {
+            load_addend<IN ? 1 : 0>(i + 1);
+            pass<0, 0>(acc[i], a, alpha, out, i);
+            if (i + 2 < W) load_addend<0>(i + 2);
+            pass<IN ? 1 : 0, 1>(acc[i + 1], a, alpha, out, i + 1);
+            if (TURN || (MIRROR && mirror)) turned<2>(a, out, i);
         }
     }
 };
@@ -473,10 +493,11 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave >> 1, wn = wave & 1;
     // workgroups go round-robin to the XCDs: each gets a stretch of tiles, range by range
-    const int all = a.tiles * a.count, total = PART == OR_RANGES ? all * a.ranges : all, per_xcd = (total + FG_XCDS - 1) / FG_XCDS;
+    const int all = a.tiles * a.count, total = all * (PART == OR_RANGES ? a.ranges : PART == OR_JOIN ? W : 1);
+    const int per_xcd = (total + FG_XCDS - 1) / FG_XCDS;
     int seq = (int)blockIdx.x % FG_XCDS * per_xcd + (int)blockIdx.x / FG_XCDS;
     if ((int)blockIdx.x / FG_XCDS >= per_xcd || seq >= total) return;
-    const int range = PART == OR_RANGES ? seq / all : 0;
+    const int range = PART == OR_WHOLE ? 0 : seq / all;   // (OR_JOIN: a workgroup does one pass of its wavefronts)
     seq -= range * all;
     const int matrix = seq / a.tiles;
     int tm, tn;
@@ -488,26 +509,46 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
 
     const f16_t* X = a.X + matrix * a.stride_x;
     const int K = PRODUCT == OR_GRAM ? a.np : a.mp, N = SYMMETRIC ? a.mp : a.np;
-    f32x16 acc[W][W];
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-#pragma unroll
-            for (int g = 0; g < 16; ++g) acc[i][j][g] = 0.f;
     // The sums of a range: accumulators as they lie, 16 bytes per lane.
-    constexpr int64_t TILE_FLOATS = (int64_t)TILE * TILE;
     auto part_at = [&](int r, int i, int j, int g) {
-        return reinterpret_cast<f32x4*>(a.part + ((int64_t)r * all + seq) * TILE_FLOATS + (((i * W + j) * 4 + g) * FG_THREADS + tid) * 4);
+        return reinterpret_cast<f32x4*>(a.part + ((int64_t)r * all + seq) * (TILE * TILE) + (((i * W + j) * 4 + g) * FG_THREADS + tid) * 4);
     };
+    float alpha = a.alpha;
+    if (PRODUCT != OR_POLY && a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : a.factor[matrix];
     OrOut<PRODUCT, PL, OUT, TILE, OutT, TALL> out;
     auto begin_out = [&]() {
         out.init(PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N, a.mp,
                  PRODUCT == OR_POLY || a.add_lo, m0 + __builtin_amdgcn_readfirstlane(wm) * (TILE / 2),
                  n0 + __builtin_amdgcn_readfirstlane(wn) * (TILE / 2), smem, lane, uwave);
-        out.template load_addend<0>(0);
     };
-    if constexpr (PART != OR_JOIN) {
+    if constexpr (PART == OR_JOIN) {
+        constexpr int AHEAD = 4;   // ranges whose loads are under way
+        begin_out();
+        out.template load_addend<0>(range);
+        f32x16 acc[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int g = 0; g < 16; ++g) acc[j][g] = 0.f;
+        for (int r0 = 0; r0 < a.ranges; r0 += AHEAD) {
+            f32x4 v[AHEAD][W][4];
+#pragma unroll
+            for (int r = 0; r < AHEAD; ++r)
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) v[r][j][g] = *part_at(min(r0 + r, a.ranges - 1), range, j, g);
+#pragma unroll
+            for (int r = 0; r < AHEAD; ++r)
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+#pragma unroll
+                    for (int g = 0; g < 16; ++g) acc[j][g] += r0 + r < a.ranges ? v[r][j][g / 4][g % 4] : 0.f;
+        }
+        OutT* to = PRODUCT == OR_LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
+        out.template pass<0, 0>(acc, a, alpha, to, range);
+        if (out.TURN || (out.MIRROR && tm != tn)) out.template turned<1>(a, to, range);
+    } else {
         // operands: X X^T, A A (A is symmetric), B X
         const f16_t* left = PRODUCT == OR_GRAM ? X : (PRODUCT == OR_POLY ? a.A : a.B) + matrix * a.stride_a;
         const f16_t* right = PRODUCT == OR_POLY ? left : X;
@@ -532,41 +573,35 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
             opb.lo_part = 0;
             nk *= 3;
         }
-        FgRaw<false> raw_a[2][W];
-        FgRaw<B_KM> raw_b[2][W];
-        or_k_loop(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
-        if constexpr (PART == OR_WHOLE) begin_out();
-        or_last_quarter(acc, raw_a, raw_b);
-        or_drain();
-    }
-    if constexpr (PART == OR_RANGES) {
+        f32x16 acc[W][W];
 #pragma unroll
         for (int i = 0; i < W; ++i)
 #pragma unroll
             for (int j = 0; j < W; ++j)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float v0 = acc[i][j][4 * g], v1 = acc[i][j][4 * g + 1], v2 = acc[i][j][4 * g + 2], v3 = acc[i][j][4 * g + 3];
-                    *part_at(range, i, j, g) = f32x4{v0, v1, v2, v3};
-                }
-    } else {
-        if constexpr (PART == OR_JOIN) {
+                for (int g = 0; g < 16; ++g) acc[i][j][g] = 0.f;
+        FgRaw<false> raw_a[2][W];
+        FgRaw<B_KM> raw_b[2][W];
+        or_k_loop(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
+        if constexpr (PART == OR_WHOLE) {
             begin_out();
-            for (int r = 0; r < a.ranges; ++r)
-#pragma unroll
-                for (int i = 0; i < W; ++i)
-#pragma unroll
-                    for (int j = 0; j < W; ++j)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const f32x4 v = *part_at(r, i, j, g);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += v[e];
-                        }
+            out.template load_addend<0>(0);
         }
-        float alpha = a.alpha;
-        if (a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : PRODUCT >= OR_APPLY ? a.factor[matrix] : 1.0f;
-        out.write(acc, a, alpha, matrix, tm != tn);
+        or_last_quarter(acc, raw_a, raw_b);
+        or_drain();
+        if constexpr (PART == OR_WHOLE) {
+            out.write(acc, a, alpha, matrix, tm != tn);
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const float v0 = acc[i][j][4 * g], v1 = acc[i][j][4 * g + 1], v2 = acc[i][j][4 * g + 2], v3 = acc[i][j][4 * g + 3];
+                        *part_at(range, i, j, g) = f32x4{v0, v1, v2, v3};
+                    }
+        }
     }
 }
 

@@ -21,6 +21,7 @@ constexpr double OR_MAX_NORM = 1024.0;                   // that a singular valu
 constexpr int64_t OR_TILES_256 = 128;                    // fewest tiles of 256 that a launch takes those for
 constexpr int64_t OR_SLOTS_128 = 512;                    // workgroups of 128-tiles that run at a time
 constexpr int64_t OR_RANGE_STEPS = 4, OR_MAX_RANGES = 16;   // fewest K steps of a range, most ranges
+constexpr int64_t OR_SAVED_STEPS = 32;                   // K steps one after the other that ranges have to save
 constexpr int64_t OR_ROUNDS = 1024;                      // tiles of a launch that more matrices would not fill better
 constexpr float OR_USUAL[3] = {3.4445f, -4.7750f, 2.0315f};
 
@@ -125,16 +126,16 @@ int launch_product(OrArgs& a, hipStream_t s) {
         HIP_TRY(hipGetLastError());
         return FLCE_OK;
     }
-    const int64_t total = tiles_of(128), steps = (PRODUCT == OR_GRAM ? a.np : a.mp) / FG_BK;
-    a.ranges = (int)std::min({OR_MAX_RANGES, OR_SLOTS_128 / total, steps * (PL == 2 ? 3 : 1) / OR_RANGE_STEPS, steps});
-    if (a.ranges <= 1) {
+    const int64_t total = tiles_of(128), steps = (PRODUCT == OR_GRAM ? a.np : a.mp) / FG_BK, turns = steps * (PL == 2 ? 3 : 1);
+    a.ranges = (int)std::min({OR_MAX_RANGES, OR_SLOTS_128 / total, turns / OR_RANGE_STEPS, steps});
+    if (a.ranges <= 1 || turns - turns / a.ranges < OR_SAVED_STEPS) {
         hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_WHOLE>), grid(total), dim3(FG_THREADS), 0, s, a);
         HIP_TRY(hipGetLastError());
         return FLCE_OK;
     }
     hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_RANGES>), grid(total * a.ranges), dim3(FG_THREADS), 0, s, a);
     HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_JOIN>), grid(total), dim3(FG_THREADS), 0, s, a);
+    hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_JOIN>), grid(2 * total), dim3(FG_THREADS), 0, s, a);
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
 }
