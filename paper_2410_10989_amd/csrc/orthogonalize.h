@@ -94,20 +94,27 @@ __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
     __shared__ double red[4];
     const T* in = static_cast<const T*>(a.in[blockIdx.y]);
     const int64_t all = (int64_t)a.rows * a.cols;
-    const int nfull = (int)(all / N), rem = (int)(all % N), nvec = nfull + (rem ? 1 : 0);
-    const int v0 = (int)((int64_t)nvec * blockIdx.x / OR_NORM_BLOCKS), v1 = (int)((int64_t)nvec * (blockIdx.x + 1) / OR_NORM_BLOCKS);
+    const int nfull = (int)(all / N), rem = (int)(all % N);
+    const int v0 = (int)((int64_t)nfull * blockIdx.x / OR_NORM_BLOCKS), v1 = (int)((int64_t)nfull * (blockIdx.x + 1) / OR_NORM_BLOCKS);
     double s = 0.0;
     for (int v = v0 + (int)threadIdx.x; v < v1; v += AHEAD * 256) {
-        u32x4 raw[AHEAD];
+        u32x4 raw[AHEAD];   // (all loads before the first sum; past the share the last one again)
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) raw[k] = row_load(in, v + k * 256, min(nfull, v1), v1 > nfull ? rem : 0);
+        for (int k = 0; k < AHEAD; ++k) raw[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)min(v + k * 256, v1 - 1) * N);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             float f[N];
             RowVec<T>::unpack(raw[k], f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) s = fma((double)f[e], (double)f[e], s);
+            for (int e = 0; e < N; ++e) {
+                const double x = v + k * 256 < v1 ? (double)f[e] : 0.0;
+                s = fma(x, x, s);
+            }
         }
+    }
+    if (blockIdx.x == OR_NORM_BLOCKS - 1 && (int)threadIdx.x < rem) {
+        const double x = (double)to_f32(in[(int64_t)nfull * N + threadIdx.x]);
+        s = fma(x, x, s);
     }
     s = wave_sum(s);
     if (threadIdx.x % WAVE == 0) red[threadIdx.x / WAVE] = s;
@@ -602,6 +609,151 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
                         *part_at(range, i, j, g) = f32x4{v0, v1, v2, v3};
                     }
         }
+    }
+}
+
+// All steps of small bf16 matrices between the first Gram product and the last B X, in m x m matrices alone (all of them
+// polynomials of A, hence symmetric, and they commute):
+//
+//     B_k = a I + b A_k + c A_k A_k,   A_{k+1} = B_k A_k B_k,   Q = B_{steps-1} ... B_0,   out = s Q X
+//
+// One workgroup per matrix, two planes throughout, in LDS.  A's rounding errors (2^-22 of its largest eigenvalue) grow with
+// a^2 per step as the smallest eigenvalues do: up to OR_ITERATE_GROWTH, so fp32 matrices do not come here (their
+// smallest eigenvalues may be as small as that), and bf16 ones are off by 1e-3 at most of what their rounding costs.
+// The launches between are what small matrices cost: 4 x 64 x 512 TIMES.
+constexpr int OR_ITERATE_MOST = 128, OR_ITERATE_STEPS = 8;   // (padded) rows, steps
+struct OrIterateArgs {
+    const f16_t* A;      // of the first matrix; and where Q goes
+    f16_t* Q;
+    f16_t* B;            // steps matrices for each
+    int64_t stride_a;
+    int steps;
+    float square[OR_ITERATE_STEPS], linear[OR_ITERATE_STEPS], diagonal[OR_ITERATE_STEPS];   // of B
+    float t[OR_ITERATE_STEPS], next[OR_ITERATE_STEPS], q[OR_ITERATE_STEPS];                 // powers of two of B A, (B A) B, B Q
+};
+
+template <int MP>
+__global__ __launch_bounds__(256) void or_iterate_kernel(OrIterateArgs a) {
+    constexpr int W = MP / 64, PITCH = MP + 8;   // (rows 16 bytes further by 4 banks each)
+    __shared__ __attribute__((aligned(16))) f16_t lds[2][2][MP * PITCH];   // two matrices of two planes
+    const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
+    const int row0 = wave / 2 * (MP / 2), col0 = wave % 2 * (MP / 2), frow = lane & 31, fhalf = lane >> 5;
+    const int64_t matrix = blockIdx.x;
+
+    f32x16 acc[W][W];
+    // acc = left * right (symmetric, so its rows are its columns), the small products first
+    auto product = [&](const f16_t (&left)[2][MP * PITCH], const f16_t (&right)[2][MP * PITCH]) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+#pragma unroll
+                for (int g = 0; g < 16; ++g) acc[i][j][g] = 0.f;
+        auto fragment = [&](const f16_t* m, int r0, int k) {
+            return *reinterpret_cast<const bf16x8*>(m + (r0 + frow) * PITCH + k * 16 + fhalf * 8);
+        };
+        auto part = [&](int pl, int pr) {
+#pragma unroll
+            for (int k = 0; k < MP / 16; ++k) {
+                bf16x8 fa[W], fb[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    fa[i] = fragment(left[pl], row0 + 32 * i, k);
+                    fb[i] = fragment(right[pr], col0 + 32 * i, k);
+                }
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) acc[i][j] = or_mfma(fb[j], fa[i], acc[i][j]);
+            }
+        };
+        part(0, 1);
+        part(1, 0);
+        part(0, 0);
+    };
+    // what to do with four consecutive values of a row of acc
+    auto each = [&](auto what) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e];
+                    what(row0 + 32 * i + frow, col0 + 32 * j + 8 * g + 4 * fhalf, v);
+                }
+    };
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    auto split4 = [](const float (&v)[4], f16x4& hi, f16x4& lo) {   // (as or_split)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float x = v[e];
+            asm("" : "+v"(x));
+            hi[e] = (f16_t)x;
+            lo[e] = (f16_t)(x - (float)hi[e]);
+        }
+    };
+    auto put = [&](f16_t (&to)[2][MP * PITCH], float scale) {
+        each([&](int row, int col, float (&v)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= scale;
+            f16x4 hi, lo;
+            split4(v, hi, lo);
+            *reinterpret_cast<f16x4*>(&to[0][row * PITCH + col]) = hi;
+            *reinterpret_cast<f16x4*>(&to[1][row * PITCH + col]) = lo;
+        });
+    };
+    auto fetch = [&](f16_t (&to)[2][MP * PITCH], const f16_t* from) {   // planes in memory: rows of [hi MP | lo MP]
+        for (int i = tid; i < MP * MP / 4; i += 256) {
+            const int row = i / (MP / 4), at = i % (MP / 4) * 8, plane = at / MP, col = at % MP;
+            *reinterpret_cast<u32x4*>(&to[plane][row * PITCH + col]) = *reinterpret_cast<const u32x4*>(from + (int64_t)row * 2 * MP + at);
+        }
+    };
+    f16_t* Bs = a.B + matrix * a.steps * a.stride_a;
+    fetch(lds[0], a.A + matrix * a.stride_a);
+    __syncthreads();
+    for (int k = 0; k < a.steps; ++k) {
+        product(lds[0], lds[0]);
+        each([&](int row, int col, float (&v)[4]) {
+            const f16x4 hi = *reinterpret_cast<const f16x4*>(&lds[0][0][row * PITCH + col]);
+            const f16x4 lo = *reinterpret_cast<const f16x4*>(&lds[0][1][row * PITCH + col]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = a.square[k] * v[e] + a.linear[k] * ((float)hi[e] + (float)lo[e]) + (row == col + e ? a.diagonal[k] : 0.f);
+            f16x4 h, l;
+            split4(v, h, l);
+            *reinterpret_cast<f16x4*>(&lds[1][0][row * PITCH + col]) = h;
+            *reinterpret_cast<f16x4*>(&lds[1][1][row * PITCH + col]) = l;
+            f16_t* to = Bs + k * a.stride_a + (int64_t)row * 2 * MP + col;
+            *reinterpret_cast<f16x4*>(to) = h;
+            *reinterpret_cast<f16x4*>(to + MP) = l;
+        });
+        __syncthreads();
+        if (k + 1 == a.steps) break;
+        product(lds[1], lds[0]);
+        __syncthreads();
+        put(lds[0], a.t[k]);
+        __syncthreads();
+        product(lds[0], lds[1]);
+        __syncthreads();
+        put(lds[0], a.next[k]);
+        __syncthreads();
+    }
+    // Q: the last B is in lds[1], the others (and it) in memory, where this workgroup wrote them
+    for (int k = a.steps - 2; k >= 0; --k) {
+        fetch(lds[0], Bs + k * a.stride_a);
+        __syncthreads();
+        product(lds[0], lds[1]);
+        __syncthreads();
+        put(lds[1], a.q[k]);
+        __syncthreads();
+    }
+    f16_t* Q = a.Q + matrix * a.stride_a;
+    for (int i = tid; i < MP * MP / 4; i += 256) {
+        const int row = i / (MP / 4), at = i % (MP / 4) * 8, plane = at / MP, col = at % MP;
+        *reinterpret_cast<u32x4*>(Q + (int64_t)row * 2 * MP + at) = *reinterpret_cast<const u32x4*>(&lds[1][plane][row * PITCH + col]);
     }
 }
 

@@ -17,6 +17,7 @@ namespace {
 constexpr int64_t OR_MAX_DIM = (int64_t)1 << 20;         // a tile's rows stay below 2^31 bytes apart
 constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: its planes stay below 2^30 bytes
 constexpr int OR_MAX_STEPS = 32;
+constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
 constexpr int64_t OR_TILES_256 = 128;                    // fewest tiles of 256 that a launch takes those for
 constexpr int64_t OR_SLOTS_128 = 512;                    // workgroups of 128-tiles that run at a time
@@ -33,11 +34,14 @@ struct OrStep {
     float a, b, c;
     int e_x, e_a, e_b;   // X, A and B are held times 2 to these
     bool lo;             // X is needed in two planes
+    double most_b;       // B's largest eigenvalue
 };
 struct OrPlan {
     int64_t mp, np;
     int planes;                       // that POLY and APPLY multiply, and of A and B
     int gram_planes;                  // that GRAM multiplies
+    bool iterate;                     // the steps in m x m matrices alone (or_iterate_kernel)
+    int b_matrices;                   // that there is room for
     int64_t group;                    // matrices at a time
     size_t x_bytes, a_bytes, bytes;   // of one matrix: X (there are two), A (and B); all of them, and its partial sums
     size_t part_bytes;                // K ranges' sums, of all matrices
@@ -71,7 +75,7 @@ int steps_of(const flce_orthogonalize_args& b, OrStep* to) {
         } else if (B != 0.0) {
             at(-A / (3.0 * B), next, most_x);
         }
-        to[k] = {p[0], p[1], p[2], exponent_for(s), exponent_for(l1), exponent_for(most_b), false};
+        to[k] = {p[0], p[1], p[2], exponent_for(s), exponent_for(l1), exponent_for(most_b), false, most_b};
         s = std::max(most_x, 0x1p-20) * 1.01;   // (what rounding may add)
         if (!(s <= OR_MAX_NORM)) return FLCE_ERR_ARG;
     }
@@ -99,7 +103,12 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     p->planes = b.dtype == FLCE_F32 || p->mp <= OR_SMALL ? 2 : 1;
     p->x_bytes = aligned_bytes((size_t)(p->mp * p->np) * 2 * sizeof(f16_t));
     p->a_bytes = aligned_bytes((size_t)(p->mp * p->mp) * p->planes * sizeof(f16_t));
-    p->bytes = 2 * p->x_bytes + 2 * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) + 256;
+    float growth = 1.0f;
+    for (int k = 0; k + 1 < b.steps; ++k) growth = std::min(growth * std::max(1.0f, p->steps[k].a * p->steps[k].a), 1e30f);
+    const bool small = b.dtype == FLCE_BF16 && p->mp <= OR_ITERATE_MOST;
+    p->iterate = small && b.steps <= OR_ITERATE_STEPS && growth <= OR_ITERATE_GROWTH;
+    p->b_matrices = small ? OR_ITERATE_STEPS + 1 : 1;   // (the same room whatever the steps are)
+    p->bytes = 2 * p->x_bytes + (1 + p->b_matrices) * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) + 256;
     p->part_bytes = OR_SLOTS_128 * 128 * 128 * sizeof(float);
     // Matrices at a time: until the launch with the fewest tiles has several rounds of them.
     const int64_t t = (p->mp + 255) / 256, tiles = t * (t + 1) / 2;
@@ -153,7 +162,7 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     f16_t* X[2];
     for (f16_t*& x : X) x = reinterpret_cast<f16_t*>(take(count * p.x_bytes));
     f16_t* A = reinterpret_cast<f16_t*>(take(count * p.a_bytes));
-    f16_t* B = reinterpret_cast<f16_t*>(take(count * p.a_bytes));
+    f16_t* B = reinterpret_cast<f16_t*>(take(count * p.b_matrices * p.a_bytes));
     OrLoadArgs l{};
     l.partial = reinterpret_cast<double*>(take(count * OR_NORM_BLOCKS * sizeof(double)));
     l.factor = reinterpret_cast<float*>(take(count * sizeof(float)));
@@ -185,6 +194,44 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     a.cols = l.cols;
     a.part = reinterpret_cast<float*>(ws);
     for (int i = 0; i < count; ++i) a.out[i] = out[i];
+    if constexpr (GP == 1 && PL == 2) {
+        if (p.iterate) {
+            const OrStep& first = p.steps[0];
+            a.factor = l.factor;
+            a.X = X[0];
+            a.to = A;
+            a.alpha = ldexpf(1.0f, first.e_a - 2 * first.e_x);
+            FLCE_TRY((launch_product<OR_GRAM, GP, PL, float, false>(a, s)));
+            OrIterateArgs it{};
+            it.A = A;
+            it.Q = B;
+            it.B = B + count * a.stride_a;
+            it.stride_a = a.stride_a;
+            it.steps = b.steps;
+            double most_q = p.steps[b.steps - 1].most_b;
+            int e_q = p.steps[b.steps - 1].e_b;
+            for (int k = b.steps - 1; k >= 0; --k) {
+                const OrStep& st = p.steps[k];
+                it.square[k] = ldexpf(st.c, st.e_b - 2 * st.e_a);
+                it.linear[k] = ldexpf(st.b, st.e_b - st.e_a);
+                it.diagonal[k] = ldexpf(st.a, st.e_b);
+                if (k + 1 == b.steps) continue;
+                const int e_t = exponent_for(st.most_b * ldexp(1.0, 14 - st.e_a));   // (A's eigenvalues: at most 2^(14 - e_a))
+                it.t[k] = ldexpf(1.0f, e_t - st.e_b - st.e_a);
+                it.next[k] = ldexpf(1.0f, p.steps[k + 1].e_a - e_t - st.e_b);
+                most_q *= st.most_b;
+                const int e = exponent_for(most_q);
+                it.q[k] = ldexpf(1.0f, e - e_q - st.e_b);
+                e_q = e;
+            }
+            if (p.mp == 64) hipLaunchKernelGGL((or_iterate_kernel<64>), dim3((unsigned)count), dim3(256), 0, s, it);
+            else hipLaunchKernelGGL((or_iterate_kernel<128>), dim3((unsigned)count), dim3(256), 0, s, it);
+            HIP_TRY(hipGetLastError());
+            a.alpha = ldexpf(b.scale, -e_q - first.e_x);
+            if (tall) return launch_product<OR_LAST, PL, 2, T, true>(a, s);
+            return launch_product<OR_LAST, PL, 2, T, false>(a, s);
+        }
+    }
     for (int k = 0; k < b.steps; ++k) {
         const OrStep& st = p.steps[k];
         a.factor = k == 0 ? l.factor : nullptr;
