@@ -5,6 +5,11 @@
 //
 // drives every singular value of X towards 1 and keeps its singular vectors.  Per step 2 m^2 n + 2 m^3 + 2 m^2 n
 // operations; A and B are symmetric, so only the tiles on and below the diagonal are computed, the others mirrored.
+// Two steps at a time, where n is twice m or more: A' = (B A) B stands for the Gram product of the X between them, which is
+// never formed, and X <- (B' B) X: three symmetric m^3 products instead of m^2 n + 2 m^2 n, and X is read and
+// written once less (24 x 4096 x 1024: TIMES).  A's rounding errors grow by a^2 in A', so never two such pairs in a
+// row: with (2, 1, 2) of five steps the result is as far off as step by step, with (2, 2, 1) up to 1.5 times, with all
+// five at once 0.2.
 //
 // Numbers.  The iteration multiplies the smallest singular values by a^steps (485 for five of the usual steps), and any
 // error in their directions with them.  The operands of the products are fp16, scaled by powers of two that keep them
@@ -36,7 +41,8 @@ constexpr int OR_NORM_BLOCKS = 64; // workgroups that add up a matrix's squares
 constexpr int OR_SMALL = 256;      // bf16: A and B in two planes up to this many (padded) rows
 constexpr float OR_CARRY = 16.0f;
 
-enum { OR_GRAM = 0, OR_POLY = 1, OR_APPLY = 2, OR_LAST = 3 };   // A = X X^T, B = a I + b A + c A A, X <- B X, out = s B X
+// A = X X^T, B = a I + b A + c A A, A B (of symmetric matrices that commute: symmetric), X <- B X, out = s B X
+enum { OR_GRAM = 0, OR_POLY = 1, OR_MULTIPLY = 2, OR_APPLY = 3, OR_LAST = 4 };
 // A launch does whole products, or K ranges of them whose sums it leaves, or adds those up and writes the results.
 enum { OR_WHOLE = 0, OR_RANGES = 1, OR_JOIN = 2 };
 
@@ -314,7 +320,7 @@ struct OrOut {
     static constexpr int WN = TILE / 2, W = TILE / 64;
     static constexpr int LANES = WN / 8, ROWS = 64 / LANES, NACC = 32 / ROWS;   // lanes per row, rows and accesses per pass
     static constexpr int PITCH = WN + 4;
-    static constexpr bool LAST = PRODUCT == OR_LAST, TURN = LAST && TALL, MIRROR = PRODUCT <= OR_POLY;
+    static constexpr bool LAST = PRODUCT == OR_LAST, TURN = LAST && TALL, MIRROR = PRODUCT <= OR_MULTIPLY;
     static constexpr int IN = PRODUCT == OR_POLY ? PL : PRODUCT >= OR_APPLY && PL == 1 ? 1 : 0;   // planes of the addend: A, X's lo
     static constexpr bool LO_ONLY = PRODUCT >= OR_APPLY;
 
@@ -492,7 +498,7 @@ __device__ __forceinline__ void or_tile(int t, int tiles_m, int tiles_n, int& tm
 // One workgroup per tile of a matrix (and K range of it), 256 x 256, or 128 x 128 and two workgroups per CU.
 template <int PRODUCT, int PL, int OUT, int TILE, typename OutT, bool TALL, int PART>
 __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_kernel(OrArgs a) {
-    constexpr bool SYMMETRIC = PRODUCT <= OR_POLY, B_KM = !SYMMETRIC;
+    constexpr bool SYMMETRIC = PRODUCT <= OR_MULTIPLY, B_KM = !SYMMETRIC;
     constexpr int ORDER = PL == 2 ? FG_PLANES : FG_PLAIN, W = TILE / 64;
     // planes of the matrices' rows: X 2; A and B what the Gram product stores
     constexpr int PA = PRODUCT == OR_GRAM ? OUT : PL;
@@ -521,7 +527,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
         return reinterpret_cast<f32x4*>(a.part + ((int64_t)r * all + seq) * (TILE * TILE) + (((i * W + j) * 4 + g) * FG_THREADS + tid) * 4);
     };
     float alpha = a.alpha;
-    if (PRODUCT != OR_POLY && a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : a.factor[matrix];
+    if ((PRODUCT == OR_GRAM || PRODUCT >= OR_APPLY) && a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : a.factor[matrix];
     OrOut<PRODUCT, PL, OUT, TILE, OutT, TALL> out;
     auto begin_out = [&]() {
         out.init(PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N, a.mp,
@@ -556,10 +562,11 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
         out.template pass<0, 0>(acc, a, alpha, to, range);
         if (out.TURN || (out.MIRROR && tm != tn)) out.template turned<1>(a, to, range);
     } else {
-        // operands: X X^T, A A (A is symmetric), B X
-        const f16_t* left = PRODUCT == OR_GRAM ? X : (PRODUCT == OR_POLY ? a.A : a.B) + matrix * a.stride_a;
-        const f16_t* right = PRODUCT == OR_POLY ? left : X;
-        const int ldl = PRODUCT == OR_GRAM ? 2 * a.np : PA * a.mp, ldr = PRODUCT == OR_POLY ? PA * a.mp : 2 * a.np;
+        // operands: X X^T, A A, A B (rows of symmetric matrices for columns), B X
+        constexpr bool RIGHT_M = PRODUCT == OR_POLY || PRODUCT == OR_MULTIPLY;   // the right one is m x m
+        const f16_t* left = PRODUCT == OR_GRAM ? X : (PRODUCT >= OR_APPLY ? a.B : a.A) + matrix * a.stride_a;
+        const f16_t* right = PRODUCT == OR_POLY ? left : PRODUCT == OR_MULTIPLY ? a.B + matrix * a.stride_a : X;
+        const int ldl = PRODUCT == OR_GRAM ? 2 * a.np : PA * a.mp, ldr = RIGHT_M ? PA * a.mp : 2 * a.np;
         FgOperand<false, TILE, ORDER> opa;
         FgOperand<B_KM, TILE, ORDER> opb;
         opa.init(reinterpret_cast<const bf16_t*>(left), ldl, m0, a.mp, K, tid, wm);
@@ -575,7 +582,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
         if constexpr (PL == 2) {
             opa.plane_steps = opb.plane_steps = nk;
             opa.plane_bytes = (PRODUCT == OR_GRAM ? a.np : a.mp) * 2;
-            opb.plane_bytes = (PRODUCT == OR_POLY ? a.mp : a.np) * 2;
+            opb.plane_bytes = (RIGHT_M ? a.mp : a.np) * 2;
             opa.lo_part = 1;
             opb.lo_part = 0;
             nk *= 3;

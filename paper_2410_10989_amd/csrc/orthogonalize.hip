@@ -17,6 +17,7 @@ namespace {
 constexpr int64_t OR_MAX_DIM = (int64_t)1 << 20;         // a tile's rows stay below 2^31 bytes apart
 constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: its planes stay below 2^30 bytes
 constexpr int OR_MAX_STEPS = 32;
+constexpr int64_t OR_PAIR_LENGTH = 2;                    // n / m from which two steps are taken at a time
 constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
 constexpr int64_t OR_TILES_256 = 128;                    // fewest tiles of 256 that a launch takes those for
@@ -107,7 +108,7 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     for (int k = 0; k + 1 < b.steps; ++k) growth = std::min(growth * std::max(1.0f, p->steps[k].a * p->steps[k].a), 1e30f);
     const bool small = b.dtype == FLCE_BF16 && p->mp <= OR_ITERATE_MOST;
     p->iterate = small && b.steps <= OR_ITERATE_STEPS && growth <= OR_ITERATE_GROWTH;
-    p->b_matrices = small ? OR_ITERATE_STEPS + 1 : 1;   // (the same room whatever the steps are)
+    p->b_matrices = small ? OR_ITERATE_STEPS + 1 : 2;   // (the same room whatever the steps are)
     p->bytes = 2 * p->x_bytes + (1 + p->b_matrices) * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) + 256;
     p->part_bytes = OR_SLOTS_128 * 128 * 128 * sizeof(float);
     // Matrices at a time: until the launch with the fewest tiles has several rounds of them.
@@ -120,7 +121,7 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
 // run at a time.
 template <int PRODUCT, int PL, int OUT, typename OutT, bool TALL>
 int launch_product(OrArgs& a, hipStream_t s) {
-    constexpr bool SYMMETRIC = PRODUCT <= OR_POLY;
+    constexpr bool SYMMETRIC = PRODUCT <= OR_MULTIPLY;
     auto tiles_of = [&](int64_t tile) {
         a.tiles_m = (int)((a.mp + tile - 1) / tile);
         a.tiles_n = SYMMETRIC ? a.tiles_m : (int)((a.np + tile - 1) / tile);
@@ -232,27 +233,66 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
             return launch_product<OR_LAST, PL, 2, T, false>(a, s);
         }
     }
-    for (int k = 0; k < b.steps; ++k) {
-        const OrStep& st = p.steps[k];
+    // Two steps at a time where launches fill the chip and X is long (see orthogonalize.h), never twice in a row.
+    const int64_t t = (p.mp + 255) / 256;
+    const bool pairs = p.np >= OR_PAIR_LENGTH * p.mp && t * (t + 1) / 2 * count >= OR_TILES_256;
+    f16_t* spare = B + count * a.stride_a;
+    bool paired = false;
+    for (int k = 0, x = 0; k < b.steps; x ^= 1) {
+        const OrStep* st = &p.steps[k];
+        const int first_x = st->e_x;
+        const bool lo = st->lo;
         a.factor = k == 0 ? l.factor : nullptr;
-        a.X = X[k % 2];
+        a.X = X[x];
+        a.A = A;
         a.to = A;
-        a.alpha = ldexpf(1.0f, st.e_a - 2 * st.e_x);
+        a.alpha = ldexpf(1.0f, st->e_a - 2 * st->e_x);
         a.beta = 0.0f;
         a.add_lo = 0;
         FLCE_TRY((launch_product<OR_GRAM, GP, PL, float, false>(a, s)));
-        a.to = B;
-        a.alpha = ldexpf(st.c, st.e_b - 2 * st.e_a);
-        a.beta = ldexpf(st.b, st.e_b - st.e_a);
-        a.diagonal = ldexpf(st.a, st.e_b);
-        FLCE_TRY((launch_product<OR_POLY, PL, PL, float, false>(a, s)));
-        const bool last = k + 1 == b.steps;
-        const float scale = last ? b.scale : ldexpf(1.0f, p.steps[k + 1].e_x);
-        a.to = X[(k + 1) % 2];
-        a.alpha = ldexpf(scale, -st.e_b - st.e_x);
-        a.beta = ldexpf(scale * st.a, -st.e_x);
-        a.add_lo = PL == 1 && st.lo;
-        a.put_lo = !last && p.steps[k + 1].lo;
+        auto poly = [&](f16_t* to) {
+            a.to = to;
+            a.alpha = ldexpf(st->c, st->e_b - 2 * st->e_a);
+            a.beta = ldexpf(st->b, st->e_b - st->e_a);
+            a.diagonal = ldexpf(st->a, st->e_b);
+            return launch_product<OR_POLY, PL, PL, float, false>(a, s);
+        };
+        auto multiply = [&](const f16_t* left, const f16_t* right, f16_t* to, int exponent) {
+            a.A = left;
+            a.B = right;
+            a.to = to;
+            a.alpha = ldexpf(1.0f, exponent);
+            return launch_product<OR_MULTIPLY, PL, PL, float, false>(a, s);
+        };
+        FLCE_TRY(poly(B));
+        a.B = B;
+        int e_b = st->e_b;
+        float carried = st->a;
+        paired = pairs && !paired && k + 1 < b.steps;
+        if (paired) {
+            const OrStep* second = st + 1;
+            const int e_t = exponent_for(st->most_b * ldexp(1.0, 14 - st->e_a));   // (A's eigenvalues: at most 2^(14 - e_a))
+            FLCE_TRY(multiply(B, A, spare, e_t - st->e_b - st->e_a));
+            FLCE_TRY(multiply(spare, B, A, second->e_a - e_t - st->e_b));
+            const double most = st->most_b * second->most_b;
+            st = second;
+            a.A = A;
+            FLCE_TRY(poly(spare));
+            const int e = exponent_for(most);
+            FLCE_TRY(multiply(spare, B, A, e - st->e_b - e_b));
+            a.B = A;
+            e_b = e;
+            carried *= st->a;
+            ++k;
+        }
+        ++k;
+        const bool last = k == b.steps;
+        const float scale = last ? b.scale : ldexpf(1.0f, p.steps[k].e_x);
+        a.to = X[x ^ 1];
+        a.alpha = ldexpf(scale, -e_b - first_x);
+        a.beta = ldexpf(scale * carried, -first_x);
+        a.add_lo = PL == 1 && lo;
+        a.put_lo = !last && p.steps[k].lo;
         if (!last) FLCE_TRY((launch_product<OR_APPLY, PL, 2, float, false>(a, s)));
         else if (tall) FLCE_TRY((launch_product<OR_LAST, PL, 2, T, true>(a, s)));
         else FLCE_TRY((launch_product<OR_LAST, PL, 2, T, false>(a, s)));

@@ -61,7 +61,8 @@ def test_one_matrix(rows, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype,count,rows,cols", [("bf16", 5, 130, 70), ("f32", 3, 70, 130), ("bf16", 130, 33, 40), ("bf16", 20, 512, 512),
-                                                   ("f32", 14, 512, 768), ("bf16", 9, 1025, 600)])
+                                                   ("f32", 14, 512, 768), ("bf16", 9, 1025, 600), ("bf16", 50, 300, 640),
+                                                   ("bf16", 45, 1300, 520), ("f32", 44, 384, 800)])
 def test_lists(dtype, count, rows, cols):
     """Many matrices of a list, on both sizes of tiles, in several groups of launches."""
     import paper_2410_10989_amd as flce
@@ -88,12 +89,13 @@ def test_other_polynomials(kw, dtype):
     check(got, G, dtype, **{k: float(np.float32(v)) if k == "eps" else v for k, v in kw.items()})
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_matrices_of_low_rank(dtype):
+@pytest.mark.parametrize("dtype,rows,cols,count", [("f32", 192, 192, 1), ("bf16", 192, 192, 1), ("bf16", 60, 100, 1), ("bf16", 128, 128, 1),
+                                                   ("bf16", 320, 320, 1), ("bf16", 300, 700, 50), ("f32", 300, 700, 50)])
+def test_matrices_of_low_rank(dtype, rows, cols, count):
     """A gradient of rank 2 and a little noise: X is carried over in more than 11 bits."""
     import paper_2410_10989_amd as flce
-    G = make(192, 192, dtype, rank=2, spike=30.0)
-    got = flce.flce_orthogonalize([torch.from_numpy(G).to(DT[dtype]).cuda()])[0]
+    G = make(rows, cols, dtype, rank=2, spike=30.0)
+    got = flce.flce_orthogonalize([torch.from_numpy(G).to(DT[dtype]).cuda() for _ in range(count)])[-1]
     check(got, G, dtype)
     ref = oracle.orthogonalize(G)
     assert np.linalg.norm(got.double().cpu().numpy() - ref) <= (5e-3 if dtype == "bf16" else 1e-4) * np.linalg.norm(ref)
