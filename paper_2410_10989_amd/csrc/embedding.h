@@ -4,12 +4,15 @@
 //     out_i = s E[t_i]   (0 for rows that are not live)          dE_v = (dE_v +) s sum_{i live, t_i = v} dY_i
 //
 // The gradient's rows are added up in the order of i, whatever the machine does: no atomics on values.
-//   1. embed_sort_kernel    the live rows' numbers ordered by token (a stable counting sort), in one launch: workgroup
-//                           b owns EM tokens and looks at all rows, so it counts what lies before its tokens itself and
-//                           waits for nobody.  Rows of the table that no token names are filled with zeros here.
-//   2. embed_sum_kernel     pieces of EM_PIECE consecutive entries of that order, a wavefront per piece and
-//                           64 vectors of the row: the same work for everybody, however often a token comes.  What
-//                           begins and ends in a piece is written at once, the rest is left as fp32 sums.
+//   1. embed_sort_kernel    the live rows' numbers, those of a token together and in order (a stable counting sort), in one
+//                           launch: a workgroup owns every `classes`-th token and looks at all rows, so it counts what
+//                           lies before its tokens itself and waits for nobody.  (Neighbouring tokens belong to different
+//                           workgroups: the frequent ones are neighbours.  With 512 tokens in a row for each, the first
+//                           workgroup had half of 16384 rows to place, 28 us; TIMES.)
+//   2. embed_sum_kernel     pieces of consecutive entries of that order, a wavefront per piece and 64 vectors of the row:
+//                           the same work for everybody, however often a token comes.  What begins and ends in a
+//                           piece is written at once, the rest is left as fp32 sums.  Further workgroups fill the rows
+//                           of the table that no token names with zeros.
 //   3. embed_join_kernel    the sums of a token that several pieces share, in order, in fp64.
 #pragma once
 #include "rowvec.h"
@@ -26,9 +29,14 @@ struct EmbedArgs {
     int64_t ldin, ldout;
     // backward
     int add;                  // to what the gradient's buffer holds
-    int range;                // tokens per workgroup of the sort, a power of two
-    int *begin;               // V + 1: entries in front of a token's
-    int *token, *row;         // of the entries in order
+    int classes, class_bits;  // workgroup c of the sort has tokens c, c + classes, ...; a power of two
+    int per_class;            // tokens of a class
+    int piece;                // entries per piece, a power of two
+    int2* span;               // per token, in the order of embed_key: its entries' first and the one behind its last
+    int* total;               // entries
+    int2* entry;              // (token, row), the tokens in the order of embed_key
+    int sum_blocks;           // workgroups of the second launch that add up; the others write zeros
+    int zero_rows;            // rows of the table per wavefront of these, at most its lanes
     float* part;              // piece p: row 2 p its first token's sum if that began before, 2 p + 1 its last one's
     int slices;               // of 64 vectors, per row
 };
@@ -38,6 +46,8 @@ __device__ __forceinline__ int embed_row(const EmbedArgs& a, int64_t t) {
     const uint64_t v = (uint64_t)t - (uint64_t)a.first;
     return t != a.ignored && v < (uint64_t)a.V ? (int)v : -1;
 }
+
+__device__ __forceinline__ int embed_key(const EmbedArgs& a, int v) { return (v & (a.classes - 1)) * a.per_class + (v >> a.class_bits); }
 
 // LPR lanes per row, K loads of a lane in flight.  One wavefront per row where a row has 64 vectors or more.
 template <typename T, int LPR, int K, bool NT>
@@ -68,34 +78,39 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a) {
 }
 
 constexpr int EM_SORT_THREADS = 1024, EM_SORT_WAVES = EM_SORT_THREADS / WAVE;
-constexpr int EM_RANGE = 512;      // most tokens of a workgroup of the sort
-constexpr int EM_PIECE = 32;       // entries that a wavefront adds up: with one on either side less than its lanes
+constexpr int EM_RANGE = 1024;     // most tokens of a class: one per thread
+constexpr int EM_PIECE = 32;       // most entries that a wavefront adds up: with one on either side less than its lanes
+constexpr int EM_PIECE_MIN = 8;
+constexpr int EM_JOIN_PIECES = 2;  // that a workgroup looks at
 constexpr int EM_AHEAD = 8;        // loads in flight, per lane
-constexpr int EM_JOIN_THREADS = 512, EM_JOIN_WAVES = EM_JOIN_THREADS / WAVE;
+constexpr int EM_JOIN_THREADS = 256, EM_JOIN_WAVES = EM_JOIN_THREADS / WAVE;
 
-// Wavefront w of a workgroup looks at the w-th part of the rows: twice, to count and to place.
-template <typename T, bool NT>
-__global__ __launch_bounds__(EM_SORT_THREADS) void embed_sort_kernel(EmbedArgs a) {
-    constexpr int AHEAD = 8;
+// Wavefront w of a workgroup looks at the w-th part of the rows: twice, to count and to place (up to 16384 rows it keeps
+// them in registers: every round of loads is a wait for memory).
+static __global__ __launch_bounds__(EM_SORT_THREADS) void embed_sort_kernel(EmbedArgs a) {
+    constexpr int AHEAD = 16;
     __shared__ int count[EM_SORT_WAVES][EM_RANGE];   // later: the next entry of a wavefront's rows of a token
-    __shared__ int total[EM_RANGE];
     __shared__ int wave_sum_of[EM_SORT_WAVES], before_of[EM_SORT_WAVES];
     const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
-    const int lo = (int)blockIdx.x * a.range, n = min(a.range, a.V - lo);
-    for (int j = tid; j < EM_SORT_WAVES * EM_RANGE; j += EM_SORT_THREADS) (&count[0][0])[j] = 0;
-    __syncthreads();
+    const int mask = a.classes - 1, c = (int)blockIdx.x;
     const int share = ((a.rows + EM_SORT_WAVES - 1) / EM_SORT_WAVES + WAVE - 1) / WAVE * WAVE;
     const int64_t i0 = (int64_t)wave * share, i1 = min((int64_t)a.rows, i0 + share);
-    int before = 0;
-    for (int64_t i = i0; i < i1; i += AHEAD * WAVE) {
-        int64_t t[AHEAD];
+    int64_t t[AHEAD];
+    auto load = [&](int64_t i) {
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) t[k] = a.tokens[min(i + k * WAVE + lane, (int64_t)a.rows - 1)];
+    };
+    load(i0);
+    for (int j = lane; j < a.per_class; j += WAVE) count[wave][j] = 0;   // (its own: no barrier)
+    int before = 0;
+    for (int64_t i = i0; i < i1; i += AHEAD * WAVE) {
+        if (i != i0) load(i);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int v = i + k * WAVE + lane < i1 ? embed_row(a, t[k]) : -1;
-            before += v >= 0 && v < lo;
-            if (v >= lo && v < lo + n) atomicAdd(&count[wave][v - lo], 1);
+            const int of = v >= 0 ? v & mask : INT32_MAX;
+            before += of < c;
+            if (of == c) atomicAdd(&count[wave][v >> a.class_bits], 1);
         }
     }
     before = wave_sum(before);
@@ -103,14 +118,14 @@ __global__ __launch_bounds__(EM_SORT_THREADS) void embed_sort_kernel(EmbedArgs a
     __syncthreads();
     // per token: where each wavefront's rows begin among them; then where the tokens begin
     int mine = 0;
-    if (tid < EM_RANGE) {
+    static_assert(EM_RANGE == EM_SORT_THREADS, "a token per thread");
+    if (tid < a.per_class) {
 #pragma unroll
         for (int w = 0; w < EM_SORT_WAVES; ++w) {
-            const int c = count[w][tid];
+            const int here = count[w][tid];
             count[w][tid] = mine;
-            mine += c;
+            mine += here;
         }
-        total[tid] = mine;
     }
     int up_to = mine;   // inclusive sum over the wavefront's tokens
 #pragma unroll
@@ -125,80 +140,87 @@ __global__ __launch_bounds__(EM_SORT_THREADS) void embed_sort_kernel(EmbedArgs a
         if (w < wave) at += wave_sum_of[w];
         at += before_of[w];
     }
-    if (tid < EM_RANGE) {
-        if (tid < n) a.begin[lo + tid] = at;
-        if (tid == n - 1 && lo + n == a.V) a.begin[a.V] = at + mine;
+    if (tid < a.per_class) {
+        a.span[c * (int64_t)a.per_class + tid] = int2{at, at + mine};
 #pragma unroll
         for (int w = 0; w < EM_SORT_WAVES; ++w) count[w][tid] += at;
     }
+    if (tid == EM_SORT_THREADS - 1 && c == mask) *a.total = at + mine;
     __syncthreads();
+    if (i1 - i0 > AHEAD * WAVE) load(i0);
     for (int64_t i = i0; i < i1; i += AHEAD * WAVE) {
-        int64_t t[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) t[k] = a.tokens[min(i + k * WAVE + lane, (int64_t)a.rows - 1)];
+        if (i != i0) load(i);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int v = i + k * WAVE + lane < i1 ? embed_row(a, t[k]) : -1;
-            const bool here = v >= lo && v < lo + n;
+            const bool here = v >= 0 && (v & mask) == c;
+            const int which = v >> a.class_bits;
             uint64_t peers = __ballot(here);
             if (!peers) continue;
             // the lanes with the same token, bit by bit
 #pragma unroll
             for (int b = 1; b < EM_RANGE; b <<= 1) {
-                const bool set = (v - lo) & b;
+                const bool set = which & b;
                 const uint64_t with = __ballot(set);
                 peers &= set ? with : ~with;
             }
             const int rank = __popcll(peers & ((1ull << lane) - 1)), leader = __ffsll((unsigned long long)peers) - 1;
             int base = 0;
-            if (here && rank == 0) base = atomicAdd(&count[wave][v - lo], __popcll(peers));
+            if (here && rank == 0) base = atomicAdd(&count[wave][which], __popcll(peers));
             base = __shfl(base, max(leader, 0), WAVE);
-            if (here) {
-                a.token[base + rank] = v;
-                a.row[base + rank] = (int)(i + k * WAVE + lane);
-            }
+            if (here) a.entry[base + rank] = int2{v, (int)(i + k * WAVE + lane)};
         }
-    }
-    if (a.add) return;
-    constexpr int N = RowVec<T>::N;
-    const int nfull = a.H / N, rem = a.H % N, nvec = nfull + (rem ? 1 : 0);
-    const float zero[N] = {};
-    for (int j = wave; j < n; j += EM_SORT_WAVES) {
-        if (total[j]) continue;
-        T* to = static_cast<T*>(a.out) + (int64_t)(lo + j) * a.ldout;
-        for (int v = lane; v < nvec; v += WAVE) row_store<T, NT>(to, v, nfull, rem, zero);
     }
 }
 
-// Writes (or adds) the finished sum of vector v of a row of the table.
-template <typename T, bool NT>
-__device__ __forceinline__ void embed_put(const EmbedArgs& a, int token, int v, int nfull, int rem, const float (&sum)[RowVec<T>::N]) {
+// Writes (or adds to `base`, what it holds) the finished sum of vector v of a row of the table.
+template <typename T>
+__device__ __forceinline__ void embed_put(const EmbedArgs& a, int token, int v, int nfull, int rem, const float (&sum)[RowVec<T>::N],
+                                          const u32x4& base) {
     constexpr int N = RowVec<T>::N;
     T* to = static_cast<T*>(a.out) + (int64_t)token * a.ldout;
     float f[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = 0.f;
-    if (a.add) RowVec<T>::unpack(row_load(to, v, nfull, rem), f);
+    RowVec<T>::unpack(base, f);
 #pragma unroll
     for (int e = 0; e < N; ++e) f[e] = a.add ? f[e] + a.scale * sum[e] : a.scale * sum[e];
-    row_store<T, NT>(to, v, nfull, rem, f);
+    row_store<T, false>(to, v, nfull, rem, f);
 }
 
-template <typename T, bool NT>
+// ADD: a.add.  What finished sums are added to is loaded with the rows of a group, not when a sum is finished (5734 rows
+// of 2304, most tokens once or twice: a wait for memory after another, 37 us; TIMES).
+template <typename T, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
     constexpr int N = RowVec<T>::N;
     static_assert(EM_PIECE + 2 <= WAVE, "a lane per entry and one on either side");
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / WAVE);
     const int nfull = a.H / N, rem = a.H % N, nvec = nfull + (rem ? 1 : 0);
-    const int entries = a.begin[a.V];
-    const int64_t units = (int64_t)((entries + EM_PIECE - 1) / EM_PIECE) * a.slices;
-    for (int64_t u = (int64_t)blockIdx.x * 4 + wave; u < units; u += (int64_t)gridDim.x * 4) {
+    if constexpr (!ADD) {
+        // zeros: a stretch of zero_rows rows of the table per wavefront, plain stores (what that reaches with nothing else to
+        // do: 1.05 GB 172 us, 176 nontemporal; rows dealt round-robin 190 to 205)
+        if ((int)blockIdx.x >= a.sum_blocks) {
+            const float zero[N] = {};
+            const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + wave) * a.zero_rows;
+            const int2 span = a.span[embed_key(a, (int)min(v0 + lane, (int64_t)a.V - 1))];   // (a lane looks at a row)
+            uint64_t empty = __ballot(lane < a.zero_rows && v0 + lane < a.V && span.x == span.y);
+            while (empty) {
+                const int r = __ffsll((unsigned long long)empty) - 1;
+                empty &= empty - 1;
+                T* to = static_cast<T*>(a.out) + (v0 + r) * a.ldout;
+                for (int v = lane; v < nvec; v += WAVE) row_store<T, false>(to, v, nfull, rem, zero);
+            }
+            return;
+        }
+    }
+    const int entries = *a.total;
+    const int64_t units = (int64_t)((entries + a.piece - 1) / a.piece) * a.slices;
+    for (int64_t u = (int64_t)blockIdx.x * 4 + wave; u < units; u += (int64_t)a.sum_blocks * 4) {
         const int piece = (int)(u / a.slices), v = (int)(u % a.slices) * WAVE + lane;
-        const int e0 = piece * EM_PIECE, count = min(EM_PIECE, entries - e0);
+        const int e0 = piece * a.piece, count = min(a.piece, entries - e0);
         // lane 1 + i holds entry i of the piece
         const int at = e0 - 1 + lane;
-        const bool there = lane <= EM_PIECE + 1 && at >= 0 && at < entries;
-        const int tokens = there ? a.token[at] : -1, rows = there ? a.row[at] : 0;
+        const bool there = lane <= a.piece + 1 && at >= 0 && at < entries;
+        const int2 mine = there ? a.entry[at] : int2{-1, 0};
+        const int tokens = mine.x, rows = mine.y;
         float sum[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] = 0.f;
@@ -210,95 +232,115 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
 #pragma unroll
             for (int e = 0; e < N; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
         };
+        auto finish = [&](bool whole, const u32x4& base) {   // the token's entries end here, or the piece does
+            if (began && whole) embed_put<T>(a, token, v, nfull, rem, sum, base);
+            else leave(began ? 1 : 0);
+        };
         for (int g = 0; g < count; g += EM_AHEAD) {
-            u32x4 raw[EM_AHEAD];
+            u32x4 raw[EM_AHEAD], base[ADD ? EM_AHEAD : 1];
+            int next[EM_AHEAD];   // the token behind entry g + k
 #pragma unroll
             for (int k = 0; k < EM_AHEAD; ++k) {
-                const int row = __builtin_amdgcn_readlane(rows, 1 + min(g + k, count - 1));
-                const T* from = static_cast<const T*>(a.in) + (int64_t)row * a.ldin;
+                const int i = min(g + k, count - 1);
+                const T* from = static_cast<const T*>(a.in) + (int64_t)__builtin_amdgcn_readlane(rows, 1 + i) * a.ldin;
                 raw[k] = a.H < N ? row_load(from, v, nfull, rem) : row_load_ahead(from, v, nvec, a.H);
+                next[k] = __builtin_amdgcn_readlane(tokens, 2 + i);
+                if constexpr (ADD) {
+                    const int t = __builtin_amdgcn_readlane(tokens, 1 + i);
+                    const T* to = static_cast<const T*>(a.out) + (int64_t)t * a.ldout;
+                    base[k] = u32x4{0u, 0u, 0u, 0u};
+                    if (next[k] != t) base[k] = a.H < N ? row_load(to, v, nfull, rem) : row_load_ahead(to, v, nvec, a.H);
+                }
             }
             if (rem && a.H >= N && v == nfull) {
 #pragma unroll
-                for (int k = 0; k < EM_AHEAD; ++k) row_shift_tail<T>(raw[k], rem);
+                for (int k = 0; k < EM_AHEAD; ++k) {
+                    row_shift_tail<T>(raw[k], rem);
+                    if constexpr (ADD) row_shift_tail<T>(base[k], rem);
+                }
             }
 #pragma unroll
             for (int k = 0; k < EM_AHEAD; ++k) {
                 if (g + k >= count) break;
-                const int t = __builtin_amdgcn_readlane(tokens, 1 + g + k);
-                if (t != token) {
-                    if (began) embed_put<T, NT>(a, token, v, nfull, rem, sum);
-                    else leave(0);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) sum[e] = 0.f;
-                    token = t;
-                    began = true;
-                }
                 float f[N];
                 RowVec<T>::unpack(raw[k], f);
 #pragma unroll
                 for (int e = 0; e < N; ++e) sum[e] += f[e];
+                const bool whole = next[k] != token;
+                if (whole || g + k == count - 1) {
+                    finish(whole, base[ADD ? k : 0]);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) sum[e] = 0.f;
+                    token = next[k];
+                    began = true;
+                }
             }
         }
-        const bool ends = __builtin_amdgcn_readlane(tokens, 1 + count) != token;
-        if (began && ends) embed_put<T, NT>(a, token, v, nfull, rem, sum);
-        else leave(began ? 1 : 0);
     }
 }
 
-// A workgroup per piece and slice: adds up the sums of the token that begins in the piece and goes on behind it.
-template <typename T, bool NT>
+// A workgroup per slice and EM_JOIN_PIECES pieces: adds up the sums of the tokens that begin in these and go on behind
+// them.
+template <typename T>
 __global__ __launch_bounds__(EM_JOIN_THREADS) void embed_join_kernel(EmbedArgs a) {
     constexpr int N = RowVec<T>::N, AHEAD = 4;
     __shared__ double sums[EM_JOIN_WAVES][WAVE * N];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / WAVE);
     const int nfull = a.H / N, rem = a.H % N, nvec = nfull + (rem ? 1 : 0);
-    const int entries = a.begin[a.V];
-    const int64_t units = (int64_t)((entries + EM_PIECE - 1) / EM_PIECE) * a.slices;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int piece = (int)(u / a.slices), slice = (int)(u % a.slices), v = slice * WAVE + lane;
-        const int64_t next = ((int64_t)piece + 1) * EM_PIECE;
-        if (next >= entries) continue;
-        const int token = a.token[next];
-        const int b = a.begin[token], e = a.begin[token + 1];
-        if (b / EM_PIECE != piece || b == next) continue;   // it began elsewhere
-        const int pieces = (e - 1) / EM_PIECE - piece + 1;
-        const int64_t pitch = (int64_t)a.slices * (WAVE * N);
-        const float* first = a.part + ((int64_t)piece * 2 + 1) * pitch + (int64_t)v * N;
-        const float* rest = a.part + (int64_t)piece * 2 * pitch + (int64_t)v * N;
-        double sum[N];
+    const int entries = *a.total;
+    const int64_t groups = ((entries + a.piece - 1) / a.piece + EM_JOIN_PIECES - 1) / EM_JOIN_PIECES;
+    for (int64_t u = blockIdx.x; u < groups * a.slices; u += gridDim.x) {
+        const int piece0 = (int)(u / a.slices) * EM_JOIN_PIECES, v = (int)(u % a.slices) * WAVE + lane;
+        // lane i looks at piece i: the token behind it is its last one's, and that began in it
+        const int64_t e0 = (int64_t)(piece0 + lane) * a.piece, e1 = e0 + a.piece;
+        const bool there = lane < EM_JOIN_PIECES && e1 < entries;
+        const int behind = there ? a.entry[e1].x : -1, last = there ? a.entry[e1 - 1].x : -2;
+        const int in_front = there && e0 > 0 ? a.entry[e0 - 1].x : -1;
+        uint64_t crossed = __ballot(behind == last && in_front != behind);
+        while (crossed) {
+            const int which = __ffsll((unsigned long long)crossed) - 1;
+            crossed &= crossed - 1;
+            const int piece = piece0 + which, token = __builtin_amdgcn_readlane(behind, which);
+            const int pieces = (a.span[embed_key(a, token)].y - 1) / a.piece - piece + 1;
+            const int64_t pitch = (int64_t)a.slices * (WAVE * N);
+            const float* first = a.part + ((int64_t)piece * 2 + 1) * pitch + (int64_t)v * N;
+            const float* rest = a.part + (int64_t)piece * 2 * pitch + (int64_t)v * N;
+            u32x4 base = {0u, 0u, 0u, 0u};
+            if (a.add && wave == 0) base = row_load(static_cast<const T*>(a.out) + (int64_t)token * a.ldout, v, nfull, rem);
+            double sum[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum[k] = 0.0;
-        const int p0 = (int)((int64_t)pieces * wave / EM_JOIN_WAVES), p1 = (int)((int64_t)pieces * (wave + 1) / EM_JOIN_WAVES);
-        if (v < nvec) {
-            for (int p = p0; p < p1; p += AHEAD) {
-                f32x4 in[AHEAD][N / 4];
+            for (int k = 0; k < N; ++k) sum[k] = 0.0;
+            const int p0 = (int)((int64_t)pieces * wave / EM_JOIN_WAVES), p1 = (int)((int64_t)pieces * (wave + 1) / EM_JOIN_WAVES);
+            if (v < nvec) {
+                for (int p = p0; p < p1; p += AHEAD) {
+                    f32x4 in[AHEAD][N / 4];
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k) {
-                    const int q = min(p + k, p1 - 1);
-                    const float* from = q ? rest + (int64_t)q * 2 * pitch : first;
+                    for (int k = 0; k < AHEAD; ++k) {
+                        const int q = min(p + k, p1 - 1);
+                        const float* from = q ? rest + (int64_t)q * 2 * pitch : first;
 #pragma unroll
-                    for (int c = 0; c < N / 4; ++c) in[k][c] = *reinterpret_cast<const f32x4*>(from + 4 * c);
+                        for (int c = 0; c < N / 4; ++c) in[k][c] = *reinterpret_cast<const f32x4*>(from + 4 * c);
+                    }
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                        for (int c = 0; c < N; ++c) sum[c] += p + k < p1 ? (double)in[k][c / 4][c % 4] : 0.0;
                 }
-#pragma unroll
-                for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-                    for (int c = 0; c < N; ++c) sum[c] += p + k < p1 ? (double)in[k][c / 4][c % 4] : 0.0;
             }
-        }
 #pragma unroll
-        for (int k = 0; k < N; ++k) sums[wave][k * WAVE + lane] = sum[k];
-        __syncthreads();
-        if (wave == 0 && v < nvec) {
-            float f[N];
+            for (int k = 0; k < N; ++k) sums[wave][k * WAVE + lane] = sum[k];
+            __syncthreads();
+            if (wave == 0 && v < nvec) {
+                float f[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                for (int w = 1; w < EM_JOIN_WAVES; ++w) sum[k] += sums[w][k * WAVE + lane];
-                f[k] = (float)sum[k];
+                for (int k = 0; k < N; ++k) {
+                    for (int w = 1; w < EM_JOIN_WAVES; ++w) sum[k] += sums[w][k * WAVE + lane];
+                    f[k] = (float)sum[k];
+                }
+                embed_put<T>(a, token, v, nfull, rem, f, base);
             }
-            embed_put<T, NT>(a, token, v, nfull, rem, f);
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 

@@ -12,6 +12,8 @@ namespace {
 constexpr int64_t EM_MAX_H = (int64_t)1 << 24;      // keeps vector numbers within 32 bits
 constexpr int64_t EM_GRID = (int64_t)1 << 20;       // workgroups of a launch; they go on in strides
 constexpr int EM_CUS = 256, EM_RANGE_MIN = 32;
+constexpr int64_t EM_WAVES = 4096;                  // wavefronts of the sums, if there is as much to add up
+constexpr int64_t EM_ZERO_BYTES = 32 << 10;         // that a wavefront fills
 constexpr int64_t EM_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
 size_t elem(int dtype) { return dtype == FLCE_F32 ? 4 : 2; }
@@ -30,19 +32,25 @@ int check_common(const flce_embedding* b) {
 int64_t table_stride(const flce_embedding& b) { return b.ldtable && b.V > 1 ? b.ldtable : b.H; }
 int64_t rows_stride(const flce_embedding& b) { return b.ldrows && b.rows > 1 ? b.ldrows : b.H; }
 
-// Where the order and the partial sums lie, in bytes from the workspace's start.
+// How the sort deals the tokens, and where the order and the partial sums lie, in bytes from the workspace's start.
 struct Plan {
-    int64_t slices, pieces;
-    size_t token, row, part, total;
+    int class_bits;
+    int64_t per_class, slices, piece, pieces;
+    size_t span, entry, part, total;
 };
 Plan plan_of(const flce_embedding& b) {
     const int64_t N = 16 / (int64_t)elem(b.dtype);
     Plan p{};
+    while ((b.V - 1) >> p.class_bits >= EM_RANGE || ((int64_t)1 << p.class_bits < EM_CUS && (b.V - 1) >> p.class_bits >= EM_RANGE_MIN)) ++p.class_bits;
+    p.per_class = ((b.V - 1) >> p.class_bits) + 1;
     p.slices = ((b.H + N - 1) / N + WAVE - 1) / WAVE;
-    p.pieces = (b.rows + EM_PIECE - 1) / EM_PIECE;
-    p.token = (size_t)align64(b.V + 1) * sizeof(int);
-    p.row = p.token + (size_t)align64(b.rows) * sizeof(int);
-    p.part = p.row + (size_t)align64(b.rows) * sizeof(int);
+    // (pieces as long as they may be while there are enough wavefronts to fill the chip)
+    p.piece = EM_PIECE;
+    while (p.piece > EM_PIECE_MIN && b.rows / p.piece * p.slices < EM_WAVES) p.piece /= 2;
+    p.pieces = (b.rows + p.piece - 1) / p.piece;
+    p.span = 256;
+    p.entry = p.span + (size_t)align64(p.per_class << p.class_bits) * sizeof(int2);
+    p.part = p.entry + (size_t)align64(b.rows) * sizeof(int2);
     p.total = p.part + (p.pieces > 1 ? (size_t)p.pieces * 2 * (size_t)(p.slices * WAVE * N) * sizeof(float) : 0);
     return p;
 }
@@ -76,16 +84,23 @@ int run_fwd(const EmbedArgs& a, bool nt, hipStream_t s) {
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
 }
-template <typename T, bool NT>
-int run_bwd(const EmbedArgs& a, const Plan& p, hipStream_t s) {
-    const int64_t ranges = ((int64_t)a.V + a.range - 1) / a.range;
-    hipLaunchKernelGGL((embed_sort_kernel<T, NT>), dim3((unsigned)ranges), dim3(EM_SORT_THREADS), 0, s, a);
+template <typename T>
+int run_bwd(EmbedArgs& a, const Plan& p, hipStream_t s) {
+    hipLaunchKernelGGL(embed_sort_kernel, dim3((unsigned)a.classes), dim3(EM_SORT_THREADS), 0, s, a);
     HIP_TRY(hipGetLastError());
     const int64_t units = p.pieces * p.slices;
-    hipLaunchKernelGGL((embed_sum_kernel<T, NT>), dim3((unsigned)std::min(EM_GRID, (units + 3) / 4)), dim3(256), 0, s, a);
+    a.sum_blocks = (int)std::min(EM_GRID, (units + 3) / 4);
+    if (a.add) {
+        hipLaunchKernelGGL((embed_sum_kernel<T, true>), dim3((unsigned)a.sum_blocks), dim3(256), 0, s, a);
+    } else {
+        a.zero_rows = (int)std::max<int64_t>(1, std::min<int64_t>(WAVE, EM_ZERO_BYTES / ((int64_t)a.H * (int64_t)sizeof(T))));
+        const int64_t zeros = ((int64_t)a.V + 4 * a.zero_rows - 1) / (4 * a.zero_rows);
+        hipLaunchKernelGGL((embed_sum_kernel<T, false>), dim3((unsigned)(a.sum_blocks + zeros)), dim3(256), 0, s, a);
+    }
     HIP_TRY(hipGetLastError());
     if (p.pieces == 1) return FLCE_OK;
-    hipLaunchKernelGGL((embed_join_kernel<T, NT>), dim3((unsigned)std::min(EM_GRID, units)), dim3(EM_JOIN_THREADS), 0, s, a);
+    const int64_t groups = (p.pieces + EM_JOIN_PIECES - 1) / EM_JOIN_PIECES;
+    hipLaunchKernelGGL((embed_join_kernel<T>), dim3((unsigned)std::min(EM_GRID, groups * p.slices)), dim3(EM_JOIN_THREADS), 0, s, a);
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
 }
@@ -108,6 +123,9 @@ int flce_embedding_fwd(const void* table, const int64_t* tokens, const flce_embe
     a.out = out;
     a.ldin = table_stride(b);
     a.ldout = rows_stride(b);
+    // Nontemporal stores where the rows do not fit the memory-side cache anyway: whoever reads them next would miss them
+    // there.  us, ordinary / nontemporal, rows of 3584 bf16 alone and with the layer norm that follows: 8192 19 / 16, 41 /
+    // 44; 16384 38 / 30, 76 / 80; 24576 54 / 44, 102 / 110.
     const bool nt = b.rows * b.H * (int64_t)es > EM_CACHE_BYTES;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return b.dtype == FLCE_F32 ? run_fwd<float>(a, nt, s) : run_fwd<bf16_t>(a, nt, s);
@@ -140,16 +158,16 @@ int flce_embedding_bwd(const void* dout, const int64_t* tokens, const flce_embed
     a.ldin = rows_stride(b);
     a.ldout = table_stride(b);
     a.add = b.accumulate;
-    a.range = EM_RANGE;
-    while (a.range > EM_RANGE_MIN && b.V / a.range < EM_CUS) a.range /= 2;
-    a.begin = reinterpret_cast<int*>(ws);
-    a.token = reinterpret_cast<int*>(ws + p.token);
-    a.row = reinterpret_cast<int*>(ws + p.row);
+    a.class_bits = p.class_bits;
+    a.classes = 1 << p.class_bits;
+    a.per_class = (int)p.per_class;
+    a.total = reinterpret_cast<int*>(ws);
+    a.span = reinterpret_cast<int2*>(ws + p.span);
+    a.entry = reinterpret_cast<int2*>(ws + p.entry);
     a.part = reinterpret_cast<float*>(ws + p.part);
+    a.piece = (int)p.piece;
     a.slices = (int)p.slices;
-    const bool nt = !b.accumulate && b.V * b.H * (int64_t)es > EM_CACHE_BYTES;
-    if (nt) return b.dtype == FLCE_F32 ? run_bwd<float, true>(a, p, s) : run_bwd<bf16_t, true>(a, p, s);
-    return b.dtype == FLCE_F32 ? run_bwd<float, false>(a, p, s) : run_bwd<bf16_t, false>(a, p, s);
+    return b.dtype == FLCE_F32 ? run_bwd<float>(a, p, s) : run_bwd<bf16_t>(a, p, s);
 }
 
 size_t flce_embedding_workspace_bytes(const flce_embedding* args) {
