@@ -79,22 +79,28 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a) {
 
 constexpr int EM_SORT_THREADS = 1024, EM_SORT_WAVES = EM_SORT_THREADS / WAVE;
 constexpr int EM_RANGE = 1024;     // most tokens of a class: one per thread
+constexpr int EM_LIST = 1024;      // rows of its class that a wavefront of the sort lists
 constexpr int EM_PIECE = 32;       // most entries that a wavefront adds up: with one on either side less than its lanes
 constexpr int EM_PIECE_MIN = 8;
 constexpr int EM_JOIN_PIECES = 2;  // that a workgroup looks at
 constexpr int EM_AHEAD = 8;        // loads in flight, per lane
 constexpr int EM_JOIN_THREADS = 256, EM_JOIN_WAVES = EM_JOIN_THREADS / WAVE;
 
-// Wavefront w of a workgroup looks at the w-th part of the rows: twice, to count and to place (up to 16384 rows it keeps
-// them in registers: every round of loads is a wait for memory).
+// Wavefront w of a workgroup looks at the w-th part of the rows, 16 x 64 of them at a time with the next ones' loads under
+// way, and keeps a list of those of its class; the list is then put in order.  Only a wavefront with more than EM_LIST of them
+// looks at its rows again, a list for every 1024.  (us, rows dealt by Zipf's law: 16384 10, 32768 15, 131072 45; before the
+// lists, every row looked at twice, 21 for 16384 and over 100 for 131072.)
 static __global__ __launch_bounds__(EM_SORT_THREADS) void embed_sort_kernel(EmbedArgs a) {
     constexpr int AHEAD = 16;
     __shared__ int count[EM_SORT_WAVES][EM_RANGE];   // later: the next entry of a wavefront's rows of a token
+    __shared__ uint32_t list[EM_SORT_WAVES][EM_LIST];   // row, counted from the wavefront's first, and token of the class
     __shared__ int wave_sum_of[EM_SORT_WAVES], before_of[EM_SORT_WAVES];
     const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
     const int mask = a.classes - 1, c = (int)blockIdx.x;
+    const uint64_t below = (1ull << lane) - 1;
     const int share = ((a.rows + EM_SORT_WAVES - 1) / EM_SORT_WAVES + WAVE - 1) / WAVE * WAVE;
     const int64_t i0 = (int64_t)wave * share, i1 = min((int64_t)a.rows, i0 + share);
+    const int listed = (int64_t)share * EM_RANGE <= ((int64_t)1 << 32) ? EM_LIST : 0;   // (an entry has 32 bits)
     int64_t t[AHEAD];
     auto load = [&](int64_t i) {
 #pragma unroll
@@ -102,18 +108,26 @@ static __global__ __launch_bounds__(EM_SORT_THREADS) void embed_sort_kernel(Embe
     };
     load(i0);
     for (int j = lane; j < a.per_class; j += WAVE) count[wave][j] = 0;   // (its own: no barrier)
-    int before = 0;
+    int before = 0, mine_all = 0;   // rows before the class's, of the class
     for (int64_t i = i0; i < i1; i += AHEAD * WAVE) {
-        if (i != i0) load(i);
+        int v[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) v[k] = i + k * WAVE + lane < i1 ? embed_row(a, t[k]) : -1;
+        if (i + AHEAD * WAVE < i1) load(i + AHEAD * WAVE);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const int v = i + k * WAVE + lane < i1 ? embed_row(a, t[k]) : -1;
-            const int of = v >= 0 ? v & mask : INT32_MAX;
-            before += of < c;
-            if (of == c) atomicAdd(&count[wave][v >> a.class_bits], 1);
+            const int of = v[k] >= 0 ? v[k] & mask : INT32_MAX;
+            before += __popcll(__ballot(of < c));
+            const uint64_t here = __ballot(of == c);
+            if (!here) continue;
+            if (of == c) {
+                const int at = mine_all + __popcll(here & below), which = v[k] >> a.class_bits;
+                atomicAdd(&count[wave][which], 1);
+                if (at < listed) list[wave][at] = (uint32_t)(i - i0 + k * WAVE + lane) * EM_RANGE + which;
+            }
+            mine_all += __popcll(here);
         }
     }
-    before = wave_sum(before);
     if (lane == 0) before_of[wave] = before;
     __syncthreads();
     // per token: where each wavefront's rows begin among them; then where the tokens begin
@@ -147,29 +161,47 @@ static __global__ __launch_bounds__(EM_SORT_THREADS) void embed_sort_kernel(Embe
     }
     if (tid == EM_SORT_THREADS - 1 && c == mask) *a.total = at + mine;
     __syncthreads();
-    if (i1 - i0 > AHEAD * WAVE) load(i0);
+    // up to 64 rows of the class, in order, each with its token's number in it (or not `here`): to their places
+    auto place = [&](bool here, int which, int row) {
+        uint64_t peers = __ballot(here);
+        // the lanes with the same token, bit by bit
+        for (int b = 1; b < a.per_class; b <<= 1) {
+            const bool set = which & b;
+            const uint64_t with = __ballot(set);
+            peers &= set ? with : ~with;
+        }
+        const int rank = __popcll(peers & below), leader = __ffsll((unsigned long long)peers) - 1;
+        int base = 0;
+        if (here && rank == 0) base = atomicAdd(&count[wave][which], __popcll(peers));
+        base = __shfl(base, max(leader, 0), WAVE);
+        if (here) a.entry[base + rank] = int2{(which << a.class_bits) | c, row};
+    };
+    auto place_list = [&](int n, int64_t first) {
+        for (int j = 0; j < n; j += WAVE) {
+            const bool here = j + lane < n;
+            const uint32_t e = list[wave][here ? j + lane : 0];
+            place(here, here ? (int)(e % EM_RANGE) : 0, (int)(first + e / EM_RANGE));
+        }
+    };
+    if (mine_all <= listed) {
+        place_list(mine_all, i0);
+        return;
+    }
+    static_assert(AHEAD * WAVE <= EM_LIST, "a round's rows fit the list");
     for (int64_t i = i0; i < i1; i += AHEAD * WAVE) {
-        if (i != i0) load(i);
+        load(i);
+        int n = 0;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int v = i + k * WAVE + lane < i1 ? embed_row(a, t[k]) : -1;
-            const bool here = v >= 0 && (v & mask) == c;
-            const int which = v >> a.class_bits;
-            uint64_t peers = __ballot(here);
-            if (!peers) continue;
-            // the lanes with the same token, bit by bit
-#pragma unroll
-            for (int b = 1; b < EM_RANGE; b <<= 1) {
-                const bool set = which & b;
-                const uint64_t with = __ballot(set);
-                peers &= set ? with : ~with;
-            }
-            const int rank = __popcll(peers & ((1ull << lane) - 1)), leader = __ffsll((unsigned long long)peers) - 1;
-            int base = 0;
-            if (here && rank == 0) base = atomicAdd(&count[wave][which], __popcll(peers));
-            base = __shfl(base, max(leader, 0), WAVE);
-            if (here) a.entry[base + rank] = int2{v, (int)(i + k * WAVE + lane)};
+            const uint64_t here = __ballot(v >= 0 && (v & mask) == c);
+            if (v >= 0 && (v & mask) == c) list[wave][n + __popcll(here & below)] = (uint32_t)(k * WAVE + lane) * EM_RANGE + (v >> a.class_bits);
+            n += __popcll(here);
         }
+        // (lanes read what others of the wavefront wrote: LDS executes a wavefront's accesses in order)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        place_list(n, i);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
 

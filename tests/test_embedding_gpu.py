@@ -66,7 +66,8 @@ BWD = [(1, 5, 64, "f32", "one", 0, False), (1, 700, 4096, "bf16", "one", 0, True
        (300, 513, 1000, "f32", "zipf", 13, True), (1025, 512, 515, "bf16", "zipf", 0, True), (700, 60000, 40, "bf16", "zipf", 0, False),
        (2000, 100, 260, "f32", "zipf", 0, False), (3000, 7, 520, "bf16", "one", 0, False), (500, 20, 2049, "f32", "zipf", 0, True),
        (400, 50, 8200, "bf16", "zipf", 5, False), (50, 31, 4097, "bf16", "none", 0, False), (50, 31, 640, "f32", "none", 0, True),
-       (9000, 3, 24, "f32", "zipf", 0, False)]
+       (9000, 3, 24, "f32", "zipf", 0, False), (40000, 500, 9, "f32", "zipf", 0, True), (33000, 70000, 8, "bf16", "spread", 0, False),
+       (20000, 5, 12, "f32", "one", 0, False), (40000, 2, 4, "bf16", "one", 0, True), (70000, 300000, 1, "f32", "zipf", 0, False)]
 
 
 def check_gradient(rows, V, H, dtype, kind, pad, add, seed=0, first=0, workspace=False):
