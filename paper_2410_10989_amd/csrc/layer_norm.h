@@ -37,7 +37,21 @@ __device__ __forceinline__ int ln_live(int v, int nfull, int rem) {
     return v < nfull ? RowVec<T>::N : v == nfull ? rem : 0;
 }
 
-// The last vectors of a group may be partial or not there: what they hold is zero, and d of it is set to zero.
+// f - mean, 0 for what is behind the row's end.  (A vector at a time: a choice per element is two instructions more for
+// each of about twenty.)
+template <typename T>
+__device__ __forceinline__ void ln_center(float (&f)[RowVec<T>::N], float mean, int v, int nfull, int rem) {
+    constexpr int N = RowVec<T>::N;
+    if (v < nfull) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] -= mean;
+    } else {
+        const int n = ln_live<T>(v, nfull, rem);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = e < n ? f[e] - mean : 0.f;
+    }
+}
+
 template <typename T, int TPR, int NV, bool NT>
 __global__ __launch_bounds__(row_block<TPR>) void layer_norm_fwd_kernel(LnArgs a) {
     constexpr int N = RowVec<T>::N, GROUPS = row_groups<TPR>;
@@ -83,12 +97,9 @@ __global__ __launch_bounds__(row_block<TPR>) void layer_norm_fwd_kernel(LnArgs a
     s = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int n = ln_live<T>(t + k * TPR, nfull, rem);
+        ln_center<T>(f[k], mean, t + k * TPR, nfull, rem);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            f[k][e] = e < n ? f[k][e] - mean : 0.f;
-            s = fmaf(f[k][e], f[k][e], s);
-        }
+        for (int e = 0; e < N; ++e) s = fmaf(f[k][e], f[k][e], s);
     }
     const float r = rsqrtf(row_sum<TPR>(s, red[1]) * inv_H + a.eps);
     T* p = static_cast<T*>(a.out_n) + at * a.ldn;
@@ -235,50 +246,49 @@ __global__ __launch_bounds__(row_block<TPR>) void layer_norm_bwd_kernel(LnArgs a
                     if (a.dh) row_shift_tail<T>(in.dh[k], rem);
                 }
         }
+        float d[NV][N];   // h, then h - mean
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float h[N];
-            RowVec<T>::unpack(in.h[k], h);
+            RowVec<T>::unpack(in.h[k], d[k]);
 #pragma unroll
-            for (int e = 0; e < N; ++e) s += h[e];
+            for (int e = 0; e < N; ++e) s += d[k][e];
         }
         const float mean = row_sum<TPR>(s, red[turn][0]) / (float)a.H;
         // sum d^2, sum u, sum u d in one exchange
         float sums[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float h[N], u[N], g[N];
-            RowVec<T>::unpack(in.h[k], h);
+            float u[N], g[N];
+            ln_center<T>(d[k], mean, t + k * TPR, nfull, rem);
             RowVec<T>::unpack(in.dn[k], u);
-            if (a.gamma) RowVec<T>::unpack(gv[k], g);
-            const int n = ln_live<T>(t + k * TPR, nfull, rem);
+            if (a.gamma) {
+                RowVec<T>::unpack(gv[k], g);
+#pragma unroll
+                for (int e = 0; e < N; ++e) u[e] *= g[e];
+            }
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float d = e < n ? h[e] - mean : 0.f;
-                if (a.gamma) u[e] *= g[e];
-                sums[0] = fmaf(d, d, sums[0]);
+                sums[0] = fmaf(d[k][e], d[k][e], sums[0]);
                 sums[1] += u[e];
-                sums[2] = fmaf(u[e], d, sums[2]);
+                sums[2] = fmaf(u[e], d[k][e], sums[2]);
             }
         }
         row_sums<TPR, 3>(sums, red[turn][1]);
-        const float r = rsqrtf(sums[0] * inv_H + a.eps), mu = sums[1] * inv_H, mx = sums[2] * r * inv_H;
+        // dx = dh + r u - r mean u - d r^3 mean(u d)
+        const float r = rsqrtf(sums[0] * inv_H + a.eps), shift = -r * (sums[1] * inv_H), slope = -(r * (r * (r * (sums[2] * inv_H))));
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float h[N], dn[N], g[N], D[N];
-            RowVec<T>::unpack(in.h[k], h);
+            float dn[N], g[N], D[N];
             RowVec<T>::unpack(in.dn[k], dn);
             if (a.gamma) RowVec<T>::unpack(gv[k], g);
             if (a.dh) RowVec<T>::unpack(in.dh[k], D);
-            const int n = ln_live<T>(t + k * TPR, nfull, rem);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float xh = e < n ? (h[e] - mean) * r : 0.f;
-                const float u = a.gamma ? dn[e] * g[e] : dn[e];
-                acc_gamma[k][e] = fmaf(dn[e], xh, acc_gamma[k][e]);
                 acc_beta[k][e] += dn[e];
-                const float v = r * (u - mu - xh * mx);
+                const float dnr = dn[e] * r;
+                acc_gamma[k][e] = fmaf(dnr, d[k][e], acc_gamma[k][e]);
+                const float v = fmaf(slope, d[k][e], a.gamma ? fmaf(dnr, g[e], shift) : dnr + shift);
                 D[e] = a.dh ? D[e] + v : v;
             }
             if (a.dx) row_store<T, NT>(static_cast<T*>(a.dx) + (base + grp) * a.lddx, t + k * TPR, nfull, rem, D);
