@@ -22,7 +22,7 @@
 //   m = OR_SMALL, where A and B cost little, they have two planes, too (64 x 512: 1.75e-3 instead of 2.4e-3 with the
 //   1.66e-3 of rounding the result to bf16).
 //   fp32 matrices: two planes everywhere, every product is hi lo + lo hi + hi hi.
-// Sums are fp32 in the matrix cores, the norm fp64.  The cores cut a sum off where it leaves fp32: each 16 terms added
+// Sums are fp32 in the matrix cores, the norm's fp64.  The cores cut a sum off where it leaves fp32: each 16 terms added
 // to a sum of S take up to 2^-23 S from it, always towards zero, so the small products come first (16 x 4099 fp32:
 // 7.2e-6 with hi hi first).
 #pragma once
@@ -93,7 +93,9 @@ __device__ __forceinline__ void or_split(const float (&v)[8], u32x4& hi, u32x4& 
     lo = __builtin_bit_cast(u32x4, l);
 }
 
-// Squares of a matrix, in fp64; workgroup (p, matrix) adds up its share.
+// Squares of a matrix; workgroup (p, matrix) adds up its share.  Those of a vector in fp32, these sums in fp64; a vector
+// whose sum leaves the middle of fp32's range (or is zero, infinite or NaN) is taken in fp64 as a whole, where no
+// square of an fp32 value overflows or vanishes.
 template <typename T>
 __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
     constexpr int N = RowVec<T>::N, AHEAD = 8;
@@ -109,13 +111,18 @@ __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
         for (int k = 0; k < AHEAD; ++k) raw[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)min(v + k * 256, v1 - 1) * N);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            float f[N];
+            if (v + k * 256 >= v1) break;
+            float f[N], q = 0.f;
             RowVec<T>::unpack(raw[k], f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const double x = v + k * 256 < v1 ? (double)f[e] : 0.0;
-                s = fma(x, x, s);
+            for (int e = 0; e < N; ++e) q = fmaf(f[e], f[e], q);
+            double d = (double)q;
+            if (!(q > 0x1p-60f && q < 0x1p120f)) {
+                d = 0.0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) d = fma((double)f[e], (double)f[e], d);
             }
+            s += d;
         }
     }
     if (blockIdx.x == OR_NORM_BLOCKS - 1 && (int)threadIdx.x < rem) {

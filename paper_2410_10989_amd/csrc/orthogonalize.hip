@@ -23,7 +23,7 @@ constexpr double OR_MAX_NORM = 1024.0;                   // that a singular valu
 constexpr int64_t OR_TILES_256 = 128;                    // fewest tiles of 256 that a launch takes those for
 constexpr int64_t OR_SLOTS_128 = 512;                    // workgroups of 128-tiles that run at a time
 constexpr int64_t OR_RANGE_STEPS = 4, OR_MAX_RANGES = 16;   // fewest K steps of a range, most ranges
-constexpr int64_t OR_SAVED_STEPS = 32;                   // K steps one after the other that ranges have to save
+constexpr int64_t OR_SAVED_STEPS = 64;                   // K steps one after the other that ranges have to save
 constexpr int64_t OR_ROUNDS = 1024;                      // tiles of a launch that more matrices would not fill better
 constexpr float OR_USUAL[3] = {3.4445f, -4.7750f, 2.0315f};
 
@@ -45,7 +45,7 @@ struct OrPlan {
     int b_matrices;                   // that there is room for
     int64_t group;                    // matrices at a time
     size_t x_bytes, a_bytes, bytes;   // of one matrix: X (there are two), A (and B); all of them, and its partial sums
-    size_t part_bytes;                // K ranges' sums, of all matrices
+    int64_t tiles;                    // of 128, of the product with the most of them
     OrStep steps[OR_MAX_STEPS];
 };
 
@@ -88,6 +88,12 @@ int steps_of(const flce_orthogonalize_args& b, OrStep* to) {
     return FLCE_OK;
 }
 
+// Workspace of a group: its matrices' and the sums of K ranges.
+size_t part_bytes(const OrPlan& p, int64_t group) {
+    return (size_t)std::min(OR_SLOTS_128, OR_MAX_RANGES * p.tiles * group) * 128 * 128 * sizeof(float);
+}
+size_t group_bytes(const OrPlan& p, int64_t group) { return part_bytes(p, group) + (size_t)group * p.bytes; }
+
 int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     if (!args) return FLCE_ERR_NULL;
     const flce_orthogonalize_args& b = *args;
@@ -110,7 +116,7 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     p->iterate = small && b.steps <= OR_ITERATE_STEPS && growth <= OR_ITERATE_GROWTH;
     p->b_matrices = small ? OR_ITERATE_STEPS + 1 : 2;   // (the same room whatever the steps are)
     p->bytes = 2 * p->x_bytes + (1 + p->b_matrices) * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) + 256;
-    p->part_bytes = OR_SLOTS_128 * 128 * 128 * sizeof(float);
+    p->tiles = ((p->mp + 127) / 128) * ((p->np + 127) / 128);
     // Matrices at a time: until the launch with the fewest tiles has several rounds of them.
     const int64_t t = (p->mp + 255) / 256, tiles = t * (t + 1) / 2;
     p->group = std::max<int64_t>(1, std::min<int64_t>({n, OR_MATRICES, (OR_ROUNDS + tiles - 1) / tiles}));
@@ -154,7 +160,7 @@ int launch_product(OrArgs& a, hipStream_t s) {
 template <typename T, int GP, int PL>
 int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* const* in, void* const* out, int count, char* ws, hipStream_t s) {
     const bool tall = b.rows > b.cols;
-    size_t at = p.part_bytes;
+    size_t at = part_bytes(p, count);
     auto take = [&](size_t bytes) {
         char* here = ws + at;
         at += aligned_bytes(bytes);
@@ -328,10 +334,10 @@ int flce_orthogonalize(const void* const* in, void* const* out, int n_matrices, 
         FLCE_TRY(shared_workspace_lent(&lent));
         if (lent) cap = lent;
     }
-    if (cap < p.part_bytes + p.bytes) return FLCE_ERR_WORKSPACE;
-    p.group = (int64_t)std::min<size_t>((size_t)p.group, (cap - p.part_bytes) / p.bytes);
+    while (p.group > 1 && group_bytes(p, p.group) > cap) --p.group;
+    if (group_bytes(p, p.group) > cap) return FLCE_ERR_WORKSPACE;
     while (!ws) {
-        const int rc = shared_workspace(p.part_bytes + (size_t)p.group * p.bytes, &ws, s, p.group == 1);
+        const int rc = shared_workspace(group_bytes(p, p.group), &ws, s, p.group == 1);
         if (rc == FLCE_OK) break;
         if (rc != FLCE_ERR_WORKSPACE || p.group == 1) return rc;
         p.group = (p.group + 1) / 2;
@@ -344,7 +350,7 @@ int flce_orthogonalize(const void* const* in, void* const* out, int n_matrices, 
         pieces[k++] = {w, w + bytes, true};
         if (r != w) pieces[k++] = {r, r + bytes, false};
     }
-    pieces[k++] = {reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + p.part_bytes + (size_t)p.group * p.bytes, true};
+    pieces[k++] = {reinterpret_cast<uintptr_t>(ws), reinterpret_cast<uintptr_t>(ws) + group_bytes(p, p.group), true};
     const bool shared = written_twice(pieces, k);
     delete[] pieces;
     if (shared) return FLCE_ERR_ARG;
@@ -359,7 +365,7 @@ int flce_orthogonalize(const void* const* in, void* const* out, int n_matrices, 
 
 size_t flce_orthogonalize_workspace_bytes(int n_matrices, const flce_orthogonalize_args* args) {
     OrPlan p;
-    return or_plan(args, n_matrices, &p) == FLCE_OK && n_matrices ? p.part_bytes + (size_t)p.group * p.bytes : 0;
+    return or_plan(args, n_matrices, &p) == FLCE_OK && n_matrices ? group_bytes(p, p.group) : 0;
 }
 
 }  // extern "C"
