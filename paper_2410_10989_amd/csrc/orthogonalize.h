@@ -48,6 +48,7 @@ enum { OR_WHOLE = 0, OR_RANGES = 1, OR_JOIN = 2 };
 
 struct OrArgs {
     const f16_t *X, *A, *B;      // planes, of the first matrix; X: rows of [hi np | lo np], A and B of [hi mp (| lo mp)]
+    int ldx, lda;                // from row to row
     f16_t* to;                   // the product's, unless OR_LAST
     int64_t stride_x, stride_a;  // elements from one matrix to the next
     int mp, np;                  // m and n, padded
@@ -68,7 +69,7 @@ struct OrLoadArgs {
     float* factor;               // of each matrix
     f16_t* X;
     int64_t stride_x;
-    int rows, cols, mp, np;
+    int rows, cols, mp, np, ldx;
     int planes;                  // of X that are read
     int exponent;                // the largest element of the first X may be 2 to this
     double eps;
@@ -103,15 +104,14 @@ __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
     const T* in = static_cast<const T*>(a.in[blockIdx.y]);
     const int64_t all = (int64_t)a.rows * a.cols;
     const int nfull = (int)(all / N), rem = (int)(all % N);
-    const int v0 = (int)((int64_t)nfull * blockIdx.x / OR_NORM_BLOCKS), v1 = (int)((int64_t)nfull * (blockIdx.x + 1) / OR_NORM_BLOCKS);
     double s = 0.0;
-    for (int v = v0 + (int)threadIdx.x; v < v1; v += AHEAD * 256) {
-        u32x4 raw[AHEAD];   // (all loads before the first sum; past the share the last one again)
+    for (int v = (int)blockIdx.x * (AHEAD * 256) + (int)threadIdx.x; v < nfull; v += OR_NORM_BLOCKS * AHEAD * 256) {
+        u32x4 raw[AHEAD];   // (all loads before the first sum; past the end the last one again)
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) raw[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)min(v + k * 256, v1 - 1) * N);
+        for (int k = 0; k < AHEAD; ++k) raw[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)min(v + k * 256, nfull - 1) * N);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            if (v + k * 256 >= v1) break;
+            if (v + k * 256 >= nfull) break;
             float f[N], q = 0.f;
             RowVec<T>::unpack(raw[k], f);
 #pragma unroll
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
         for (int k = 0; k < 8; ++k) v[k] = TALL ? tile[c + k][r] : tile[r][c + k];
         u32x4 hi, lo;
         or_split(v, hi, lo);
-        f16_t* to = X + (int64_t)(m0 + r) * 2 * a.np + n0 + c;
+        f16_t* to = X + (int64_t)(m0 + r) * a.ldx + n0 + c;
         *reinterpret_cast<u32x4*>(to) = hi;
         if (a.planes == 2) *reinterpret_cast<u32x4*>(to + a.np) = lo;
     }
@@ -332,7 +332,7 @@ struct OrOut {
     static constexpr bool LO_ONLY = PRODUCT >= OR_APPLY;
 
     __amdgpu_buffer_rsrc_t rsrc_in, rsrc_out;
-    int ld;          // columns of a plane, of the addend and of the output
+    int ld, pitch;   // columns of a plane and from row to row, of the addend and of the output
     int rows_all;    // their rows
     int row0, col0;  // of the wavefront's part
     int lane;
@@ -340,23 +340,21 @@ struct OrOut {
     u32x4 addend[IN ? 2 : 1][NACC][IN ? IN : 1];
     static_assert(64 * PITCH * 4 <= fg_lds_bytes(TILE) / 4, "two passes fit a wavefront's share of LDS");
 
-    __device__ __forceinline__ void init(const f16_t* in, f16_t* to, int ld_, int rows_, bool add, int r0, int c0, unsigned char* smem,
+    __device__ __forceinline__ void init(const f16_t* in, f16_t* to, int ld_, int pitch_, int rows_, bool add, int r0, int c0, unsigned char* smem,
                                          int lane_, int uwave) {
         ld = ld_;
+        pitch = pitch_;
         rows_all = rows_;
         row0 = r0;
         col0 = c0;
         lane = lane_;
         stage = reinterpret_cast<float*>(smem + uwave * (fg_lds_bytes(TILE) / 4));
         // (a range of zero bytes makes every load return zero without touching memory)
-        if constexpr (IN > 0) rsrc_in = fg_make_rsrc(in, add ? (uint32_t)rows_all * (uint32_t)ld * (LO_ONLY ? 4u : 2u * IN) : 0u);
-        if constexpr (!LAST) rsrc_out = fg_make_rsrc(to, (uint32_t)rows_all * (uint32_t)ld * (2u * OUT));
+        if constexpr (IN > 0) rsrc_in = fg_make_rsrc(in, add ? (uint32_t)rows_all * (uint32_t)pitch * 2u : 0u);
+        if constexpr (!LAST) rsrc_out = fg_make_rsrc(to, (uint32_t)rows_all * (uint32_t)pitch * 2u);
     }
-    // byte offset of 8 values in a matrix of P planes, or one past its end
-    template <int P>
-    __device__ __forceinline__ int at(int row, int col) const {
-        return row < rows_all && col < ld ? (row * (P * ld) + col) * 2 : 0x7fffffff;
-    }
+    // byte offset of 8 values in the first plane, or one past the end
+    __device__ __forceinline__ int at(int row, int col) const { return row < rows_all && col < ld ? (row * pitch + col) * 2 : 0x7fffffff; }
     __device__ __forceinline__ int lane_row(int k) const { return k * ROWS + lane / LANES; }
     __device__ __forceinline__ int lane_col() const { return lane % LANES * 8; }
 
@@ -365,7 +363,7 @@ struct OrOut {
         if constexpr (IN > 0) {
 #pragma unroll
             for (int k = 0; k < NACC; ++k) {
-                const int off = at<LO_ONLY ? 2 : IN>(row0 + pass * 32 + lane_row(k), col0 + lane_col());
+                const int off = at(row0 + pass * 32 + lane_row(k), col0 + lane_col());
 #pragma unroll
                 for (int p = 0; p < IN; ++p)
                     addend[BUF][k][p] = __builtin_amdgcn_raw_buffer_load_b128(rsrc_in, off, (LO_ONLY ? 1 : p) * ld * 2, 0);
@@ -378,7 +376,7 @@ struct OrOut {
     __device__ __forceinline__ void put_planes(int row, int col, const float (&v)[8], bool put_lo) {
         u32x4 hi, lo;
         or_split(v, hi, lo);
-        const uint32_t off = (uint32_t)at<OUT>(row, col);
+        const uint32_t off = (uint32_t)at(row, col);
         __builtin_amdgcn_raw_buffer_store_b128(hi, rsrc_out, (int)off, 0, 0);
         if (OUT == 2 && put_lo) __builtin_amdgcn_raw_buffer_store_b128(lo, rsrc_out, (int)(off + 2u * (uint32_t)ld), 0, 0);
     }
@@ -507,8 +505,6 @@ template <int PRODUCT, int PL, int OUT, int TILE, typename OutT, bool TALL, int 
 __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_kernel(OrArgs a) {
     constexpr bool SYMMETRIC = PRODUCT <= OR_MULTIPLY, B_KM = !SYMMETRIC;
     constexpr int ORDER = PL == 2 ? FG_PLANES : FG_PLAIN, W = TILE / 64;
-    // planes of the matrices' rows: X 2; A and B what the Gram product stores
-    constexpr int PA = PRODUCT == OR_GRAM ? OUT : PL;
     __shared__ __attribute__((aligned(16))) unsigned char smem[fg_lds_bytes(TILE)];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave >> 1, wn = wave & 1;
@@ -537,7 +533,8 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
     if ((PRODUCT == OR_GRAM || PRODUCT >= OR_APPLY) && a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : a.factor[matrix];
     OrOut<PRODUCT, PL, OUT, TILE, OutT, TALL> out;
     auto begin_out = [&]() {
-        out.init(PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N, a.mp,
+        out.init(PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N,
+                 SYMMETRIC ? a.lda : a.ldx, a.mp,
                  PRODUCT == OR_POLY || a.add_lo, m0 + __builtin_amdgcn_readfirstlane(wm) * (TILE / 2),
                  n0 + __builtin_amdgcn_readfirstlane(wn) * (TILE / 2), smem, lane, uwave);
     };
@@ -573,7 +570,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
         constexpr bool RIGHT_M = PRODUCT == OR_POLY || PRODUCT == OR_MULTIPLY;   // the right one is m x m
         const f16_t* left = PRODUCT == OR_GRAM ? X : (PRODUCT >= OR_APPLY ? a.B : a.A) + matrix * a.stride_a;
         const f16_t* right = PRODUCT == OR_POLY ? left : PRODUCT == OR_MULTIPLY ? a.B + matrix * a.stride_a : X;
-        const int ldl = PRODUCT == OR_GRAM ? 2 * a.np : PA * a.mp, ldr = RIGHT_M ? PA * a.mp : 2 * a.np;
+        const int ldl = PRODUCT == OR_GRAM ? a.ldx : a.lda, ldr = RIGHT_M ? a.lda : a.ldx;
         FgOperand<false, TILE, ORDER> opa;
         FgOperand<B_KM, TILE, ORDER> opb;
         opa.init(reinterpret_cast<const bf16_t*>(left), ldl, m0, a.mp, K, tid, wm);
@@ -641,6 +638,7 @@ struct OrIterateArgs {
     f16_t* Q;
     f16_t* B;            // steps matrices for each
     int64_t stride_a;
+    int lda;
     int steps;
     float square[OR_ITERATE_STEPS], linear[OR_ITERATE_STEPS], diagonal[OR_ITERATE_STEPS];   // of B
     float t[OR_ITERATE_STEPS], next[OR_ITERATE_STEPS], q[OR_ITERATE_STEPS];                 // powers of two of B A, (B A) B, B Q
@@ -722,7 +720,7 @@ __global__ __launch_bounds__(256) void or_iterate_kernel(OrIterateArgs a) {
     auto fetch = [&](f16_t (&to)[2][MP * PITCH], const f16_t* from) {   // planes in memory: rows of [hi MP | lo MP]
         for (int i = tid; i < MP * MP / 4; i += 256) {
             const int row = i / (MP / 4), at = i % (MP / 4) * 8, plane = at / MP, col = at % MP;
-            *reinterpret_cast<u32x4*>(&to[plane][row * PITCH + col]) = *reinterpret_cast<const u32x4*>(from + (int64_t)row * 2 * MP + at);
+            *reinterpret_cast<u32x4*>(&to[plane][row * PITCH + col]) = *reinterpret_cast<const u32x4*>(from + (int64_t)row * a.lda + at);
         }
     };
     f16_t* Bs = a.B + matrix * a.steps * a.stride_a;
@@ -740,7 +738,7 @@ __global__ __launch_bounds__(256) void or_iterate_kernel(OrIterateArgs a) {
             split4(v, h, l);
             *reinterpret_cast<f16x4*>(&lds[1][0][row * PITCH + col]) = h;
             *reinterpret_cast<f16x4*>(&lds[1][1][row * PITCH + col]) = l;
-            f16_t* to = Bs + k * a.stride_a + (int64_t)row * 2 * MP + col;
+            f16_t* to = Bs + k * a.stride_a + (int64_t)row * a.lda + col;
             *reinterpret_cast<f16x4*>(to) = h;
             *reinterpret_cast<f16x4*>(to + MP) = l;
         });
@@ -767,7 +765,7 @@ __global__ __launch_bounds__(256) void or_iterate_kernel(OrIterateArgs a) {
     f16_t* Q = a.Q + matrix * a.stride_a;
     for (int i = tid; i < MP * MP / 4; i += 256) {
         const int row = i / (MP / 4), at = i % (MP / 4) * 8, plane = at / MP, col = at % MP;
-        *reinterpret_cast<u32x4*>(Q + (int64_t)row * 2 * MP + at) = *reinterpret_cast<const u32x4*>(&lds[1][plane][row * PITCH + col]);
+        *reinterpret_cast<u32x4*>(Q + (int64_t)row * a.lda + at) = *reinterpret_cast<const u32x4*>(&lds[1][plane][row * PITCH + col]);
     }
 }
 

@@ -38,7 +38,7 @@ struct OrStep {
     double most_b;       // B's largest eigenvalue
 };
 struct OrPlan {
-    int64_t mp, np;
+    int64_t mp, np, ldx, lda;
     int planes;                       // that POLY and APPLY multiply, and of A and B
     int gram_planes;                  // that GRAM multiplies
     bool iterate;                     // the steps in m x m matrices alone (or_iterate_kernel)
@@ -108,8 +108,10 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     FLCE_TRY(steps_of(b, p->steps));
     p->gram_planes = b.dtype == FLCE_F32 ? 2 : 1;
     p->planes = b.dtype == FLCE_F32 || p->mp <= OR_SMALL ? 2 : 1;
-    p->x_bytes = aligned_bytes((size_t)(p->mp * p->np) * 2 * sizeof(f16_t));
-    p->a_bytes = aligned_bytes((size_t)(p->mp * p->mp) * p->planes * sizeof(f16_t));
+    p->ldx = 2 * p->np;
+    p->lda = p->planes * p->mp;
+    p->x_bytes = aligned_bytes((size_t)(p->mp * p->ldx) * sizeof(f16_t));
+    p->a_bytes = aligned_bytes((size_t)(p->mp * p->lda) * sizeof(f16_t));
     float growth = 1.0f;
     for (int k = 0; k + 1 < b.steps; ++k) growth = std::min(growth * std::max(1.0f, p->steps[k].a * p->steps[k].a), 1e30f);
     const bool small = b.dtype == FLCE_BF16 && p->mp <= OR_ITERATE_MOST;
@@ -179,6 +181,7 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     l.cols = (int)b.cols;
     l.mp = (int)p.mp;
     l.np = (int)p.np;
+    l.ldx = (int)p.ldx;
     l.planes = PL;
     l.exponent = p.steps[0].e_x;
     l.eps = b.eps;
@@ -196,6 +199,8 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     a.stride_a = (int64_t)(p.a_bytes / sizeof(f16_t));
     a.mp = l.mp;
     a.np = l.np;
+    a.ldx = (int)p.ldx;
+    a.lda = (int)p.lda;
     a.count = count;
     a.rows = l.rows;
     a.cols = l.cols;
@@ -214,6 +219,7 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
             it.Q = B;
             it.B = B + count * a.stride_a;
             it.stride_a = a.stride_a;
+            it.lda = a.lda;
             it.steps = b.steps;
             double most_q = p.steps[b.steps - 1].most_b;
             int e_q = p.steps[b.steps - 1].e_b;
