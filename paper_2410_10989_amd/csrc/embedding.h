@@ -8,7 +8,7 @@
 //                           launch: a workgroup owns every `classes`-th token and looks at all rows, so it counts what
 //                           lies before its tokens itself and waits for nobody.  (Neighbouring tokens belong to different
 //                           workgroups: the frequent ones are neighbours.  With 512 tokens in a row for each, the first
-//                           workgroup had half of 16384 rows to place, 28 us; TIMES.)
+//                           workgroup had half of 16384 rows to place, 28 us; 10 so.)
 //   2. embed_sum_kernel     pieces of consecutive entries of that order, a wavefront per piece and 64 vectors of the row:
 //                           the same work for everybody, however often a token comes.  What begins and ends in a
 //                           piece is written at once, the rest is left as fp32 sums.  Further workgroups fill the rows
@@ -219,7 +219,7 @@ __device__ __forceinline__ void embed_put(const EmbedArgs& a, int token, int v, 
 }
 
 // ADD: a.add.  What finished sums are added to is loaded with the rows of a group, not when a sum is finished (5734 rows
-// of 2304, most tokens once or twice: a wait for memory after another, 37 us; TIMES).
+// of 2304, most tokens once or twice: a wait for memory after another, 37 us; 13 so).
 template <typename T, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a) {
     constexpr int N = RowVec<T>::N;

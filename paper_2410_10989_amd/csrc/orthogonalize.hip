@@ -41,7 +41,7 @@ struct OrPlan {
     int64_t mp, np, ldx, lda;
     int planes;                       // that POLY and APPLY multiply, and of A and B
     int gram_planes;                  // that GRAM multiplies
-    bool iterate;                     // the steps in m x m matrices alone (or_iterate_kernel)
+    bool iterate;                     // all steps in m x m matrices alone (or_iterate_kernel)
     int b_matrices;                   // that there is room for
     int64_t group;                    // matrices at a time
     size_t x_bytes, a_bytes, bytes;   // of one matrix: X (there are two), A (and B); all of them, and its partial sums
@@ -116,7 +116,7 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     for (int k = 0; k + 1 < b.steps; ++k) growth = std::min(growth * std::max(1.0f, p->steps[k].a * p->steps[k].a), 1e30f);
     const bool small = b.dtype == FLCE_BF16 && p->mp <= OR_ITERATE_MOST;
     p->iterate = small && b.steps <= OR_ITERATE_STEPS && growth <= OR_ITERATE_GROWTH;
-    p->b_matrices = small ? OR_ITERATE_STEPS + 1 : 2;   // (the same room whatever the steps are)
+    p->b_matrices = small ? 1 + OR_ITERATE_STEPS : 2;   // (whatever the steps are)
     p->bytes = 2 * p->x_bytes + (1 + p->b_matrices) * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) + 256;
     p->tiles = ((p->mp + 127) / 128) * ((p->np + 127) / 128);
     // Matrices at a time: until the launch with the fewest tiles has several rounds of them.
@@ -156,6 +156,29 @@ int launch_product(OrArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_JOIN>), grid(2 * total), dim3(FG_THREADS), 0, s, a);
     HIP_TRY(hipGetLastError());
     return FLCE_OK;
+}
+
+// What or_iterate_kernel needs for it->steps steps; returns the exponent that Q is held with.
+int iterate_args(const OrPlan& p, OrIterateArgs* it) {
+    const OrStep* steps = p.steps;
+    const int last = it->steps - 1;
+    double most_q = steps[last].most_b;
+    int e_q = steps[last].e_b;
+    for (int i = last; i >= 0; --i) {
+        const OrStep& st = steps[i];
+        it->square[i] = ldexpf(st.c, st.e_b - 2 * st.e_a);
+        it->linear[i] = ldexpf(st.b, st.e_b - st.e_a);
+        it->diagonal[i] = ldexpf(st.a, st.e_b);
+        if (i == last) continue;
+        const int e_t = exponent_for(st.most_b * ldexp(1.0, 14 - st.e_a));   // (A's eigenvalues: at most 2^(14 - e_a))
+        it->t[i] = ldexpf(1.0f, e_t - st.e_b - st.e_a);
+        it->next[i] = ldexpf(1.0f, steps[i + 1].e_a - e_t - st.e_b);
+        most_q *= st.most_b;
+        const int e = exponent_for(most_q);
+        it->q[i] = ldexpf(1.0f, e - e_q - st.e_b);
+        e_q = e;
+    }
+    return e_q;
 }
 
 // `count` matrices, in the workspace from ws on.  GP: planes that GRAM multiplies, PL: that the others do.
@@ -206,13 +229,13 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     a.cols = l.cols;
     a.part = reinterpret_cast<float*>(ws);
     for (int i = 0; i < count; ++i) a.out[i] = out[i];
+    // Small matrices: all steps between the first and the last product with X in one launch.
     if constexpr (GP == 1 && PL == 2) {
         if (p.iterate) {
-            const OrStep& first = p.steps[0];
             a.factor = l.factor;
             a.X = X[0];
             a.to = A;
-            a.alpha = ldexpf(1.0f, first.e_a - 2 * first.e_x);
+            a.alpha = ldexpf(1.0f, p.steps[0].e_a - 2 * p.steps[0].e_x);
             FLCE_TRY((launch_product<OR_GRAM, GP, PL, float, false>(a, s)));
             OrIterateArgs it{};
             it.A = A;
@@ -221,28 +244,13 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
             it.stride_a = a.stride_a;
             it.lda = a.lda;
             it.steps = b.steps;
-            double most_q = p.steps[b.steps - 1].most_b;
-            int e_q = p.steps[b.steps - 1].e_b;
-            for (int k = b.steps - 1; k >= 0; --k) {
-                const OrStep& st = p.steps[k];
-                it.square[k] = ldexpf(st.c, st.e_b - 2 * st.e_a);
-                it.linear[k] = ldexpf(st.b, st.e_b - st.e_a);
-                it.diagonal[k] = ldexpf(st.a, st.e_b);
-                if (k + 1 == b.steps) continue;
-                const int e_t = exponent_for(st.most_b * ldexp(1.0, 14 - st.e_a));   // (A's eigenvalues: at most 2^(14 - e_a))
-                it.t[k] = ldexpf(1.0f, e_t - st.e_b - st.e_a);
-                it.next[k] = ldexpf(1.0f, p.steps[k + 1].e_a - e_t - st.e_b);
-                most_q *= st.most_b;
-                const int e = exponent_for(most_q);
-                it.q[k] = ldexpf(1.0f, e - e_q - st.e_b);
-                e_q = e;
-            }
+            const int e_q = iterate_args(p, &it);
             if (p.mp == 64) hipLaunchKernelGGL((or_iterate_kernel<64>), dim3((unsigned)count), dim3(256), 0, s, it);
             else hipLaunchKernelGGL((or_iterate_kernel<128>), dim3((unsigned)count), dim3(256), 0, s, it);
             HIP_TRY(hipGetLastError());
-            a.alpha = ldexpf(b.scale, -e_q - first.e_x);
-            if (tall) return launch_product<OR_LAST, PL, 2, T, true>(a, s);
-            return launch_product<OR_LAST, PL, 2, T, false>(a, s);
+            a.B = B;
+            a.alpha = ldexpf(b.scale, -e_q - p.steps[0].e_x);
+            return tall ? launch_product<OR_LAST, PL, 2, T, true>(a, s) : launch_product<OR_LAST, PL, 2, T, false>(a, s);
         }
     }
     // Two steps at a time where launches fill the chip and X is long (see orthogonalize.h), never twice in a row.
