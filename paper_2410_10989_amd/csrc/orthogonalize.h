@@ -78,6 +78,12 @@ struct OrLoadArgs {
 __device__ __forceinline__ f32x16 or_mfma(bf16x8 b, bf16x8 a, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
 }
+// Adds the product of the operands' blocks i and j; TURN: to its transpose.
+template <bool TURN, int W>
+__device__ __forceinline__ void or_multiply(f32x16 (&acc)[W][W], int i, int j, bf16x8 a, bf16x8 b) {
+    if constexpr (TURN) acc[j][i] = or_mfma(a, b, acc[j][i]);
+    else acc[i][j] = or_mfma(b, a, acc[i][j]);
+}
 
 // 8 values as two planes: hi, and what it leaves of them.  (Each value is made to be an fp32 number first: a product that
 // the compiler rounds to fp16 at once for the one plane and by way of fp32 for the other gives two his now and then.)
@@ -106,14 +112,14 @@ __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
     const int nfull = (int)(all / N), rem = (int)(all % N);
     double s = 0.0;
     for (int v = (int)blockIdx.x * (AHEAD * 256) + (int)threadIdx.x; v < nfull; v += OR_NORM_BLOCKS * AHEAD * 256) {
-        u32x4 raw[AHEAD];   // (all loads before the first sum; past the end the last one again)
+        u32x4 raw[AHEAD];   // (all loads before the first sum; past the end the last vector again, which counts as zeros)
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) raw[k] = *reinterpret_cast<const u32x4_any*>(in + (int64_t)min(v + k * 256, nfull - 1) * N);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            if (v + k * 256 >= nfull) break;
             float f[N], q = 0.f;
-            RowVec<T>::unpack(raw[k], f);
+            RowVec<T>::unpack(v + k * 256 < nfull ? raw[k] : u32x4{0, 0, 0, 0}, f);
 #pragma unroll
             for (int e = 0; e < N; ++e) q = fmaf(f[e], f[e], q);
             double d = (double)q;
@@ -181,10 +187,11 @@ __global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
 }
 
 // A workgroup's K loop over nk K steps, from the first loads on, up to the last step's last sub-step, whose fragments are
-// left in raw_a[1], raw_b[1] (or_last_quarter multiplies them; loads past the end are still under way: or_drain).  The
+// left in raw_a[1], raw_b[1] (or_last_quarter multiplies them; loads past the end are still under way: or_drain).  TURN: of
+// the product's transpose, whose rows are the operand b's (the matrix instruction takes its operands the other way round).  The
 // loop of fg_product (gemm_bf16_nt.h), which stays as it is there: as a function that both call it compiled to other
 // code for those products.  acc: zeros.  smem: fg_lds_bytes(TILE) of LDS.
-template <bool A_KM, bool B_KM, int TILE, int ORDER, int W>
+template <bool TURN, bool A_KM, bool B_KM, int TILE, int ORDER, int W>
 __device__ __forceinline__ void or_k_loop(FgOperand<A_KM, TILE, ORDER>& opa, FgOperand<B_KM, TILE, ORDER>& opb, int nk,
                                           unsigned char* smem, int uwave, f32x16 (&acc)[W][W], FgRaw<A_KM> (&raw_a)[2][W],
                                           FgRaw<B_KM> (&raw_b)[2][W]) {
@@ -223,8 +230,7 @@ __device__ __forceinline__ void or_k_loop(FgOperand<A_KM, TILE, ORDER>& opa, FgO
         }
         const unsigned sa_addr = lds0 + SA * SLOT, sb_addr = lds0 + SB * SLOT;
         __builtin_amdgcn_sched_barrier(0);
-#define FG_MFMA(q) \
-        acc[(q) / W][(q) % W] = or_mfma(fb[(q) % W], fa[(q) / W], acc[(q) / W][(q) % W])
+#define FG_MFMA(q) or_multiply<TURN>(acc, (q) / W, (q) % W, fa[(q) / W], fb[(q) % W])
 #define FG_DMA(n)                                                          \
         if constexpr (DMA == 1) opb.load_one(smem, SD, kt, uwave, R0 + (n));   \
         if constexpr (DMA == 2) opa.load_one(smem, SD, kt, uwave, R0 + (n))
@@ -305,13 +311,13 @@ __device__ __forceinline__ void or_k_loop(FgOperand<A_KM, TILE, ORDER>& opa, FgO
 }
 
 // Sub-step 3 of the last K step.
-template <bool A_KM, bool B_KM, int W>
+template <bool TURN, bool A_KM, bool B_KM, int W>
 __device__ __forceinline__ void or_last_quarter(f32x16 (&acc)[W][W], FgRaw<A_KM> (&raw_a)[2][W], FgRaw<B_KM> (&raw_b)[2][W]) {
     fg_wait(raw_a[1], raw_b[1]);
 #pragma unroll
     for (int i = 0; i < W; ++i)
 #pragma unroll
-        for (int j = 0; j < W; ++j) acc[i][j] = or_mfma(fg_value(raw_b[1][j]), fg_value(raw_a[1][i]), acc[i][j]);
+        for (int j = 0; j < W; ++j) or_multiply<TURN>(acc, i, j, fg_value(raw_a[1][i]), fg_value(raw_b[1][j]));
 }
 
 // The loads of the tiles past the end still target LDS: let them land, for every
@@ -320,8 +326,9 @@ __device__ __forceinline__ void or_last_quarter(f32x16 (&acc)[W][W], FgRaw<A_KM>
 __device__ __forceinline__ void or_drain() { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Writes a wavefront's part of a tile out, 32 rows at a time through LDS (see FgOut in gemm_bf16_nt.h for the layout of
-// the accumulators), as planes of 8 values per lane, the mirrored tile too; or (OR_LAST) rounded to out, whose rows are
-// the tile's columns where the matrix is tall.  PL: planes that are multiplied, OUT: of A.
+// the accumulators), as planes of 8 values per lane, the mirrored tile too; or (OR_LAST) rounded to out.  Where the matrix
+// is tall, the accumulators hold the transpose (24 matrices of 4096 x 1024, bf16: turning the finished tile around took
+// LASTTIME).  PL: planes that are multiplied, OUT: of A.
 template <int PRODUCT, int PL, int OUT, int TILE, typename OutT, bool TALL>
 struct OrOut {
     static constexpr int WN = TILE / 2, W = TILE / 64;
@@ -329,6 +336,7 @@ struct OrOut {
     static constexpr int PITCH = WN + 4;
     static constexpr bool LAST = PRODUCT == OR_LAST, TURN = LAST && TALL, MIRROR = PRODUCT <= OR_MULTIPLY;
     static constexpr int IN = PRODUCT == OR_POLY ? PL : PRODUCT >= OR_APPLY && PL == 1 ? 1 : 0;   // planes of the addend: A, X's lo
+    static constexpr int AHEAD = TURN ? 0 : IN;   // of these, loaded ahead
     static constexpr bool LO_ONLY = PRODUCT >= OR_APPLY;
 
     __amdgpu_buffer_rsrc_t rsrc_in, rsrc_out;
@@ -337,7 +345,7 @@ struct OrOut {
     int row0, col0;  // of the wavefront's part
     int lane;
     float* stage;
-    u32x4 addend[IN ? 2 : 1][NACC][IN ? IN : 1];
+    u32x4 addend[AHEAD ? 2 : 1][NACC][AHEAD ? AHEAD : 1];
     static_assert(64 * PITCH * 4 <= fg_lds_bytes(TILE) / 4, "two passes fit a wavefront's share of LDS");
 
     __device__ __forceinline__ void init(const f16_t* in, f16_t* to, int ld_, int pitch_, int rows_, bool add, int r0, int c0, unsigned char* smem,
@@ -360,7 +368,7 @@ struct OrOut {
 
     template <int BUF>
     __device__ __forceinline__ void load_addend(int pass) {
-        if constexpr (IN > 0) {
+        if constexpr (AHEAD > 0) {
 #pragma unroll
             for (int k = 0; k < NACC; ++k) {
                 const int off = at(row0 + pass * 32 + lane_row(k), col0 + lane_col());
@@ -404,7 +412,7 @@ struct OrOut {
     __device__ __forceinline__ f32x4* staged(int row, int group) const {
         return reinterpret_cast<f32x4*>(stage + row * PITCH + (group ^ ((row >> 3) & 7)) * 4);
     }
-    // Rows 32 i .. of the wavefront's part, from its accumulators of them; their addend is in buffer BUF.  TURN, MIRROR:
+    // Rows 32 i .. of the wavefront's part, from its accumulators of them; their addend is in buffer BUF.  MIRROR:
     // they are left in half H of the stage, for turned().
     template <int BUF, int H>
     __device__ __forceinline__ void pass(f32x16 (&acc)[W], const OrArgs& a, float alpha, OutT* out, int i) {
@@ -428,7 +436,8 @@ struct OrOut {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) v[e + u] = alpha * q[u];
             }
-            if constexpr (IN > 0) {
+            const int row = row0 + 32 * i + lane_row(k), col = col0 + lane_col();
+            if constexpr (AHEAD > 0) {
 #pragma unroll
                 for (int p = IN - 1; p >= 0; --p) {
                     const f16x8 w = __builtin_bit_cast(f16x8, addend[BUF][k][p]);
@@ -436,14 +445,20 @@ struct OrOut {
                     for (int e = 0; e < 8; ++e) v[e] = fmaf(a.beta, (float)w[e], v[e]);
                 }
             }
-            const int row = row0 + 32 * i + lane_row(k), col = col0 + lane_col();
+            if constexpr (TURN && IN > 0) {
+                if (a.add_lo) {   // (a last step that multiplies an error by more than OR_CARRY: columns of X)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[e] = fmaf(a.beta, (float)__builtin_bit_cast(f16_t, __builtin_amdgcn_raw_buffer_load_b16(rsrc_in, at(col + e, row), ld * 2, 0)), v[e]);
+                }
+            }
             if constexpr (PRODUCT == OR_POLY) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += row == col + e ? a.diagonal : 0.f;
             }
-            if constexpr (!LAST) put_planes(row, col, v, put_lo);
-            else if constexpr (!TALL) put_out(out, a.rows, a.cols, row, col, v);
-            if constexpr (TURN || MIRROR) {
+            if constexpr (LAST) put_out(out, a.rows, a.cols, row, col, v);
+            else put_planes(row, col, v, put_lo);
+            if constexpr (MIRROR) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 4)
                     *staged(H * 32 + lane_row(k), (lane_col() + e) / 4) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
@@ -454,7 +469,7 @@ struct OrOut {
     // The 64 rows (PASSES = 2) or 32 in the stage, whose first is row 32 i, as columns: whole lines of 128 bytes of 16-bit
     // values.
     template <int PASSES>
-    __device__ __forceinline__ void turned(const OrArgs& a, OutT* out, int i) {
+    __device__ __forceinline__ void turned(const OrArgs& a, int i) {
         constexpr int LPC = 4 * PASSES;   // lanes per column
         const bool put_lo = PRODUCT != OR_APPLY || PL == 2 || a.put_lo;
 #pragma unroll
@@ -463,8 +478,7 @@ struct OrOut {
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const float*>(staged(r + e, c / 4))[c % 4];
-            if constexpr (TURN) put_out(out, a.rows, a.cols, col0 + c, row0 + 32 * i + r, v);
-            else put_planes(col0 + c, row0 + 32 * i + r, v, put_lo);
+            put_planes(col0 + c, row0 + 32 * i + r, v, put_lo);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -473,11 +487,11 @@ struct OrOut {
         OutT* out = LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
 #pragma unroll
         for (int i = 0; i < W; i += 2) {
-            load_addend<IN ? 1 : 0>(i + 1);
+            load_addend<AHEAD ? 1 : 0>(i + 1);
             pass<0, 0>(acc[i], a, alpha, out, i);
             if (i + 2 < W) load_addend<0>(i + 2);
-            pass<IN ? 1 : 0, 1>(acc[i + 1], a, alpha, out, i + 1);
-            if (TURN || (MIRROR && mirror)) turned<2>(a, out, i);
+            pass<AHEAD ? 1 : 0, 1>(acc[i + 1], a, alpha, out, i + 1);
+            if (MIRROR && mirror) turned<2>(a, i);
         }
     }
 };
@@ -531,12 +545,13 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
     };
     float alpha = a.alpha;
     if ((PRODUCT == OR_GRAM || PRODUCT >= OR_APPLY) && a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : a.factor[matrix];
+    constexpr bool TURN = PRODUCT == OR_LAST && TALL;
     OrOut<PRODUCT, PL, OUT, TILE, OutT, TALL> out;
     auto begin_out = [&]() {
+        const int row0 = m0 + __builtin_amdgcn_readfirstlane(wm) * (TILE / 2), col0 = n0 + __builtin_amdgcn_readfirstlane(wn) * (TILE / 2);
         out.init(PRODUCT == OR_POLY ? a.A + matrix * a.stride_a : X, a.to + matrix * (SYMMETRIC ? a.stride_a : a.stride_x), N,
                  SYMMETRIC ? a.lda : a.ldx, a.mp,
-                 PRODUCT == OR_POLY || a.add_lo, m0 + __builtin_amdgcn_readfirstlane(wm) * (TILE / 2),
-                 n0 + __builtin_amdgcn_readfirstlane(wn) * (TILE / 2), smem, lane, uwave);
+                 PRODUCT == OR_POLY || a.add_lo, TURN ? col0 : row0, TURN ? row0 : col0, smem, lane, uwave);
     };
     if constexpr (PART == OR_JOIN) {
         constexpr int AHEAD = 4;   // ranges whose loads are under way
@@ -564,7 +579,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
         }
         OutT* to = PRODUCT == OR_LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
         out.template pass<0, 0>(acc, a, alpha, to, range);
-        if (out.TURN || (out.MIRROR && tm != tn)) out.template turned<1>(a, to, range);
+        if (out.MIRROR && tm != tn) out.template turned<1>(a, range);
     } else {
         // operands: X X^T, A A, A B (rows of symmetric matrices for columns), B X
         constexpr bool RIGHT_M = PRODUCT == OR_POLY || PRODUCT == OR_MULTIPLY;   // the right one is m x m
@@ -600,12 +615,12 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
                 for (int g = 0; g < 16; ++g) acc[i][j][g] = 0.f;
         FgRaw<false> raw_a[2][W];
         FgRaw<B_KM> raw_b[2][W];
-        or_k_loop(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
+        or_k_loop<TURN>(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
         if constexpr (PART == OR_WHOLE) {
             begin_out();
             out.template load_addend<0>(0);
         }
-        or_last_quarter(acc, raw_a, raw_b);
+        or_last_quarter<TURN>(acc, raw_a, raw_b);
         or_drain();
         if constexpr (PART == OR_WHOLE) {
             out.write(acc, a, alpha, matrix, tm != tn);

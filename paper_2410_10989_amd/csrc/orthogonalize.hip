@@ -20,7 +20,7 @@ constexpr int OR_MAX_STEPS = 32;
 constexpr int64_t OR_PAIR_LENGTH = 2;                    // n / m from which two steps are taken at a time
 constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
-constexpr int64_t OR_TILES_256 = 128;                    // fewest tiles of 256 that a launch takes those for
+constexpr int64_t OR_TILES_256 = 144;                    // fewest tiles of 256 that a launch takes those for
 constexpr int64_t OR_SLOTS_128 = 256;                    // workgroups of 128-tiles that run at a time
 constexpr int64_t OR_RANGE_STEPS = 4, OR_MAX_RANGES = 16;   // fewest K steps of a range, most ranges
 constexpr int64_t OR_SAVED_STEPS = 20;                   // K steps one after the other that ranges have to save

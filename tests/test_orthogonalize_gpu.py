@@ -62,7 +62,7 @@ def test_one_matrix(rows, cols, dtype):
 
 @pytest.mark.parametrize("dtype,count,rows,cols", [("bf16", 5, 130, 70), ("f32", 3, 70, 130), ("bf16", 130, 33, 40), ("bf16", 20, 512, 512),
                                                    ("f32", 14, 512, 768), ("bf16", 9, 1025, 600), ("bf16", 50, 300, 640),
-                                                   ("bf16", 45, 1300, 520), ("f32", 44, 384, 800)])
+                                                   ("bf16", 45, 1300, 520), ("f32", 44, 384, 800), ("f32", 50, 777, 323)])
 def test_lists(dtype, count, rows, cols):
     """Many matrices of a list, on both sizes of tiles, in several groups of launches."""
     import paper_2410_10989_amd as flce
@@ -87,6 +87,17 @@ def test_other_polynomials(kw, dtype):
     got = flce.flce_orthogonalize([torch.from_numpy(G).to(DT[dtype]).cuda()], **kw)[0]
     torch.cuda.synchronize()
     check(got, G, dtype, **{k: float(np.float32(v)) if k == "eps" else v for k, v in kw.items()})
+
+
+@pytest.mark.parametrize("rows,cols,count", [(700, 400, 1), (400, 700, 1), (301, 450, 50), (450, 301, 50)])
+def test_last_step_that_multiplies_errors(rows, cols, count):
+    """The last product adds X's second plane, of columns where the matrix is tall."""
+    import paper_2410_10989_amd as flce
+    G = make(rows, cols, "bf16")
+    kw = dict(steps=2, coefficients=[(3.4445, -4.775, 2.0315), (20.0, -30.0, 11.0)])
+    got = flce.flce_orthogonalize([torch.from_numpy(G).bfloat16().cuda() for _ in range(count)], **kw)
+    check(got[-1], G, "bf16", **{**kw, "coefficients": np.float32(kw["coefficients"]).astype(float).tolist()})
+    assert torch.equal(got[0], got[-1])
 
 
 @pytest.mark.parametrize("dtype,rows,cols,count", [("f32", 192, 192, 1), ("bf16", 192, 192, 1), ("bf16", 60, 100, 1), ("bf16", 128, 128, 1),
