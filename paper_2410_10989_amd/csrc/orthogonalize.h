@@ -320,6 +320,121 @@ __device__ __forceinline__ void or_last_quarter(f32x16 (&acc)[W][W], FgRaw<A_KM>
         for (int j = 0; j < W; ++j) or_multiply<TURN>(acc, i, j, fg_value(raw_a[1][i]), fg_value(raw_b[1][j]));
 }
 
+// The same for operands in two planes and tiles of 128: a K step has both planes of both operands, and takes the three
+// products of them, 48 MFMAs per wavefront between two barriers instead of three times 16 (2 x 1000 x 2047 fp32:
+// 457 us with the three one after the other; PLANESTIME).  The small products have sums of their own.
+// A slot of the ring holds [hi | lo] of an operand's tile, 32 KB, so one workgroup has the LDS of a CU; fragments
+// raw[.][0 .. 1] are of the hi plane, [2 .. 3] of the lo plane.  lo_a, lo_b: bytes from a plane to the other.
+template <bool TURN>
+__device__ __forceinline__ void or_planes_multiply(f32x16 (&acc)[2][2], f32x16 (&small)[2][2], const bf16x8 (&fa)[4], const bf16x8 (&fb)[4], int q) {
+    const int i = q / 2 % 2, j = q % 2;
+    if (q < 4) or_multiply<TURN>(small, i, j, fa[i], fb[2 + j]);
+    else if (q < 8) or_multiply<TURN>(acc, i, j, fa[i], fb[j]);
+    else or_multiply<TURN>(small, i, j, fa[2 + i], fb[j]);
+}
+template <bool TURN, bool B_KM>
+__device__ __forceinline__ void or_planes_loop(const FgOperand<false, 128>& opa, const FgOperand<B_KM, 128>& opb, int lo_a, int lo_b, int nk,
+                                               unsigned char* smem, int uwave, f32x16 (&acc)[2][2], f32x16 (&small)[2][2]) {
+    constexpr int PLANE = fg_slot_bytes(128), SLOT = 2 * PLANE;
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    FgRaw<false> raw_a[2][4];
+    FgRaw<B_KM> raw_b[2][4];
+    auto pipeline_barrier = [&]() { asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };   // (all but the youngest slot)
+    // one of the 8 loads of a wavefront for K step kt into a slot
+    auto load_one = [&](const auto& op, int lo, int slot, int kt, int r) {
+        fg_load_lds(op.rsrc, smem + slot * SLOT + r / 4 * PLANE + uwave * 1024 + r % 4 * 4096, op.off[r % 4], kt * op.kstep + r / 4 * lo);
+    };
+    auto values = [&](auto mb_, bf16x8 (&fa)[4], bf16x8 (&fb)[4]) {
+        constexpr int MB = decltype(mb_)::value;
+        fg_wait(raw_a[MB], raw_b[MB]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            fa[i] = fg_value(raw_a[MB][i]);
+            fb[i] = fg_value(raw_b[MB][i]);
+        }
+    };
+    // One sub-step of K = 16: see or_k_loop.
+    auto quarter = [&](auto mb_, auto kk_, auto sa_, auto sb_, auto dma_, auto sd_, auto r0_, int kt) {
+        constexpr int RB = 1 - decltype(mb_)::value, KK = decltype(kk_)::value, DMA = decltype(dma_)::value, SD = decltype(sd_)::value;
+        constexpr int R0 = decltype(r0_)::value;
+        bf16x8 fa[4], fb[4];
+        values(mb_, fa, fb);
+        const unsigned a_hi = lds0 + decltype(sa_)::value * SLOT, b_hi = lds0 + decltype(sb_)::value * SLOT, a_lo = a_hi + PLANE, b_lo = b_hi + PLANE;
+        __builtin_amdgcn_sched_barrier(0);
+#define OR_MFMA(q) or_planes_multiply<TURN>(acc, small, fa, fb, q)
+#define OR_DMA(n) \
+        if constexpr (DMA == 1) load_one(opb, lo_b, SD, kt, R0 + (n)); \
+        else load_one(opa, lo_a, SD, kt, R0 + (n))
+#define OR_END __builtin_amdgcn_sched_barrier(0)
+        OR_MFMA(0);  fg_issue<KK, 0>(raw_a[RB][0], opa, a_hi); OR_END;
+        OR_MFMA(1);  fg_issue<KK, 0>(raw_b[RB][2], opb, b_lo); OR_END;
+        OR_MFMA(2);  fg_issue<KK, 1>(raw_b[RB][3], opb, b_lo); OR_DMA(0); OR_END;
+        OR_MFMA(3);  fg_issue<KK, 1>(raw_a[RB][1], opa, a_hi); OR_END;
+        OR_MFMA(4);  fg_issue<KK, 0>(raw_b[RB][0], opb, b_hi); OR_END;
+        OR_MFMA(5);  fg_issue<KK, 1>(raw_b[RB][1], opb, b_hi); OR_DMA(1); OR_END;
+        OR_MFMA(6);  fg_issue<KK, 0>(raw_a[RB][2], opa, a_lo); OR_END;
+        OR_MFMA(7);  fg_issue<KK, 1>(raw_a[RB][3], opa, a_lo); OR_END;
+        OR_MFMA(8);  OR_DMA(2); OR_END;
+        OR_MFMA(9);  OR_END;
+        OR_MFMA(10); OR_DMA(3); OR_END;
+        OR_MFMA(11); OR_END;
+#undef OR_MFMA
+#undef OR_DMA
+#undef OR_END
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+    using I4 = std::integral_constant<int, 4>;
+    auto step = [&](auto phase, int t) {
+        constexpr int PH = decltype(phase)::value;
+        using SA = std::integral_constant<int, (2 * PH) % 5>;
+        using SB = std::integral_constant<int, (2 * PH + 1) % 5>;
+        using SB1 = std::integral_constant<int, (2 * PH + 3) % 5>;
+        using SA2 = std::integral_constant<int, (2 * PH + 4) % 5>;
+        quarter(I1{}, I0{}, SA{}, SB{}, I1{}, SB1{}, I0{}, t + 1);
+        quarter(I0{}, I1{}, SA{}, SB{}, I1{}, SB1{}, I4{}, t + 1);
+        quarter(I1{}, I2{}, SA{}, SB{}, I2{}, SA2{}, I0{}, t + 2);
+        quarter(I0{}, I3{}, SA{}, SB{}, I2{}, SA2{}, I4{}, t + 2);
+        pipeline_barrier();
+    };
+#pragma unroll
+    for (int r = 0; r < 8; ++r) load_one(opa, lo_a, 0, 0, r);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) load_one(opb, lo_b, 1, 0, r);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) load_one(opa, lo_a, 2, 1, r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        fg_zero(raw_a[1][i]);
+        fg_zero(raw_b[1][i]);
+    }
+    pipeline_barrier();
+    int t = 0;
+    for (; t + 5 <= nk; t += 5) {
+        step(I0{}, t);
+        step(I1{}, t + 1);
+        step(I2{}, t + 2);
+        step(I3{}, t + 3);
+        step(I4{}, t + 4);
+    }
+    if (t < nk) step(I0{}, t++);
+    if (t < nk) step(I1{}, t++);
+    if (t < nk) step(I2{}, t++);
+    if (t < nk) step(I3{}, t++);
+    bf16x8 fa[4], fb[4];
+    values(I1{}, fa, fb);
+#pragma unroll
+    for (int q = 0; q < 12; ++q) or_planes_multiply<TURN>(acc, small, fa, fb, q);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int g = 0; g < 16; ++g) acc[i][j][g] += small[i][j][g];
+}
+
 // The loads of the tiles past the end still target LDS: let them land, for every
 // wavefront of the workgroup, before LDS is reused (and before the workgroup can
 // retire and its LDS be handed to another one).
@@ -514,12 +629,14 @@ __device__ __forceinline__ void or_tile(int t, int tiles_m, int tiles_n, int& tm
     }
 }
 
-// One workgroup per tile of a matrix (and K range of it), 256 x 256, or 128 x 128 and two workgroups per CU.
+// One workgroup per tile of a matrix (and K range of it), 256 x 256, or 128 x 128 and, unless it multiplies both planes, two
+// workgroups per CU.
 template <int PRODUCT, int PL, int OUT, int TILE, typename OutT, bool TALL, int PART>
-__global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_kernel(OrArgs a) {
+__global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_JOIN) ? 1 : 2) void or_product_kernel(OrArgs a) {
     constexpr bool SYMMETRIC = PRODUCT <= OR_MULTIPLY, B_KM = !SYMMETRIC;
-    constexpr int ORDER = PL == 2 ? FG_PLANES : FG_PLAIN, W = TILE / 64;
-    __shared__ __attribute__((aligned(16))) unsigned char smem[fg_lds_bytes(TILE)];
+    constexpr bool PLANES = PL == 2 && TILE == 128;   // both at a time
+    constexpr int ORDER = PL == 2 && !PLANES ? FG_PLANES : FG_PLAIN, W = TILE / 64;
+    __shared__ __attribute__((aligned(16))) unsigned char smem[fg_lds_bytes(PLANES && PART != OR_JOIN ? 256 : TILE)];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave >> 1, wn = wave & 1;
     // workgroups go round-robin to the XCDs: each gets a stretch of tiles, range by range
@@ -598,10 +715,11 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
         }
         opa.start_at(k0);
         opb.start_at(k0);
-        if constexpr (PL == 2) {
+        const int lo_a = (PRODUCT == OR_GRAM ? a.np : a.mp) * 2, lo_b = (RIGHT_M ? a.mp : a.np) * 2;
+        if constexpr (ORDER == FG_PLANES) {
             opa.plane_steps = opb.plane_steps = nk;
-            opa.plane_bytes = (PRODUCT == OR_GRAM ? a.np : a.mp) * 2;
-            opb.plane_bytes = (RIGHT_M ? a.mp : a.np) * 2;
+            opa.plane_bytes = lo_a;
+            opb.plane_bytes = lo_b;
             opa.lo_part = 1;
             opb.lo_part = 0;
             nk *= 3;
@@ -613,14 +731,27 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 ? 1 : 2) void or_product_ke
             for (int j = 0; j < W; ++j)
 #pragma unroll
                 for (int g = 0; g < 16; ++g) acc[i][j][g] = 0.f;
-        FgRaw<false> raw_a[2][W];
-        FgRaw<B_KM> raw_b[2][W];
-        or_k_loop<TURN>(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
-        if constexpr (PART == OR_WHOLE) {
+        if constexpr (PLANES) {
+            f32x16 small[W][W];
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+#pragma unroll
+                for (int j = 0; j < W; ++j) small[i][j] = acc[i][j];
+            or_planes_loop<TURN>(opa, opb, lo_a, lo_b, nk, smem, uwave, acc, small);
+        } else {
+            FgRaw<false> raw_a[2][W];
+            FgRaw<B_KM> raw_b[2][W];
+            or_k_loop<TURN>(opa, opb, nk, smem, uwave, acc, raw_a, raw_b);
+            if constexpr (PART == OR_WHOLE) {
+                begin_out();
+                out.template load_addend<0>(0);
+            }
+            or_last_quarter<TURN>(acc, raw_a, raw_b);
+        }
+        if constexpr (PLANES && PART == OR_WHOLE) {
             begin_out();
             out.template load_addend<0>(0);
         }
-        or_last_quarter<TURN>(acc, raw_a, raw_b);
         or_drain();
         if constexpr (PART == OR_WHOLE) {
             out.write(acc, a, alpha, matrix, tm != tn);
