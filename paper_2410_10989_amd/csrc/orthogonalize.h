@@ -322,7 +322,7 @@ __device__ __forceinline__ void or_last_quarter(f32x16 (&acc)[W][W], FgRaw<A_KM>
 
 // The same for operands in two planes and tiles of 128: a K step has both planes of both operands, and takes the three
 // products of them, 48 MFMAs per wavefront between two barriers instead of three times 16 (2 x 1000 x 2047 fp32:
-// 457 us with the three one after the other; PLANESTIME).  The small products have sums of their own.
+// 457 us with the three one after the other, 381 so).  The small products have sums of their own.
 // A slot of the ring holds [hi | lo] of an operand's tile, 32 KB, so one workgroup has the LDS of a CU; fragments
 // raw[.][0 .. 1] are of the hi plane, [2 .. 3] of the lo plane.  lo_a, lo_b: bytes from a plane to the other.
 template <bool TURN>
@@ -442,8 +442,8 @@ __device__ __forceinline__ void or_drain() { asm volatile("s_waitcnt vmcnt(0)\n\
 
 // Writes a wavefront's part of a tile out, 32 rows at a time through LDS (see FgOut in gemm_bf16_nt.h for the layout of
 // the accumulators), as planes of 8 values per lane, the mirrored tile too; or (OR_LAST) rounded to out.  Where the matrix
-// is tall, the accumulators hold the transpose (24 matrices of 4096 x 1024, bf16: turning the finished tile around took
-// LASTTIME).  PL: planes that are multiplied, OUT: of A.
+// is tall, the accumulators hold the transpose (24 matrices of 4096 x 1024, bf16: turning the finished tile around
+// took 25 us more).  PL: planes that are multiplied, OUT: of A.
 template <int PRODUCT, int PL, int OUT, int TILE, typename OutT, bool TALL>
 struct OrOut {
     static constexpr int WN = TILE / 2, W = TILE / 64;

@@ -17,13 +17,20 @@ namespace {
 constexpr int64_t OR_MAX_DIM = (int64_t)1 << 20;         // a tile's rows stay below 2^31 bytes apart
 constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: its planes stay below 2^30 bytes
 constexpr int OR_MAX_STEPS = 32;
-constexpr int64_t OR_PAIR_LENGTH = 2;                    // n / m from which two steps are taken at a time
-constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A
+// n / m from which two steps are taken at a time.  24 matrices, bf16, us in pairs and step by step: 1024 x 1024 851 and 821,
+// 1024 x 2048 1062 and 1191, 1024 x 4096 1639 and 2075.
+constexpr int64_t OR_PAIR_LENGTH = 2;
+constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A (see or_iterate_kernel)
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
-constexpr int64_t OR_TILES_256 = 144;                    // fewest tiles of 256 that a launch takes those for
-constexpr int64_t OR_SLOTS_128 = 256;                    // workgroups of 128-tiles that run at a time
-constexpr int64_t OR_RANGE_STEPS = 4, OR_MAX_RANGES = 16;   // fewest K steps of a range, most ranges
-constexpr int64_t OR_SAVED_STEPS = 20;                   // K steps one after the other that ranges have to save
+// Fewest tiles of 256 that a launch takes those for.  bf16, whole calls in tiles of 256 and of 128: 2 x 2048 x 2048 (128 tiles)
+// 574 and 524 us, 16 x 1024 x 1024 (160) 598 and 628.  Operands in two planes, whose tiles of 128 take both at a time:
+// 4 x 2048 x 2048 fp32 (144 and 256 tiles) 2192 with both in tiles of 256, 2046 with the larger ones so, 2101 with none.
+constexpr int64_t OR_TILES_256 = 144, OR_TILES_256_PLANES = 256;
+constexpr int64_t OR_SLOTS_128 = 256;                    // workgroups that ranges of K may make: one per CU
+// Fewest turns of a range's K loop, most ranges, and turns one after the other that ranges have to save (a turn: 64 of K and
+// one product).  us: a range of 8 turns or of 4: 512 x 512 fp32 198 and 223, 256 x 4096 bf16 168 and 182; ranges that
+// save 20 turns or none: 1024 x 1024 bf16 199 and 259; 20 or 32: 512 x 2048 bf16 164 and 191.
+constexpr int64_t OR_RANGE_STEPS = 8, OR_MAX_RANGES = 16, OR_SAVED_STEPS = 20;
 constexpr int64_t OR_ROUNDS = 1024;                      // tiles of a launch that more matrices would not fill better
 constexpr float OR_USUAL[3] = {3.4445f, -4.7750f, 2.0315f};
 
@@ -139,7 +146,7 @@ int launch_product(OrArgs& a, hipStream_t s) {
     };
     auto grid = [](int64_t total) { return dim3((unsigned)((total + FG_XCDS - 1) / FG_XCDS * FG_XCDS)); };
     const int64_t large = tiles_of(256);
-    if (large >= OR_TILES_256) {
+    if (large >= (PL == 2 ? OR_TILES_256_PLANES : OR_TILES_256)) {
         hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 256, OutT, TALL, OR_WHOLE>), grid(large), dim3(FG_THREADS), 0, s, a);
         HIP_TRY(hipGetLastError());
         return FLCE_OK;
