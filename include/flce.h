@@ -428,12 +428,13 @@ FLCE_API size_t flce_grad_norm_workspace_bytes(int n_tensors);
  * which keeps the singular vectors and drives the singular values towards 1.
  *
  * Products are taken in the matrix cores on fp16 operands scaled by powers of two, accumulated in fp32, the X that is
- * carried over in 22 bits.  bf16 matrices: operands of 11 bits; what the result is off by, relative to
- * its norm, is about 1e-3 (its rounding to bf16: 1.7e-3).  fp32 matrices: operands of 22 bits, three products for
- * one, about 5e-7 (fp32 arithmetic: 2e-6).  Both are for the usual coefficients; small singular values and the
- * errors in their directions grow by a factor a per step.  The norm is summed in fp64.  No atomics: the same call
- * gives the same bits.  A matrix that holds infinities or NaN gives NaN, and leaves the others of the list alone;
- * zeros give zeros.
+ * carried over in 22 bits where later steps multiply its errors.  bf16 matrices: operands of 11 bits (up to 256 rows or
+ * columns 22); what the result is off by, relative to its norm, is about 1e-3 next to its rounding to bf16 (1.7e-3).
+ * fp32 matrices: operands of 22 bits, three products for one, about 1e-6 (fp32 arithmetic: 1e-6 for 16 rows, 3e-6 for
+ * 1000).  Both are for the usual coefficients; small singular values and the errors in their directions grow by a factor
+ * a per step.  The norm is summed in fp64 (16 bytes at a time, whose squares are added in fp32 where that can neither
+ * overflow nor vanish).  No atomics: the same call with the same workspace gives the same bits.  A matrix that holds
+ * infinities or NaN gives NaN, and leaves the others of the list alone; zeros give zeros.
  *
  *   in, out       HOST arrays of n_matrices DEVICE pointers to dense row-major rows x cols matrices, aligned to
  *                 their elements; read before the call returns.  out == NULL, or out[i] == in[i]: in place.  No
