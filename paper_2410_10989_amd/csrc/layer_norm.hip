@@ -13,7 +13,11 @@ namespace {
 
 constexpr int64_t LN_MAX_H = (int64_t)1 << 24;      // keeps launches and column numbers within 32 bits
 constexpr int64_t LN_GRID_X = (int64_t)1 << 20;     // workgroups along x, the rest along y
-constexpr int LN_CU_THREADS = 512;                  // threads per CU that the backward is launched for
+// Threads per CU that the backward is launched for; more where a workgroup's row is so short that two of them have too little
+// on the way.  us with 512 and 768, 8192 rows with a residual: 1280 bf16 30.0 and 27.2, 2048 32.1 and 31.3, 2816 42.7
+// and 42.7, 4096 53.7 and 58.5, 1600 fp32 40.9 and 41.5; several rows per workgroup: 16384 x 1024 bf16 29.7 and 35.7.
+constexpr int LN_CU_THREADS = 512, LN_SHORT_CU_THREADS = 768;
+constexpr int64_t LN_SHORT_BYTES = 5632;
 constexpr int64_t LN_CUS = 256, LN_FEW_BLOCKS = 128, LN_ONE_STEPS = 3;
 constexpr int64_t LN_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
@@ -80,7 +84,8 @@ Plan plan_for(const Shape& s, const flce_layer_norm& b, bool gamma, bool beta, i
 Plan plan_of(const Shape& s, const flce_layer_norm& b, bool gamma, bool beta, size_t cap) {
     int64_t target = 1;
     if (!s.tpr || b.rows > LN_ONE_STEPS * groups_of(s)) {
-        const int64_t most = LN_CUS * std::max(1, LN_CU_THREADS / threads_of(s));
+        const bool is_short = s.tpr == 256 && b.H * (int64_t)elem(b.dtype) <= LN_SHORT_BYTES;
+        const int64_t most = LN_CUS * std::max(1, (is_short ? LN_SHORT_CU_THREADS : LN_CU_THREADS) / threads_of(s));
         target = std::min(most, std::max({LN_FEW_BLOCKS, std::min<int64_t>(LN_CUS, b.rows / 4), b.rows / 8}));
     }
     for (;; target /= 2) {
