@@ -136,6 +136,47 @@ def test_zeros_infinities_and_nan():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(37, 90), (90, 37), (300, 261), (261, 300)])
+def test_matrices_at_any_element(rows, cols, dtype):
+    """Neither matrix nor result begins on 16 bytes, nor do their rows; what lies around the result stays."""
+    import paper_2410_10989_amd as flce
+    G = make(rows, cols, dtype)
+    n = rows * cols
+    room = torch.zeros(n + 16, dtype=DT[dtype], device="cuda")
+    to = torch.full((n + 16,), 77.0, dtype=DT[dtype], device="cuda")
+    t, out = room[1:1 + n].view(rows, cols), to[3:3 + n].view(rows, cols)
+    t.copy_(torch.from_numpy(G))
+    flce.flce_orthogonalize([t], outs=[out])
+    check(out, G, dtype)
+    assert (to[:3] == 77.0).all() and (to[3 + n:] == 77.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_zeros_without_eps(dtype):
+    import paper_2410_10989_amd as flce
+    for shape in ((5, 9), (300, 200)):
+        ts = [torch.zeros(shape, dtype=DT[dtype], device="cuda") for _ in range(2)]
+        ts[1][2, 3] = 4.0
+        got = flce.flce_orthogonalize(ts, outs=[torch.empty_like(t) for t in ts], eps=0.0)
+        assert (got[0] == 0).all()
+        check(got[1], ts[1].double().cpu().numpy(), dtype, eps=0.0)
+
+
+def test_a_matrix_that_is_read_twice():
+    """The same update under two results, and in place among others."""
+    import paper_2410_10989_amd as flce
+    a, b = (torch.randn(80, 70, device="cuda") for _ in range(2))
+    want = flce.flce_orthogonalize([a, b], outs=[torch.empty_like(a) for _ in range(2)])
+    outs = [torch.empty_like(a), torch.empty_like(a), b]
+    flce.flce_orthogonalize([a, a, b], outs=outs)
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[0]) and torch.equal(b, want[1])
+    with pytest.raises(flce.FlceError):
+        flce.flce_orthogonalize([a, a])
+    with pytest.raises(flce.FlceError):
+        flce.flce_orthogonalize([a, b], outs=[torch.empty_like(a), a])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_smaller_workspaces_take_fewer_matrices_at_a_time(dtype):
     import paper_2410_10989_amd as flce
     G = [make(140, 90, dtype, seed=i) for i in range(6)]
