@@ -33,6 +33,8 @@ namespace flce {
 
 typedef _Float16 f16_t;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int OR_MATRICES = 120;   // a launch's arguments stay below 4 KB
 constexpr int OR_PAD = 64;         // rows and columns are padded with zeros to whole K steps
@@ -85,19 +87,28 @@ __device__ __forceinline__ void or_multiply(f32x16 (&acc)[W][W], int i, int j, b
     else acc[i][j] = or_mfma(b, a, acc[i][j]);
 }
 
-// 8 values as two planes: hi, and what it leaves of them.  (Each value is made to be an fp32 number first: a product that
-// the compiler rounds to fp16 at once for the one plane and by way of fp32 for the other gives two his now and then.)
-__device__ __forceinline__ void or_split(const float (&v)[8], u32x4& hi, u32x4& lo) {
-    f16x8 h, l;
+// N values as two planes: their hi plane, and what it leaves of them.  (Each value is made to be an fp32 number first, and each
+// pair of the hi plane to be in a register: a product that the compiler rounds to fp16 at once for the one plane and by way of
+// fp32 for the other gives two his now and then.  Pairs take half the conversions, and what is left is one mixed multiply-add:
+// 4 x 64 x 512 fp32 123 us before, 119 so; large matrices, which the power limit holds back, no difference.)
+template <int N>
+__device__ __forceinline__ void or_hi(float (&v)[N], uint32_t (&hi)[N / 2]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float x = v[e];
-        asm("" : "+v"(x));
-        h[e] = (f16_t)x;
-        l[e] = (f16_t)(x - (float)h[e]);
+    for (int p = 0; p < N / 2; ++p) {
+        asm("" : "+v"(v[2 * p]));
+        asm("" : "+v"(v[2 * p + 1]));
+        hi[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2 * p], v[2 * p + 1]}), f16x2));
+        asm("" : "+v"(hi[p]));
     }
-    hi = __builtin_bit_cast(u32x4, h);
-    lo = __builtin_bit_cast(u32x4, l);
+}
+template <int N>
+__device__ __forceinline__ void or_lo(const float (&v)[N], const uint32_t (&hi)[N / 2], uint32_t (&lo)[N / 2]) {
+#pragma unroll
+    for (int p = 0; p < N / 2; ++p) {
+        const f16x2 h = __builtin_bit_cast(f16x2, hi[p]);
+        const float l0 = fmaf((float)h[0], -1.0f, v[2 * p]), l1 = fmaf((float)h[1], -1.0f, v[2 * p + 1]);
+        lo[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{l0, l1}), f16x2));
+    }
 }
 
 // Squares of a matrix; workgroup (p, matrix) adds up its share.  Those of a vector in fp32, these sums in fp64; a vector
@@ -178,11 +189,14 @@ __global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = TALL ? tile[c + k][r] : tile[r][c + k];
-        u32x4 hi, lo;
-        or_split(v, hi, lo);
+        uint32_t hi[4], lo[4];
+        or_hi(v, hi);
         f16_t* to = X + (int64_t)(m0 + r) * a.ldx + n0 + c;
-        *reinterpret_cast<u32x4*>(to) = hi;
-        if (a.planes == 2) *reinterpret_cast<u32x4*>(to + a.np) = lo;
+        *reinterpret_cast<u32x4*>(to) = u32x4{hi[0], hi[1], hi[2], hi[3]};
+        if (a.planes == 2) {
+            or_lo(v, hi, lo);
+            *reinterpret_cast<u32x4*>(to + a.np) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+        }
     }
 }
 
@@ -496,12 +510,15 @@ struct OrOut {
     // (Both stores have their whole offset in a vector register.  With part of it in a scalar one the compiler takes the
     // data for read at once and may let the very next instruction overwrite it; on this chip the store then wrote some of
     // the new values: one lo plane in 10^5, more where the memory pipe was full.)
-    __device__ __forceinline__ void put_planes(int row, int col, const float (&v)[8], bool put_lo) {
-        u32x4 hi, lo;
-        or_split(v, hi, lo);
+    __device__ __forceinline__ void put_planes(int row, int col, float (&v)[8], bool put_lo) {
+        uint32_t hi[4], lo[4];
+        or_hi(v, hi);
         const uint32_t off = (uint32_t)at(row, col);
-        __builtin_amdgcn_raw_buffer_store_b128(hi, rsrc_out, (int)off, 0, 0);
-        if (OUT == 2 && put_lo) __builtin_amdgcn_raw_buffer_store_b128(lo, rsrc_out, (int)(off + 2u * (uint32_t)ld), 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{hi[0], hi[1], hi[2], hi[3]}, rsrc_out, (int)off, 0, 0);
+        if (OUT == 2 && put_lo) {
+            or_lo(v, hi, lo);
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{lo[0], lo[1], lo[2], lo[3]}, rsrc_out, (int)(off + 2u * (uint32_t)ld), 0, 0);
+        }
     }
     static __device__ __forceinline__ void put_out(OutT* out, int rows, int cols, int row, int col, const float (&v)[8]) {
         if (row >= rows || col >= cols) return;
@@ -846,23 +863,15 @@ __global__ __launch_bounds__(256) void or_iterate_kernel(OrIterateArgs a) {
                 }
     };
     typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-    auto split4 = [](const float (&v)[4], f16x4& hi, f16x4& lo) {   // (as or_split)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float x = v[e];
-            asm("" : "+v"(x));
-            hi[e] = (f16_t)x;
-            lo[e] = (f16_t)(x - (float)hi[e]);
-        }
-    };
     auto put = [&](f16_t (&to)[2][MP * PITCH], float scale) {
         each([&](int row, int col, float (&v)[4]) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= scale;
-            f16x4 hi, lo;
-            split4(v, hi, lo);
-            *reinterpret_cast<f16x4*>(&to[0][row * PITCH + col]) = hi;
-            *reinterpret_cast<f16x4*>(&to[1][row * PITCH + col]) = lo;
+            uint32_t hi[2], lo[2];
+            or_hi(v, hi);
+            or_lo(v, hi, lo);
+            *reinterpret_cast<uint2*>(&to[0][row * PITCH + col]) = uint2{hi[0], hi[1]};
+            *reinterpret_cast<uint2*>(&to[1][row * PITCH + col]) = uint2{lo[0], lo[1]};
         });
     };
     auto fetch = [&](f16_t (&to)[2][MP * PITCH], const f16_t* from) {   // planes in memory: rows of [hi MP | lo MP]
@@ -882,13 +891,14 @@ __global__ __launch_bounds__(256) void or_iterate_kernel(OrIterateArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 v[e] = a.square[k] * v[e] + a.linear[k] * ((float)hi[e] + (float)lo[e]) + (row == col + e ? a.diagonal[k] : 0.f);
-            f16x4 h, l;
-            split4(v, h, l);
-            *reinterpret_cast<f16x4*>(&lds[1][0][row * PITCH + col]) = h;
-            *reinterpret_cast<f16x4*>(&lds[1][1][row * PITCH + col]) = l;
+            uint32_t h[2], l[2];
+            or_hi(v, h);
+            or_lo(v, h, l);
+            *reinterpret_cast<uint2*>(&lds[1][0][row * PITCH + col]) = uint2{h[0], h[1]};
+            *reinterpret_cast<uint2*>(&lds[1][1][row * PITCH + col]) = uint2{l[0], l[1]};
             f16_t* to = Bs + k * a.stride_a + (int64_t)row * a.lda + col;
-            *reinterpret_cast<f16x4*>(to) = h;
-            *reinterpret_cast<f16x4*>(to + MP) = l;
+            *reinterpret_cast<uint2*>(to) = uint2{h[0], h[1]};
+            *reinterpret_cast<uint2*>(to + MP) = uint2{l[0], l[1]};
         });
         __syncthreads();
         if (k + 1 == a.steps) break;
