@@ -694,8 +694,8 @@ class FlceOrthogonalizeArgs(ctypes.Structure):
 def _orthogonalize_args(rows, cols, code, steps, coefficients, scale, eps) -> FlceOrthogonalizeArgs:
     args = FlceOrthogonalizeArgs(ctypes.sizeof(FlceOrthogonalizeArgs), rows, cols, code, steps, None, 0, scale, eps)
     if coefficients is not None:
-        triples = list(coefficients)
-        args.per_step = 0 if not hasattr(triples[0], "__len__") else 1
+        triples = coefficients.tolist() if hasattr(coefficients, "tolist") else list(coefficients)   # (tensors, arrays)
+        args.per_step = 1 if triples and hasattr(triples[0], "__len__") else 0
         flat = [float(x) for t in triples for x in t] if args.per_step else [float(x) for x in triples]
         if len(flat) != 3 * (steps if args.per_step else 1):
             raise ValueError("coefficients must be three numbers, or three for each step")

@@ -273,3 +273,18 @@ def test_orthogonalisation_binding_refusals():
     with pytest.raises(ValueError):
         flce.flce_orthogonalize([t, torch.zeros(8, 4)])
     assert flce.flce_orthogonalize([]) == []
+
+
+def test_orthogonalisation_coefficients():
+    from paper_2410_10989_amd.binding import _orthogonalize_args
+    import numpy as np
+    one, two = (2.0, -1.5, 0.5), [(8.0, -22.0, 16.0), (4.0, -3.0, 0.5)]
+    for given in (one, list(one), np.array(one), torch.tensor(one)):
+        args = _orthogonalize_args(4, 8, flce.FLCE_F32, 2, given, 1.0, 1e-7)
+        assert args.per_step == 0 and list(args._coefficients) == list(one)
+    for given in (two, np.array(two), torch.tensor(two)):
+        args = _orthogonalize_args(4, 8, flce.FLCE_F32, 2, given, 1.0, 1e-7)
+        assert args.per_step == 1 and list(args._coefficients) == [x for t in two for x in t]
+    for given in ([], (1.0, 2.0), [(1.0, 2.0, 3.0)], two + two, torch.zeros(2, 2)):
+        with pytest.raises(ValueError):
+            _orthogonalize_args(4, 8, flce.FLCE_F32, 2, given, 1.0, 1e-7)
