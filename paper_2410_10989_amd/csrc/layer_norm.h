@@ -10,7 +10,9 @@
 // zero.  A row lies in the registers of a group of TPR threads (see block_norm.h), so the second pass over it reads
 // nothing; what it costs is a second exchange between the threads, in which the backward takes its other sums along.
 //
-// Bound by HBM.
+// Bound by HBM.  Forward, 16384 x 3584 bf16 with a residual: 80 us, 5.9 TB/s.  Backward, 8192 x 4096 bf16 with a residual: 54
+// to 56 us, 4.8 TB/s (a workgroup has one row on the way while it does another, whose two exchanges it waits for), and 4.8
+// for the sums over rows.
 #pragma once
 #include "rowsums.h"
 #include "rowvec.h"

@@ -18,6 +18,9 @@ constexpr int64_t LN_GRID_X = (int64_t)1 << 20;     // workgroups along x, the r
 // and 42.7, 4096 53.7 and 58.5, 1600 fp32 40.9 and 41.5; several rows per workgroup: 16384 x 1024 bf16 29.7 and 35.7.
 constexpr int LN_CU_THREADS = 512, LN_SHORT_CU_THREADS = 768;
 constexpr int64_t LN_SHORT_BYTES = 5632;
+// Fewest workgroups of a backward with partial sums, while there are rows for them (us with 32, 128 and 256: 128 rows of 4096
+// bf16 12.3, 9.3, 9.3; 256 rows 12.9, 10.7, 11.9); rows that one workgroup takes one after the other and writes the sums of
+// itself (2 rows of 4096: 5.8, with partial sums 7.1; 4 rows 8.8 and 7.0).
 constexpr int64_t LN_CUS = 256, LN_FEW_BLOCKS = 128, LN_ONE_STEPS = 3;
 constexpr int64_t LN_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
