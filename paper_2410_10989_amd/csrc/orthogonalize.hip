@@ -11,6 +11,7 @@
 #include "flce_host.h"
 
 using namespace flce;
+static_assert(OR_SMALL <= 256, "one tile of 256");
 
 namespace {
 
@@ -26,6 +27,7 @@ constexpr double OR_MAX_NORM = 1024.0;                   // that a singular valu
 // 574 and 524 us, 16 x 1024 x 1024 (160) 598 and 628.  Operands in two planes, whose tiles of 128 take both at a time:
 // 4 x 2048 x 2048 fp32 (144 and 256 tiles) 2192 with both in tiles of 256, 2046 with the larger ones so, 2101 with none.
 constexpr int64_t OR_TILES_256 = 144, OR_TILES_256_PLANES = 256;
+static_assert(OR_MATRICES < OR_TILES_256, "Gram products of up to OR_SMALL rows never take them");
 constexpr int64_t OR_SLOTS_128 = 256;                    // workgroups that ranges of K may make: one per CU
 // Fewest turns of a range's K loop, most ranges, and turns one after the other that ranges have to save (a turn: 64 of K and
 // one product).  us: a range of 8 turns or of 4: 512 x 512 fp32 198 and 223, 256 x 4096 bf16 168 and 182; ranges that
@@ -145,23 +147,31 @@ int launch_product(OrArgs& a, hipStream_t s) {
         return tiles * a.count;
     };
     auto grid = [](int64_t total) { return dim3((unsigned)((total + FG_XCDS - 1) / FG_XCDS * FG_XCDS)); };
-    const int64_t large = tiles_of(256);
-    if (large >= (PL == 2 ? OR_TILES_256_PLANES : OR_TILES_256)) {
-        hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 256, OutT, TALL, OR_WHOLE>), grid(large), dim3(FG_THREADS), 0, s, a);
-        HIP_TRY(hipGetLastError());
-        return FLCE_OK;
+    constexpr bool PAIRED = PRODUCT == OR_MULTIPLY;    // only of two steps at a time: its launches fill the chip (run_group)
+    if constexpr (PRODUCT != OR_GRAM || PL == OUT) {   // (else OR_MATRICES tiles of 256 at most: see OR_SMALL)
+        const int64_t large = tiles_of(256);
+        if ((PAIRED && PL == 1) || large >= (PL == 2 ? OR_TILES_256_PLANES : OR_TILES_256)) {
+            hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 256, OutT, TALL, OR_WHOLE>), grid(large), dim3(FG_THREADS), 0, s, a);
+            HIP_TRY(hipGetLastError());
+            return FLCE_OK;
+        }
     }
-    const int64_t total = tiles_of(128), steps = (PRODUCT == OR_GRAM ? a.np : a.mp) / FG_BK, turns = steps * (PL == 2 ? 3 : 1);
-    a.ranges = (int)std::min({OR_MAX_RANGES, OR_SLOTS_128 / total, turns / OR_RANGE_STEPS, steps});
-    if (a.ranges <= 1 || turns - turns / a.ranges < OR_SAVED_STEPS) {
+    if constexpr (!PAIRED || PL == 2) {
+        const int64_t total = tiles_of(128);
+        if constexpr (!PAIRED) {
+            const int64_t steps = (PRODUCT == OR_GRAM ? a.np : a.mp) / FG_BK, turns = steps * (PL == 2 ? 3 : 1);
+            a.ranges = (int)std::min({OR_MAX_RANGES, OR_SLOTS_128 / total, turns / OR_RANGE_STEPS, steps});
+            if (a.ranges > 1 && turns - turns / a.ranges >= OR_SAVED_STEPS) {
+                hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_RANGES>), grid(total * a.ranges), dim3(FG_THREADS), 0, s, a);
+                HIP_TRY(hipGetLastError());
+                hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_JOIN>), grid(2 * total), dim3(FG_THREADS), 0, s, a);
+                HIP_TRY(hipGetLastError());
+                return FLCE_OK;
+            }
+        }
         hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_WHOLE>), grid(total), dim3(FG_THREADS), 0, s, a);
         HIP_TRY(hipGetLastError());
-        return FLCE_OK;
     }
-    hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_RANGES>), grid(total * a.ranges), dim3(FG_THREADS), 0, s, a);
-    HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL((or_product_kernel<PRODUCT, PL, OUT, 128, OutT, TALL, OR_JOIN>), grid(2 * total), dim3(FG_THREADS), 0, s, a);
-    HIP_TRY(hipGetLastError());
     return FLCE_OK;
 }
 

@@ -62,7 +62,7 @@ def test_one_matrix(rows, cols, dtype):
 
 @pytest.mark.parametrize("dtype,count,rows,cols", [("bf16", 5, 130, 70), ("f32", 3, 70, 130), ("bf16", 130, 33, 40), ("bf16", 20, 512, 512),
                                                    ("f32", 14, 512, 768), ("bf16", 9, 1025, 600), ("bf16", 50, 300, 640),
-                                                   ("bf16", 45, 1300, 520), ("f32", 44, 384, 800), ("f32", 50, 777, 323)])
+                                                   ("bf16", 45, 1300, 520), ("f32", 44, 384, 800), ("f32", 50, 777, 323), ("f32", 90, 300, 640)])
 def test_lists(dtype, count, rows, cols):
     """Many matrices of a list, on both sizes of tiles, in several groups of launches."""
     import paper_2410_10989_amd as flce
