@@ -281,7 +281,10 @@ struct FgOut {
                         else v[e] += __uint_as_float((e & 1) ? (old[k][e >> 1] & 0xffff0000u) : (old[k][e >> 1] << 16));
                     }
                 }
-                const int soff = ((row0 + k * ROWS_PER_ACCESS) * ldc + colw) * ES;
+                // (The whole offset in a vector register.  With part of it in a scalar one the compiler takes the data for
+                // read at once and may let the very next vector instruction overwrite it; on this chip the store then
+                // writes some of the new values.)
+                const int off = lane_off + ((row0 + k * ROWS_PER_ACCESS) * ldc + colw) * ES;
                 u32x4 out;
                 if constexpr (ES == 4) {
 #pragma unroll
@@ -293,7 +296,7 @@ struct FgOut {
                         out[e] = __builtin_bit_cast(uint32_t, p2);
                     }
                 }
-                if (col_ok) __builtin_amdgcn_raw_buffer_store_b128(out, rsrc_c, lane_off, soff, 0);
+                if (col_ok) __builtin_amdgcn_raw_buffer_store_b128(out, rsrc_c, off, 0, 0);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // reads done before the next pass rewrites the region
         }
