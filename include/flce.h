@@ -447,7 +447,8 @@ FLCE_API size_t flce_grad_norm_workspace_bytes(int n_tensors);
  *   steps         1 .. 32
  *   coefficients  HOST array of 3 floats for all steps (per_step = 0) or 3 * steps (per_step = 1), or NULL: 3.4445,
  *                 -4.7750, 2.0315.  Finite, and such that no singular value in [0, 1] can exceed 1024 on the
- *                 way (FLCE_ERR_ARG).
+ *                 way (FLCE_ERR_ARG).  Polynomials that are steep where the largest singular values are multiply
+ *                 those's rounding errors as well.
  *   scale, eps    finite, eps >= 0
  *   workspace     device buffer (256-byte aligned), or NULL for the device's shared workspace; workspace_bytes:
  *                 flce_orthogonalize_workspace_bytes of the same arguments, or less (what one matrix takes at the

@@ -23,6 +23,7 @@ constexpr int OR_MAX_STEPS = 32;
 constexpr int64_t OR_PAIR_LENGTH = 2;
 constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A (see or_iterate_kernel)
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
+constexpr double OR_LIFT = 4.0;                          // see steps_of (fp16 has room for another 4)
 // Fewest tiles of 256 that a launch takes those for.  bf16, whole calls in tiles of 256 and of 128: 2 x 2048 x 2048 (128 tiles)
 // 574 and 524 us, 16 x 1024 x 1024 (160) 598 and 628.  Operands in two planes, whose tiles of 128 take both at a time:
 // 4 x 2048 x 2048 fp32 (144 and 256 tiles) 2192 with both in tiles of 256, 2046 with the larger ones so, 2101 with none.
@@ -61,33 +62,48 @@ struct OrPlan {
 // The exponent that brings values of up to `most` below 2^14.
 int exponent_for(double most) { return 14 - (int)ceil(log2(std::max(most, 0x1p-40))); }
 
-// Singular values of X_k lie in [0, s]; every step's polynomial says where those of X_{k+1} do.
-int steps_of(const flce_orthogonalize_args& b, OrStep* to) {
-    double s = 1.0;
+// What a step's polynomial a + b l + c l^2, l = x^2, does to singular values x of up to s: its largest magnitude, and the
+// largest singular value that follows.
+struct OrRange {
+    double most_b, most_x;
+};
+OrRange range_of(double A, double B, double C, double s) {
+    const double l1 = s * s;
+    auto poly = [&](double l) { return fabs(A + B * l + C * l * l); };
+    auto next = [&](double l) { return sqrt(l) * poly(l); };
+    OrRange r{std::max(poly(0.0), poly(l1)), next(l1)};
+    auto at = [&](double l, auto f, double& most) {
+        if (l > 0.0 && l < l1) most = std::max(most, f(l));
+    };
+    if (C != 0.0) {
+        at(-B / (2.0 * C), poly, r.most_b);
+        const double disc = 9.0 * B * B - 20.0 * A * C;
+        if (disc >= 0.0) {
+            at((-3.0 * B + sqrt(disc)) / (10.0 * C), next, r.most_x);
+            at((-3.0 * B - sqrt(disc)) / (10.0 * C), next, r.most_x);
+        }
+    } else if (B != 0.0) {
+        at(-A / (3.0 * B), next, r.most_x);
+    }
+    return r;
+}
+
+// Singular values of X_k lie in [0, s]; every step's polynomial says where those of X_{k+1} do.  What is held lies in
+// [0, held]: an operand's rounding lifts a singular value by up to `rounding` of it, which polynomials that are steep there
+// multiply, step after step (five that stay below 2 from 1 on make 3056 of 1.001).  That decides about exponents alone, not
+// about what is taken, and up to OR_LIFT times: what is lifted higher is rounding errors, and the room for them would
+// cost the others their bits.
+int steps_of(const flce_orthogonalize_args& b, double rounding, OrStep* to) {
+    double s = 1.0, held = 1.0;
     for (int k = 0; k < b.steps; ++k) {
         const float* p = !b.coefficients ? OR_USUAL : b.coefficients + (b.per_step ? 3 * k : 0);
         for (int i = 0; i < 3; ++i)
             if (p[i] - p[i] != 0.0f) return FLCE_ERR_ARG;
-        const double A = p[0], B = p[1], C = p[2], l1 = s * s;
-        auto poly = [&](double l) { return fabs(A + B * l + C * l * l); };
-        auto next = [&](double l) { return sqrt(l) * poly(l); };
-        double most_b = std::max(poly(0.0), poly(l1)), most_x = next(l1);
-        auto at = [&](double l, auto f, double& most) {
-            if (l > 0.0 && l < l1) most = std::max(most, f(l));
-        };
-        if (C != 0.0) {
-            at(-B / (2.0 * C), poly, most_b);
-            const double disc = 9.0 * B * B - 20.0 * A * C;
-            if (disc >= 0.0) {
-                at((-3.0 * B + sqrt(disc)) / (10.0 * C), next, most_x);
-                at((-3.0 * B - sqrt(disc)) / (10.0 * C), next, most_x);
-            }
-        } else if (B != 0.0) {
-            at(-A / (3.0 * B), next, most_x);
-        }
-        to[k] = {p[0], p[1], p[2], exponent_for(s), exponent_for(l1), exponent_for(most_b), false, most_b};
-        s = std::max(most_x, 0x1p-20) * 1.01;   // (what rounding may add)
+        const OrRange lifted = range_of(p[0], p[1], p[2], held);
+        to[k] = {p[0], p[1], p[2], exponent_for(held), exponent_for(held * held), exponent_for(lifted.most_b), false, lifted.most_b};
+        s = std::max(range_of(p[0], p[1], p[2], s).most_x, 0x1p-20);
         if (!(s <= OR_MAX_NORM)) return FLCE_ERR_ARG;
+        held = std::min(std::max(lifted.most_x, 0x1p-20) * (1.0 + rounding), OR_LIFT * s);
     }
     float grows = 1.0f;   // what an error of X_k may be multiplied by in what follows
     for (int k = b.steps - 1; k >= 0; --k) {
@@ -114,8 +130,8 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     p->mp = padded(std::min(b.rows, b.cols));
     p->np = padded(std::max(b.rows, b.cols));
     if (p->mp * p->np > OR_MAX_ELEMENTS) return FLCE_ERR_SHAPE;
-    FLCE_TRY(steps_of(b, p->steps));
     p->gram_planes = b.dtype == FLCE_F32 ? 2 : 1;
+    FLCE_TRY(steps_of(b, p->gram_planes == 2 ? 0x1p-20 : 0x1p-10, p->steps));
     p->planes = b.dtype == FLCE_F32 || p->mp <= OR_SMALL ? 2 : 1;
     p->ldx = 2 * p->np;
     p->lda = p->planes * p->mp;
