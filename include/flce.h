@@ -431,9 +431,10 @@ FLCE_API size_t flce_grad_norm_workspace_bytes(int n_tensors);
  * carried over in 22 bits where later steps multiply its errors.  bf16 matrices: operands of 11 bits (up to 256 rows or
  * columns 22); what the result is off by, relative to its norm, is about 1e-3 next to its rounding to bf16 (1.7e-3).
  * fp32 matrices: operands of 22 bits, three products for one, about 1e-6 up to 1000 rows or columns, 3e-6 for 4096 x
- * 16384 (fp32 arithmetic: 1e-6 for 16 rows, 3e-6 for 1000, 9e-6 for 4096).  Both are for the usual coefficients; small
- * singular values and the errors in their directions grow by a factor a per step.  The norm is summed in fp64 (16 bytes
- * at a time, whose squares are added in fp32 where that can neither overflow nor vanish).  No atomics: the same call with
+ * 16384 (fp32 arithmetic: 1e-6 for 16 rows, 3e-6 for 1000, 9e-6 for 4096).  Both are for the usual coefficients, however
+ * small |G| is beside eps (with a = 0 what is left then is of higher order in |G| / eps, and loses its bits); small
+ * singular values and the errors in their directions grow by a factor a per step.  The norm is summed in fp64 (16 bytes at
+ * a time, whose squares are added in fp32 where that can neither overflow nor vanish).  No atomics: the same call with
  * the same workspace gives the same bits.  A matrix that holds infinities or NaN gives NaN, and leaves the others of
  * the list alone; zeros give zeros.
  *

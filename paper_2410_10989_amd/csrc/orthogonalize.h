@@ -22,6 +22,10 @@
 //   m = OR_SMALL, where A and B cost little, they have two planes, too (64 x 512: 1.75e-3 instead of 2.4e-3 with the
 //   1.66e-3 of rounding the result to bf16).
 //   fp32 matrices: two planes everywhere, every product is hi lo + lo hi + hi hi.
+//   Where |G| is far below eps, X stays small for many steps (it grows by a in each).  Held times powers of two that
+//   leave room for singular values near 1 it would lose its bits below fp16's range, so each matrix has powers of
+//   two of its own beside those of all (or_load_kernel; |G| = 1e-15 and eps = 1e-7, 300 x 400 fp32: 2.4e-2 without them).
+//   A has none: where that would matter, B = a I to the last bit.
 // Sums are fp32 in the matrix cores, the norm's fp64.  The cores cut a sum off where it leaves fp32: each 16 terms added
 // to a sum of S take up to 2^-23 S from it, always towards zero, so the small products come first (16 x 4099 fp32:
 // 7.2e-6 with hi hi first).
@@ -39,6 +43,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 constexpr int OR_MATRICES = 120;   // a launch's arguments stay below 4 KB
 constexpr int OR_PAD = 64;         // rows and columns are padded with zeros to whole K steps
 constexpr int OR_NORM_BLOCKS = 64; // workgroups that add up a matrix's squares
+constexpr int OR_MAX_STEPS = 32;
 
 constexpr int OR_SMALL = 256;      // bf16: A and B in two planes up to this many (padded) rows
 constexpr float OR_CARRY = 16.0f;
@@ -59,7 +64,8 @@ struct OrArgs {
     // to = alpha * (the accumulated product) + beta * A (OR_POLY), beta * X's lo plane (add_lo), diagonal (OR_POLY)
     float alpha, beta, diagonal;
     int add_lo, put_lo;          // OR_APPLY, OR_LAST: X's lo plane is added; the result has one
-    const float* factor;         // the first step: of each matrix, what its X is to be multiplied by; or null
+    const double* size;          // of each matrix, OR_MAX_STEPS: X_k is what is held times size[k]
+    int step, next;              // of the X that is read, of the one that is written (not OR_LAST)
     int ranges;                  // of K
     float* part;                 // the ranges' sums
     int rows, cols;              // OR_LAST: of out
@@ -68,7 +74,9 @@ struct OrArgs {
 struct OrLoadArgs {
     const void* in[OR_MATRICES];
     double* partial;             // OR_NORM_BLOCKS per matrix
-    float* factor;               // of each matrix
+    double* size;                // of each matrix, OR_MAX_STEPS: see OrArgs
+    int steps;
+    int16_t growth[OR_MAX_STEPS]; // X_k is at most 2^(growth[k] - bits) of what its exponent allows where X_0 is at most 2^-bits
     f16_t* X;
     int64_t stride_x;
     int rows, cols, mp, np, ldx;
@@ -154,7 +162,7 @@ __global__ __launch_bounds__(256) void or_norm_kernel(OrLoadArgs a) {
 
 // The first X: a workgroup writes 64 x 64 elements of G times the power of two that brings its norm to 2^exponent, zeros
 // where the matrix ends.  TALL: it is turned around in LDS.  The factor that is left, norm / (norm + eps) up to a power
-// of two: see OrArgs.
+// of two, is X_0's size (see OrArgs), and the powers of two that norm / (norm + eps) lets the others be held larger by.
 template <typename T, bool TALL>
 __global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
     constexpr int N = RowVec<T>::N, LANES = 64 / N;   // lanes per row of the tile
@@ -167,8 +175,11 @@ __global__ __launch_bounds__(256) void or_load_kernel(OrLoadArgs a) {
     const bool usual = norm > 0.0 && norm - norm == 0.0;
     const int e = usual ? ilogb(norm) + 1 : 0;   // norm <= 2^e
     const double scale = ldexp(1.0, a.exponent - e);
-    if (blockIdx.x == 0 && threadIdx.x == 0)   // (zeros stay zeros; infinities and NaN make all of the result NaN)
-        a.factor[matrix] = usual ? (float)(ldexp(1.0, e) / (norm + a.eps)) : norm == 0.0 ? 1.0f : __builtin_nanf("");
+    if (blockIdx.x == 0 && (int)threadIdx.x < a.steps) {   // (zeros stay zeros; infinities and NaN make all of the result NaN)
+        const int k = threadIdx.x, bits = usual ? -1 - ilogb(norm / (norm + a.eps)) : 0;   // norm / (norm + eps) <= 2^-bits
+        const double first = usual ? ldexp(1.0, e) / (norm + a.eps) : norm == 0.0 ? 1.0 : __builtin_nan("");
+        a.size[matrix * OR_MAX_STEPS + k] = k == 0 ? first : bits > 0 ? ldexp(1.0, -max(0, bits - a.growth[k])) : 1.0;
+    }
     const int r0 = TALL ? n0 : m0, c0 = TALL ? m0 : n0;   // the tile's origin in the matrix
     for (int i = threadIdx.x; i < 64 * LANES; i += 256) {
         const int r = i / LANES, c = i % LANES * N;
@@ -454,6 +465,28 @@ __device__ __forceinline__ void or_planes_loop(const FgOperand<false, 128>& opa,
 // retire and its LDS be handed to another one).
 __device__ __forceinline__ void or_drain() { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// OrArgs' alpha and beta, with the sizes of a matrix's X, and (OR_LAST) a power of two apart: the result times a small
+// size may be an ordinary number while alpha alone is below fp32's normal range.
+struct OrFactors {
+    float alpha, beta;
+    int exponent;
+};
+template <int PRODUCT>
+__device__ __forceinline__ OrFactors or_factors(const OrArgs& a, int matrix) {
+    auto uniform = [](float f) { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(f))); };
+    if constexpr (PRODUCT == OR_POLY || PRODUCT == OR_MULTIPLY) return {a.alpha, a.beta, 0};
+    const double* size = a.size + matrix * OR_MAX_STEPS;
+    const double from = size[a.step];
+    if constexpr (PRODUCT == OR_GRAM) return {uniform((float)(a.alpha * from * from)), 0.0f, 0};
+    if constexpr (PRODUCT == OR_APPLY) {
+        const double f = from / size[a.next];
+        return {uniform((float)(a.alpha * f)), uniform((float)(a.beta * f)), 0};
+    }
+    const double alpha = a.alpha * from;
+    const int e = alpha != 0.0 && alpha - alpha == 0.0 ? ilogb(alpha) : 0;
+    return {uniform((float)ldexp(alpha, -e)), uniform((float)ldexp(a.beta * from, -e)), __builtin_amdgcn_readfirstlane(e)};
+}
+
 // Writes a wavefront's part of a tile out, 32 rows at a time through LDS (see FgOut in gemm_bf16_nt.h for the layout of
 // the accumulators), as planes of 8 values per lane, the mirrored tile too; or (OR_LAST) rounded to out.  Where the matrix
 // is tall, the accumulators hold the transpose (24 matrices of 4096 x 1024, bf16: turning the finished tile around
@@ -547,7 +580,7 @@ struct OrOut {
     // Rows 32 i .. of the wavefront's part, from its accumulators of them; their addend is in buffer BUF.  MIRROR:
     // they are left in half H of the stage, for turned().
     template <int BUF, int H>
-    __device__ __forceinline__ void pass(f32x16 (&acc)[W], const OrArgs& a, float alpha, OutT* out, int i) {
+    __device__ __forceinline__ void pass(f32x16 (&acc)[W], const OrArgs& a, const OrFactors& f, OutT* out, int i) {
         const int frow = lane & 31, fhalf = lane >> 5;
         const bool put_lo = PRODUCT != OR_APPLY || PL == 2 || a.put_lo;
 #pragma unroll
@@ -566,7 +599,7 @@ struct OrOut {
             for (int e = 0; e < 8; e += 4) {
                 const f32x4 q = *staged(H * 32 + lane_row(k), (lane_col() + e) / 4);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[e + u] = alpha * q[u];
+                for (int u = 0; u < 4; ++u) v[e + u] = f.alpha * q[u];
             }
             const int row = row0 + 32 * i + lane_row(k), col = col0 + lane_col();
             if constexpr (AHEAD > 0) {
@@ -574,22 +607,27 @@ struct OrOut {
                 for (int p = IN - 1; p >= 0; --p) {
                     const f16x8 w = __builtin_bit_cast(f16x8, addend[BUF][k][p]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = fmaf(a.beta, (float)w[e], v[e]);
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(f.beta, (float)w[e], v[e]);
                 }
             }
             if constexpr (TURN && IN > 0) {
                 if (a.add_lo) {   // (a last step that multiplies an error by more than OR_CARRY: columns of X)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        v[e] = fmaf(a.beta, (float)__builtin_bit_cast(f16_t, __builtin_amdgcn_raw_buffer_load_b16(rsrc_in, at(col + e, row), ld * 2, 0)), v[e]);
+                        v[e] = fmaf(f.beta, (float)__builtin_bit_cast(f16_t, __builtin_amdgcn_raw_buffer_load_b16(rsrc_in, at(col + e, row), ld * 2, 0)), v[e]);
                 }
             }
             if constexpr (PRODUCT == OR_POLY) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += row == col + e ? a.diagonal : 0.f;
             }
-            if constexpr (LAST) put_out(out, a.rows, a.cols, row, col, v);
-            else put_planes(row, col, v, put_lo);
+            if constexpr (LAST) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_ldexpf(v[e], f.exponent);
+                put_out(out, a.rows, a.cols, row, col, v);
+            } else {
+                put_planes(row, col, v, put_lo);
+            }
             if constexpr (MIRROR) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 4)
@@ -614,15 +652,15 @@ struct OrOut {
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    // All of it; load_addend<0>(0) has been issued before.  alpha: with the matrix's factor.
-    __device__ __forceinline__ void write(f32x16 (&acc)[W][W], const OrArgs& a, float alpha, int matrix, bool mirror) {
+    // All of it; load_addend<0>(0) has been issued before.
+    __device__ __forceinline__ void write(f32x16 (&acc)[W][W], const OrArgs& a, const OrFactors& f, int matrix, bool mirror) {
         OutT* out = LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
 #pragma unroll
         for (int i = 0; i < W; i += 2) {
             load_addend<AHEAD ? 1 : 0>(i + 1);
-            pass<0, 0>(acc[i], a, alpha, out, i);
+            pass<0, 0>(acc[i], a, f, out, i);
             if (i + 2 < W) load_addend<0>(i + 2);
-            pass<AHEAD ? 1 : 0, 1>(acc[i + 1], a, alpha, out, i + 1);
+            pass<AHEAD ? 1 : 0, 1>(acc[i + 1], a, f, out, i + 1);
             if (MIRROR && mirror) turned<2>(a, i);
         }
     }
@@ -677,8 +715,6 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
     auto part_at = [&](int r, int i, int j, int g) {
         return reinterpret_cast<f32x4*>(a.part + ((int64_t)r * all + seq) * (TILE * TILE) + (((i * W + j) * 4 + g) * FG_THREADS + tid) * 4);
     };
-    float alpha = a.alpha;
-    if ((PRODUCT == OR_GRAM || PRODUCT >= OR_APPLY) && a.factor) alpha *= PRODUCT == OR_GRAM ? a.factor[matrix] * a.factor[matrix] : a.factor[matrix];
     constexpr bool TURN = PRODUCT == OR_LAST && TALL;
     OrOut<PRODUCT, PL, OUT, TILE, OutT, TALL> out;
     auto begin_out = [&]() {
@@ -690,6 +726,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
     if constexpr (PART == OR_JOIN) {
         constexpr int AHEAD = 4;   // ranges whose loads are under way
         begin_out();
+        const OrFactors factors = or_factors<PRODUCT>(a, matrix);
         out.template load_addend<0>(range);
         f32x16 acc[W];
 #pragma unroll
@@ -712,7 +749,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
                     for (int g = 0; g < 16; ++g) acc[j][g] += r0 + r < a.ranges ? v[r][j][g / 4][g % 4] : 0.f;
         }
         OutT* to = PRODUCT == OR_LAST ? static_cast<OutT*>(a.out[matrix]) : nullptr;
-        out.template pass<0, 0>(acc, a, alpha, to, range);
+        out.template pass<0, 0>(acc, a, factors, to, range);
         if (out.MIRROR && tm != tn) out.template turned<1>(a, range);
     } else {
         // operands: X X^T, A A, A B (rows of symmetric matrices for columns), B X
@@ -741,6 +778,8 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
             opb.lo_part = 0;
             nk *= 3;
         }
+        OrFactors factors{};
+        if constexpr (PART == OR_WHOLE) factors = or_factors<PRODUCT>(a, matrix);   // (its loads are done long before the K loop is)
         f32x16 acc[W][W];
 #pragma unroll
         for (int i = 0; i < W; ++i)
@@ -771,7 +810,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
         }
         or_drain();
         if constexpr (PART == OR_WHOLE) {
-            out.write(acc, a, alpha, matrix, tm != tn);
+            out.write(acc, a, factors, matrix, tm != tn);
         } else {
 #pragma unroll
             for (int i = 0; i < W; ++i)

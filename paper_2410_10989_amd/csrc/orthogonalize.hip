@@ -17,7 +17,6 @@ namespace {
 
 constexpr int64_t OR_MAX_DIM = (int64_t)1 << 20;         // a tile's rows stay below 2^31 bytes apart
 constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: its planes stay below 2^30 bytes
-constexpr int OR_MAX_STEPS = 32;
 // n / m from which two steps are taken at a time.  24 matrices, bf16, us in pairs and step by step: 1024 x 1024 851 and 821,
 // 1024 x 2048 1062 and 1191, 1024 x 4096 1639 and 2075.
 constexpr int64_t OR_PAIR_LENGTH = 2;
@@ -46,6 +45,7 @@ struct OrStep {
     int e_x, e_a, e_b;   // X, A and B are held times 2 to these
     bool lo;             // X is needed in two planes
     double most_b;       // B's largest eigenvalue
+    int growth;          // see OrLoadArgs
 };
 struct OrPlan {
     int64_t mp, np, ldx, lda;
@@ -94,13 +94,16 @@ OrRange range_of(double A, double B, double C, double s) {
 // about what is taken, and up to OR_LIFT times: what is lifted higher is rounding errors, and the room for them would
 // cost the others their bits.
 int steps_of(const flce_orthogonalize_args& b, double rounding, OrStep* to) {
-    double s = 1.0, held = 1.0;
+    double s = 1.0, held = 1.0, small = 1.0;   // small: what singular values far below 1 grow by at most
+    int growth = 0;
     for (int k = 0; k < b.steps; ++k) {
         const float* p = !b.coefficients ? OR_USUAL : b.coefficients + (b.per_step ? 3 * k : 0);
         for (int i = 0; i < 3; ++i)
             if (p[i] - p[i] != 0.0f) return FLCE_ERR_ARG;
         const OrRange lifted = range_of(p[0], p[1], p[2], held);
-        to[k] = {p[0], p[1], p[2], exponent_for(held), exponent_for(held * held), exponent_for(lifted.most_b), false, lifted.most_b};
+        growth = std::max(growth, (int)ceil(log2(small)) + exponent_for(held) - 14);   // (never less: they stay in range anyway)
+        to[k] = {p[0], p[1], p[2], exponent_for(held), exponent_for(held * held), exponent_for(lifted.most_b), false, lifted.most_b, growth};
+        small = std::min(std::max(small * lifted.most_b * (1.0 + rounding), 0x1p-1000), 0x1p1000);
         s = std::max(range_of(p[0], p[1], p[2], s).most_x, 0x1p-20);
         if (!(s <= OR_MAX_NORM)) return FLCE_ERR_ARG;
         held = std::min(std::max(lifted.most_x, 0x1p-20) * (1.0 + rounding), OR_LIFT * s);
@@ -142,7 +145,8 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     const bool small = b.dtype == FLCE_BF16 && p->mp <= OR_ITERATE_MOST;
     p->iterate = small && b.steps <= OR_ITERATE_STEPS && growth <= OR_ITERATE_GROWTH;
     p->b_matrices = small ? 1 + OR_ITERATE_STEPS : 2;   // (whatever the steps are)
-    p->bytes = 2 * p->x_bytes + (1 + p->b_matrices) * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) + 256;
+    p->bytes = 2 * p->x_bytes + (1 + p->b_matrices) * p->a_bytes + aligned_bytes(OR_NORM_BLOCKS * sizeof(double)) +
+               aligned_bytes(OR_MAX_STEPS * sizeof(double));
     p->tiles = ((p->mp + 127) / 128) * ((p->np + 127) / 128);
     // Matrices at a time: until the launch with the fewest tiles has several rounds of them.
     const int64_t t = (p->mp + 255) / 256, tiles = t * (t + 1) / 2;
@@ -230,7 +234,7 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     f16_t* B = reinterpret_cast<f16_t*>(take(count * p.b_matrices * p.a_bytes));
     OrLoadArgs l{};
     l.partial = reinterpret_cast<double*>(take(count * OR_NORM_BLOCKS * sizeof(double)));
-    l.factor = reinterpret_cast<float*>(take(count * sizeof(float)));
+    l.size = reinterpret_cast<double*>(take(count * OR_MAX_STEPS * sizeof(double)));
     l.X = X[0];
     l.stride_x = (int64_t)(p.x_bytes / sizeof(f16_t));
     l.rows = (int)b.rows;
@@ -241,6 +245,8 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     l.planes = PL;
     l.exponent = p.steps[0].e_x;
     l.eps = b.eps;
+    l.steps = b.steps;
+    for (int k = 0; k < b.steps; ++k) l.growth[k] = (int16_t)p.steps[k].growth;
     for (int i = 0; i < count; ++i) l.in[i] = in[i];
     hipLaunchKernelGGL((or_norm_kernel<T>), dim3(OR_NORM_BLOCKS, (unsigned)count), dim3(256), 0, s, l);
     HIP_TRY(hipGetLastError());
@@ -261,11 +267,11 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
     a.rows = l.rows;
     a.cols = l.cols;
     a.part = reinterpret_cast<float*>(ws);
+    a.size = l.size;
     for (int i = 0; i < count; ++i) a.out[i] = out[i];
     // Small matrices: all steps between the first and the last product with X in one launch.
     if constexpr (GP == 1 && PL == 2) {
         if (p.iterate) {
-            a.factor = l.factor;
             a.X = X[0];
             a.to = A;
             a.alpha = ldexpf(1.0f, p.steps[0].e_a - 2 * p.steps[0].e_x);
@@ -295,7 +301,7 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
         const OrStep* st = &p.steps[k];
         const int first_x = st->e_x;
         const bool lo = st->lo;
-        a.factor = k == 0 ? l.factor : nullptr;
+        a.step = k;
         a.X = X[x];
         a.A = A;
         a.to = A;
@@ -340,6 +346,7 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
         }
         ++k;
         const bool last = k == b.steps;
+        a.next = k;
         const float scale = last ? b.scale : ldexpf(1.0f, p.steps[k].e_x);
         a.to = X[x ^ 1];
         a.alpha = ldexpf(scale, -e_b - first_x);
