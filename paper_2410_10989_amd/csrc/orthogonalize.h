@@ -7,9 +7,11 @@
 // operations; A and B are symmetric, so only the tiles on and below the diagonal are computed, the others mirrored.
 // Two steps at a time, where n is twice m or more: A' = (B A) B stands for the Gram product of the X between them, which is
 // never formed, and X <- (B' B) X: three symmetric m^3 products instead of m^2 n + 2 m^2 n, and X is read and
-// written once less (24 matrices of 4096 x 1024, bf16: 1988 us step by step, 1606 so).  A's rounding errors grow by a^2 in A', so never two such pairs in a
-// row: with (2, 1, 2) of five steps the result is as far off as step by step, with (2, 2, 1) up to 1.5 times, with all
-// five at once 0.2.
+// written once less (24 matrices of 4096 x 1024, bf16: 1988 us step by step, 1606 so).  A's rounding errors grow by a^2 in A' and
+// those of B' B reach X without an A between, so never two such pairs in a row, and only where the first step
+// multiplies by little (OR_PAIR_GROWTH).  With (2, 1, 2) of five usual steps a matrix of noise is as far off as step by step
+// (320 x 704 bf16: 2.15e-3 and 2.09e-3), one of rank 2, 300 times as large as noise, 1.3 times (3.2e-3 and 2.5e-3); with (2, 2, 1)
+// noise is up to 1.5 times, and with all five at once 0.2.
 //
 // Numbers.  The iteration multiplies the smallest singular values by a^steps (485 for five of the usual steps), and any
 // error in their directions with them.  The operands of the products are fp16, scaled by powers of two that keep them
@@ -24,7 +26,7 @@
 //   fp32 matrices: two planes everywhere, every product is hi lo + lo hi + hi hi.
 //   Where |G| is far below eps, X stays small for many steps (it grows by a in each).  Held times powers of two that
 //   leave room for singular values near 1 it would lose its bits below fp16's range, so each matrix has powers of
-//   two of its own beside those of all (or_load_kernel; |G| = 1e-15 and eps = 1e-7, 300 x 400 fp32: 2.4e-2 without them).
+//   two of its own beside those of all (or_load_kernel; |G| = 1e-15 and eps = 1e-7, 300 x 400 fp32: off by 2.2e-2 without them, 1.6e-7 so).
 //   A has none: where that would matter, B = a I to the last bit.
 // Sums are fp32 in the matrix cores, the norm's fp64.  The cores cut a sum off where it leaves fp32: each 16 terms added
 // to a sum of S take up to 2^-23 S from it, always towards zero, so the small products come first (16 x 4099 fp32:
@@ -833,7 +835,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
 // One workgroup per matrix, two planes throughout, in LDS.  A's rounding errors (2^-22 of its largest eigenvalue) grow by
 // a^2 per step as its smallest eigenvalues do: for bf16 matrices, up to OR_ITERATE_GROWTH, nothing but the result's
 // rounding is left to see (1.6e-3; where one direction is 3000 times as large as the others 2.1e-3).  fp32 matrices do not
-// come here (two steps at a time cost them up to 2.5 times the error of fp32 arithmetic).
+// come here (all steps at once cost them up to 2.5 times the error of fp32 arithmetic).
 // The launches between are what small matrices cost: 4 x 64 x 512 bf16 101 us with three per step, 38 with this one (19 of
 // them here, 17 products of 1 us).
 constexpr int OR_ITERATE_MOST = 128, OR_ITERATE_STEPS = 8;   // (padded) rows, steps

@@ -20,6 +20,12 @@ constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: 
 // n / m from which two steps are taken at a time.  24 matrices, bf16, us in pairs and step by step: 1024 x 1024 851 and 821,
 // 1024 x 2048 1062 and 1191, 1024 x 4096 1639 and 2075.
 constexpr int64_t OR_PAIR_LENGTH = 2;
+// Most that the first of two such steps may multiply by (its largest |a + b l + c l^2|).  What rounding B' B to 11 or 22 bits
+// leaves of the large singular values in the directions of the small ones grows with that, and no A of an X between sees
+// it.  Matrices of rank 2, 30 to 300 times as large as noise, 320 x 704 bf16, off by so much step by step and in pairs:
+// 3.44 (the usual steps) 1.7e-3 .. 2.5e-3 and 1.8e-3 .. 3.2e-3; 4.08 and less 1.8e-3 .. 2.5e-3 and 2.2e-3 .. 6.8e-3; 8 twice 2.0e-3 ..
+// 2.7e-3 and 1.2e-2 .. 2.5e-2.
+constexpr double OR_PAIR_GROWTH = 3.5;
 constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A (see or_iterate_kernel)
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
 constexpr double OR_LIFT = 4.0;                          // see steps_of (fp16 has room for another 4)
@@ -327,7 +333,7 @@ int run_group(const flce_orthogonalize_args& b, const OrPlan& p, const void* con
         a.B = B;
         int e_b = st->e_b;
         float carried = st->a;
-        paired = pairs && !paired && k + 1 < b.steps;
+        paired = pairs && !paired && k + 1 < b.steps && st->most_b <= OR_PAIR_GROWTH;
         if (paired) {
             const OrStep* second = st + 1;
             const int e_t = exponent_for(st->most_b * ldexp(1.0, 14 - st->e_a));   // (A's eigenvalues: at most 2^(14 - e_a))

@@ -63,3 +63,37 @@ def test_a_list_of_norms_on_either_side_of_eps():
             for o in (g, w):   # (they may be cut into other ranges of K)
                 assert np.linalg.norm(o.double().cpu().numpy() - ref) <= 5 * 3 * 2.0 ** -21 * np.linalg.norm(ref)
         assert (got[-1] == 0).all()
+
+
+USUAL = [oracle.COEFFICIENTS] * 5
+FALLING = [(4.0848, -6.8946, 2.9270), (3.9505, -6.3029, 2.6377), (3.7418, -5.5913, 2.3037), (2.8769, -3.1427, 1.2046), (2.8366, -3.0525, 1.2012)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("spike", [0.0, 30.0, 100.0, 300.0])
+@pytest.mark.parametrize("rows,cols", [(300, 700), (700, 300)])
+@pytest.mark.parametrize("coefficients", [USUAL, FALLING, [(8.0, -22.0, 16.0)] * 2], ids=["usual", "falling", "steep"])
+def test_long_lists_of_long_matrices(coefficients, rows, cols, spike, dtype):
+    """A list that fills the chip takes two steps at a time where its matrices are long.  Low rank and noise: that may cost half
+    as much again as the matrix alone is off by, and no more, whatever the coefficients are.
+
+    Tolerances are of the 2-norm, that of `check` among them.  Its bar for single elements is four times the largest of another
+    sample, which holds for errors that are alike in all elements; here they lie along the large singular vectors, u_i v_j
+    times what two directions are off by, so the largest may be any share of the 2-norm, and its square is at most the sum of
+    all squares, which is bounded here."""
+    import paper_2410_10989_amd as flce
+    G = make(rows, cols, dtype, rank=2 if spike else 0, spike=spike)
+    c = np.float32(coefficients).astype(float).tolist()
+    t = torch.from_numpy(G).to(DT[dtype]).cuda()
+    ref = oracle.orthogonalize(G, steps=len(c), coefficients=c)
+    model = oracle.orthogonalize_rounded(G, 2 if dtype == "f32" else 1, steps=len(c), coefficients=c)
+    size = np.linalg.norm(ref)
+    off = []
+    for count in (1, 50):
+        got = flce.flce_orthogonalize([t] * count, outs=[torch.empty_like(t) for _ in range(count)], steps=len(c), coefficients=c)[-1]
+        off.append(np.linalg.norm(got.double().cpu().numpy() - ref) / size)
+    may = 2 * np.linalg.norm(model - ref) / size + half(dtype) + 2.0 ** -21
+    print(f"alone {off[0]:.2e}, in a list {off[1]:.2e}, may be {may:.2e}", flush=True)
+    assert max(off) <= may
+    # (fp32: two samples of roundings at the end of fp32, 2^-21 apart at the most)
+    assert off[1] <= 1.5 * off[0] + 2.0 ** -21
