@@ -339,8 +339,9 @@ FLCE_API size_t flce_block_norm_workspace_bytes(const flce_block_norm* args);
  *     dx = dh + layer-norm backward of dn      (the gradient of x, of y and of all of h)
  *     dgamma = sum over rows of dn * (h - mean) / sqrt(...)          dbeta = sum over rows of dn
  *
- * The mean is taken first and the squares are those of h - mean, so rows that lie far from zero keep their
- * accuracy; statistics are fp32.  dgamma and dbeta are summed in fp32 within a workgroup and in fp64 over the
+ * The mean is taken first, its rounding (the mean of h - mean) off it, and the squares are those of h - mean: rows that
+ * lie far from zero keep their accuracy, and rows of equal elements give beta up to 2^-36 of h / sqrt(eps); statistics
+ * are fp32.  dgamma and dbeta are summed in fp32 within a workgroup and in fp64 over the
  * workgroups, without atomics, in an order that depends on the shape and the room for partial sums alone; k rows
  * added up one after the other are off by at most k 2^-24 of the sum of their magnitudes, with k as for
  * flce_block_norm.  Every output is rounded to dtype once.
