@@ -44,7 +44,7 @@ struct EmbedArgs {
 // The row of the table that token t names, or -1.
 __device__ __forceinline__ int embed_row(const EmbedArgs& a, int64_t t) {
     const uint64_t v = (uint64_t)t - (uint64_t)a.first;
-    return t != a.ignored && v < (uint64_t)a.V ? (int)v : -1;
+    return t != a.ignored && t >= a.first && v < (uint64_t)a.V ? (int)v : -1;
 }
 
 __device__ __forceinline__ int embed_key(const EmbedArgs& a, int v) { return (v & (a.classes - 1)) * a.per_class + (v >> a.class_bits); }
