@@ -17,8 +17,9 @@ namespace {
 
 constexpr int64_t OR_MAX_DIM = (int64_t)1 << 20;         // a tile's rows stay below 2^31 bytes apart
 constexpr int64_t OR_MAX_ELEMENTS = (int64_t)1 << 28;    // of a padded matrix: its planes stay below 2^30 bytes
-// n / m from which two steps are taken at a time.  24 matrices, bf16, us in pairs and step by step: 1024 x 1024 851 and 821,
-// 1024 x 2048 1062 and 1191, 1024 x 4096 1639 and 2075.
+// n / m from which two steps are taken at a time.  24 matrices, us in pairs and step by step: bf16 1024 x 1024 827 and 805,
+// 1024 x 2048 1078 and 1207, 1024 x 4096 1640 and 2098; fp32 1024 x 1024 2007 and 1884, 1024 x 1536 2435 and 2562, 1024 x 2048
+// 2627 and 2870, 1024 x 4096 3970 and 5030.
 constexpr int64_t OR_PAIR_LENGTH = 2;
 // Most that the first of two such steps may multiply by (its largest |a + b l + c l^2|).  What rounding B' B to 11 or 22 bits
 // leaves of the large singular values in the directions of the small ones grows with that, and no A of an X between sees
@@ -29,10 +30,12 @@ constexpr double OR_PAIR_GROWTH = 3.5;
 constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A (see or_iterate_kernel)
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
 constexpr double OR_LIFT = 4.0;                          // see steps_of (fp16 has room for another 4)
-// Fewest tiles of 256 that a launch takes those for.  bf16, whole calls in tiles of 256 and of 128: 2 x 2048 x 2048 (128 tiles)
-// 574 and 524 us, 16 x 1024 x 1024 (160) 598 and 628.  Operands in two planes, whose tiles of 128 take both at a time:
-// 4 x 2048 x 2048 fp32 (144 and 256 tiles) 2192 with both in tiles of 256, 2046 with the larger ones so, 2101 with none.
-constexpr int64_t OR_TILES_256 = 144, OR_TILES_256_PLANES = 256;
+// Fewest tiles of 256 that a launch takes those for, and that two steps at a time take.  Whole calls in tiles of 256 and of
+// 128, us: bf16 2 x 2048 x 2048 (128 tiles) 557 and 505, 1 x 4096 x 4096 (136) 1528 and 1605, 16 x 1024 x 1024 (160) 598 and
+// 628; 1 x 4096 x 14336 (136), two steps at a time or one, bf16 3170 and 4350, fp32 8540 and 11100.  Operands in two planes, whose
+// tiles of 128 take both at a time: 4 x 2048 x 2048 fp32 (144 and 256 tiles) 2192 with both in tiles of 256, 2046 with the
+// larger ones so, 2101 with none.
+constexpr int64_t OR_TILES_256 = 132, OR_TILES_256_PLANES = 256;
 static_assert(OR_MATRICES < OR_TILES_256, "Gram products of up to OR_SMALL rows never take them");
 constexpr int64_t OR_SLOTS_128 = 256;                    // workgroups that ranges of K may make: one per CU
 // Fewest turns of a range's K loop, most ranges, and turns one after the other that ranges have to save (a turn: 64 of K and
