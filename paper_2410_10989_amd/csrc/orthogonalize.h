@@ -833,9 +833,11 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
 //     B_k = a I + b A_k + c A_k A_k,   A_{k+1} = B_k A_k B_k,   Q = B_{steps-1} ... B_0,   out = s Q X
 //
 // One workgroup per matrix, two planes throughout, in LDS.  A's rounding errors (2^-22 of its largest eigenvalue) grow by
-// a^2 per step as its smallest eigenvalues do: for bf16 matrices, up to OR_ITERATE_GROWTH, nothing but the result's
-// rounding is left to see (1.6e-3; where one direction is 3000 times as large as the others 2.1e-3).  fp32 matrices do not
-// come here (all steps at once cost them up to 2.5 times the error of fp32 arithmetic).
+// the square of the most that B multiplies by per step, as its smallest eigenvalues do: for bf16 matrices, up to
+// OR_ITERATE_GROWTH, little but the result's rounding is left to see (60 x 100 of rank 1, whose other directions are its
+// rounding to bf16: five of the usual steps, 19800, 1.8e-3; five that begin with 4.08 and 3.95, 30300, 1.4e-2, and one by
+// one, as they are taken, 1.7e-3).  fp32 matrices do not come here (all steps at once cost them up to 2.5 times the error of
+// fp32 arithmetic).
 // The launches between are what small matrices cost: 4 x 64 x 512 bf16 101 us with three per step, 38 with this one (19 of
 // them here, 17 products of 1 us).
 constexpr int OR_ITERATE_MOST = 128, OR_ITERATE_STEPS = 8;   // (padded) rows, steps

@@ -27,7 +27,7 @@ constexpr int64_t OR_PAIR_LENGTH = 2;
 // 3.44 (the usual steps) 1.7e-3 .. 2.5e-3 and 1.8e-3 .. 3.2e-3; 4.08 and less 1.8e-3 .. 2.5e-3 and 2.2e-3 .. 6.8e-3; 8 twice 2.0e-3 ..
 // 2.7e-3 and 1.2e-2 .. 2.5e-2.
 constexpr double OR_PAIR_GROWTH = 3.5;
-constexpr float OR_ITERATE_GROWTH = 32768.0f;            // of a rounding error of A (see or_iterate_kernel)
+constexpr double OR_ITERATE_GROWTH = 20000.0;            // of a rounding error of A (see or_iterate_kernel)
 constexpr double OR_MAX_NORM = 1024.0;                   // that a singular value of an iterate may reach
 constexpr double OR_LIFT = 4.0;                          // see steps_of (fp16 has room for another 4)
 // Fewest tiles of 256 that a launch takes those for, and that two steps at a time take.  Whole calls in tiles of 256 and of
@@ -149,8 +149,8 @@ int or_plan(const flce_orthogonalize_args* args, int n, OrPlan* p) {
     p->lda = p->planes * p->mp;
     p->x_bytes = aligned_bytes((size_t)(p->mp * p->ldx) * sizeof(f16_t));
     p->a_bytes = aligned_bytes((size_t)(p->mp * p->lda) * sizeof(f16_t));
-    float growth = 1.0f;
-    for (int k = 0; k + 1 < b.steps; ++k) growth = std::min(growth * std::max(1.0f, p->steps[k].a * p->steps[k].a), 1e30f);
+    double growth = 1.0;
+    for (int k = 0; k + 1 < b.steps; ++k) growth = std::min(growth * std::max(1.0, p->steps[k].most_b * p->steps[k].most_b), 1e30);
     const bool small = b.dtype == FLCE_BF16 && p->mp <= OR_ITERATE_MOST;
     p->iterate = small && b.steps <= OR_ITERATE_STEPS && growth <= OR_ITERATE_GROWTH;
     p->b_matrices = small ? 1 + OR_ITERATE_STEPS : 2;   // (whatever the steps are)

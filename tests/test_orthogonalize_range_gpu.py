@@ -97,3 +97,29 @@ def test_long_lists_of_long_matrices(coefficients, rows, cols, spike, dtype):
     assert max(off) <= may
     # (fp32: two samples of roundings at the end of fp32, 2^-21 apart at the most)
     assert off[1] <= 1.5 * off[0] + 2.0 ** -21
+
+
+@pytest.mark.parametrize("second", [0.0, 0.01])
+@pytest.mark.parametrize("rows,cols", [(60, 100), (100, 60), (120, 128), (20, 500), (200, 300)])
+@pytest.mark.parametrize("coefficients", [USUAL, FALLING, [(8.0, -22.0, 16.0)] * 2, [(1.5, -0.5, 0.0)] * 8], ids=["usual", "falling", "steep", "cubic"])
+def test_small_matrices_of_rank_one_and_two(coefficients, rows, cols, second, dtype="bf16"):
+    """What is left of such a matrix in all other directions is its rounding to bf16, which all steps lift: those that
+    a small matrix takes in one launch are to be as good as one by one.  Of the 2-norm, for the reason in
+    test_long_lists_of_long_matrices.
+
+    The steep steps take a singular value of 1 to 2 and 352, which is beyond the model's one scale of 2^13.  Where it
+    overflows: with l = x^2 off by 2^-11 of itself (A in one plane), x (a + b l + c l^2) is off by |b l + 2 c l^2| / |a + b l +
+    c l^2| of that, 10 / 2 of it at l = 1 and 424 / 176 at l = 4, where an error of x counts |a + 3 b l + 5 c l^2| / 176 = 5.82
+    times: 5 * 5.82 + 2.41 < 32 times 2^-11 in all."""
+    import paper_2410_10989_amd as flce
+    print(f"case {rows} {cols} {second}", flush=True)
+    g = np.random.Generator(np.random.Philox(key=[rows, cols]))
+    outer = lambda: np.outer(g.standard_normal(rows), g.standard_normal(cols))
+    G = rounded(outer() + second * outer(), dtype)
+    c = np.float32(coefficients).astype(float).tolist()
+    got = flce.flce_orthogonalize([torch.from_numpy(G).to(DT[dtype]).cuda()], steps=len(c), coefficients=c)[0].double().cpu().numpy()
+    ref, model = oracle.orthogonalize(G, steps=len(c), coefficients=c), oracle.orthogonalize_rounded(G, 1, steps=len(c), coefficients=c)
+    lost = np.linalg.norm(model - ref) / np.linalg.norm(ref)
+    off, may = np.linalg.norm(got - ref) / np.linalg.norm(ref), (2 * lost if np.isfinite(lost) else 32 * 2.0 ** -11) + half(dtype) + 2.0 ** -21
+    print(f"off {off:.2e}, may be {may:.2e}", flush=True)
+    assert off <= may
