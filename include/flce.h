@@ -340,8 +340,8 @@ FLCE_API size_t flce_block_norm_workspace_bytes(const flce_block_norm* args);
  *     dgamma = sum over rows of dn * (h - mean) / sqrt(...)          dbeta = sum over rows of dn
  *
  * The mean is taken first, its rounding (the mean of h - mean) off it, and the squares are those of h - mean: rows that
- * lie far from zero keep their accuracy, and rows of equal elements give beta up to 2^-36 of h / sqrt(eps); statistics
- * are fp32.  dgamma and dbeta are summed in fp32 within a workgroup and in fp64 over the
+ * lie far from zero keep their accuracy, and rows of equal elements give beta up to 2^-36 of h / sqrt(eps).  Statistics
+ * are fp32: rows whose mean square leaves that type's range give what fp32 arithmetic gives.  dgamma and dbeta are summed in fp32 within a workgroup and in fp64 over the
  * workgroups, without atomics, in an order that depends on the shape and the room for partial sums alone; k rows
  * added up one after the other are off by at most k 2^-24 of the sum of their magnitudes, with k as for
  * flce_block_norm.  Every output is rounded to dtype once.
@@ -430,11 +430,12 @@ FLCE_API size_t flce_grad_norm_workspace_bytes(int n_tensors);
  *
  * Products are taken in the matrix cores on fp16 operands scaled by powers of two, accumulated in fp32, the X that is
  * carried over in 22 bits where later steps multiply its errors.  bf16 matrices: operands of 11 bits (up to 256 rows or
- * columns 22); what the result is off by, relative to its norm, is about 1e-3 next to its rounding to bf16 (1.7e-3).
- * fp32 matrices: operands of 22 bits, three products for one, about 1e-6 up to 1000 rows or columns, 3e-6 for 4096 x
- * 16384 (fp32 arithmetic: 1e-6 for 16 rows, 3e-6 for 1000, 9e-6 for 4096).  Both are for the usual coefficients, however
- * small |G| is beside eps (with a = 0 what is left then is of higher order in |G| / eps, and loses its bits); small
- * singular values and the errors in their directions grow by a factor a per step.  The norm is summed in fp64 (16 bytes at
+ * columns 22, but for X in X X^T); what the result is off by, relative to its norm, is about 1e-3 next to its rounding to
+ * bf16 (1.7e-3).  fp32 matrices: operands of 22 bits, three products for one, about 1e-6 up to 1000 rows or columns, 3e-6
+ * for 4096 x 16384 (fp32 arithmetic: 1e-6 for 16 rows, 3e-6 for 1000, 9e-6 for 4096).  Both are for the usual coefficients,
+ * however small |G| is beside eps (with a = 0 what is left then is of higher order in |G| / eps, and loses its bits).  Small
+ * singular values and the errors in their directions grow by a factor a per step: a part of rank 2 that is 300 times as
+ * large as the rest makes the above 2e-3 (in lists that take two steps at a time 2.8e-3) and 2.5e-5.  The norm is summed in fp64 (16 bytes at
  * a time, whose squares are added in fp32 where that can neither overflow nor vanish).  No atomics: the same call with
  * the same workspace gives the same bits.  A matrix that holds infinities or NaN gives NaN, and leaves the others of
  * the list alone; zeros give zeros.
@@ -492,6 +493,9 @@ FLCE_API size_t flce_orthogonalize_workspace_bytes(int n_matrices, const flce_or
  * Every row of the gradient is a sum in the order of i: up to 32 consecutive terms in fp32 (which terms
  * stand together depends on the tokens), those sums in fp64, scaled in fp32 and rounded to dtype once
  * (accumulate: added in fp32 first).  No atomics: the same call gives the same bits.
+ *
+ * Each 1024 rows of the table have a workgroup that looks at all tokens: 2^20 of them take 1 ms for 2^20 rows of the
+ * table or fewer, 13 ms for 2^24, 53 for 2^26.
  *
  *   size            must be sizeof(flce_embedding) (FLCE_ERR_ARG otherwise)
  *   rows            number of tokens, 1 .. 2^30

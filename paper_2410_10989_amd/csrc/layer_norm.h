@@ -7,8 +7,8 @@
 //     u = dn gamma      dx = dh + r (u - mean u - d r mean(u d r))      dgamma = sum_i dn d r      dbeta = sum_i dn
 //
 // The mean is taken first and the squares are those of h - mean: their sum does not cancel, however far a row lies from
-// zero.  The mean's own rounding (up to 2^-19 of |h|, which r may multiply by eps^-1/2: rows of a thousand equal elements of
-// 100 had n off by up to 0.029 gamma) is the mean of h - mean, whose sum is taken with the squares':
+// zero.  The mean's own rounding (up to 2^-19 of |h|, which r may multiply by eps^-1/2: fp32 rows of a thousand equal elements,
+// 10 to 1000 large, had n off by up to 0.19 gamma) is the mean of h - mean, whose sum is taken with the squares':
 //
 //     p = fl(mean h),  q = mean (h - p),     d = (h - p) - q,  mean d^2 = mean (h - p)^2 - q^2
 //
@@ -19,8 +19,8 @@
 // (see block_norm.h), so the second pass over it reads nothing; what it costs is a second exchange between the threads,
 // in which the backward takes its other sums along.
 //
-// Bound by HBM.  Forward, 16384 x 3584 bf16 with a residual: 80 us, 5.9 TB/s.  Backward, 8192 x 4096 bf16 with a residual: 54
-// to 56 us, 4.8 TB/s (a workgroup has one row on the way while it does another, whose two exchanges it waits for), and 4.8
+// Bound by HBM.  Forward, 16384 x 3584 bf16 with a residual: 80 us, 5.9 TB/s.  Backward, 8192 x 4096 bf16 with a residual: 53
+// to 55 us, 4.9 TB/s (a workgroup has one row on the way while it does another, whose two exchanges it waits for), and 5
 // for the sums over rows.
 #pragma once
 #include "rowsums.h"

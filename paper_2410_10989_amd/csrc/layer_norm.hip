@@ -14,13 +14,13 @@ namespace {
 constexpr int64_t LN_MAX_H = (int64_t)1 << 24;      // keeps launches and column numbers within 32 bits
 constexpr int64_t LN_GRID_X = (int64_t)1 << 20;     // workgroups along x, the rest along y
 // Threads per CU that the backward is launched for; more where a workgroup's row is so short that two of them have too little
-// on the way.  us with 512 and 768, 8192 rows with a residual: 1280 bf16 30.0 and 27.2, 2048 32.1 and 31.3, 2816 42.7
-// and 42.7, 4096 53.7 and 58.5, 1600 fp32 40.9 and 41.5; several rows per workgroup: 16384 x 1024 bf16 29.7 and 35.7.
+// on the way.  us with 512 and 768, 8192 rows with a residual: 1280 bf16 30.8 and 28.9, 2304 44.0 and 41.2, 2816 45.5 and
+// 44.8, 4096 57.2 and 58.8, 1600 fp32 42.4 and 43.6; several rows per workgroup: 16384 x 1024 bf16 31.3 and 37.4.
 constexpr int LN_CU_THREADS = 512, LN_SHORT_CU_THREADS = 768;
 constexpr int64_t LN_SHORT_BYTES = 5632;
 // Fewest workgroups of a backward with partial sums, while there are rows for them (us with 32, 128 and 256: 128 rows of 4096
-// bf16 12.3, 9.3, 9.3; 256 rows 12.9, 10.7, 11.9); rows that one workgroup takes one after the other and writes the sums of
-// itself (2 rows of 4096: 5.8, with partial sums 7.1; 4 rows 8.8 and 7.0).
+// bf16 12.4, 9.2, 9.2; 256 rows 18.9, 11.2, 12.5); rows that one workgroup takes one after the other and writes the sums of
+// itself (2 rows of 4096: 5.8, with partial sums 7.0; 4 rows 9.0 and 7.0).
 constexpr int64_t LN_CUS = 256, LN_FEW_BLOCKS = 128, LN_ONE_STEPS = 3;
 constexpr int64_t LN_CACHE_BYTES = (int64_t)256 << 20;   // memory-side cache
 
