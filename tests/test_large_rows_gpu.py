@@ -25,7 +25,7 @@ def padded(rows, H, dtype, pad, seed, mean=0.0):
 
 
 @pytest.mark.parametrize("rows,V,H,dtype,pad", [(33000, 500, 4099, "bf16", 5), (17000, 500, 4099, "f32", 3), (2_300_000, 70, 60, "bf16", 0),
-                                                ((1 << 24) + 1000, 40, 3, "bf16", 0), ((1 << 22) + 77, 40, 130, "f32", 1)])
+                                                ((1 << 24) + 1000, 40, 3, "bf16", 0), ((1 << 22) + 77, 40, 130, "f32", 1), (140_000, 90, 1001, "bf16", 1)])
 def test_lookup(rows, V, H, dtype, pad):
     import paper_2410_10989_amd as flce
     print(f"case lookup {rows} {V} {H} {dtype}", flush=True)
@@ -68,7 +68,8 @@ def statistics(h):
 
 
 LARGE = [(9000, 4099, "bf16", 5), (4600, 4099, "f32", 3), (300_000, 130, "bf16", 1), (70_000, 1000, "bf16", 0), (2500, 14001, "bf16", 1),
-         (1300, 14001, "f32", 0), (4000, 16401, "bf16", 3), (2100, 16401, "f32", 1), ((1 << 24) + 777, 8, "bf16", 0)]
+         (1300, 14001, "f32", 0), (20_000, 2001, "bf16", 3), (10_000, 2001, "f32", 0),
+         (12_000, 3001, "bf16", 0), (6000, 3001, "f32", 1), (4000, 16401, "bf16", 3), (2100, 16401, "f32", 1), ((1 << 24) + 777, 8, "bf16", 0)]
 
 
 @pytest.mark.parametrize("rows,H,dtype,pad", LARGE)
