@@ -239,7 +239,9 @@ __global__ __launch_bounds__(row_block<TPR>) void layer_norm_bwd_kernel(LnArgs a
         for (int k = 0; k < NV; ++k) gv[k] = row_load(static_cast<const T*>(a.gamma), t + k * TPR, nfull, rem);
     float acc_gamma[NV][N], acc_beta[NV][N];
     // IN_LDS: four of them, in set 0 (gamma's) or 1; a thread has its own
-    auto sums_at = [&](int set, int k, int e) { return reinterpret_cast<f32x4*>(cols + (((set * NV + k) * N + e) * BLOCK + (int)threadIdx.x * 4)); };
+    auto sums_at = [&](int set, int k, int e) {
+        return reinterpret_cast<f32x4*>(cols + ((set * NV + k) * N + e) * BLOCK + (int)threadIdx.x * 4);
+    };
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll

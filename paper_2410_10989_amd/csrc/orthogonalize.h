@@ -26,8 +26,8 @@
 //   fp32 matrices: two planes everywhere, every product is hi lo + lo hi + hi hi.
 //   Where |G| is far below eps, X stays small for many steps (it grows by a in each).  Held times powers of two that
 //   leave room for singular values near 1 it would lose its bits below fp16's range, so each matrix has powers of
-//   two of its own beside those of all (or_load_kernel; |G| = 1e-15 and eps = 1e-7, 300 x 400 fp32: off by 2.2e-2 without them, 1.6e-7 so).
-//   A has none: where that would matter, B = a I to the last bit.
+//   two of its own beside those of all (or_load_kernel; |G| = 1e-15 and eps = 1e-7, 300 x 400 fp32: off by 2.2e-2 without
+//   them, 1.6e-7 so).  A has none: where that would matter, B = a I to the last bit.
 // Sums are fp32 in the matrix cores, the norm's fp64.  The cores cut a sum off where it leaves fp32: each 16 terms added
 // to a sum of S take up to 2^-23 S from it, always towards zero, so the small products come first (16 x 4099 fp32:
 // 7.2e-6 with hi hi first).
@@ -781,7 +781,7 @@ __global__ __launch_bounds__(FG_THREADS, TILE == 256 || (PL == 2 && PART != OR_J
             nk *= 3;
         }
         OrFactors factors{};
-        if constexpr (PART == OR_WHOLE) factors = or_factors<PRODUCT>(a, matrix);   // (its loads are done long before the K loop is)
+        if constexpr (PART == OR_WHOLE) factors = or_factors<PRODUCT>(a, matrix);   // (its loads end long before the K loop)
         f32x16 acc[W][W];
 #pragma unroll
         for (int i = 0; i < W; ++i)
